@@ -38,6 +38,13 @@
  *   - 8-bit (the precision of the paper's homogeneous 8-bit comparison model, §4 Table 1) follows the same scheme:
  *     asymmetric uint8, groups of 64 columns with an fp16 scale and an fp16 zero, one code per byte;
  *     dequantized weight = fp16_rne( fp32(code) * fp32(scale) + fp32(zero) ).
+ *   - 8-bit floating point (MOE_PREC_FP8B128) means e4m3: 1 sign, 4 exponent and 3 mantissa bits, largest value 448, NaN but
+ *     no infinity; one code per byte and one fp32 scale per block of 128 x 128 of a matrix (ceil(out/128) x ceil(in/128),
+ *     row-major; blocks at the edges are smaller) and, for rows, per 128 columns of a row.  Of a block whose largest
+ *     magnitude is `most`:  scale = fp32_rne(most / 448),  code = e4m3_rne( fp32_rne( w * fp32_rne(448 / most) ) ),
+ *     all 0 where most == 0;  value = fp32(code) * scale.  A block that holds an infinity or a NaN makes every result
+ *     that depends on it NaN.  An expert of this precision multiplies quantized rows: the block's input rows, and the
+ *     hidden rows (rounded to fp16 as everywhere), are brought into this form, 128 columns to a scale, on the fly.
  *   - d_model and d_ff must be multiples of 64, d_model <= 8192, d_ff <= 16384 (else MOE_ESHAPE);
  *     n_experts <= MOE_MAX_EXPERTS; 1 <= top_k <= min(n_experts, MOE_MAX_TOPK).
  */
@@ -52,6 +59,7 @@ extern "C" {
 #endif
 
 #define MOE_GROUP 64
+#define MOE_FP8_BLOCK 128
 #define MOE_MAX_EXPERTS 32
 #define MOE_MAX_TOPK 8
 #define MOE_STATIC_SCRATCH_BYTES (8u << 20) /* scratch held by the library for moe_layer_forward_static */
@@ -66,13 +74,13 @@ typedef enum {
 } moe_status;
 
 /* The "quantized?" attribute of the paper's expert table (§3). */
-typedef enum { MOE_PREC_FP16 = 0, MOE_PREC_INT4G64 = 1, MOE_PREC_INT8G64 = 2 } moe_prec;
+typedef enum { MOE_PREC_FP16 = 0, MOE_PREC_INT4G64 = 1, MOE_PREC_INT8G64 = 2, MOE_PREC_FP8B128 = 3 } moe_prec;
 
 /* One weight matrix [out, in] in device memory, rows end to end; every pointer 16-byte aligned (MOE_EINVAL otherwise). */
 typedef struct {
-    const void* data;  /* device: fp16 [out,in]; uint8 [out,in/2] of packed 4-bit codes; or uint8 [out,in] of 8-bit codes */
-    const void* scale; /* device: fp16 [out,in/64]; NULL for a 16-bit matrix */
-    const void* zero;  /* device: fp16 [out,in/64]; NULL for a 16-bit matrix */
+    const void* data;  /* device: fp16 [out,in]; uint8 [out,in/2] of packed 4-bit codes; or uint8 [out,in] of 8-bit codes (integer or e4m3) */
+    const void* scale; /* device: fp16 [out,in/64]; fp32 [ceil(out/128),ceil(in/128)] of an e4m3 matrix; NULL for a 16-bit matrix */
+    const void* zero;  /* device: fp16 [out,in/64]; NULL for a 16-bit or an e4m3 matrix */
 } moe_mat;
 
 /* One expert = SwiGLU feed-forward layer y = W2 ( silu(W1 x) * (W3 x) ).
@@ -99,7 +107,9 @@ typedef void* moe_stream_t; /* hipStream_t; NULL = the default stream */
  * d_model or d_ff an odd multiple of 64: the bytes include partial results of a split contraction as long as the whole
  * stays within MOE_STATIC_SCRATCH_BYTES (so they may fall where T grows past that).  A smaller workspace that holds the
  * unsplit call is accepted as well and split less, so that one sized for more tokens always serves fewer; the fp32 sums
- * are then added in another order. */
+ * are then added in another order.
+ * Layers with experts of MOE_PREC_FP8B128 also keep quantized rows there: `layer->experts` has to be filled in when this is
+ * asked.  (If it is NULL the bytes are those of a layer without such experts.) */
 size_t moe_workspace_bytes(const moe_layer* layer, int n_tokens);
 
 /*
@@ -206,7 +216,8 @@ int moe_layer_forward_swap(const moe_layer* layer, const moe_swap* swap, const v
  *   n = fp16_rne( h / sqrt(mean(h^2) + eps) * rms_gain[layer] );   h <- fp16_rne( h + MoE_layer(n) )
  * layers: host array [n_layers]; rms_gain: host array of n_layers device pointers to fp16 [d_model];
  * h: device fp16 [T, d_model], updated in place; topk_idx_out: device int32 [n_layers, T, top_k] or NULL.
- * All layers must share d_model, d_ff, n_experts, top_k.  ws sized by moe_workspace_bytes(&layers[0], T).
+ * All layers must share d_model, d_ff, n_experts, top_k.  ws sized by moe_workspace_bytes(&layers[0], T), or of a layer with an
+ * expert of MOE_PREC_FP8B128 where there is one.
  */
 int moe_chain_forward(const moe_layer* layers, const void* const* rms_gain, int n_layers, float eps, void* h,
                       int T, int32_t* topk_idx_out, void* ws, size_t ws_bytes, moe_stream_t stream);
@@ -236,6 +247,84 @@ int moe_quantize_int4(const void* w_fp16, int out, int in, void* packed, void* s
  */
 int moe_dequant_int8(const moe_mat* m, int out, int in, void* w_fp16, moe_stream_t stream);
 int moe_quantize_int8(const void* w_fp16, int out, int in, void* codes, void* scale, void* zero, moe_stream_t stream);
+
+/* ---------------------------------------------------------------- 8-bit floating point
+ *
+ * The hooks of the e4m3 form: a matrix quantized with a scale per block of 128 x 128, and back
+ * (w_fp16[r,c] = fp16_rne( fp32(code[r,c]) * scale[r/128,c/128] )).  w_fp16: device fp16 [out,in]; codes: device uint8 [out,in],
+ * 16-byte aligned; scale: device fp32 [ceil(out/128), ceil(in/128)].  in: a multiple of 16 (MOE_ESHAPE otherwise).  Both are bit-exact
+ * against the definition above.  out and in: at most 2^20.
+ */
+int moe_quantize_fp8(const void* w_fp16, int out, int in, void* codes, float* scale, moe_stream_t stream);
+int moe_dequant_fp8(const moe_mat* m, int out, int in, void* w_fp16, moe_stream_t stream);
+
+/* Rows for the products below: codes: device uint8 [n,in], 16-byte aligned; scale: device fp32 [ceil(in/128), n], the scales of all rows
+ * for one block of columns side by side.  x: device fp16 [n,in].  in: a multiple of 16.  n up to 2^22, 0 does nothing. */
+int moe_quantize_fp8_rows(const void* x, int n, int in, void* codes, float* scale, moe_stream_t stream);
+
+/* The transposed matrix: codes_t: device uint8 [in,out], 16-byte aligned, scale_t: device fp32 [ceil(in/128), ceil(out/128)].  A block of 128 x 128
+ * keeps its scale, so nothing is rounded.  For g: [n,out], a gradient with respect to y = x W^T, the gradient with respect to x
+ * is g W = moe_matmul_fp8 of the transposed matrix with g quantized by rows.  out and in: multiples of 16. */
+int moe_transpose_fp8(const moe_mat* m, int out, int in, void* codes_t, float* scale_t, moe_stream_t stream);
+
+/*
+ * Products of quantized rows with e4m3 matrices:
+ *   y[r, o] = sum over blocks b of 128 columns:  x_scale[b, row(r)] * w_scale[o/128, b] * sum_{c in b} x_codes[row(r), c] * w_codes[o, c]
+ * moe_matmul_fp8: one matrix w [out,in], row(r) = r, n rows.
+ * moe_matmul_fp8_grouped: w is a HOST array of n_experts matrices [out,in] (at most MOE_MAX_EXPERTS); row r in
+ *   [offsets[e], offsets[e+1]) is multiplied with matrix e; row(r) = perm[r] / top_k, or r where perm is NULL; the offsets and perm of
+ *   moe_permute.  offsets: device int32 [n_experts + 1], increasing; perm: device int32 [n_pairs] or NULL; x has n_rows rows, y n_pairs.  Rows of y
+ *   outside [offsets[0], offsets[n_experts]) are left as they were.  (Whatever offsets and perm hold, nothing outside the arrays is read or
+ *   written.)
+ * x_codes: device [n,in], 16-byte aligned; x_scale: device fp32 [ceil(in/128), n]; y: device, fp32 (MOE_OUT_F32) or fp16 (MOE_OUT_F16, rounded once).
+ * in: a multiple of 16; out: any.  n, n_rows and n_pairs: at most 2^20, 0 does nothing.  Sums are fp32.
+ */
+typedef enum { MOE_OUT_F32 = 0, MOE_OUT_F16 = 1 } moe_out;
+int moe_matmul_fp8(const moe_mat* w, int out, int in, const void* x_codes, const float* x_scale, int n, void* y, int y_type,
+                   moe_stream_t stream);
+int moe_matmul_fp8_grouped(const moe_mat* w, int n_experts, int out, int in, const void* x_codes, const float* x_scale, int n_rows,
+                           const int32_t* offsets, const int32_t* perm, int top_k, int n_pairs, void* y, int y_type,
+                           moe_stream_t stream);
+
+/* ---------------------------------------------------------------- training the gate
+ *
+ * moe_route that also keeps the logits [T, n_experts] (device fp32), which the calls below take.  Same bits as moe_route.
+ */
+int moe_route_logits(const moe_layer* layer, const void* x, int T, float* logits, int32_t* topk_idx, float* topk_gate,
+                     moe_stream_t stream);
+
+/* Bytes of scratch of the two calls below for T tokens; same rules as moe_workspace_bytes.  moe_read_status reads their status. */
+size_t moe_gate_workspace_bytes(const moe_layer* layer, int T);
+
+/*
+ * Load balance of a routing, as a loss:  with n valid tokens, p[t,:] = softmax(logits[t,:]),
+ *   counts[e]    = pairs (t, s) of valid tokens with topk_idx[t,s] == e;  counts[n_experts] = n
+ *   mean_prob[e] = 1/n sum_t p[t,e]                                    (0 where n == 0)
+ *   loss         = n_experts / (n top_k) * sum_e counts[e] * mean_prob[e]   (1 for even loads; 0 where n == 0)
+ * valid: device uint8 [T], 0 marks padding whose logits and indices are not looked at; NULL: all tokens are valid.
+ * A token whose logits are all -infinity has p = 0.  An index outside [0, n_experts) is left out and sets the MOE_EINVAL bit of the status.
+ * logits: device fp32 [T, n_experts]; topk_idx: device int32 [T, top_k]; counts: device int32 [n_experts + 1];
+ * mean_prob: device fp32 [n_experts]; loss: device fp32 [1].  The same inputs give the same bits.
+ */
+int moe_balance_loss(const moe_layer* layer, const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int32_t* counts,
+                     float* mean_prob, float* loss, void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/*
+ * Backward pass of moe_route_logits and moe_balance_loss: from the gradients with respect to the gates and to the loss,
+ *   d_logits[t,j] = sum_s [topk_idx[t,s] == j] g[t,s] (d_gate[t,s] - sum_r g[t,r] d_gate[t,r])
+ *                 + d_loss * n_experts / (n top_k) * 1/n * p[t,j] * (counts[j] - sum_e counts[e] p[t,e])
+ *   d_x = d_logits W_gate,   d_w_gate = d_logits^T x,   d_bias = sum_t d_logits[t,:]
+ * g = topk_gate, worked out again from the logits; counts as moe_balance_loss gives them (no gradient flows through them).
+ * Rows of padding get zeros and count nowhere, whatever they hold; so does a token's gate term if its chosen logits are all
+ * -infinity, and its loss term if all its logits are.
+ * d_gate: device fp32 [T, top_k] or NULL; d_loss: device fp32 [1] with counts, or both NULL; one of the two gradients has to be given.
+ * Each result may be NULL, at least one has to be asked for: d_logits: device fp32 [T, n_experts]; d_x: device fp32 or fp16 (d_x_type, a moe_out) [T, d_model];
+ * d_w_gate: device fp32 [n_experts, d_model]; d_bias: device fp32 [n_experts].  x: device fp16 [T, d_model], needed for d_w_gate only.
+ * All are overwritten; the same inputs give the same bits.
+ */
+int moe_route_backward(const moe_layer* layer, const void* x, const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T,
+                       const int32_t* counts, const float* d_gate, const float* d_loss, float* d_logits, void* d_x, int d_x_type,
+                       float* d_w_gate, float* d_bias, void* ws, size_t ws_bytes, moe_stream_t stream);
 
 /*
  * Seeded synthetic tensors written directly in device memory (stand-ins for trained weights and real

@@ -15,8 +15,11 @@ from typing import List, Optional, Sequence
 _LIB_PATH = Path(__file__).resolve().parent / "libmoemix.so"
 
 MOE_OK, MOE_EINVAL, MOE_ESHAPE, MOE_ENOTRESIDENT, MOE_EWORKSPACE, MOE_EHIP = 0, -1, -2, -3, -4, -5
-PREC_FP16, PREC_INT4G64, PREC_INT8G64 = 0, 1, 2
+PREC_FP16, PREC_INT4G64, PREC_INT8G64, PREC_FP8B128 = 0, 1, 2, 3
 GROUP = 64
+FP8_BLOCK = 128
+OUT_F32, OUT_F16 = 0, 1
+MAX_EXPERTS = 32
 STATUS_BAD_INDEX = 1 << 1
 STATUS_NOT_RESIDENT = 1 << 3
 
@@ -25,7 +28,9 @@ EXPORTS = (
     "moe_chain_forward", "moe_dequant_int4", "moe_quantize_int4", "moe_synth_fill_f16", "moe_read_status",
     "moe_last_error", "moe_version", "moe_trace_kernel", "moe_plan", "moe_swap_slot_bytes", "moe_layer_forward_swap",
     "moe_stream_read", "moe_static_scratch_bytes", "moe_layer_forward_static",
-    "moe_dequant_int8", "moe_quantize_int8",
+    "moe_dequant_int8", "moe_quantize_int8", "moe_quantize_fp8", "moe_dequant_fp8", "moe_quantize_fp8_rows",
+    "moe_transpose_fp8", "moe_matmul_fp8", "moe_matmul_fp8_grouped", "moe_route_logits", "moe_gate_workspace_bytes",
+    "moe_balance_loss", "moe_route_backward",
 )
 
 
@@ -94,6 +99,18 @@ def lib():
         L.moe_quantize_int4.argtypes = [vp, i32, i32, vp, vp, vp, vp]
         L.moe_dequant_int8.argtypes = [ctypes.POINTER(CMat), i32, i32, vp, vp]
         L.moe_quantize_int8.argtypes = [vp, i32, i32, vp, vp, vp, vp]
+        MP = ctypes.POINTER(CMat)
+        L.moe_quantize_fp8.argtypes = [vp, i32, i32, vp, vp, vp]
+        L.moe_dequant_fp8.argtypes = [MP, i32, i32, vp, vp]
+        L.moe_quantize_fp8_rows.argtypes = [vp, i32, i32, vp, vp, vp]
+        L.moe_transpose_fp8.argtypes = [MP, i32, i32, vp, vp, vp]
+        L.moe_matmul_fp8.argtypes = [MP, i32, i32, vp, vp, i32, vp, i32, vp]
+        L.moe_matmul_fp8_grouped.argtypes = [MP, i32, i32, i32, vp, vp, i32, vp, vp, i32, i32, vp, i32, vp]
+        L.moe_route_logits.argtypes = [LP, vp, i32, vp, vp, vp, vp]
+        L.moe_gate_workspace_bytes.argtypes = [LP, i32]
+        L.moe_gate_workspace_bytes.restype = sz
+        L.moe_balance_loss.argtypes = [LP, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.moe_route_backward.argtypes = [LP, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
         L.moe_synth_fill_f16.argtypes = [vp, sz, sz, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_float, i32, vp]
         L.moe_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int)]
         L.moe_trace_kernel.argtypes = [i32, vp, vp]
@@ -110,7 +127,7 @@ def lib():
         L.moe_version.restype = i32
         for name in EXPORTS:
             if name not in ("moe_workspace_bytes", "moe_last_error", "moe_version", "moe_swap_slot_bytes",
-                            "moe_static_scratch_bytes"):
+                            "moe_static_scratch_bytes", "moe_gate_workspace_bytes"):
                 getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -134,7 +151,8 @@ def _stream() -> int:
 
 @dataclass
 class Mat:
-    """One weight matrix in device memory: fp16 ``data`` [out,in], or uint8 ``data`` [out,in/2] + fp16 scale/zero."""
+    """One weight matrix in device memory: fp16 ``data`` [out,in], uint8 ``data`` [out,in/2] + fp16 scale/zero, or e4m3 ``data`` [out,in]
+    (uint8 or float8_e4m3fn) + fp32 ``scale`` [ceil(out/128),ceil(in/128)]."""
     data: "torch.Tensor"
     scale: Optional["torch.Tensor"] = None
     zero: Optional["torch.Tensor"] = None
@@ -283,6 +301,181 @@ def moe_quantize_int8(w_fp16, codes, scale, zero) -> None:
     _check(lib().moe_quantize_int8(_ptr(w_fp16), out, inn, _ptr(codes), _ptr(scale), _ptr(zero), _stream()))
 
 
+# ---------------------------------------------------------------- 8-bit floating point and the training of the gate
+#
+# Shapes, types and places of the tensors are looked at before a call (MoeError with MOE_EINVAL or MOE_ESHAPE): the kernels read and write what they
+# are told to.  Tensors have to be contiguous and on the current device.
+
+def _need(t, what: str, dtypes, shape) -> int:
+    """Pointer of tensor ``t``, which has to be contiguous, of one of ``dtypes`` and of ``shape``, on the current device."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise MoeError(MOE_EINVAL, f"{what}: a tensor is needed")
+    if t.dtype not in dtypes or not t.is_contiguous():
+        raise MoeError(MOE_EINVAL, f"{what}: {t.dtype}, strides {t.stride()}: contiguous {dtypes} is needed")
+    if t.shape != shape:
+        raise MoeError(MOE_ESHAPE, f"{what}: {tuple(t.shape)}, {tuple(shape)} is needed")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise MoeError(MOE_EINVAL, f"{what}: on {t.device}, which is not the current GPU")
+    return t.data_ptr()
+
+
+def _types():
+    import torch
+    return ((torch.float16,), (torch.float32,), (torch.int32,), (torch.uint8, torch.float8_e4m3fn),
+            (torch.uint8, torch.bool))
+
+
+def _rows_cols(t, what: str):
+    if getattr(t, "ndim", 0) != 2:
+        raise MoeError(MOE_ESHAPE, f"{what}: two dimensions are needed")
+    return t.shape
+
+
+def _blocks(n: int) -> int:
+    return (n + FP8_BLOCK - 1) // FP8_BLOCK
+
+
+def _need_fp8(m: Mat, what: str):
+    """(out, in) of an e4m3 matrix whose tensors fit each other."""
+    _, f32, _, codes, _ = _types()
+    out, inn = _rows_cols(m.data, what)
+    _need(m.data, what, codes, (out, inn))
+    _need(m.scale, what + " scale", f32, (_blocks(out), _blocks(inn)))
+    return out, inn
+
+
+def _out_type(t, what: str) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return OUT_F32
+    if t.dtype == torch.float16:
+        return OUT_F16
+    raise MoeError(MOE_EINVAL, f"{what}: {t.dtype}: float32 or float16 is needed")
+
+
+def moe_quantize_fp8(w_fp16, codes, scale) -> None:
+    f16, f32, _, c8, _ = _types()
+    out, inn = _rows_cols(w_fp16, "w_fp16")
+    _check(lib().moe_quantize_fp8(_need(w_fp16, "w_fp16", f16, (out, inn)), out, inn, _need(codes, "codes", c8, (out, inn)),
+                                  _need(scale, "scale", f32, (_blocks(out), _blocks(inn))), _stream()))
+
+
+def moe_dequant_fp8(m: Mat, out: int, inn: int, w_fp16) -> None:
+    f16 = _types()[0]
+    if _need_fp8(m, "m") != (out, inn):
+        raise MoeError(MOE_ESHAPE, f"m: {tuple(m.data.shape)}, {(out, inn)} is needed")
+    cm = m.c()
+    _check(lib().moe_dequant_fp8(ctypes.byref(cm), out, inn, _need(w_fp16, "w_fp16", f16, (out, inn)), _stream()))
+
+
+def moe_quantize_fp8_rows(x, codes, scale) -> None:
+    f16, f32, _, c8, _ = _types()
+    n, inn = _rows_cols(x, "x")
+    _check(lib().moe_quantize_fp8_rows(_need(x, "x", f16, (n, inn)), n, inn, _need(codes, "codes", c8, (n, inn)),
+                                       _need(scale, "scale", f32, (_blocks(inn), n)), _stream()))
+
+
+def moe_transpose_fp8(m: Mat, codes_t, scale_t) -> None:
+    _, f32, _, c8, _ = _types()
+    out, inn = _need_fp8(m, "m")
+    cm = m.c()
+    _check(lib().moe_transpose_fp8(ctypes.byref(cm), out, inn, _need(codes_t, "codes_t", c8, (inn, out)),
+                                   _need(scale_t, "scale_t", f32, (_blocks(inn), _blocks(out))), _stream()))
+
+
+def moe_matmul_fp8(w: Mat, x_codes, x_scale, y) -> None:
+    """y = x W^T: ``x_codes`` [n,in] and ``x_scale`` [ceil(in/128),n] of moe_quantize_fp8_rows, ``y`` [n,out] float32 or float16."""
+    _, f32, _, c8, _ = _types()
+    out, inn = _need_fp8(w, "w")
+    n = _rows_cols(x_codes, "x_codes")[0]
+    cm = w.c()
+    _check(lib().moe_matmul_fp8(ctypes.byref(cm), out, inn, _need(x_codes, "x_codes", c8, (n, inn)),
+                                _need(x_scale, "x_scale", f32, (_blocks(inn), n)), n, _need(y, "y", (y.dtype,), (n, out)),
+                                _out_type(y, "y"), _stream()))
+
+
+class MatGroup:
+    """Host array of e4m3 matrices of one shape for moe_matmul_fp8_grouped, built once; keeps their tensors alive."""
+
+    def __init__(self, mats: Sequence[Mat]):
+        self.mats = list(mats)
+        if not 1 <= len(self.mats) <= MAX_EXPERTS:
+            raise MoeError(MOE_ESHAPE, f"{len(self.mats)} matrices, 1 to {MAX_EXPERTS} are possible")
+        self.shape = _need_fp8(self.mats[0], "matrix 0")
+        for i, m in enumerate(self.mats):
+            if _need_fp8(m, f"matrix {i}") != self.shape:
+                raise MoeError(MOE_ESHAPE, f"matrix {i}: {tuple(m.data.shape)}, {tuple(self.shape)} is needed")
+        self.c = (CMat * len(self.mats))(*[m.c() for m in self.mats])
+
+
+def moe_matmul_fp8_grouped(group: MatGroup, x_codes, x_scale, offsets, perm, top_k: int, y) -> None:
+    """``perm`` None: rows of x in order."""
+    _, f32, i32, c8, _ = _types()
+    (out, inn), E = group.shape, len(group.mats)
+    n, P = _rows_cols(x_codes, "x_codes")[0], _rows_cols(y, "y")[0]
+    _check(lib().moe_matmul_fp8_grouped(group.c, E, out, inn, _need(x_codes, "x_codes", c8, (n, inn)),
+                                        _need(x_scale, "x_scale", f32, (_blocks(inn), n)), n,
+                                        _need(offsets, "offsets", i32, (E + 1,)),
+                                        None if perm is None else _need(perm.view(-1), "perm", i32, (P,)), top_k, P,
+                                        _need(y, "y", (y.dtype,), (P, out)), _out_type(y, "y"), _stream()))
+
+
+def moe_route_logits(layer: Layer, x, logits, topk_idx, topk_gate) -> None:
+    f16, f32, i32, _, _ = _types()
+    T, E, k = _rows_cols(x, "x")[0], layer.n_experts, layer.top_k
+    _check(lib().moe_route_logits(ctypes.byref(layer.c), _need(x, "x", f16, (T, layer.d_model)), T,
+                                  _need(logits, "logits", f32, (T, E)), _need(topk_idx, "topk_idx", i32, (T, k)),
+                                  _need(topk_gate, "topk_gate", f32, (T, k)), _stream()))
+
+
+def gate_workspace_bytes(layer: Layer, n_tokens: int) -> int:
+    return int(lib().moe_gate_workspace_bytes(ctypes.byref(layer.c), n_tokens))
+
+
+def alloc_gate_workspace(layer: Layer, n_tokens: int):
+    import torch
+    n = gate_workspace_bytes(layer, n_tokens)
+    if n == 0:
+        raise MoeError(MOE_EINVAL, "moe_gate_workspace_bytes rejected the arguments")
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def _need_ws(ws):
+    import torch
+    if ws is None:
+        return None, 0
+    return _need(ws, "ws", (torch.uint8,), ws.shape), ws.numel()
+
+
+def moe_balance_loss(layer: Layer, logits, topk_idx, counts, mean_prob, loss, ws, valid=None) -> None:
+    _, f32, i32, _, u8 = _types()
+    T, E, k = _rows_cols(logits, "logits")[0], layer.n_experts, layer.top_k
+    p, nbytes = _need_ws(ws)
+    _check(lib().moe_balance_loss(ctypes.byref(layer.c), _need(logits, "logits", f32, (T, E)), _need(topk_idx, "topk_idx", i32, (T, k)),
+                                  None if valid is None else _need(valid, "valid", u8, (T,)), T,
+                                  _need(counts, "counts", i32, (E + 1,)), _need(mean_prob, "mean_prob", f32, (E,)),
+                                  _need(loss, "loss", f32, (1,)), p, nbytes, _stream()))
+
+
+def moe_route_backward(layer: Layer, x, logits, topk_idx, ws, valid=None, counts=None, d_gate=None, d_loss=None, d_logits=None,
+                       d_x=None, d_w_gate=None, d_bias=None) -> None:
+    """The gradients that are not None are written; ``d_x`` float32 or float16."""
+    f16, f32, i32, _, u8 = _types()
+    T, E, k, d = _rows_cols(logits, "logits")[0], layer.n_experts, layer.top_k, layer.d_model
+
+    def opt(t, what, dtypes, shape):
+        return None if t is None else _need(t, what, dtypes, shape)
+
+    p, nbytes = _need_ws(ws)
+    _check(lib().moe_route_backward(
+        ctypes.byref(layer.c), opt(x, "x", f16, (T, d)), _need(logits, "logits", f32, (T, E)),
+        _need(topk_idx, "topk_idx", i32, (T, k)), opt(valid, "valid", u8, (T,)), T, opt(counts, "counts", i32, (E + 1,)),
+        opt(d_gate, "d_gate", f32, (T, k)), opt(d_loss, "d_loss", f32, (1,)), opt(d_logits, "d_logits", f32, (T, E)),
+        opt(d_x, "d_x", f16 + f32, (T, d)), OUT_F32 if d_x is None else _out_type(d_x, "d_x"),
+        opt(d_w_gate, "d_w_gate", f32, (E, d)), opt(d_bias, "d_bias", f32, (E,)), p, nbytes, _stream()))
+
+
 def moe_synth_fill_f16(dst, first: int, seed: int, stream_id: int, scale: float, kind: int) -> None:
     _check(lib().moe_synth_fill_f16(_ptr(dst), dst.numel(), first, seed, stream_id, scale, kind, _stream()))
 
@@ -345,3 +538,23 @@ def quantize_mat8(w_fp16) -> Mat:
     zero = torch.empty((out, inn // GROUP), dtype=torch.float16, device=w_fp16.device)
     moe_quantize_int8(w_fp16, codes, scale, zero)
     return Mat(codes, scale, zero)
+
+
+def quantize_mat_fp8(w_fp16) -> Mat:
+    """Device-side 16-bit -> e4m3 switch of one matrix (moe_quantize_fp8)."""
+    import torch
+    out, inn = w_fp16.shape
+    codes = torch.empty((out, inn), dtype=torch.uint8, device=w_fp16.device)
+    scale = torch.empty((_blocks(out), _blocks(inn)), dtype=torch.float32, device=w_fp16.device)
+    moe_quantize_fp8(w_fp16, codes, scale)
+    return Mat(codes, scale)
+
+
+def transpose_mat_fp8(m: Mat) -> Mat:
+    """The transposed e4m3 matrix (moe_transpose_fp8)."""
+    import torch
+    out, inn = m.data.shape
+    codes = torch.empty((inn, out), dtype=torch.uint8, device=m.data.device)
+    scale = torch.empty((_blocks(inn), _blocks(out)), dtype=torch.float32, device=m.data.device)
+    moe_transpose_fp8(m, codes, scale)
+    return Mat(codes, scale)

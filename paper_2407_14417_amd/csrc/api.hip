@@ -8,6 +8,8 @@
 #include <cstring>
 
 #include "common.hpp"
+#include "fp8.hpp"
+#include "gate_grad.hpp"
 #include "kernels.hpp"
 
 using namespace moemix;
@@ -30,6 +32,16 @@ int check_hip(hipStream_t) {
     return MOE_OK;
 }
 
+// Quantized matrices come with scales, and those of integer codes with zeros.
+bool lacks_scales(const moe_expert& x) {
+    if (x.prec == MOE_PREC_FP16) return false;
+    const bool scales = x.w1.scale && x.w3.scale && x.w2.scale;
+    return !scales || (x.prec != MOE_PREC_FP8B128 && (!x.w1.zero || !x.w3.zero || !x.w2.zero));
+}
+const char* scales_needed(const moe_expert& x) {
+    return x.prec == MOE_PREC_FP8B128 ? "e4m3 matrices need scale" : "quantized matrices need scale and zero";
+}
+
 int check_layer(const moe_layer* L) {
     if (!L) return fail(MOE_EINVAL, "layer is NULL");
     if (!L->w_gate || !L->experts) return fail(MOE_EINVAL, "layer.w_gate / layer.experts is NULL");
@@ -43,11 +55,9 @@ int check_layer(const moe_layer* L) {
         return fail(MOE_ESHAPE, "top_k=%d outside [1, min(n_experts, %d)]", L->top_k, MOE_MAX_TOPK);
     for (int e = 0; e < L->n_experts; ++e) {
         const moe_expert& x = L->experts[e];
-        if (x.prec != MOE_PREC_FP16 && x.prec != MOE_PREC_INT4G64 && x.prec != MOE_PREC_INT8G64)
+        if (x.prec != MOE_PREC_FP16 && x.prec != MOE_PREC_INT4G64 && x.prec != MOE_PREC_INT8G64 && x.prec != MOE_PREC_FP8B128)
             return fail(MOE_EINVAL, "expert %d: unknown precision %d", e, x.prec);
-        if (x.resident && x.prec != MOE_PREC_FP16 &&
-            (!x.w1.scale || !x.w1.zero || !x.w3.scale || !x.w3.zero || !x.w2.scale || !x.w2.zero))
-            return fail(MOE_EINVAL, "expert %d: quantized matrices need scale and zero", e);
+        if (x.resident && lacks_scales(x)) return fail(MOE_EINVAL, "expert %d: %s", e, scales_needed(x));
         if (x.resident) {   // the kernels read weights, scales and zeros with 128-bit loads
             const moe_mat* mats[3] = {&x.w1, &x.w3, &x.w2};
             for (const moe_mat* m : mats)
@@ -64,7 +74,14 @@ constexpr int kDecodeUpBlocks = 1024;
 
 // Which kernels serve T tokens of a block: T == 1 the batch-1 kernels, otherwise the matrix-core path when
 // the shape allows it, else the shape-agnostic kernels.
-bool use_decode(int T) { return T == 1; }
+// Layers with an e4m3 expert take no one-token kernels: those of the e4m3 products read a grouping.
+bool any_fp8(const moe_layer* L) {
+    if (!L->experts || L->n_experts > MOE_MAX_EXPERTS) return false;
+    for (int e = 0; e < L->n_experts; ++e)
+        if (L->experts[e].prec == MOE_PREC_FP8B128) return true;
+    return false;
+}
+bool use_decode(const moe_layer* L, int T) { return T == 1 && !any_fp8(L); }
 bool use_mfma(const moe_layer* L, int rows) {
     return rows > 1 && mfma_shape_ok(L->d_model, L->d_ff) && mfma_rows_ok(rows, L->d_model, L->d_ff);
 }
@@ -93,7 +110,7 @@ bool copies_tokens(const DevExperts& table, int E, const RowMap& rows, int P, co
 }
 
 int y_splits_for(const moe_layer* L, int T) {
-    if (!use_mfma(L, T * L->top_k)) return 1;
+    if (!use_mfma(L, T * L->top_k) || any_fp8(L)) return 1;     // (the e4m3 products write whole sums)
     // (of the shape alone: the experts need not be known when a workspace is sized)
     return plan_mfma(T * L->top_k, L->d_model, L->d_ff, L->n_experts, L->top_k, false).down_splits;
 }
@@ -120,11 +137,12 @@ DevExperts device_table(const moe_layer* L) {
     return t;
 }
 
-int check_ws(const moe_layer* L, int T, void* ws, size_t ws_bytes, Workspace* out) {
+// fp8: room for quantized rows, and no split contractions
+int check_ws(const moe_layer* L, int T, void* ws, size_t ws_bytes, Workspace* out, bool fp8) {
     if (!ws) return fail(MOE_EWORKSPACE, "workspace is NULL");
     if ((uintptr_t)ws % 256) return fail(MOE_EWORKSPACE, "workspace must be 256-byte aligned");
-    int splits = y_splits_for(L, T);
-    *out = carve_workspace(ws, T, L->d_model, L->d_ff, L->n_experts, L->top_k, splits);
+    int splits = fp8 ? 1 : y_splits_for(L, T);
+    *out = carve_workspace(ws, T, L->d_model, L->d_ff, L->n_experts, L->top_k, splits, fp8);
     // (at these widths every workspace that holds the unsplit call has always been enough)
     while (out->bytes > ws_bytes && splits > 1 && half_step_width(L->d_model, L->d_ff)) {
         splits = fewer_splits(L->d_ff, splits, T * L->top_k);
@@ -134,6 +152,78 @@ int check_ws(const moe_layer* L, int T, void* ws, size_t ws_bytes, Workspace* ou
         return fail(MOE_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, out->bytes);
     return MOE_OK;
 }
+int check_ws(const moe_layer* L, int T, void* ws, size_t ws_bytes, Workspace* out) {
+    return check_ws(L, T, ws, ws_bytes, out, any_fp8(L));
+}
+
+// ---- experts held in e4m3: launches of their own; the other kernels see them as deferred
+
+Fp8Mat fp8_mat(const DevMat& m) { return Fp8Mat{m.data, (const float*)m.scale}; }
+
+int32_t fp8_todo(const DevExpert& x) {
+    if (x.prec != MOE_PREC_FP8B128 || x.resident == kDeferred) return kFp8Skip;
+    return x.resident ? kFp8Run : kFp8Missing;
+}
+
+// Does the table hold an expert that the launches of the other precisions have to look at?
+bool others_todo(const DevExperts& table, int E) {
+    for (int e = 0; e < E; ++e)
+        if (table.e[e].prec != MOE_PREC_FP8B128 && table.e[e].resident != kDeferred) return true;
+    return false;
+}
+
+DevExperts without_fp8(const DevExperts& table, int E) {
+    DevExperts t = table;
+    for (int e = 0; e < E; ++e)
+        if (t.e[e].prec == MOE_PREC_FP8B128) t.e[e].resident = kDeferred;
+    return t;
+}
+
+// Rows of x quantized, up-projection, hidden rows quantized, down-projection into y, for every e4m3 expert that the table does
+// not defer.  x has x_rows rows, P rows are multiplied.
+void run_fp8(const DevExperts& table, int E, const RowMap& rows, const half_t* x, int x_rows, int P, int d, int f, const Workspace& w,
+             float* y, hipStream_t st) {
+    Fp8Args a;
+    memset(&a, 0, sizeof(a));
+    const bool alone = rows.direct_expert >= 0;
+    bool any = false;
+    a.E = alone ? 1 : E;
+    for (int e = 0; e < a.E; ++e) {
+        const DevExpert& x = table.e[alone ? rows.direct_expert : e];
+        a.todo[e] = fp8_todo(x);
+        a.w[e] = fp8_mat(x.w1);
+        a.w3[e] = fp8_mat(x.w3);
+        any |= a.todo[e] != kFp8Skip;
+    }
+    if (!any) return;
+    a.x = w.x8;
+    a.xs = w.xs;
+    a.offsets = rows.offsets;
+    a.perm = rows.perm;
+    a.status = w.status;
+    a.y = w.h;
+    a.P = P;
+    a.top_k = rows.top_k;
+    a.x_rows = x_rows;
+    a.N = f;
+    a.K = d;
+    launch_quantize_fp8_rows(x, x_rows, d, w.x8, w.xs, st);
+    {
+        TraceScope trace(kKernelUp, st);
+        launch_fp8_matmul(a, true, true, st);
+    }
+    launch_quantize_fp8_rows(w.h, P, f, w.h8, w.hs, st);
+    for (int e = 0; e < a.E; ++e) a.w[e] = fp8_mat(table.e[alone ? rows.direct_expert : e].w2);
+    a.x = w.h8;
+    a.xs = w.hs;
+    a.perm = nullptr;
+    a.y = y;
+    a.x_rows = P;
+    a.N = d;
+    a.K = f;
+    TraceScope trace(kKernelDown, st);
+    launch_fp8_matmul(a, false, false, st);
+}
 
 // (RMSNorm +) gating -> grouping -> experts -> weighted average (+ residual), all on `st`.
 // rms_gain != null: the block input is RMSNorm(x) * rms_gain, computed by the gating kernel into ws.xn.
@@ -141,7 +231,7 @@ int layer_body(const moe_layer* L, const DevExperts& table, const half_t* x, int
                const half_t* residual, half_t* out, int32_t* idx_out, float* gate_out, const Workspace& w,
                bool reset_status, hipStream_t st) {
     const int d = L->d_model, f = L->d_ff, E = L->n_experts, k = L->top_k;
-    if (use_decode(T)) {
+    if (use_decode(L, T)) {
         // batch-1 decode: two launches.  The gating network (and the RMSNorm of the chain) runs inside the
         // up-projection launch, no grouping is needed, the weighted average is fused into the down-projection.
         // The up-projection launch clears the word it is given: the status word for the first block of a call, a
@@ -160,11 +250,25 @@ int layer_body(const moe_layer* L, const DevExperts& table, const half_t* x, int
                  reset_status ? w.status : nullptr, st, rms_gain, eps, to_xn ? w.xn : nullptr);
     if (to_xn) x = w.xn;
     // few pairs: no launch for the grouping, unless that is the kernel the caller wants to measure
-    const bool inline_groups = mfma && group_inline_ok(T * k, p.ct) && !trace_armed(kKernelPermute);
+    const bool fp8 = any_fp8(L);
+    const bool inline_groups = mfma && group_inline_ok(T * k, p.ct) && !trace_armed(kKernelPermute) && !fp8;
     if (!inline_groups) launch_permute(w.idx, T * k, E, w.counts, w.offsets, w.perm, w.inv, w.status, st);
     RowMap rows{w.offsets, w.perm, k, -1, 0};
     if (inline_groups) rows.idx = w.idx;
-    if (mfma) {
+    if (fp8) {
+        const DevExperts others = without_fp8(table, E);
+        if (others_todo(table, E)) {
+            if (mfma) {
+                launch_ffn_up_mfma(others, E, rows, T * k, x, d, f, w.h, p.ct, w.status, st);
+                launch_ffn_down_mfma(others, E, rows, T * k, w.h, d, f, w.y, p.ct, 1, split_stride, w.status, st);
+            } else {
+                launch_ffn_up(others, E, rows, x, d, f, w.h, w.status, st);
+                launch_ffn_down(others, E, rows, w.h, d, f, w.y, w.status, st);
+            }
+        }
+        run_fp8(table, E, rows, x, T, T * k, d, f, w, w.y, st);
+        launch_combine(w.y, 1, split_stride, w.gate, w.inv, T, d, k, residual, out, st);
+    } else if (mfma) {
         launch_ffn_up_mfma(table, E, rows, T * k, x, d, f, w.h, p.ct, w.status, st);
         launch_ffn_down_mfma(table, E, rows, T * k, w.h, d, f, w.y, p.ct, w.y_splits, split_stride, w.status, st);
         launch_combine(w.y, w.y_splits, split_stride, w.gate, inline_groups ? nullptr : w.inv, T, d, k, residual, out, st,
@@ -222,7 +326,8 @@ int moe_trace_kernel(int kernel, void* start_event, void* stop_event) {
 size_t moe_workspace_bytes(const moe_layer* layer, int n_tokens) {
     if (!layer || n_tokens < 1 || layer->d_model < 1 || layer->d_ff < 1 || layer->n_experts < 1 || layer->top_k < 1)
         return 0;
-    return carve_workspace(nullptr, n_tokens, layer->d_model, layer->d_ff, layer->n_experts, layer->top_k, asked_splits(layer, n_tokens)).bytes;
+    return carve_workspace(nullptr, n_tokens, layer->d_model, layer->d_ff, layer->n_experts, layer->top_k, asked_splits(layer, n_tokens),
+                           any_fp8(layer)).bytes;
 }
 
 int moe_route(const moe_layer* layer, const void* x, int T, int32_t* topk_idx, float* topk_gate, moe_stream_t stream) {
@@ -263,7 +368,9 @@ int moe_expert_ffn_mixed(const moe_layer* layer, int expert, const void* x_rows,
     RowMap rows{nullptr, nullptr, layer->top_k, expert, n};
     const int d = layer->d_model, f = layer->d_ff;
     launch_zero_words(w.status, 1, st);   // the status word describes this call
-    if (use_decode(n)) {
+    if (table.e[expert].prec == MOE_PREC_FP8B128) {
+        run_fp8(table, layer->n_experts, rows, (const half_t*)x_rows, n, n, d, f, w, y, st);
+    } else if (n == 1) {
         // one row: the batch-1 kernels, with the routing result "this expert, weight 1" written to the workspace
         launch_single_route(w.idx, w.gate, expert, st);
         launch_decode_up(table, w.idx, (const half_t*)x_rows, d, f, 1, w.h, w.status, kDecodeUpBlocks, st);
@@ -299,7 +406,7 @@ static int launch_form(const moe_layer* layer, int expert, int n, size_t ws_byte
     const int T = alone ? (n + k - 1) / k : n, P = alone ? n : n * k;
     Workspace w;
     if (int rc = check_ws(layer, T, (void*)256, ws_bytes, &w)) return rc;
-    if (use_decode(n) || !use_mfma(layer, P)) return fail(MOE_ESHAPE, "moemix_launch_form: not on the matrix cores");
+    if (use_decode(layer, n) || !use_mfma(layer, P)) return fail(MOE_ESHAPE, "moemix_launch_form: not on the matrix cores");
     const DevExperts table = device_table(layer);
     const RowMap rows{nullptr, nullptr, k, alone ? expert : -1, alone ? n : 0};
     MfmaPlan p = alone ? lone_plan(layer, n, w) : plan_for(layer, P);
@@ -400,6 +507,10 @@ struct MatBytes {
     size_t total() const { return align256(data) + align256(scale) + align256(zero); }
 };
 MatBytes mat_bytes(int prec, int out, int in) {
+    if (prec == MOE_PREC_FP8B128) {
+        const size_t b = (size_t)((out + MOE_FP8_BLOCK - 1) / MOE_FP8_BLOCK) * ((in + MOE_FP8_BLOCK - 1) / MOE_FP8_BLOCK);
+        return MatBytes{(size_t)out * in, b * sizeof(float), 0};
+    }
     if (prec == MOE_PREC_INT4G64 || prec == MOE_PREC_INT8G64) {
         const size_t g = (size_t)out * (in / MOE_GROUP) * 2;
         return MatBytes{prec == MOE_PREC_INT4G64 ? (size_t)out * in / 2 : (size_t)out * in, g, g};
@@ -417,7 +528,9 @@ hipError_t copy_mat(const moe_mat& src, const MatBytes& b, char*& cursor, DevMat
         e = hipMemcpyAsync(cursor, src.scale, b.scale, hipMemcpyHostToDevice, st);
         dst->scale = (const half_t*)cursor;
         cursor += align256(b.scale);
-        if (e == hipSuccess) e = hipMemcpyAsync(cursor, src.zero, b.zero, hipMemcpyHostToDevice, st);
+    }
+    if (b.zero && e == hipSuccess) {
+        e = hipMemcpyAsync(cursor, src.zero, b.zero, hipMemcpyHostToDevice, st);
         dst->zero = (const half_t*)cursor;
         cursor += align256(b.zero);
     }
@@ -429,7 +542,7 @@ hipError_t copy_mat(const moe_mat& src, const MatBytes& b, char*& cursor, DevMat
 void run_experts(const moe_layer* L, const DevExperts& table, const half_t* x, int T, const Workspace& w,
                  const half_t* decode_residual, half_t* out, hipStream_t st) {
     const int d = L->d_model, f = L->d_ff, E = L->n_experts, k = L->top_k;
-    if (use_decode(T)) {
+    if (use_decode(L, T)) {
         launch_decode_up(table, w.idx, x, d, f, k, w.h, w.status, kDecodeUpBlocks, st);
         if (decode_shape_ok(d, f)) launch_decode_down(table, w.idx, w.gate, w.h, d, f, k, decode_residual, out, w.status, st);
         else launch_decode_down_slots(table, w.idx, w.h, d, f, k, w.y, w.status, st);
@@ -437,6 +550,20 @@ void run_experts(const moe_layer* L, const DevExperts& table, const half_t* x, i
     }
     RowMap rows{w.offsets, w.perm, k, -1, 0};
     const size_t split_stride = (size_t)T * k * d;
+    if (any_fp8(L)) run_fp8(table, E, rows, x, T, T * k, d, f, w, w.y, st);
+    if (!others_todo(table, E)) return;
+    if (any_fp8(L)) {
+        const DevExperts others = without_fp8(table, E);
+        if (use_mfma(L, T * k)) {
+            const MfmaPlan p = plan_for(L, T * k);
+            launch_ffn_up_mfma(others, E, rows, T * k, x, d, f, w.h, p.ct, w.status, st);
+            launch_ffn_down_mfma(others, E, rows, T * k, w.h, d, f, w.y, p.ct, w.y_splits, split_stride, w.status, st);
+        } else {
+            launch_ffn_up(others, E, rows, x, d, f, w.h, w.status, st);
+            launch_ffn_down(others, E, rows, w.h, d, f, w.y, w.status, st);
+        }
+        return;
+    }
     if (use_mfma(L, T * k)) {
         const MfmaPlan p = plan_for(L, T * k);
         launch_ffn_up_mfma(table, E, rows, T * k, x, d, f, w.h, p.ct, w.status, st);
@@ -480,7 +607,7 @@ int moe_layer_forward_swap(const moe_layer* layer, const moe_swap* swap, const v
     const half_t* xin = (const half_t*)x;
 
     // gating, then the one host round trip of this path: which experts were chosen?
-    const bool to_xn = !use_decode(T) && use_mfma(layer, T * k) &&
+    const bool to_xn = !use_decode(layer, T) && use_mfma(layer, T * k) &&
                        copies_tokens(device_table(layer), E, RowMap{w.offsets, w.perm, k, -1, 0}, T * k, xin, d, f, plan_for(layer, T * k).ct);
     launch_route(xin, (const half_t*)layer->w_gate, layer->gate_bias, T, d, E, k, w.idx, w.gate, topk_idx_out, topk_gate_out,
                  w.status, st, nullptr, 0.0f, to_xn ? w.xn : nullptr);
@@ -496,9 +623,9 @@ int moe_layer_forward_swap(const moe_layer* layer, const moe_swap* swap, const v
         seen |= 1u << ex;
         const moe_expert& he = swap->host_experts[ex];
         if (expert_resident(layer->experts[ex]) || !he.w1.data || !he.w3.data || !he.w2.data) continue;
-        if (layer->experts[ex].prec != MOE_PREC_FP16 &&
-            (!he.w1.scale || !he.w1.zero || !he.w3.scale || !he.w3.zero || !he.w2.scale || !he.w2.zero))
-            return fail(MOE_EINVAL, "host expert %d: quantized matrices need scale and zero", ex);
+        moe_expert stored = he;
+        stored.prec = layer->experts[ex].prec;
+        if (lacks_scales(stored)) return fail(MOE_EINVAL, "host expert %d: %s", ex, scales_needed(stored));
         missed[n_miss++] = ex;
     }
     if (n_missed) *n_missed = n_miss;
@@ -506,7 +633,7 @@ int moe_layer_forward_swap(const moe_layer* layer, const moe_swap* swap, const v
     // pass over the resident experts; the missed ones wait for their copies
     DevExperts table = device_table(layer);
     for (int i = 0; i < n_miss; ++i) table.e[missed[i]].resident = kDeferred;
-    const bool decode = use_decode(T);
+    const bool decode = use_decode(layer, T);
     if (!decode) launch_permute(w.idx, T * k, E, w.counts, w.offsets, w.perm, w.inv, w.status, st);
     run_experts(layer, table, xin, T, w, nullptr, (half_t*)out, st);
 
@@ -562,8 +689,10 @@ int moe_chain_forward(const moe_layer* layers, const void* const* rms_gain, int 
             layers[l].n_experts != layers[0].n_experts || layers[l].top_k != layers[0].top_k)
             return fail(MOE_ESHAPE, "layer %d differs in shape from layer 0", l);
     }
+    bool fp8 = false;
+    for (int l = 0; l < n_layers; ++l) fp8 |= any_fp8(&layers[l]);
     Workspace w;
-    if (int rc = check_ws(&layers[0], T, ws, ws_bytes, &w)) return rc;
+    if (int rc = check_ws(&layers[0], T, ws, ws_bytes, &w, fp8)) return rc;
     hipStream_t st = (hipStream_t)stream;
     const int k = layers[0].top_k;
     for (int l = 0; l < n_layers; ++l) {
@@ -609,6 +738,172 @@ int moe_quantize_int8(const void* w_fp16, int out, int in, void* codes, void* sc
     if (in % MOE_GROUP) return fail(MOE_ESHAPE, "moe_quantize_int8: in=%d not a multiple of %d", in, MOE_GROUP);
     launch_quantize_int8((const half_t*)w_fp16, out, in, (uint8_t*)codes, (half_t*)scale, (half_t*)zero,
                          (hipStream_t)stream);
+    return check_hip((hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------- 8-bit floating point
+
+namespace {
+
+constexpr int kFp8MaxDim = 1 << 20, kFp8MaxRows = 1 << 22;
+
+int check_fp8_shape(const char* who, int out, int in) {
+    if (out < 0 || in < 0) return fail(MOE_EINVAL, "%s: negative size", who);
+    if (in % 16) return fail(MOE_ESHAPE, "%s: in=%d not a multiple of 16", who, in);
+    if (out > kFp8MaxDim || in > kFp8MaxDim) return fail(MOE_ESHAPE, "%s: out=%d, in=%d past %d", who, out, in, kFp8MaxDim);
+    return MOE_OK;
+}
+
+int check_fp8_mat(const char* who, const moe_mat& m) {
+    if (!m.data || !m.scale) return fail(MOE_EINVAL, "%s: a matrix without codes or scales", who);
+    if ((uintptr_t)m.data % 16 || (uintptr_t)m.scale % 4)
+        return fail(MOE_EINVAL, "%s: codes must be 16-byte aligned, scales 4-byte", who);
+    return MOE_OK;
+}
+
+int matmul_fp8(const char* who, const moe_mat* w, int n_experts, int out, int in, const void* x_codes, const float* x_scale, int n_rows,
+               const int32_t* offsets, const int32_t* perm, int top_k, int n_pairs, void* y, int y_type, hipStream_t st) {
+    if (int rc = check_fp8_shape(who, out, in)) return rc;
+    if (n_rows < 0 || n_pairs < 0) return fail(MOE_EINVAL, "%s: negative size", who);
+    if (n_rows > kFp8MaxDim || n_pairs > kFp8MaxDim) return fail(MOE_ESHAPE, "%s: %d rows, %d pairs past %d", who, n_rows, n_pairs, kFp8MaxDim);
+    if (y_type != MOE_OUT_F32 && y_type != MOE_OUT_F16) return fail(MOE_EINVAL, "%s: y_type=%d", who, y_type);
+    if (!w) return fail(MOE_EINVAL, "%s: NULL argument", who);
+    Fp8Args a;
+    memset(&a, 0, sizeof(a));
+    for (int e = 0; e < n_experts; ++e) {
+        if (int rc = check_fp8_mat(who, w[e])) return rc;
+        a.w[e] = Fp8Mat{(const uint8_t*)w[e].data, (const float*)w[e].scale};
+        a.todo[e] = kFp8Run;
+    }
+    if (n_pairs == 0 || out == 0) return MOE_OK;
+    if (!y || (in && (!x_codes || !x_scale))) return fail(MOE_EINVAL, "%s: NULL argument", who);
+    if (n_rows < 1) return fail(MOE_ESHAPE, "%s: %d pairs of no rows", who, n_pairs);
+    if (!perm && n_rows < n_pairs) return fail(MOE_ESHAPE, "%s: %d rows for %d rows of y", who, n_rows, n_pairs);
+    if ((uintptr_t)x_codes % 16 || (uintptr_t)x_scale % 4 || (uintptr_t)y % (y_type == MOE_OUT_F16 ? 2 : 4))
+        return fail(MOE_EINVAL, "%s: x_codes must be 16-byte aligned, x_scale and y naturally", who);
+    a.x = (const uint8_t*)x_codes;
+    a.xs = x_scale;
+    a.offsets = offsets;
+    a.perm = perm;
+    a.y = y;
+    a.E = n_experts;
+    a.P = n_pairs;
+    a.top_k = top_k;
+    a.x_rows = n_rows;
+    a.N = out;
+    a.K = in;
+    launch_fp8_matmul(a, false, y_type == MOE_OUT_F16, st);
+    return check_hip(st);
+}
+
+}  // namespace
+
+int moe_quantize_fp8(const void* w_fp16, int out, int in, void* codes, float* scale, moe_stream_t stream) {
+    if (int rc = check_fp8_shape("moe_quantize_fp8", out, in)) return rc;
+    if (!w_fp16 || !codes || !scale) return fail(MOE_EINVAL, "moe_quantize_fp8: NULL argument");
+    if ((uintptr_t)codes % 16) return fail(MOE_EINVAL, "moe_quantize_fp8: codes must be 16-byte aligned");
+    launch_quantize_fp8((const half_t*)w_fp16, out, in, (uint8_t*)codes, scale, (hipStream_t)stream);
+    return check_hip((hipStream_t)stream);
+}
+
+int moe_dequant_fp8(const moe_mat* m, int out, int in, void* w_fp16, moe_stream_t stream) {
+    if (int rc = check_fp8_shape("moe_dequant_fp8", out, in)) return rc;
+    if (!m || !w_fp16) return fail(MOE_EINVAL, "moe_dequant_fp8: NULL argument");
+    if (int rc = check_fp8_mat("moe_dequant_fp8", *m)) return rc;
+    if ((uintptr_t)w_fp16 % 16) return fail(MOE_EINVAL, "moe_dequant_fp8: w_fp16 must be 16-byte aligned");
+    launch_dequant_fp8(Fp8Mat{(const uint8_t*)m->data, (const float*)m->scale}, out, in, (half_t*)w_fp16, (hipStream_t)stream);
+    return check_hip((hipStream_t)stream);
+}
+
+int moe_quantize_fp8_rows(const void* x, int n, int in, void* codes, float* scale, moe_stream_t stream) {
+    if (int rc = check_fp8_shape("moe_quantize_fp8_rows", 0, in)) return rc;
+    if (n < 0) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: negative size");
+    if (n > kFp8MaxRows) return fail(MOE_ESHAPE, "moe_quantize_fp8_rows: n=%d past %d", n, kFp8MaxRows);
+    if (!x || !codes || !scale) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: NULL argument");
+    if ((uintptr_t)codes % 16) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: codes must be 16-byte aligned");
+    launch_quantize_fp8_rows((const half_t*)x, n, in, (uint8_t*)codes, scale, (hipStream_t)stream);
+    return check_hip((hipStream_t)stream);
+}
+
+int moe_transpose_fp8(const moe_mat* m, int out, int in, void* codes_t, float* scale_t, moe_stream_t stream) {
+    if (int rc = check_fp8_shape("moe_transpose_fp8", out, in)) return rc;
+    if (out % 16) return fail(MOE_ESHAPE, "moe_transpose_fp8: out=%d not a multiple of 16", out);
+    if (!m || !codes_t || !scale_t) return fail(MOE_EINVAL, "moe_transpose_fp8: NULL argument");
+    if (int rc = check_fp8_mat("moe_transpose_fp8", *m)) return rc;
+    if ((uintptr_t)codes_t % 16) return fail(MOE_EINVAL, "moe_transpose_fp8: codes_t must be 16-byte aligned");
+    launch_transpose_fp8(Fp8Mat{(const uint8_t*)m->data, (const float*)m->scale}, out, in, (uint8_t*)codes_t, scale_t, (hipStream_t)stream);
+    return check_hip((hipStream_t)stream);
+}
+
+int moe_matmul_fp8(const moe_mat* w, int out, int in, const void* x_codes, const float* x_scale, int n, void* y, int y_type,
+                   moe_stream_t stream) {
+    return matmul_fp8("moe_matmul_fp8", w, 1, out, in, x_codes, x_scale, n, nullptr, nullptr, 1, n, y, y_type, (hipStream_t)stream);
+}
+
+int moe_matmul_fp8_grouped(const moe_mat* w, int n_experts, int out, int in, const void* x_codes, const float* x_scale, int n_rows,
+                           const int32_t* offsets, const int32_t* perm, int top_k, int n_pairs, void* y, int y_type,
+                           moe_stream_t stream) {
+    if (n_experts < 1 || n_experts > MOE_MAX_EXPERTS)
+        return fail(MOE_ESHAPE, "moe_matmul_fp8_grouped: n_experts=%d outside [1, %d]", n_experts, MOE_MAX_EXPERTS);
+    if (!offsets) return fail(MOE_EINVAL, "moe_matmul_fp8_grouped: offsets is NULL");
+    if (perm && top_k < 1) return fail(MOE_ESHAPE, "moe_matmul_fp8_grouped: top_k=%d < 1", top_k);
+    return matmul_fp8("moe_matmul_fp8_grouped", w, n_experts, out, in, x_codes, x_scale, n_rows, offsets, perm, top_k, n_pairs, y, y_type,
+                      (hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------- training the gate
+
+int moe_route_logits(const moe_layer* layer, const void* x, int T, float* logits, int32_t* topk_idx, float* topk_gate,
+                     moe_stream_t stream) {
+    if (int rc = check_layer(layer)) return rc;
+    if (!x || !logits || !topk_idx || !topk_gate) return fail(MOE_EINVAL, "moe_route_logits: NULL argument");
+    if (T < 1) return fail(MOE_ESHAPE, "moe_route_logits: T=%d < 1", T);
+    launch_route_logits((const half_t*)x, (const half_t*)layer->w_gate, layer->gate_bias, T, layer->d_model, layer->n_experts, layer->top_k,
+                        topk_idx, topk_gate, logits, (hipStream_t)stream);
+    return check_hip((hipStream_t)stream);
+}
+
+size_t moe_gate_workspace_bytes(const moe_layer* layer, int T) {
+    if (!layer || T < 1 || layer->d_model < 1 || layer->n_experts < 1) return 0;
+    return carve_gate_workspace(nullptr, T, layer->d_model, layer->n_experts).bytes;
+}
+
+static int check_gate_ws(const moe_layer* L, int T, void* ws, size_t ws_bytes, GateWorkspace* out) {
+    if (!ws) return fail(MOE_EWORKSPACE, "workspace is NULL");
+    if ((uintptr_t)ws % 256) return fail(MOE_EWORKSPACE, "workspace must be 256-byte aligned");
+    *out = carve_gate_workspace(ws, T, L->d_model, L->n_experts);
+    if (ws_bytes < out->bytes) return fail(MOE_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, out->bytes);
+    return MOE_OK;
+}
+
+int moe_balance_loss(const moe_layer* layer, const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int32_t* counts,
+                     float* mean_prob, float* loss, void* ws, size_t ws_bytes, moe_stream_t stream) {
+    if (int rc = check_layer(layer)) return rc;
+    if (!logits || !topk_idx || !counts || !mean_prob || !loss) return fail(MOE_EINVAL, "moe_balance_loss: NULL argument");
+    if (T < 1) return fail(MOE_ESHAPE, "moe_balance_loss: T=%d < 1", T);
+    GateWorkspace w;
+    if (int rc = check_gate_ws(layer, T, ws, ws_bytes, &w)) return rc;
+    launch_balance_loss(logits, topk_idx, valid, T, layer->n_experts, layer->top_k, counts, mean_prob, loss, w, (hipStream_t)stream);
+    return check_hip((hipStream_t)stream);
+}
+
+int moe_route_backward(const moe_layer* layer, const void* x, const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T,
+                       const int32_t* counts, const float* d_gate, const float* d_loss, float* d_logits, void* d_x, int d_x_type,
+                       float* d_w_gate, float* d_bias, void* ws, size_t ws_bytes, moe_stream_t stream) {
+    if (int rc = check_layer(layer)) return rc;
+    if (!logits || !topk_idx) return fail(MOE_EINVAL, "moe_route_backward: NULL argument");
+    if (!d_gate && !d_loss) return fail(MOE_EINVAL, "moe_route_backward: neither d_gate nor d_loss");
+    if (!d_loss != !counts) return fail(MOE_EINVAL, "moe_route_backward: d_loss and counts go together");
+    if (!d_logits && !d_x && !d_w_gate && !d_bias) return fail(MOE_EINVAL, "moe_route_backward: no gradient asked for");
+    if (d_w_gate && !x) return fail(MOE_EINVAL, "moe_route_backward: d_w_gate needs x");
+    if (d_x_type != MOE_OUT_F32 && d_x_type != MOE_OUT_F16) return fail(MOE_EINVAL, "moe_route_backward: d_x_type=%d", d_x_type);
+    if (T < 1) return fail(MOE_ESHAPE, "moe_route_backward: T=%d < 1", T);
+    GateWorkspace w;
+    if (int rc = check_gate_ws(layer, T, ws, ws_bytes, &w)) return rc;
+    const GateGradArgs a{(const half_t*)x, (const half_t*)layer->w_gate, logits, topk_idx, valid, counts, d_gate, d_loss,
+                         d_logits ? d_logits : w.dl, d_x, d_w_gate, d_bias, T, layer->d_model, layer->n_experts, layer->top_k,
+                         d_x_type == MOE_OUT_F16};
+    launch_route_backward(a, w, (hipStream_t)stream);
     return check_hip((hipStream_t)stream);
 }
 

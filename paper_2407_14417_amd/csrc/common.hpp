@@ -56,13 +56,17 @@ struct Workspace {
     half_t* xn;         // [T, d]    normed input of the chain
     half_t* h;          // [T * k, f]  SwiGLU hidden rows, grouped order
     float* y;           // [y_splits][T * k, d]  expert outputs, grouped order, one partial per contraction split
+    uint8_t* x8;        // [T * k, d]    layers with e4m3 experts: quantized rows of the input ([T] of a block, all of one expert alone)
+    float* xs;          // [ceil(d/128), T * k]  and their scales
+    uint8_t* h8;        // [T * k, f]    the same of the hidden rows, grouped order
+    float* hs;          // [ceil(f/128), T * k]
     int y_splits;
     size_t bytes;
 };
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-inline Workspace carve_workspace(void* base, int T, int d, int f, int E, int k, int y_splits = 1) {
+inline Workspace carve_workspace(void* base, int T, int d, int f, int E, int k, int y_splits = 1, bool fp8 = false) {
     Workspace w;
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -83,6 +87,11 @@ inline Workspace carve_workspace(void* base, int T, int d, int f, int E, int k, 
     w.h = (half_t*)take(P * f * sizeof(half_t));
     w.y = (float*)take((size_t)y_splits * P * d * sizeof(float));
     w.y_splits = y_splits;
+    const size_t p8 = fp8 ? P : 0;
+    w.x8 = (uint8_t*)take(p8 * d);
+    w.xs = (float*)take(p8 * ((d + MOE_FP8_BLOCK - 1) / MOE_FP8_BLOCK) * sizeof(float));
+    w.h8 = (uint8_t*)take(p8 * f);
+    w.hs = (float*)take(p8 * ((f + MOE_FP8_BLOCK - 1) / MOE_FP8_BLOCK) * sizeof(float));
     w.bytes = off;
     return w;
 }

@@ -33,6 +33,9 @@ inline bool group_inline_ok(int P, int ct) { return P <= kInlinePairs && ct <= 2
 void launch_route(const half_t* x, const half_t* wg, const float* bias, int T, int d, int E, int k, int32_t* idx,
                   float* gate, int32_t* idx2, float* gate2, int32_t* status, hipStream_t st,
                   const half_t* rms_gain = nullptr, float eps = 0.0f, half_t* xn = nullptr);
+// launch_route with the logits [T, E] written as well
+void launch_route_logits(const half_t* x, const half_t* wg, const float* bias, int T, int d, int E, int k, int32_t* idx, float* gate,
+                         float* logits, hipStream_t st);
 void launch_permute(const int32_t* idx, int P, int E, int32_t* counts, int32_t* offsets, int32_t* perm, int32_t* inv,
                     int32_t* status, hipStream_t st);
 

@@ -14,13 +14,14 @@ namespace moemix {
 // memory; the first wavefront then selects the top_k and computes the softmax over the selected logits.
 // COPY: the token row goes to xn as it is.  (A kernel of its own: with the same line taken by all calls the one for 4096 columns
 // had 213 registers instead of 117, 1792 tokens, 32 experts of 2560 x 640, top-1, 104 -> 113 us a block.)
-template <int NCHUNK, bool COPY>
+// LOGITS: the logits go to logits_out (also a kernel of its own).
+template <int NCHUNK, bool COPY, bool LOGITS = false>
 __global__ __launch_bounds__(256) void route_kernel(const half_t* __restrict__ x, const half_t* __restrict__ wg,
                                                      const float* __restrict__ bias, int d, int E, int k,
                                                      int32_t* __restrict__ idx, float* __restrict__ gate,
                                                      int32_t* __restrict__ idx2, float* __restrict__ gate2,
                                                      int32_t* __restrict__ status, const half_t* __restrict__ rms_gain,
-                                                     float eps, half_t* __restrict__ xn) {
+                                                     float eps, half_t* __restrict__ xn, float* __restrict__ logits_out) {
     __shared__ float logit[MOE_MAX_EXPERTS];
     const int t = blockIdx.x;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -55,6 +56,7 @@ __global__ __launch_bounds__(256) void route_kernel(const half_t* __restrict__ x
         }
     }
     __syncthreads();
+    if (LOGITS && tid < E) logits_out[(size_t)t * E + tid] = logit[tid];
     if (wave == 0) {
         int sel[MOE_MAX_TOPK];
         float lsel[MOE_MAX_TOPK], g[MOE_MAX_TOPK];
@@ -79,15 +81,27 @@ void launch_route(const half_t* x, const half_t* wg, const float* bias, int T, i
     const auto launch = [&](auto copy) {
         constexpr bool COPY = decltype(copy)::value;
         if (d <= 2048)
-            route_kernel<4, COPY><<<T, 256, 0, st>>>(x, wg, bias, d, E, k, idx, gate, idx2, gate2, status, rms_gain, eps, xn);
+            route_kernel<4, COPY><<<T, 256, 0, st>>>(x, wg, bias, d, E, k, idx, gate, idx2, gate2, status, rms_gain, eps, xn, nullptr);
         else if (d <= 4096)
-            route_kernel<8, COPY><<<T, 256, 0, st>>>(x, wg, bias, d, E, k, idx, gate, idx2, gate2, status, rms_gain, eps, xn);
+            route_kernel<8, COPY><<<T, 256, 0, st>>>(x, wg, bias, d, E, k, idx, gate, idx2, gate2, status, rms_gain, eps, xn, nullptr);
         else
             route_kernel<kGateMaxChunks, COPY><<<T, 256, 0, st>>>(x, wg, bias, d, E, k, idx, gate, idx2, gate2, status,
-                                                                   rms_gain, eps, xn);
+                                                                   rms_gain, eps, xn, nullptr);
     };
     if (xn && !rms_gain) launch(std::true_type{});
     else launch(std::false_type{});
+}
+
+void launch_route_logits(const half_t* x, const half_t* wg, const float* bias, int T, int d, int E, int k, int32_t* idx, float* gate,
+                         float* logits, hipStream_t st) {
+    TraceScope trace(kKernelRoute, st);
+    const auto launch = [&](auto chunks) {
+        route_kernel<decltype(chunks)::value, false, true><<<T, 256, 0, st>>>(x, wg, bias, d, E, k, idx, gate, nullptr, nullptr, nullptr,
+                                                                              nullptr, 0.0f, nullptr, logits);
+    };
+    if (d <= 2048) launch(std::integral_constant<int, 4>{});
+    else if (d <= 4096) launch(std::integral_constant<int, 8>{});
+    else launch(std::integral_constant<int, kGateMaxChunks>{});
 }
 
 // One workgroup of 16 wavefronts; wavefront w owns the w-th of 16 contiguous runs of pairs and walks it 64 at a time.

@@ -1,0 +1,527 @@
+"""The e4m3 form on the device: quantizers bit for bit, products against 64 bits within bounds derived from the arithmetic, and experts of this
+precision in the block."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2407_14417_amd import binding as mm
+from tests import common, fp8_ref
+from tests.common import assert_ffn_close
+from tests.gpu_common import dev, device_layer, device_mat, host_expert
+
+pytestmark = pytest.mark.gpu
+
+
+def rng_of(*key):
+    return np.random.default_rng(list(key))
+
+
+def normal(rng, *shape, scale=1.0):
+    return (rng.standard_normal(shape) * scale).astype(np.float16)
+
+
+def quantized_matrix(rng, out, inn, scale=0.02):
+    codes, s = fp8_ref.quantize_matrix(normal(rng, out, inn, scale=scale))
+    return codes, s
+
+
+def on_device(m):
+    return mm.Mat(dev(m[0]), dev(m[1]))
+
+
+def spoiled(shape, dtype):
+    return torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+
+
+# ---------------------------------------------------------------- quantizers
+
+HARD = ["plain", "zeros", "tiny", "huge", "outlier", "inf", "nan"]
+
+
+def hard_rows(kind, n, inn, rng):
+    x = normal(rng, n, inn)
+    if kind == "zeros":
+        x[n // 2] = 0
+        x[0, : 128] = -0.0
+    elif kind == "tiny":
+        x = (x.astype(np.float32) * 6e-8).astype(np.float16)          # subnormal halves
+    elif kind == "huge":
+        x = np.clip(x.astype(np.float32) * 3e4, -65504, 65504).astype(np.float16)
+    elif kind == "outlier":
+        x[:, ::37] *= np.float16(300)
+    elif kind == "inf":
+        x[n // 2, inn // 2] = -np.inf
+    elif kind == "nan":
+        x[n - 1, inn - 1] = np.nan
+    return x
+
+
+@pytest.mark.parametrize("n,inn", [(1, 16), (3, 48), (7, 128), (33, 144), (5, 1488), (70, 4096)])
+@pytest.mark.parametrize("kind", HARD)
+def test_quantized_rows_bit_for_bit(n, inn, kind):
+    x = hard_rows(kind, n, inn, rng_of(n, inn, 1))
+    codes, scale = spoiled((-(-inn // 128), n), torch.float32), None
+    scale, codes = codes, torch.full((n, inn), 0x55, dtype=torch.uint8, device="cuda")
+    mm.moe_quantize_fp8_rows(dev(x), codes, scale)
+    want, want_scale = fp8_ref.quantize_rows(x)
+    got = codes.cpu().numpy()
+    nan = (want & 0x7F) == 0x7F
+    assert np.array_equal(got[~nan], want[~nan]) and np.all((got[nan] & 0x7F) == 0x7F)
+    assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
+
+
+def test_quantized_rows_off_16_byte_boundaries():
+    x = normal(rng_of(2), 9 * 272 + 3)
+    t = dev(x)[3:].view(9, 272)
+    codes, scale = torch.empty(9, 272, dtype=torch.uint8, device="cuda"), torch.empty(3, 9, device="cuda")
+    mm.moe_quantize_fp8_rows(t, codes, scale)
+    want, want_scale = fp8_ref.quantize_rows(x[3:].reshape(9, 272))
+    assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scale.cpu().numpy(), want_scale)
+
+
+@pytest.mark.parametrize("out,inn", [(1, 16), (15, 48), (128, 128), (129, 144), (200, 640), (1001, 272)])
+@pytest.mark.parametrize("kind", ["plain", "zeros", "outlier", "inf", "nan"])
+def test_quantized_matrix_and_back_bit_for_bit(out, inn, kind):
+    w = hard_rows(kind, out, inn, rng_of(out, inn, 3))
+    m = mm.quantize_mat_fp8(dev(w))
+    codes, scale = fp8_ref.quantize_matrix(w)
+    got = m.data.cpu().numpy()
+    nan = (codes & 0x7F) == 0x7F
+    assert np.array_equal(got[~nan], codes[~nan]) and np.all((got[nan] & 0x7F) == 0x7F)
+    assert np.array_equal(m.scale.cpu().numpy(), scale, equal_nan=True)
+    back = spoiled((out, inn), torch.float16)
+    mm.moe_dequant_fp8(m, out, inn, back)
+    with np.errstate(invalid="ignore"):
+        want = fp8_ref.matrix_values(codes, scale).astype(np.float32).astype(np.float16)
+    assert np.array_equal(back.cpu().numpy(), want, equal_nan=True)
+    # quantizing once more changes nothing: the largest value of a block is a code's
+    if kind == "plain":
+        half_step = np.abs(w.astype(np.float64)) * 2.0 ** -4 * (1 + 2.0 ** -20) + np.repeat(np.repeat(scale, 128, 0), 128, 1)[:out, :inn] * 2.0 ** -10
+        assert np.all(np.abs(fp8_ref.matrix_values(codes, scale) - w.astype(np.float64)) <= half_step)
+
+
+@pytest.mark.parametrize("out,inn", [(16, 16), (128, 256), (144, 48), (272, 400)])
+def test_transposed_codes(out, inn):
+    codes, scale = quantized_matrix(rng_of(out, inn), out, inn)
+    t = mm.transpose_mat_fp8(on_device((codes, scale)))
+    assert np.array_equal(t.data.cpu().numpy(), codes.T) and np.array_equal(t.scale.cpu().numpy(), scale.T)
+
+
+# ---------------------------------------------------------------- products
+
+def check_product(y, xv, wv, inn, half, what, cut=True):
+    ref, mag = fp8_ref.product(xv, wv)
+    bound = fp8_ref.sum_bound(inn, mag) + fp8_ref.rounded(ref, half)
+    if half and cut:        # fp16 results may come from the instructions for 8-bit operands
+        bound = bound + fp8_ref.cut_bound(xv, wv)
+    err = np.abs(y.astype(np.float64) - ref)
+    assert np.all(err <= bound), f"{what}: {np.nanmax(err / bound):.3g} of the bound at {np.unravel_index(np.argmax(err / bound), err.shape)}"
+    # far inside: no more than the rounding to the type and one part in 2^14 of the whole
+    norm = np.linalg.norm(ref)
+    assert np.linalg.norm(err) <= norm * (2.0 ** -11 + 2.0 ** -13 if half else 2.0 ** -19), what
+
+
+def run_product(x, wq, y_type, rows=None):
+    n, inn = x.shape
+    codes, scale = torch.empty(n, inn, dtype=torch.uint8, device="cuda"), torch.empty(-(-inn // 128), n, device="cuda")
+    mm.moe_quantize_fp8_rows(dev(x), codes, scale)
+    y = spoiled((n, wq[0].shape[0]), y_type)
+    mm.moe_matmul_fp8(on_device(wq), codes, scale, y)
+    return y.cpu().numpy()
+
+
+SHAPES = [(1, 16, 1), (1, 4096, 129), (2, 128, 16), (15, 144, 17), (16, 272, 128), (17, 640, 200), (33, 1488, 101), (64, 256, 256),
+          (65, 512, 130), (100, 1024, 384), (129, 400, 257), (130, 2048, 96), (257, 128, 300), (300, 1152, 513)]
+
+
+@pytest.mark.parametrize("n,inn,out", SHAPES)
+@pytest.mark.parametrize("half", [False, True])
+def test_product(n, inn, out, half):
+    print(f"product {n} x {inn} -> {out}, half {half}", flush=True)
+    rng = rng_of(n, inn, out)
+    x, wq = normal(rng, n, inn), quantized_matrix(rng, out, inn)
+    y = run_product(x, wq, torch.float16 if half else torch.float32)
+    check_product(y, fp8_ref.row_values(*fp8_ref.quantize_rows(x)), fp8_ref.matrix_values(*wq), inn, half, (n, inn, out))
+
+
+@pytest.mark.parametrize("n,inn,out", [(272, 272, 200), (40, 144, 33), (1488, 1488, 130)])
+@pytest.mark.parametrize("half", [False, True])
+def test_every_column_meets_its_own(n, inn, out, half):
+    """Row r of x holds one value, at column r: the product is column r of the matrix."""
+    rng = rng_of(n, inn, out, 5)
+    x = np.zeros((n, inn), np.float16)
+    x[np.arange(n), np.arange(n) % inn] = 1.0
+    wq = quantized_matrix(rng, out, inn, 1.0)
+    y = run_product(x, wq, torch.float16 if half else torch.float32).astype(np.float64)
+    want = fp8_ref.matrix_values(*wq)[:, np.arange(n) % inn].T
+    # one product, two scales: 448/448 and the matrix's, three roundings
+    assert np.all(np.abs(y - want) <= np.abs(want) * (4 * 2.0 ** -24) + fp8_ref.rounded(want, half))
+
+
+@pytest.mark.parametrize("n", [3, 150])
+def test_one_value_in_a_far_block_of_large_ones(n):
+    """Scales of very different size: blocks meet their own scales, and nothing else's."""
+    rng = rng_of(n, 6)
+    inn, out = 896, 160
+    x = normal(rng, n, inn)
+    x *= np.repeat(2.0 ** rng.integers(-9, 10, (n, inn // 128)), 128, 1).astype(np.float16)
+    w = normal(rng, out, inn, scale=0.02)
+    w *= np.repeat(np.repeat(2.0 ** rng.integers(-6, 7, (2, 7)), 128, 0)[:out], 128, 1).astype(np.float16)
+    wq = fp8_ref.quantize_matrix(w)
+    for half in (False, True):
+        y = run_product(x, wq, torch.float16 if half else torch.float32)
+        check_product(y, fp8_ref.row_values(*fp8_ref.quantize_rows(x)), fp8_ref.matrix_values(*wq), inn, half, n)
+
+
+@pytest.mark.parametrize("n", [2, 140])
+def test_infinities_and_nan_stay_in_their_rows(n):
+    rng = rng_of(n, 7)
+    x, wq = normal(rng, n, 384), quantized_matrix(rng, 144, 384)
+    clean = run_product(x, wq, torch.float32)
+    x[n - 1, 200] = np.inf
+    x[n // 2 - 1, 5] = np.nan
+    y = run_product(x, wq, torch.float32)
+    bad = [n - 1, n // 2 - 1]
+    assert np.isnan(y[bad]).all()
+    keep = [r for r in range(n) if r not in bad]
+    assert np.array_equal(y[keep], clean[keep])
+    # a block of the matrix: its 128 results and no others
+    w = normal(rng, 300, 384, scale=0.02)
+    w[130, 10] = np.nan
+    y = run_product(normal(rng, n, 384), fp8_ref.quantize_matrix(w), torch.float32)
+    assert np.isnan(y[:, 130]).all() and np.isfinite(y[:, :128]).all() and np.isfinite(y[:, 256:]).all()
+
+
+def test_product_of_nothing():
+    wq = on_device(quantized_matrix(rng_of(8), 32, 64))
+    empty = torch.empty(0, 64, dtype=torch.uint8, device="cuda")
+    mm.moe_quantize_fp8_rows(torch.empty(0, 64, dtype=torch.float16, device="cuda"), empty, torch.empty(1, 0, device="cuda")) \
+        if empty.data_ptr() else None
+    y = spoiled((5, 32), torch.float32)
+    m = mm.CMat(wq.data.data_ptr(), wq.scale.data_ptr(), None)
+    import ctypes
+    assert mm.lib().moe_matmul_fp8(ctypes.byref(m), 32, 64, None, None, 0, None, 0, None) == mm.MOE_OK
+    assert mm.lib().moe_matmul_fp8(ctypes.byref(m), 32, 0, None, None, 5, y.data_ptr(), 0, torch.cuda.current_stream().cuda_stream) == mm.MOE_OK
+    assert torch.equal(y, torch.zeros_like(y))           # a sum over no columns
+
+
+@pytest.mark.parametrize("n,inn,out,half", [(5, 256, 272, False), (200, 1024, 512, True), (150, 384, 144, False)])
+def test_gradient_with_respect_to_rows(n, inn, out, half):
+    """Of sum(g * (x W^T)): g W by the transposed codes, and by differences of the product in 64 bits."""
+    rng = rng_of(n, inn, out, 9)
+    wq, g = quantized_matrix(rng, out, inn), normal(rng, n, out)
+    wv, gv = fp8_ref.matrix_values(*wq), fp8_ref.row_values(*fp8_ref.quantize_rows(g))
+    t = mm.transpose_mat_fp8(on_device(wq))
+    codes, scale = torch.empty(n, out, dtype=torch.uint8, device="cuda"), torch.empty(-(-out // 128), n, device="cuda")
+    mm.moe_quantize_fp8_rows(dev(g), codes, scale)
+    dx = spoiled((n, inn), torch.float16 if half else torch.float32)
+    mm.moe_matmul_fp8(t, codes, scale, dx)
+    dx = dx.cpu().numpy()
+    check_product(dx, gv, wv.T, out, half, "gradient")
+    x, c = rng.standard_normal((n, inn)), rng.integers(0, inn, 8)
+    ref, mag = fp8_ref.product(gv, wv.T)
+    bound = fp8_ref.sum_bound(out, mag) + fp8_ref.rounded(ref, half) + (fp8_ref.cut_bound(gv, wv.T) if half else 0)
+    for col in c:           # linear in x: the difference quotient over 2 is exact but for 64-bit sums
+        step = np.zeros((n, inn))
+        step[:, col] = 1.0
+        diff = ((gv * ((x + step) @ wv.T)).sum(1) - (gv * ((x - step) @ wv.T)).sum(1)) / 2
+        assert np.all(np.abs(diff - dx[:, col]) <= bound[:, col] + 1e-9 * np.abs(gv * (x @ wv.T)).sum(1))
+
+
+def grouping(rng, T, E, k, favour=None, drop=0):
+    """idx, offsets, perm of T tokens; the last `drop` pairs belong to no expert."""
+    idx = np.stack([rng.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
+    if favour is not None:
+        idx[:, 0] = favour
+    flat = idx.reshape(-1).copy()
+    flat[len(flat) - drop:] = E
+    perm = np.argsort(flat, kind="stable").astype(np.int32)
+    counts = np.bincount(flat, minlength=E + 1)[:E]
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32), perm
+
+
+@pytest.mark.parametrize("T,E,k,inn,out,favour,drop", [(1, 4, 2, 128, 100, None, 0), (9, 32, 3, 272, 144, None, 4), (40, 8, 2, 640, 257, 3, 0),
+                                                       (150, 5, 1, 384, 200, 0, 0), (300, 3, 2, 512, 384, None, 30), (260, 32, 8, 256, 130, 7, 11)])
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("gather", [True, False])
+def test_grouped_product(T, E, k, inn, out, favour, drop, half, gather):
+    print(f"grouped T={T} E={E} k={k} {inn} -> {out} half {half} gather {gather}", flush=True)
+    rng = rng_of(T, E, inn)
+    offsets, perm = grouping(rng, T, E, k, favour, drop)
+    P = T * k
+    x = normal(rng, T if gather else P, inn)
+    ws = [quantized_matrix(rng, out, inn) for _ in range(E)]
+    codes, scale = fp8_ref.quantize_rows(x)
+    y = spoiled((P, out), torch.float16 if half else torch.float32)
+    group = mm.MatGroup([on_device(w) for w in ws])
+    mm.moe_matmul_fp8_grouped(group, dev(codes), dev(scale), dev(offsets), dev(perm) if gather else None, k, y)
+    got, xv = y.cpu().numpy(), fp8_ref.row_values(codes, scale)
+    rows = perm // k if gather else np.arange(P)
+    for e in range(E):
+        a, b = offsets[e], offsets[e + 1]
+        if a < b:
+            check_product(got[a:b], xv[rows[a:b]], fp8_ref.matrix_values(*ws[e]), inn, half, f"expert {e}")
+    assert np.isnan(got[offsets[E]:]).all()              # rows behind the last expert are left as they were
+
+
+def test_offsets_and_perm_that_lie_stay_inside():
+    rng = rng_of(11)
+    T, E, inn, out = 70, 4, 128, 64
+    x8, xs = fp8_ref.quantize_rows(normal(rng, T, inn))
+    room = torch.full((T + 64, out), 7.0, device="cuda")
+    y = room[32: 32 + T]
+    group = mm.MatGroup([on_device(quantized_matrix(rng, out, inn)) for _ in range(E)])
+    perm = dev(np.array([-5, 1 << 30, T, -1] + [3] * (T - 4), dtype=np.int32))
+    for off in ([0, -9, 1 << 30, 5, 9], [-100, 30, 20, 10, 1 << 20], [50, 0, 0, 0, 0], [1 << 30] * 5):
+        mm.moe_matmul_fp8_grouped(group, dev(x8), dev(xs), dev(np.array(off, dtype=np.int32)), perm, 1, y)
+    torch.cuda.synchronize()
+    assert bool((room[:32] == 7.0).all()) and bool((room[32 + T:] == 7.0).all())
+
+
+def test_rows_and_matrices_past_32_bit_offsets():
+    """n * in and out * in past 2^31 bytes."""
+    n, inn, out = 270_016, 8192, 16
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(n, inn, generator=g, device="cuda", dtype=torch.float16)
+    codes, scale = torch.empty(n, inn, dtype=torch.uint8, device="cuda"), torch.empty(inn // 128, n, device="cuda")
+    mm.moe_quantize_fp8_rows(x, codes, scale)
+    last = x[-3:].cpu().numpy()
+    want, want_scale = fp8_ref.quantize_rows(last)
+    assert np.array_equal(codes[-3:].cpu().numpy(), want) and np.array_equal(scale[:, -3:].cpu().numpy(), want_scale)
+    wq = quantized_matrix(rng_of(12), out, inn)
+    y = spoiled((n, out), torch.float32)
+    mm.moe_matmul_fp8(on_device(wq), codes, scale, y)
+    check_product(y[-3:].cpu().numpy(), fp8_ref.row_values(want, want_scale), fp8_ref.matrix_values(*wq), inn, False, "last rows")
+    # the same codes as a matrix of n rows
+    del x
+    big = mm.Mat(codes, torch.full((-(-n // 128), inn // 128), 0.5, device="cuda"))
+    few, few_scale = fp8_ref.quantize_rows(normal(rng_of(13), 2, inn))
+    y = spoiled((2, n), torch.float32)
+    mm.moe_matmul_fp8(big, dev(few), dev(few_scale), y)
+    check_product(y[:, -200:].cpu().numpy(), fp8_ref.row_values(few, few_scale), fp8_ref.VALUES[codes[-200:].cpu().numpy()] * 0.5, inn, False, "last results")
+
+
+def test_product_in_a_graph_and_on_another_stream():
+    rng = rng_of(14)
+    T, E, k, inn, out = 48, 6, 2, 512, 320
+    offsets, perm = grouping(rng, T, E, k)
+    ws = [quantized_matrix(rng, out, inn) for _ in range(E)]
+    group = mm.MatGroup([on_device(w) for w in ws])
+    off, per = dev(offsets), dev(perm)
+    x = torch.empty(T, inn, dtype=torch.float16, device="cuda")
+    codes, scale = torch.empty(T, inn, dtype=torch.uint8, device="cuda"), torch.empty(inn // 128, T, device="cuda")
+    y = torch.empty(T * k, out, device="cuda")
+
+    def step():
+        mm.moe_quantize_fp8_rows(x, codes, scale)
+        mm.moe_matmul_fp8_grouped(group, codes, scale, off, per, k, y)
+
+    side = torch.cuda.Stream()
+    x.copy_(dev(normal(rng, T, inn)))
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        x.copy_(dev(normal(rng, T, inn)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        y.fill_(float("nan"))
+        step()
+        assert torch.equal(y, got), i
+
+
+# ---------------------------------------------------------------- experts of this precision in the block
+
+def with_fp8(layer, wl, which):
+    """`layer` with the 16-bit experts of `which` brought into the e4m3 form on the device; their values in 64 bits."""
+    values = {}
+    for e in which:
+        ex = layer.experts[e]
+        assert ex.prec == mm.PREC_FP16
+        mats = [mm.quantize_mat_fp8(m.data) for m in (ex.w1, ex.w3, ex.w2)]
+        layer.experts[e] = mm.Expert(mm.PREC_FP8B128, *mats)
+        values[e] = [fp8_ref.matrix_values(m.data.cpu().numpy(), m.scale.cpu().numpy()) for m in mats]
+    return mm.Layer(layer.d_model, layer.d_ff, layer.top_k, layer.w_gate, layer.experts, layer.gate_bias), values
+
+
+def fp8_ffn(x, values):
+    """y = W2 q( fp16( silu(W1 q(x)) * (W3 q(x)) ) ), q: rows quantized."""
+    w1, w3, w2 = values
+    xq = fp8_ref.row_values(*fp8_ref.quantize_rows(x))
+    a, b = xq @ w1.T, xq @ w3.T
+    h = (a / (1 + np.exp(-a)) * b).astype(np.float16)
+    return fp8_ref.row_values(*fp8_ref.quantize_rows(h)) @ w2.T
+
+
+def reference_block(orc, wl, values, x):
+    """The oracle's routing; its experts' outputs, or those of the definition above for the e4m3 ones."""
+    _, idx, gate = orc.layer_forward(x, wl.wg, wl.experts, wl.cfg.k, wl.bias)
+    out = np.zeros((x.shape[0], wl.cfg.d))
+    for e in range(wl.cfg.E):
+        t, s = np.nonzero(idx == e)
+        if len(t):
+            y = fp8_ffn(x[t], values[e]) if e in values else orc.expert_ffn(wl.experts[e], x[t])
+            out[t] += gate[t, s].astype(np.float64)[:, None] * y
+    return out, idx, gate
+
+
+FP8_BLOCK = common.Config("fp8_block", 512, 1024, 8, 2, 40, ())
+FP8_MIXED = common.Config("fp8_mixed", 512, 768, 8, 2, 40, (1, 4), int8_experts=(6,))
+FP8_ODD = common.Config("fp8_odd", 320, 704, 6, 3, 150, (5,), zipf=1.2)
+FP8_SMALL = common.Config("fp8_small", 192, 128, 4, 1, 9, (0,))
+
+
+@pytest.mark.parametrize("cfg,which", [(FP8_BLOCK, tuple(range(8))), (FP8_MIXED, (0, 2, 7)), (FP8_ODD, (0, 1, 3)), (FP8_SMALL, (1, 2, 3))],
+                         ids=lambda v: getattr(v, "name", None))
+@pytest.mark.parametrize("T", [1, 2, None])
+def test_block_with_fp8_experts(orc, cfg, which, T):
+    print(f"block {cfg.name} T={T}", flush=True)
+    wl = common.build_workload(cfg, orc)
+    layer, values = with_fp8(device_layer(wl), wl, which)
+    x = np.ascontiguousarray(wl.x[: T or cfg.T])
+    ref, ref_idx, ref_gate = reference_block(orc, wl, values, x)
+    out, idx = spoiled(x.shape, torch.float16), torch.empty(x.shape[0], cfg.k, dtype=torch.int32, device="cuda")
+    ws = mm.alloc_workspace(layer, x.shape[0])
+    mm.moe_layer_forward(layer, dev(x), out, ws, idx)
+    assert mm.moe_read_status(ws) == 0
+    assert np.array_equal(idx.cpu().numpy(), ref_idx)
+    assert_ffn_close(out.cpu().numpy(), ref, cfg.name)
+    if mm.workspace_bytes(layer, x.shape[0]) <= mm.moe_static_scratch_bytes():
+        again = spoiled(x.shape, torch.float16)
+        mm.moe_layer_forward_static(layer, dev(x), again)
+        torch.cuda.synchronize()
+        assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("n", [1, 3, 40, 150])
+def test_expert_alone(orc, n):
+    wl = common.build_workload(FP8_MIXED, orc)
+    layer, values = with_fp8(device_layer(wl), wl, (2, 7))
+    x = normal(rng_of(n, 20), n, FP8_MIXED.d)
+    for e in (2, 0, 4):
+        y = spoiled((n, FP8_MIXED.d), torch.float32)
+        mm.moe_expert_ffn_mixed(layer, e, dev(x), y, mm.alloc_workspace(layer, n))
+        ref = fp8_ffn(x, values[e]) if e in values else orc.expert_ffn(wl.experts[e], x)
+        assert_ffn_close(y.cpu().numpy(), ref, f"expert {e}, {n} rows")
+
+
+def test_block_is_the_run_of_its_parts(orc):
+    """moe_route, moe_permute, quantizer, grouped products, quantizer, grouped product, weighted average: as a program would chain
+    the calls.  Same routing, and the block's result within what one rounding of a hidden value can make."""
+    cfg = FP8_BLOCK
+    wl = common.build_workload(cfg, orc)
+    layer, _ = with_fp8(device_layer(wl), wl, range(8))
+    T, E, k, d, f = cfg.T, cfg.E, cfg.k, cfg.d, cfg.f
+    x = dev(wl.x)
+    new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+    logits, idx, gate = new(T, E), new(T, k, t=torch.int32), new(T, k)
+    mm.moe_route_logits(layer, x, logits, idx, gate)
+    ws = mm.alloc_workspace(layer, T)
+    counts, offsets, perm = new(E, t=torch.int32), new(E + 1, t=torch.int32), new(T * k, t=torch.int32)
+    mm.moe_permute(layer, idx, counts, offsets, perm, ws)
+    x8, xs = new(T, d, t=torch.uint8), new(-(-d // 128), T)
+    mm.moe_quantize_fp8_rows(x, x8, xs)
+    parts = []
+    for w in ("w1", "w3"):
+        y = new(T * k, f)
+        mm.moe_matmul_fp8_grouped(mm.MatGroup([getattr(e, w) for e in layer.experts]), x8, xs, offsets, perm, k, y)
+        parts.append(y)
+    h = (torch.nn.functional.silu(parts[0]) * parts[1]).half()
+    h8, hs = new(T * k, f, t=torch.uint8), new(-(-f // 128), T * k)
+    mm.moe_quantize_fp8_rows(h, h8, hs)
+    y = new(T * k, d)
+    mm.moe_matmul_fp8_grouped(mm.MatGroup([e.w2 for e in layer.experts]), h8, hs, offsets, None, k, y)
+    pairs = torch.empty_like(y)
+    pairs[perm.long()] = y
+    want = (pairs.view(T, k, d) * gate[:, :, None]).sum(1)
+    out = new(T, d, t=torch.float16)
+    mm.moe_layer_forward(layer, x, out, ws)
+    assert_ffn_close(out.cpu().numpy(), want.cpu().numpy(), "block against its parts")
+    # and the loss of the same routing
+    gws = mm.alloc_gate_workspace(layer, T)
+    cnt, mean, loss = new(E + 1, t=torch.int32), new(E), new(1)
+    mm.moe_balance_loss(layer, logits, idx, cnt, mean, loss, gws)
+    assert torch.equal(cnt[:E], counts) and int(cnt[E]) == T
+
+
+def test_experts_that_are_not_there(orc):
+    """A missing e4m3 expert is left out and reported; with the swap space its contribution is added."""
+    cfg, which = FP8_MIXED, (0, 2, 7)
+    wl = common.build_workload(cfg, orc)
+    layer, values = with_fp8(device_layer(wl), wl, which)
+    x = dev(wl.x)
+    whole = torch.empty_like(x)
+    mm.moe_layer_forward(layer, x, whole, mm.alloc_workspace(layer, cfg.T))
+    gone, hosts = [], []
+    for e, ex in enumerate(layer.experts):
+        if e in (2, 4):
+            pin = lambda m: mm.Mat(*[None if t is None else t.cpu().pin_memory() for t in (m.data, m.scale, m.zero)])  # noqa: E731
+            hosts.append(mm.Expert(ex.prec, pin(ex.w1), pin(ex.w3), pin(ex.w2), resident=False))
+            gone.append(mm.Expert(ex.prec, None, None, None, resident=False))
+        else:
+            hosts.append(None)
+            gone.append(ex)
+    part = mm.Layer(cfg.d, cfg.f, cfg.k, layer.w_gate, gone, layer.gate_bias)
+    ws, out = mm.alloc_workspace(part, cfg.T), spoiled(x.shape, torch.float16)
+    mm.moe_layer_forward(part, x, out, ws)
+    assert mm.moe_read_status(ws) == mm.STATUS_NOT_RESIDENT
+    _, idx, gate = orc.layer_forward(wl.x, wl.wg, wl.experts, cfg.k, wl.bias)
+    assert np.isfinite(out.cpu().numpy()).all() and not torch.equal(out, whole)
+    swap = mm.Swap(part, hosts, n_slots=1, n_tokens=cfg.T)
+    out = spoiled(x.shape, torch.float16)
+    n = mm.moe_layer_forward_swap(part, swap, x, out, ws)
+    torch.cuda.synchronize()
+    assert n == len({2, 4} & set(idx.reshape(-1).tolist()))
+    assert torch.equal(out, whole)
+    one = spoiled((1, cfg.d), torch.float16)                  # one token
+    for t in range(8):
+        mm.moe_layer_forward_swap(part, swap, x[t:t + 1], one, ws)
+        want = spoiled((1, cfg.d), torch.float16)
+        mm.moe_layer_forward(layer, x[t:t + 1], want, mm.alloc_workspace(layer, 1))
+        torch.cuda.synchronize()
+        assert torch.equal(one, want), t
+
+
+@pytest.mark.parametrize("T", [1, 12])
+def test_chain_with_layers_of_both_kinds(orc, T):
+    """Two blocks, the second one with e4m3 experts: equal to the blocks one after the other."""
+    wl = common.build_workload(FP8_BLOCK, orc)
+    plain = device_layer(wl)
+    fp8, _ = with_fp8(device_layer(wl), wl, (0, 3, 4, 5))
+    d = FP8_BLOCK.d
+    gain = torch.ones(d, dtype=torch.float16, device="cuda")
+    x = dev(wl.x[:T])
+    for layers in ([plain, fp8], [fp8, plain], [fp8, fp8]):
+        h = x.clone()
+        mm.moe_chain_forward(mm.Chain(layers, [gain, gain]), 1e-5, h, mm.alloc_workspace(fp8, T))
+        want = x.clone()
+        for layer in layers:
+            mm.moe_chain_forward(mm.Chain([layer], [gain]), 1e-5, want, mm.alloc_workspace(layer, T))
+        torch.cuda.synchronize()
+        # (the plain layer's contraction is not split in a chain that keeps quantized rows: sums in another order)
+        assert_ffn_close(h.cpu().numpy(), want.cpu().numpy(), "chain")
+
+
+def test_block_in_a_graph(orc):
+    wl = common.build_workload(FP8_MIXED, orc)
+    layer, _ = with_fp8(device_layer(wl), wl, (0, 2, 7))
+    T = FP8_MIXED.T
+    x, out, ws = dev(wl.x), torch.empty(T, FP8_MIXED.d, dtype=torch.float16, device="cuda"), mm.alloc_workspace(layer, T)
+    mm.moe_layer_forward(layer, x, out, ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mm.moe_layer_forward(layer, x, out, ws)
+    for i in range(3):
+        x.copy_(x.flip(0))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        out.fill_(0)
+        mm.moe_layer_forward(layer, x, out, ws)
+        assert torch.equal(out, got), i
