@@ -210,7 +210,7 @@ void run_fp8(const DevExperts& table, int E, const RowMap& rows, const half_t* x
     launch_quantize_fp8_rows(x, x_rows, d, w.x8, w.xs, st);
     {
         TraceScope trace(kKernelUp, st);
-        launch_fp8_matmul(a, true, true, st);
+        launch_fp8_matmul(a, true, true, false, st);
     }
     launch_quantize_fp8_rows(w.h, P, f, w.h8, w.hs, st);
     for (int e = 0; e < a.E; ++e) a.w[e] = fp8_mat(table.e[alone ? rows.direct_expert : e].w2);
@@ -222,7 +222,7 @@ void run_fp8(const DevExperts& table, int E, const RowMap& rows, const half_t* x
     a.N = d;
     a.K = f;
     TraceScope trace(kKernelDown, st);
-    launch_fp8_matmul(a, false, false, st);
+    launch_fp8_matmul(a, false, false, false, st);
 }
 
 // (RMSNorm +) gating -> grouping -> experts -> weighted average (+ residual), all on `st`.
@@ -792,7 +792,7 @@ int matmul_fp8(const char* who, const moe_mat* w, int n_experts, int out, int in
     a.x_rows = n_rows;
     a.N = out;
     a.K = in;
-    launch_fp8_matmul(a, false, y_type == MOE_OUT_F16, st);
+    launch_fp8_matmul(a, false, y_type == MOE_OUT_F16, y_type != MOE_OUT_F16, st);
     return check_hip(st);
 }
 

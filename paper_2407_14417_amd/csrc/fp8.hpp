@@ -31,8 +31,18 @@ struct Fp8Args {
     int E, P, top_k, x_rows, N, K;
 };
 
-// up: y[r, :] = fp16( silu(W1 x) * (W3 x) ); else fp32 or fp16 (half_out) rows of W x.
-void launch_fp8_matmul(const Fp8Args& a, bool up, bool half_out, hipStream_t st);
+// up: y[r, :] = fp16( silu(W1 x) * (W3 x) ); else fp32 or fp16 (half_out) rows of W x.  exact: sums as exact as 32 bits allow (else they
+// may come from the matrix instructions for 8-bit operands, see fp8_tile.hip).
+void launch_fp8_matmul(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st);
+bool fp8_tile_serves(const Fp8Args& a);
+void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st);
+
+// Chunks of `per` rows that P rows over E experts make at most.
+inline int most_chunks(const Fp8Args& a, int per) {
+    if (!a.offsets) return (a.P + per - 1) / per;
+    const int with_rows = a.E < a.P ? a.E : a.P;
+    return (a.P - with_rows) / per + with_rows;
+}
 void launch_quantize_fp8_rows(const half_t* x, int n, int in, uint8_t* codes, float* scale, hipStream_t st);
 void launch_quantize_fp8(const half_t* w, int out, int in, uint8_t* codes, float* scale, hipStream_t st);
 void launch_dequant_fp8(const Fp8Mat& m, int out, int in, half_t* w, hipStream_t st);
@@ -77,6 +87,48 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
     const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
     return v > o ? v : o;
+}
+
+// The chunks of `per` rows of all experts, in expert order, for a whole wavefront: lane e holds expert e's rows and the chunks up
+// to its last one.  (Offsets come from the caller: whatever they hold, rows stay within [0, P).)
+struct Chunks {
+    int lo, hi, mine, end, per, E;
+    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(end, E - 1); }
+    // chunk i: its expert, first row and number of rows; false if there is none
+    __device__ __forceinline__ bool find(int i, int& expert, int& begin, int& rows) const {
+        const unsigned long long past = __ballot((int)(threadIdx.x & 63) < E && end > i);
+        if (!past) return false;
+        expert = __builtin_ctzll(past);
+        const int first = i - (__builtin_amdgcn_readlane(end, expert) - __builtin_amdgcn_readlane(mine, expert));
+        begin = __builtin_amdgcn_readlane(lo, expert) + first * per;
+        rows = min(per, __builtin_amdgcn_readlane(hi, expert) - begin);
+        return true;
+    }
+};
+
+__device__ __forceinline__ Chunks count_chunks(const Fp8Args& a, int per, int lane) {
+    Chunks c{0, 0, 0, 0, per, a.offsets ? a.E : 1};
+    if (!a.offsets) {
+        c.hi = lane == 0 ? a.P : 0;
+    } else if (lane < a.E) {
+        c.lo = min(max(a.offsets[lane], 0), a.P);
+        c.hi = min(max(a.offsets[lane + 1], c.lo), a.P);
+    }
+    c.mine = (c.hi - c.lo + per - 1) / per;
+    c.end = c.mine;                                   // inclusive prefix sum over the experts
+#pragma unroll
+    for (int m = 1; m < MOE_MAX_EXPERTS; m <<= 1) {
+        const int below = __shfl_up(c.end, m, kWave);
+        if (lane >= m) c.end += below;
+    }
+    return c;
+}
+
+// The row of x that row r of y multiplies.
+__device__ __forceinline__ int row_of(const Fp8Args& a, int r) {
+    if (!a.perm) return r;
+    const int t = a.perm[r] / a.top_k;
+    return min(max(t, 0), a.x_rows - 1);
 }
 
 #endif

@@ -10,42 +10,6 @@ namespace {
 
 __device__ const uint32_t zeros[4] __attribute__((aligned(16))) = {0u, 0u, 0u, 0u};
 
-// Chunk y of `per` rows: its expert, first row and number of rows.  Experts' chunks follow each other in expert order;
-// lane e counts those of expert e.  (Offsets come from the caller: whatever they hold, rows stay within [0, P).)
-__device__ __forceinline__ bool find_chunk(const Fp8Args& a, int y, int per, int lane, int& expert, int& begin, int& rows) {
-    if (!a.offsets) {
-        expert = 0;
-        begin = y * per;
-        rows = min(per, a.P - begin);
-        return rows > 0;
-    }
-    int lo = 0, hi = 0;
-    if (lane < a.E) {
-        lo = min(max(a.offsets[lane], 0), a.P);
-        hi = min(max(a.offsets[lane + 1], lo), a.P);
-    }
-    const int mine = (hi - lo + per - 1) / per;
-    int end = mine;                                   // inclusive prefix sum over the experts
-#pragma unroll
-    for (int m = 1; m < MOE_MAX_EXPERTS; m <<= 1) {
-        const int below = __shfl_up(end, m, kWave);
-        if (lane >= m) end += below;
-    }
-    const unsigned long long past = __ballot(lane < a.E && end > y);
-    if (!past) return false;
-    expert = __builtin_ctzll(past);
-    const int first = y - (__builtin_amdgcn_readlane(end, expert) - __builtin_amdgcn_readlane(mine, expert));
-    begin = __builtin_amdgcn_readlane(lo, expert) + first * per;
-    rows = min(per, __builtin_amdgcn_readlane(hi, expert) - begin);
-    return true;
-}
-
-__device__ __forceinline__ int row_of(const Fp8Args& a, int r) {
-    if (!a.perm) return r;
-    const int t = a.perm[r] / a.top_k;
-    return min(max(t, 0), a.x_rows - 1);
-}
-
 // Few rows: one workgroup = 16 weight rows (up: of w1 and of w3) and up to 16 CT rows; its wavefronts take the blocks of 128
 // columns in turn and their sums are added at the end, in order.  Codes go from memory to registers, DEPTH blocks ahead, are
 // expanded to fp16 (exact) and multiplied by v_mfma_f32_16x16x32_f16, so a block's sum is as exact as 32 bits allow.
@@ -58,7 +22,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_kernel(Fp8Args a) {
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int e, begin, rows;
-    if (!find_chunk(a, blockIdx.y, 16 * CT, lane, e, begin, rows)) return;
+    if (!count_chunks(a, 16 * CT, lane).find(blockIdx.y, e, begin, rows)) return;
     e = __builtin_amdgcn_readfirstlane(e);
     const int todo = a.todo[e], n0 = blockIdx.x * 16;
     if (todo == kFp8Skip) return;
@@ -182,17 +146,14 @@ void launch_few(const Fp8Args& a, bool up, bool half_out, dim3 grid, hipStream_t
     else fp8_few_kernel<CT, false, float><<<grid, 64 * kFewWaves, 0, st>>>(a);
 }
 
-// Chunks of `per` rows that P rows over E experts make at most.
-unsigned most_chunks(const Fp8Args& a, int per) {
-    if (!a.offsets) return (unsigned)((a.P + per - 1) / per);
-    const int with_rows = a.E < a.P ? a.E : a.P;
-    return (unsigned)((a.P - with_rows) / per + with_rows);
-}
-
 }  // namespace
 
-void launch_fp8_matmul(const Fp8Args& a, bool up, bool half_out, hipStream_t st) {
+void launch_fp8_matmul(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st) {
     if (a.P == 0 || a.N == 0) return;
+    if (fp8_tile_serves(a)) {
+        launch_fp8_tile(a, up, half_out, exact, st);
+        return;
+    }
     const int mean = (a.P + a.E - 1) / a.E;
     const int ct = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
     dim3 grid((a.N + 15) / 16, most_chunks(a, 16 * ct));
