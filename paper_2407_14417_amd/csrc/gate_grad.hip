@@ -12,7 +12,7 @@ namespace moemix {
 
 namespace {
 
-typedef half4_t __attribute__((aligned(2))) half4_anywhere_t;    // (tokens may lie anywhere)
+typedef uint4_t __attribute__((aligned(2))) uint4_anywhere_t;    // (tokens may lie anywhere)
 
 template <int LANES, class F>
 __device__ __forceinline__ float over_experts(float v, F f) {
@@ -278,64 +278,180 @@ __global__ __launch_bounds__(1024) void gate_dbias_kernel(const float* __restric
     }
 }
 
-// Four columns per lane, 256 per workgroup; its four wavefronts take the range's tokens in turn.  Rows of padding have d_logits of 0
-// and are left out, whatever x holds there.
-template <int EMAX, typename OUT>
-__global__ __launch_bounds__(256) void gate_dx_dw_kernel(GateGradArgs a, int per_split, float* __restrict__ dw) {
-    __shared__ float wave_sums[2][EMAX][256];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), E = a.E;
-    const int col = (blockIdx.x * 64 + lane) * 4;
-    const bool in = col < a.d;                           // (d is a multiple of 64: a lane has all four or none)
-    float4_t acc[EMAX], w[EMAX];
+// ---- d_x = d_logits W and d_w = d_logits^T x in one pass over x, on the matrix cores
+//
+// A wavefront works on units of 32 tokens x 128 columns: a lane loads 8 columns of 8 tokens, lane l columns 8 (l & 15) .. and tokens
+// 8 (l >> 4) .. of the unit.  Its 8 x 8 halves are transposed in registers (32 byte permutes) into the operands of d_w, whose
+// contraction runs over tokens; the contraction of d_x over (up to 32) experts is one v_mfma_f32_16x16x32_f16 long.
+// x and W are fp16 as they are.  d_logits are 32-bit: a power of two brings the largest of a contraction's values to 2^14, then
+// each is the sum of two halves, hi = fp16(v), lo = fp16(v - hi), good to 2^-22 of the value (or 2^-39 of the largest): two products each.
+// With fp32 products of the vector units this took 64 multiply-adds per element of x at 32 experts, twice the time of its
+// bytes, and the registers of 256 accumulators spilled: 16384 tokens, 4096 columns, 32 experts 3757 us.
+
+constexpr int kGradWaves = 8;
+
+// v, w -> 2^k with the largest magnitude `most` brought to 2^14 .. 2^15 (1 for zeros, infinities and NaN)
+__device__ __forceinline__ float half_scale(float most) {
+    const int e = (int)(__builtin_bit_cast(uint32_t, most) >> 23) & 255;
+    const int k = e == 255 || most == 0.0f ? 0 : min(14 + 127 - e, 120);
+    return __builtin_bit_cast(float, (uint32_t)(127 + k) << 23);
+}
+__device__ __forceinline__ void split_halves(const float (&v)[8], float scale, half8_t& hi, half8_t& lo) {
 #pragma unroll
-    for (int e = 0; e < EMAX; ++e) {
-        acc[e] = w[e] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.d_x && in && e < E) {
-            const half4_t h = *(const half4_t*)(a.wg + (size_t)e * a.d + col);
+    for (int i = 0; i < 8; ++i) {
+        const float f = v[i] * scale;
+        hi[i] = (half_t)f;
+        lo[i] = (half_t)(f - (float)hi[i]);
+    }
+}
+__device__ __forceinline__ float largest(const float (&v)[8]) {
+    float m = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[e][i] = (float)h[i];
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+    return m;
+}
+
+// ET: tiles of 16 experts.  Workgroup (x, y): columns 128 x .., the y-th share of the units' token tiles, its wavefronts in turn.
+template <int ET, typename OUT>
+__global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGradArgs a, int tiles_per_split, float* __restrict__ dw) {
+    __shared__ float4_t sums[kGradWaves / 2][8 * ET][64];
+    const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4, E = a.E, d = a.d;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col0 = blockIdx.x * 128, col = col0 + 8 * r16;
+    const bool in = col < d;                             // (d is a multiple of 64)
+    // W for d_x: row r of tile j is column 32 (j >> 1) + 8 (r >> 2) + 4 (j & 1) + (r & 3), so that a lane's results of two tiles
+    // are eight neighbouring columns
+    half8_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = col0 + 32 * (j >> 1) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = 8 * q + i;
+            w[j][i] = a.d_x && e < E && c < d ? a.wg[(size_t)e * d + c] : (half_t)0.0f;
         }
     }
-    const long long t0 = (long long)blockIdx.y * per_split, t1 = t0 + per_split < a.T ? t0 + per_split : a.T;
-    for (long long t = t0 + wave; t < t1; t += 4) {
-        const bool counts = !a.valid || a.valid[t];
-        half4_t h = {};
-        if (in && a.d_w && counts) h = *(const half4_anywhere_t*)(a.x + (size_t)t * a.d + col);
-        float4_t dx = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (counts)
+    float4_t acc[8][ET];
 #pragma unroll
-            for (int e = 0; e < EMAX; ++e) {
-                if (e >= E) break;
-                const float g = a.d_logits[(size_t)t * E + e];
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    acc[e][i] = fmaf(g, (float)h[i], acc[e][i]);
-                    dx[i] = fmaf(g, w[e][i], dx[i]);
+        for (int s = 0; s < ET; ++s) acc[j][s] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const int tiles = (a.T + 31) / 32;
+    const int first = blockIdx.y * tiles_per_split, end = min(first + tiles_per_split, tiles);
+    for (int tile = first + wave; tile < end; tile += kGradWaves) {
+        const size_t t0 = (size_t)tile * 32;
+        const int left = a.T - tile * 32;                // tokens of the tile (32 or more: all)
+        uint4_t x[8];
+        if (a.d_w) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int t = 8 * q + k;
+                x[k] = uint4_t{0u, 0u, 0u, 0u};
+                // padding may hold anything: it is not read
+                if (in && t < left && (!a.valid || a.valid[t0 + t])) x[k] = *(const uint4_anywhere_t*)(a.x + (t0 + t) * d + col);
+            }
+        }
+        if (a.d_x) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int t = 16 * h + r16;
+                const bool here = t < left;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = here && 8 * q + i < E ? a.d_logits[(t0 + t) * E + 8 * q + i] : 0.0f;
+                float most = largest(v);
+                most = fmaxf(most, __shfl_xor(most, 16, kWave));
+                most = fmaxf(most, __shfl_xor(most, 32, kWave));
+                const float scale = half_scale(most), back = 1.0f / scale;      // (a power of two: exact)
+                half8_t hi, lo;
+                split_halves(v, scale, hi, lo);
+                const bool zero = here && a.valid && !a.valid[t0 + t];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    float4_t o[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], lo, float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], hi, o[c], 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[c][i] = zero ? 0.0f : o[c][i] * back;
+                    }
+                    const int c = col0 + 32 * p + 8 * q;
+                    if (!here || c >= d) continue;
+                    OUT* const out = (OUT*)a.d_x + (t0 + t) * d + c;
+                    if (sizeof(OUT) == 2) {
+                        half8_t r;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) r[i] = (half_t)o[i >> 2][i & 3];
+                        *(uint4_anywhere_t*)out = __builtin_bit_cast(uint4_t, r);
+                    } else {
+                        *(uint4_anywhere_t*)out = __builtin_bit_cast(uint4_t, o[0]);
+                        *(uint4_anywhere_t*)(out + 4) = __builtin_bit_cast(uint4_t, o[1]);
+                    }
                 }
             }
-        if (a.d_x && in) {
-            OUT* const o = (OUT*)a.d_x + (size_t)t * a.d + col;
+        }
+        if (a.d_w) {
+            half8_t hi[ET], lo[ET];
+            float back[ET];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = (OUT)dx[i];
+            for (int s = 0; s < ET; ++s) {
+                const int e = 16 * s + r16;
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = e < E && 8 * q + k < left ? a.d_logits[(t0 + 8 * q + k) * E + e] : 0.0f;
+                float most = largest(v);
+                most = fmaxf(most, __shfl_xor(most, 16, kWave));
+                most = fmaxf(most, __shfl_xor(most, 32, kWave));
+                const float scale = half_scale(most);
+                back[s] = 1.0f / scale;
+                split_halves(v, scale, hi[s], lo[s]);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {                // row r of tile j is column 8 r + j: its halves of the 8 tokens
+                uint4_t op;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    op[k] = __builtin_amdgcn_perm(x[2 * k + 1][j >> 1], x[2 * k][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                for (int s = 0; s < ET; ++s) {
+                    float4_t o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, op), lo[s], float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, op), hi[s], o, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[j][s][i] = fmaf(o[i], back[s], acc[j][s][i]);
+                }
+            }
         }
     }
     if (!a.d_w) return;
-    // wavefronts 2 and 3 add to 0 and 1, 1 to 0
-    for (int half = 2; half >= 1; half >>= 1) {
+    // the wavefronts' sums: the upper half adds to the lower one, three times
+#pragma unroll
+    for (int half = kGradWaves / 2; half >= 1; half >>= 1) {
         __syncthreads();
         if (wave >= half && wave < 2 * half)
 #pragma unroll
-            for (int e = 0; e < EMAX; ++e) *(float4_t*)&wave_sums[wave - half][e][lane * 4] = acc[e];
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int s = 0; s < ET; ++s) sums[wave - half][j * ET + s][lane] = acc[j][s];
         __syncthreads();
         if (wave < half)
 #pragma unroll
-            for (int e = 0; e < EMAX; ++e) acc[e] += *(const float4_t*)&wave_sums[wave][e][lane * 4];
-    }
-    if (wave == 0 && in) {
-        float* const o = dw + (size_t)blockIdx.y * E * a.d + col;
+            for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int e = 0; e < EMAX; ++e)
-            if (e < E) *(float4_t*)(o + (size_t)e * a.d) = acc[e];
+                for (int s = 0; s < ET; ++s) acc[j][s] += sums[wave][j * ET + s][lane];
+    }
+    if (wave) return;
+#pragma unroll
+    for (int s = 0; s < ET; ++s) {
+        const int e = 16 * s + r16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int c = col0 + 8 * (4 * q + i);
+            if (e >= E || c >= d) continue;
+            float* const o = dw + ((size_t)blockIdx.y * E + e) * d + c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = acc[j][s][i];
+        }
     }
 }
 
@@ -371,8 +487,9 @@ void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t*
     balance_finish_kernel<<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss);
 }
 
-int gate_dw_splits(int T, int d, int E) {
-    const int by_work = (T + 63) / 64, by_chip = 1024 / ((d + 255) / 256) + 1;
+// A compute unit per workgroup, as far as every wavefront has a tile of 32 tokens.
+int gate_dw_splits(int T, int d, int) {
+    const int by_work = ((T + 31) / 32 + kGradWaves - 1) / kGradWaves, by_chip = 256 / ((d + 127) / 128);
     const int s = by_work < by_chip ? by_work : by_chip;
     return s < 1 ? 1 : s;
 }
@@ -389,17 +506,16 @@ void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStr
     });
     if (a.d_bias) gate_dbias_kernel<<<1, 1024, 0, st>>>(w.sums, blocks, a.E, a.d_bias);
     if (!a.d_x && !a.d_w) return;
-    const int splits = w.dw_splits, per_split = (a.T - 1) / splits + 1;
+    const int splits = w.dw_splits, tiles_per_split = ((a.T + 31) / 32 - 1) / splits + 1;
     float* const dw = splits > 1 ? w.dw : a.d_w;
-    const dim3 grid((a.d + 255) / 256, splits);
-    const auto go = [&](auto most) {
-        constexpr int EMAX = decltype(most)::value;
-        if (a.d_x_half) gate_dx_dw_kernel<EMAX, half_t><<<grid, 256, 0, st>>>(a, per_split, dw);
-        else gate_dx_dw_kernel<EMAX, float><<<grid, 256, 0, st>>>(a, per_split, dw);
+    const dim3 grid((a.d + 127) / 128, splits);
+    const auto go = [&](auto tiles) {
+        constexpr int ET = decltype(tiles)::value;
+        if (a.d_x_half) gate_dx_dw_kernel<ET, half_t><<<grid, 64 * kGradWaves, 0, st>>>(a, tiles_per_split, dw);
+        else gate_dx_dw_kernel<ET, float><<<grid, 64 * kGradWaves, 0, st>>>(a, tiles_per_split, dw);
     };
-    if (a.E <= 8) go(std::integral_constant<int, 8>{});
-    else if (a.E <= 16) go(std::integral_constant<int, 16>{});
-    else go(std::integral_constant<int, 32>{});
+    if (a.E <= 16) go(std::integral_constant<int, 1>{});
+    else go(std::integral_constant<int, 2>{});
     const size_t n = (size_t)a.E * a.d;
     if (a.d_w && splits > 1) launch_reduce_splits(w.dw, splits, n, n, a.d_w, st);
 }
