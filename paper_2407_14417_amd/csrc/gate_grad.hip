@@ -13,6 +13,7 @@ namespace moemix {
 namespace {
 
 typedef uint4_t __attribute__((aligned(2))) uint4_anywhere_t;    // (tokens may lie anywhere)
+typedef float4_t __attribute__((aligned(4))) float4_anywhere_t;
 
 template <int LANES, class F>
 __device__ __forceinline__ float over_experts(float v, F f) {
@@ -314,22 +315,27 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
 // ET: tiles of 16 experts.  Workgroup (x, y): columns 128 x .., the y-th share of the units' token tiles, its wavefronts in turn.
 template <int ET, typename OUT>
 __global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGradArgs a, int tiles_per_split, float* __restrict__ dw) {
-    __shared__ float4_t sums[kGradWaves / 2][8 * ET][64];
+    __shared__ float4_t sums[kGradWaves / 2][16][64];
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4, E = a.E, d = a.d;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col0 = blockIdx.x * 128, col = col0 + 8 * r16;
     const bool in = col < d;                             // (d is a multiple of 64)
     // W for d_x: row r of tile j is column 32 (j >> 1) + 8 (r >> 2) + 4 (j & 1) + (r & 3), so that a lane's results of two tiles
     // are eight neighbouring columns
-    half8_t w[8];
+    half8_t w[8] = {};
+    if (a.d_x) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = col0 + 32 * (j >> 1) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
+        for (int j = 0; j < 8; ++j) {
+            const int c = col0 + 32 * (j >> 1) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
+            const half_t* const src = a.wg + (c < d ? c : 0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = 8 * q + i;
-            w[j][i] = a.d_x && e < E && c < d ? a.wg[(size_t)e * d + c] : (half_t)0.0f;
+            for (int i = 0; i < 8; ++i) w[j][i] = src[(size_t)min(8 * q + i, E - 1) * d];
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)                      // (experts past the last one; columns past the last one are not stored)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (8 * q + i >= E) w[j][i] = (half_t)0.0f;
     }
     float4_t acc[8][ET];
 #pragma unroll
@@ -338,73 +344,65 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGrad
         for (int s = 0; s < ET; ++s) acc[j][s] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
     const int tiles = (a.T + 31) / 32;
     const int first = blockIdx.y * tiles_per_split, end = min(first + tiles_per_split, tiles);
+    float* const dl = (float*)sums + wave * 1024;        // the unit's d_logits, [32][E]
+    // What the next unit needs is asked for between the two products of this one.  Tokens past the last one: the last one again; their d_logits are 0.
+    uint4_t x[8];
+    float4_t part[4];
+    uint32_t valid[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+    auto ask = [&](int tile) {
+        const size_t t0 = (size_t)tile * 32;
+        const int left = a.T - tile * 32;
+        if (a.d_w) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = *(const uint4_anywhere_t*)(a.x + (t0 + min(8 * q + k, left - 1)) * d + (in ? col : 0));
+            if (a.valid)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) valid[k] = a.valid[t0 + min(8 * q + k, left - 1)];
+        }
+        const int n = min(left, 32) * E;
+        const float* const src = a.d_logits + t0 * E;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 256 * i + 4 * lane;
+            part[i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            if (at + 4 <= n) {
+                part[i] = *(const float4_anywhere_t*)(src + at);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (at + c < n) part[i][c] = src[at + c];
+            }
+        }
+    };
+    if (first + wave < end) ask(first + wave);
     for (int tile = first + wave; tile < end; tile += kGradWaves) {
         const size_t t0 = (size_t)tile * 32;
         const int left = a.T - tile * 32;                // tokens of the tile (32 or more: all)
-        uint4_t x[8];
+        wave_lds_handover();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (256 * i < 32 * E) *(float4_t*)(dl + 256 * i + 4 * lane) = part[i];
+        wave_lds_handover();
         if (a.d_w) {
+            if (a.valid) {                               // padding may hold anything
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int t = 8 * q + k;
-                x[k] = uint4_t{0u, 0u, 0u, 0u};
-                // padding may hold anything: it is not read
-                if (in && t < left && (!a.valid || a.valid[t0 + t])) x[k] = *(const uint4_anywhere_t*)(a.x + (t0 + t) * d + col);
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[k][c] = valid[k] ? x[k][c] : 0u;
             }
-        }
-        if (a.d_x) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int t = 16 * h + r16;
-                const bool here = t < left;
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = here && 8 * q + i < E ? a.d_logits[(t0 + t) * E + 8 * q + i] : 0.0f;
-                float most = largest(v);
-                most = fmaxf(most, __shfl_xor(most, 16, kWave));
-                most = fmaxf(most, __shfl_xor(most, 32, kWave));
-                const float scale = half_scale(most), back = 1.0f / scale;      // (a power of two: exact)
-                half8_t hi, lo;
-                split_halves(v, scale, hi, lo);
-                const bool zero = here && a.valid && !a.valid[t0 + t];
-#pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    float4_t o[2];
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], lo, float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], hi, o[c], 0, 0, 0);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[c][i] = zero ? 0.0f : o[c][i] * back;
-                    }
-                    const int c = col0 + 32 * p + 8 * q;
-                    if (!here || c >= d) continue;
-                    OUT* const out = (OUT*)a.d_x + (t0 + t) * d + c;
-                    if (sizeof(OUT) == 2) {
-                        half8_t r;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) r[i] = (half_t)o[i >> 2][i & 3];
-                        *(uint4_anywhere_t*)out = __builtin_bit_cast(uint4_t, r);
-                    } else {
-                        *(uint4_anywhere_t*)out = __builtin_bit_cast(uint4_t, o[0]);
-                        *(uint4_anywhere_t*)(out + 4) = __builtin_bit_cast(uint4_t, o[1]);
-                    }
-                }
-            }
-        }
-        if (a.d_w) {
             half8_t hi[ET], lo[ET];
             float back[ET];
 #pragma unroll
             for (int s = 0; s < ET; ++s) {
-                const int e = 16 * s + r16;
+                const int e = min(16 * s + r16, E - 1);  // (columns past the last expert are not stored)
                 float v[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = e < E && 8 * q + k < left ? a.d_logits[(t0 + 8 * q + k) * E + e] : 0.0f;
+                for (int k = 0; k < 8; ++k) v[k] = dl[(8 * q + k) * E + e];
                 float most = largest(v);
                 most = fmaxf(most, __shfl_xor(most, 16, kWave));
                 most = fmaxf(most, __shfl_xor(most, 32, kWave));
                 const float scale = half_scale(most);
-                back[s] = 1.0f / scale;
+                back[s] = 1.0f / scale;                  // (a power of two: exact)
                 split_halves(v, scale, hi[s], lo[s]);
             }
 #pragma unroll
@@ -419,6 +417,47 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGrad
                     o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, op), hi[s], o, 0, 0, 0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[j][s][i] = fmaf(o[i], back[s], acc[j][s][i]);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (tile + kGradWaves < end) ask(tile + kGradWaves);
+        __builtin_amdgcn_sched_barrier(0);
+        if (a.d_x) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int t = 16 * h + r16;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = 8 * q + i < E ? dl[t * E + 8 * q + i] : 0.0f;
+                float most = largest(v);
+                most = fmaxf(most, __shfl_xor(most, 16, kWave));
+                most = fmaxf(most, __shfl_xor(most, 32, kWave));
+                const float scale = half_scale(most), back = 1.0f / scale;
+                half8_t hi, lo;
+                split_halves(v, scale, hi, lo);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    float4_t o[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], lo, float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], hi, o[c], 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[c][i] *= back;
+                    }
+                    const int c = col0 + 32 * p + 8 * q;
+                    if (t >= left || c >= d) continue;
+                    OUT* const out = (OUT*)a.d_x + (t0 + t) * d + c;
+                    if (sizeof(OUT) == 2) {
+                        half8_t r;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) r[i] = (half_t)o[i >> 2][i & 3];
+                        *(uint4_anywhere_t*)out = __builtin_bit_cast(uint4_t, r);
+                    } else {
+                        *(uint4_anywhere_t*)out = __builtin_bit_cast(uint4_t, o[0]);
+                        *(uint4_anywhere_t*)(out + 4) = __builtin_bit_cast(uint4_t, o[1]);
+                    }
                 }
             }
         }
