@@ -225,6 +225,41 @@ void run_fp8(const DevExperts& table, int E, const RowMap& rows, const half_t* x
     launch_fp8_matmul(a, false, false, false, st);
 }
 
+// One token, all experts in e4m3: gating, then two launches that quantize the rows they multiply.
+bool one_token_fp8(const moe_layer* L, int T) {
+    if (T != 1 || !fp8_one_serves(L->top_k, L->d_model, L->d_ff)) return false;
+    for (int e = 0; e < L->n_experts; ++e)
+        if (L->experts[e].prec != MOE_PREC_FP8B128) return false;
+    return true;
+}
+
+void run_one_fp8(const moe_layer* L, const DevExperts& table, const half_t* x, const half_t* residual, half_t* out, const Workspace& w,
+                 hipStream_t st) {
+    Fp8OneArgs a;
+    memset(&a, 0, sizeof(a));
+    for (int e = 0; e < L->n_experts; ++e) {
+        a.todo[e] = fp8_todo(table.e[e]);
+        a.w[e] = fp8_mat(table.e[e].w1);
+        a.w3[e] = fp8_mat(table.e[e].w3);
+    }
+    a.idx = w.idx;
+    a.gate = w.gate;
+    a.x = x;
+    a.y = w.h;
+    a.status = w.status;
+    a.k = L->top_k;
+    a.N = L->d_ff;
+    a.K = L->d_model;
+    launch_fp8_one(a, true, st);
+    for (int e = 0; e < L->n_experts; ++e) a.w[e] = fp8_mat(table.e[e].w2);
+    a.x = w.h;
+    a.residual = residual;
+    a.y = out;
+    a.N = L->d_model;
+    a.K = L->d_ff;
+    launch_fp8_one(a, false, st);
+}
+
 // (RMSNorm +) gating -> grouping -> experts -> weighted average (+ residual), all on `st`.
 // rms_gain != null: the block input is RMSNorm(x) * rms_gain, computed by the gating kernel into ws.xn.
 int layer_body(const moe_layer* L, const DevExperts& table, const half_t* x, int T, const half_t* rms_gain, float eps,
@@ -249,6 +284,10 @@ int layer_body(const moe_layer* L, const DevExperts& table, const half_t* x, int
     launch_route(x, (const half_t*)L->w_gate, L->gate_bias, T, d, E, k, w.idx, w.gate, idx_out, gate_out,
                  reset_status ? w.status : nullptr, st, rms_gain, eps, to_xn ? w.xn : nullptr);
     if (to_xn) x = w.xn;
+    if (one_token_fp8(L, T)) {
+        run_one_fp8(L, table, x, residual, out, w, st);
+        return check_hip(st);
+    }
     // few pairs: no launch for the grouping, unless that is the kernel the caller wants to measure
     const bool fp8 = any_fp8(L);
     const bool inline_groups = mfma && group_inline_ok(T * k, p.ct) && !trace_armed(kKernelPermute) && !fp8;

@@ -34,8 +34,25 @@ struct Fp8Args {
 // up: y[r, :] = fp16( silu(W1 x) * (W3 x) ); else fp32 or fp16 (half_out) rows of W x.  exact: sums as exact as 32 bits allow (else they
 // may come from the matrix instructions for 8-bit operands, see fp8_tile.hip).
 void launch_fp8_matmul(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st);
-bool fp8_tile_serves(const Fp8Args& a);
+bool fp8_tile_can(const Fp8Args& a);
+float fp8_tile_us(const Fp8Args& a, bool up, bool exact);
 void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st);
+
+// One token: up (y: [k, N] hidden rows of the slots, x: the token) or down (y: [N] the block's output, x: the hidden rows), rows quantized on the way.
+struct Fp8OneArgs {
+    Fp8Mat w[MOE_MAX_EXPERTS];    // up: w1
+    Fp8Mat w3[MOE_MAX_EXPERTS];   // up
+    int32_t todo[MOE_MAX_EXPERTS];
+    const int32_t* idx;           // [k]
+    const float* gate;            // [k], down
+    const half_t* x;
+    const half_t* residual;       // [N] or null, down
+    half_t* y;
+    int32_t* status;
+    int k, N, K;
+};
+bool fp8_one_serves(int k, int d, int f);
+void launch_fp8_one(const Fp8OneArgs& a, bool up, hipStream_t st);
 
 // Chunks of `per` rows that P rows over E experts make at most.
 inline int most_chunks(const Fp8Args& a, int per) {
@@ -100,9 +117,12 @@ struct Chunks {
         if (!past) return false;
         expert = __builtin_ctzll(past);
         const int first = i - (__builtin_amdgcn_readlane(end, expert) - __builtin_amdgcn_readlane(mine, expert));
-        begin = __builtin_amdgcn_readlane(lo, expert) + first * per;
-        rows = min(per, __builtin_amdgcn_readlane(hi, expert) - begin);
-        return true;
+        const int from = __builtin_amdgcn_readlane(lo, expert), to = __builtin_amdgcn_readlane(hi, expert);
+        // an expert's chunks are of equal length, to a whole number of 32 rows
+        const int even = (to - from - 1) / __builtin_amdgcn_readlane(mine, expert) + 1, size = min(per, (even + 31) & ~31);
+        begin = from + first * size;
+        rows = min(size, to - begin);
+        return rows > 0;
     }
 };
 

@@ -18,259 +18,321 @@ __device__ __forceinline__ int8v_t join(uint4_t a, uint4_t b) {
     return int8v_t{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
 
-// 8 wavefronts = 2 (rows of x) x 4 (rows of w); each multiplies 16 MT rows of x with 64 rows of w.
+constexpr int kLds = 163840;             // of a compute unit
+constexpr int kCols = 256;               // rows of w per tile (up: 128 of w1 and 128 of w3)
+
+// A chunk of 32 MT rows of x: 8 wavefronts = 2 (rows of x) x 4 (rows of w), each multiplies 16 MT rows of x with 64 of w.  A stage of LDS holds
+// a block of 128 columns: x [32 MT][128], w [256][128], scales [8][64].
 template <int MT>
 struct Tile {
-    static constexpr int kRows = 32 * MT, kCols = 256;
-    static constexpr int kX = kRows * 128, kW = kCols * 128, kScales = 8 * 64 * 4;
-    static constexpr int kStage = kX + kW + kScales, kStages = MT == 8 ? 2 : 3;
-    static constexpr int kXRuns = kRows / 64;               // 1 KB runs (8 rows) of x per wavefront and stage
-    static constexpr int kTransfers = kXRuns + 4 + 1;       // ... with those of w and the scales
-    static constexpr int kLds = kStage * kStages;
-    static_assert(kLds <= 163840, "LDS");
+    static constexpr int kX = MT * 4096, kW = kCols * 128, kScales = 2048;
+    static constexpr int kStage = kX + kW + kScales;
+    static constexpr int kStages = 3 * kStage <= kLds ? 3 : 2;
+    static_assert(kStages * kStage <= kLds, "LDS");
+    static constexpr int kRuns = 4 * MT;                     // runs of 8 rows (1 KB) of x; the first kRuns % 8 wavefronts (0: all) bring one more
+    static constexpr int kMost = (kRuns + 7) / 8, kMore = kRuns % 8;
+};
+
+struct TileWork {
+    int expert, n0, begin, rows;         // rows [begin, begin + rows) of y, results from n0 on
 };
 
 template <int MT, bool F8, bool UP, typename OUT>
-__global__ __launch_bounds__(512, 2) void fp8_tile_kernel(Fp8Args a, int n_tiles) {
+__device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, uint8_t* lds) {
     typedef Tile<MT> L;
-    extern __shared__ uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
-    // ---- which tile
-    const Chunks chunks = count_chunks(a, L::kRows, lane);
-    const int n_chunks = chunks.total(), total = n_chunks * n_tiles, per_xcd = (total + 7) >> 3;
-    const int slot = blockIdx.x >> 3, t = (blockIdx.x & 7) * per_xcd + slot;
-    if (slot >= per_xcd || t >= total) return;
-    const int group = t / (8 * n_tiles), rest = t - group * 8 * n_tiles, in_group = min(8, n_chunks - group * 8);
-    const int tile = rest / in_group;
-    int e, begin, rows;
-    if (!chunks.find(group * 8 + rest - tile * in_group, e, begin, rows)) return;
-    e = __builtin_amdgcn_readfirstlane(e);
-    constexpr int kOut = UP ? 128 : 256;                     // results of a tile
-    const int todo = a.todo[e], n0 = tile * kOut, N = a.N, K = a.K;
-    if (todo == kFp8Skip) return;
-    OUT* const y = (OUT*)a.y;
-    if (todo == kFp8Missing) {
-        if (tid == 0 && tile == 0 && a.status) atomicOr(a.status, kStatusNotResident);
-        if (!UP)
-            for (int i = tid; i < rows * kOut; i += 512)
-                if (n0 + i % kOut < N) y[(size_t)(begin + i / kOut) * N + n0 + i % kOut] = (OUT)0.0f;
-        return;
-    }
+    const int N = a.N, K = a.K, e = c.expert, n0 = c.n0, rows = c.rows;
     const int blocks = (K + kFp8Block - 1) / kFp8Block, tail = K - (blocks - 1) * kFp8Block;   // bytes of the last block
-    // ---- what it brings: lane l the 16-byte slot l & 7 of row l >> 3 of a run of 8 rows
+    const bool more = !L::kMore || wave < L::kMore;
+    // ---- what it brings: lane l the 16-byte slot l & 7 of row l >> 3 of a run of 8 rows; runs wave, wave + 8, ...
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    uint32_t xv[L::kXRuns], wv[4], sv;
-    const int piece_of[2] = {((lane & 7) ^ swizzle128(lane >> 3)) * 16, ((lane & 7) ^ swizzle128(8 + (lane >> 3))) * 16};
-    gptr_t xb = scalar_ptr(a.perm ? a.x : a.x + (size_t)begin * K);
+    // a run's first row modulo 16 is 8 (run & 1), and run and wave have the same parity
+    const int piece = ((lane & 7) ^ swizzle128(8 * (wave & 1) + (lane >> 3))) * 16;
+    uint32_t xv[L::kMost], wv[4];
+    gptr_t xb = scalar_ptr(a.perm ? a.x : a.x + (size_t)c.begin * K);
 #pragma unroll
-    for (int k = 0; k < L::kXRuns; ++k) {
-        const int run = wave * L::kXRuns + k, row = min(run * 8 + (lane >> 3), rows - 1);
-        xv[k] = (uint32_t)(a.perm ? row_of(a, begin + row) : row) * (uint32_t)K + piece_of[run & 1];
+    for (int k = 0; k < L::kMost; ++k) {
+        const int row = min((wave + 8 * k) * 8 + (lane >> 3), rows - 1);      // (rows past the last one: the last one again)
+        xv[k] = (uint32_t)(a.perm ? row_of(a, c.begin + row) : row) * (uint32_t)K + piece;
     }
-    {
-        const int row = min((wave % L::kXRuns) * 64 + lane, rows - 1);
-        sv = (uint32_t)row_of(a, begin + row) * 4;
+    // w: runs wave, wave + 8, .. of 32; up: the first 16 are w1's
+    gptr_t wb[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const Fp8Mat& m = UP && t ? a.w3[e] : a.w[e];
+        const int row0 = min(UP ? n0 : n0 + 128 * t, N - 1);
+        wb[t] = scalar_ptr(m.data + (size_t)row0 * K);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) wv[2 * t + k] = (uint32_t)min((wave + 8 * k) * 8 + (lane >> 3), N - 1 - row0) * (uint32_t)K + piece;
     }
-    gptr_t sb = scalar_ptr(a.xs);
-    const Fp8Mat m = UP && wave >= 4 ? a.w3[e] : a.w[e];
-    const int row0 = min(UP ? n0 + (wave & 3) * 32 : n0 + wave * 32, N - 1);      // (rows past the last one: the last one again)
-    gptr_t wb = scalar_ptr(m.data + (size_t)row0 * K);
+    // scales of a block: wavefront k < 4 those of rows 64 k .. of x, wavefronts 6 and 7 a scale of w each (up: of w1 and w3; else of the tile's
+    // two blocks of 128 rows), 64 times over
+    const int nb = UP ? n0 / kFp8Block : min(n0 / kFp8Block + (wave & 1), (N - 1) / kFp8Block);
+    gptr_t sb = scalar_ptr(wave < 6 ? a.xs : (UP && wave == 7 ? a.w3[e].scale : a.w[e].scale) + (size_t)nb * blocks);
+    const uint32_t sv = wave < 6 ? (uint32_t)row_of(a, c.begin + min((wave & 3) * 64 + lane, rows - 1)) * 4 : 0u;
+    const size_t scales_of_block = wave < 6 ? (size_t)a.x_rows * 4 : 4;
+    uint32_t put = lds0;                                     // the stage that is filled next
+    auto bring_stage = [&](bool last) {                      // (of the blocks in order)
+        uint32_t back = 0;
+        if (last && tail < kFp8Block) back = piece > tail - 16 ? piece - (tail - 16) : 0;   // pieces past the end of a row: its last one
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int row = min(row0 + k * 8 + (lane >> 3), N - 1) - row0;
-        wv[k] = (uint32_t)row * (uint32_t)K + piece_of[k & 1];
-    }
-    auto bring_stage = [&](int b) {
-        const uint32_t at = lds0 + (b % L::kStages) * L::kStage;
-        const gptr_t x = xb + (size_t)b * kFp8Block, w = wb + (size_t)b * kFp8Block;
-        if (b == blocks - 1 && tail < kFp8Block) {            // pieces past the end of a row: its last one, cleared when it is read
-            const int most = tail - 16;
+        for (int k = 0; k < L::kMost; ++k)
+            if (k < L::kMost - 1 || more) bring<0>(put + (wave + 8 * k) * 1024, xb, xv[k] - back);
 #pragma unroll
-            for (int k = 0; k < L::kXRuns; ++k) {
-                const int p = piece_of[(wave * L::kXRuns + k) & 1];
-                bring<0>(at + (wave * L::kXRuns + k) * 1024, x, xv[k] - (p > most ? p - most : 0));
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int p = piece_of[k & 1];
-                bring<0>(at + L::kX + (wave * 4 + k) * 1024, w, wv[k] - (p > most ? p - most : 0));
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < L::kXRuns; ++k) bring<0>(at + (wave * L::kXRuns + k) * 1024, x, xv[k]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) bring<0>(at + L::kX + (wave * 4 + k) * 1024, w, wv[k]);
-        }
-        bring_words(at + L::kX + L::kW + wave * 256, sb + (size_t)b * a.x_rows * 4, sv);
+        for (int k = 0; k < 4; ++k) bring<0>(put + L::kX + (wave + 8 * k) * 1024, wb[k >> 1], wv[k] - back);
+        bring_words(put + L::kX + L::kW + wave * 256, sb, sv);
+        xb += kFp8Block;
+        wb[0] += kFp8Block;
+        wb[1] += kFp8Block;
+        sb += scales_of_block;
+        put = put == lds0 + (L::kStages - 1) * L::kStage ? lds0 : put + L::kStage;
     };
-    // ---- scales of w: one (up: one of each matrix) per block and wavefront
-    const int last = (N - 1) / kFp8Block;
-    const float* ws[2] = {a.w[e].scale, a.w3[e].scale};
-    ws[0] += (size_t)min(UP ? n0 / kFp8Block : n0 / kFp8Block + (wn >> 1), last) * blocks;
-    if (UP) ws[1] += (size_t)(n0 / kFp8Block) * blocks;
-    // ---- what it reads
+    // Stage b is there, and nobody reads stage b - 1 any more.  The pieces past the end of the rows are cleared by who brought them.
+    auto meet = [&](int b, uint32_t at) {
+        if (b == blocks - 1 && tail < kFp8Block) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (piece >= tail) {
+#pragma unroll
+                for (int k = 0; k < L::kMost; ++k)
+                    if (k < L::kMost - 1 || more) *(uint4_t*)(lds + at + (wave + 8 * k) * 1024 + lane * 16) = uint4_t{0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) *(uint4_t*)(lds + at + L::kX + (wave + 8 * k) * 1024 + lane * 16) = uint4_t{0u, 0u, 0u, 0u};
+            }
+        }
+        if (L::kStages == 2 || b + 1 >= blocks) wait_and_meet<0>();
+        else if (more) wait_and_meet<L::kMost + 5>();
+        else wait_and_meet<L::kMost + 4>();
+    };
+    // ---- what it reads: lane l row r16 of 16, bytes 32 q .. 32 q + 31
     uint32_t off[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) off[h] = r16 * 128 + (((2 * q + h) ^ swizzle128(r16)) * 16);
-    auto w_tile = [&](int j) { return UP ? (j >> 1) * 8 + wn * 2 + (j & 1) : wn * 4 + j; };
+    // operand j of w: rows 64 wn + 16 j; up: 32 wn + 16 j of w1 (j < 2) and of w3
+    auto read_w = [&](uint32_t at, int j, uint4_t (&v)[2]) {
+        const uint32_t row0 = UP ? (j >> 1) * 128 + wn * 32 + (j & 1) * 16 : wn * 64 + j * 16;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h] = *(const uint4_t*)(lds + at + L::kX + row0 * 128 + off[h]);
+    };
+    auto read_x = [&](uint32_t at, int i, uint4_t (&v)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h] = *(const uint4_t*)(lds + at + (wm * MT + i) * 2048 + off[h]);
+    };
     float4_t acc[4][MT];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc[j][i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (int b = 0; b < L::kStages - 1; ++b)
-        if (b < blocks) bring_stage(b);
-    auto step = [&](int b, auto cut_c) {
-        constexpr bool kCut = decltype(cut_c)::value;         // the block ends within 128 columns
-        if (L::kStages == 3 && b + 1 < blocks) wait_and_meet<L::kTransfers>();
-        else wait_and_meet<0>();
-        if (b + L::kStages - 1 < blocks) bring_stage(b + L::kStages - 1);
-        const uint8_t* const xs = lds + (b % L::kStages) * L::kStage;
-        const uint8_t* const wl = xs + L::kX;
-        const float* const sl = (const float*)(wl + L::kW) + wm * 16 * MT + r16;
-        const float w0 = ws[0][b], w1 = UP ? ws[1][b] : 0.0f;
-        auto read = [&](const uint8_t* base, int rows16, uint4_t (&v)[2]) {
+    // ---- The operands that a block starts with are read while the last products of the block before it are under way, after the
+    // wavefronts have met for it: then they find the matrix cores busy whenever they meet.
+    uint4_t w[4][2], x[2], x_next[2];
+    float w0, w1 = 0.0f;
+    auto read_first = [&](uint32_t at) {                     // half 0 of w, tile 0 of x, the scales of w
+        read_w(at, 0, w[0]);
+        read_w(at, 1, w[1]);
+        read_x(at, 0, x_next);
+        const float* const sw = (const float*)(lds + at + L::kX + L::kW) + 6 * 64;
+        w0 = sw[UP ? 0 : (wn >> 1) * 64];
+        if (UP) w1 = sw[64];
+    };
+    for (int b = 0; b < L::kStages && b < blocks; ++b) bring_stage(b == blocks - 1);
+    // (all stages asked for: the first one is there when those after it may be under way)
+    if (blocks > 2 && L::kStages == 3) {
+        if (more) wait_and_meet<2 * (L::kMost + 5)>();
+        else wait_and_meet<2 * (L::kMost + 4)>();
+    } else if (blocks > 1) {
+        if (more) wait_and_meet<L::kMost + 5>();
+        else wait_and_meet<L::kMost + 4>();
+    } else {
+        meet(0, 0);
+    }
+    uint32_t at = 0;
+    read_first(0);
+    for (int b = 0; b < blocks; ++b) {
+        const uint32_t next = at == (L::kStages - 1) * L::kStage ? 0u : at + L::kStage;
+        const float* const sx = (const float*)(lds + at + L::kX + L::kW) + wm * 16 * MT + r16;
+        float4_t part[2][2];
+        half8_t wf[F8 ? 1 : 4][4];
+        const float scale_w0 = w0, scale_w1 = w1;
+        float s_now = 0.0f, s_before = 0.0f;
+        auto add = [&](int i, int h, float s) {              // half h of tile i (up: 0 is w1's, 1 w3's)
+            const float f = s * (UP && h ? scale_w1 : scale_w0);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) v[h] = *(const uint4_t*)(base + rows16 * 2048 + off[h]);
-            if (kCut) {
+            for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if ((2 * q + h) * 16 >= tail) v[h] = uint4_t{0u, 0u, 0u, 0u};
+                for (int k = 0; k < 4; ++k) acc[2 * h + j][i][k] = fmaf(part[h][j][k], f, acc[2 * h + j][i][k]);
+                asm volatile("" : "+v"(acc[2 * h + j][i]));  // added here: sinking it to the end of the block would keep all products alive
             }
         };
-        if (F8) {
-            int8v_t wf[4];
+        read_w(at, 2, w[2]);
+        read_w(at, 3, w[3]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint4_t v[2];
-                read(wl, w_tile(j), v);
-                wf[j] = join(v[0], v[1]);
-            }
-            // A pair of products is under way while the one before it is scaled and added.
-            float4_t part[2][2];
-            int8v_t xf[2];
-            uint4_t v[2];
-            read(xs, wm * MT, v);
-            xf[0] = join(v[0], v[1]);
-            float s_before = 0.0f;
-            auto add = [&](int i, int h, float s) {           // pair h of tile i
+        for (int i = 0; i < MT; ++i) {
+            x[0] = x_next[0];
+            x[1] = x_next[1];
+            if (i + 1 < MT) read_x(at, i + 1, x_next);
+            s_now = sx[16 * i];
+            half8_t xf[4];
+            if (!F8)
 #pragma unroll
-                for (int c2 = 0; c2 < 2; ++c2) {
-                    const float f = s * (UP && h ? w1 : w0);
+                for (int p = 0; p < 4; ++p) xf[p] = fp8_expand(x[p >> 1][2 * (p & 1)], x[p >> 1][2 * (p & 1) + 1]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[2 * h + c2][i][c] = fmaf(part[h][c2][c], f, acc[2 * h + c2][i][c]);
+            for (int h = 0; h < 2; ++h) {
+                if (!F8 && i == 0)
+#pragma unroll
+                    for (int j = 2 * h; j < 2 * h + 2; ++j)
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) wf[F8 ? 0 : j][p] = fp8_expand(w[j][p >> 1][2 * (p & 1)], w[j][p >> 1][2 * (p & 1) + 1]);
+                if (F8) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        part[h][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(join(w[2 * h + j][0], w[2 * h + j][1]), join(x[0], x[1]),
+                                                                                      float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            part[h][j] = mfma16(wf[F8 ? 0 : 2 * h + j][p], xf[p], p ? part[h][j] : float4_t{0.0f, 0.0f, 0.0f, 0.0f});
                 }
-            };
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                if (i + 1 < MT) {
-                    read(xs, wm * MT + i + 1, v);
-                    xf[(i + 1) & 1] = join(v[0], v[1]);
+                pin_schedule();
+                if (i == MT - 1 && h == 0) {                 // (past the last block: whatever lies there, never used)
+                    meet(b + 1, next);
+                    if (b + L::kStages < blocks) bring_stage(b + L::kStages == blocks - 1);
+                    read_first(next);                        // (w's half 0 has been handed to the matrix cores)
+                    pin_schedule();
                 }
-                const float s = sl[16 * i];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                    for (int c2 = 0; c2 < 2; ++c2)
-                        part[h][c2] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[2 * h + c2], xf[i & 1], float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
-                    if (h) add(i, 0, s);
-                    else if (i) add(i - 1, 1, s_before);
-                }
-                s_before = s;
+                if (h) add(i, 0, s_now);
+                else if (i) add(i - 1, 1, s_before);
                 pin_schedule();
             }
-            add(MT - 1, 1, s_before);
-        } else {
-            half8_t wf[4][4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint4_t v[2];
-                read(wl, w_tile(j), v);
-#pragma unroll
-                for (int p = 0; p < 4; ++p) wf[j][p] = fp8_expand(v[p >> 1][2 * (p & 1)], v[p >> 1][2 * (p & 1) + 1]);
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                uint4_t v[2];
-                read(xs, wm * MT + i, v);
-                half8_t xf[4];
-#pragma unroll
-                for (int p = 0; p < 4; ++p) xf[p] = fp8_expand(v[p >> 1][2 * (p & 1)], v[p >> 1][2 * (p & 1) + 1]);
-                float4_t part[4];
-#pragma unroll
-                for (int p = 0; p < 4; ++p)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) part[j] = mfma16(wf[j][p], xf[p], p ? part[j] : float4_t{0.0f, 0.0f, 0.0f, 0.0f});
-                const float s = sl[16 * i], s0 = s * w0, s1 = s * w1;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[j][i][c] = fmaf(part[j][c], UP && j >= 2 ? s1 : s0, acc[j][i][c]);
-            }
+            s_before = s_now;
         }
-    };
-    for (int b = 0; b < blocks - 1; ++b) step(b, std::false_type{});
-    if (tail < kFp8Block) step(blocks - 1, std::true_type{});
-    else step(blocks - 1, std::false_type{});
+        add(MT - 1, 1, s_before);
+        at = next;
+    }
     // ---- lane: row r16 of a tile of x, results 4 q .. 4 q + 3 of a tile of w
+    OUT* const y = (OUT*)a.y;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int r = (wm * MT + i) * 16 + r16;
         if (r >= rows) continue;
 #pragma unroll
         for (int j = 0; j < (UP ? 2 : 4); ++j) {
-            const int n = n0 + w_tile(j) * 16 + 4 * q;
+            const int n = n0 + (UP ? wn * 32 : wn * 64) + j * 16 + 4 * q;
             float4_t v = acc[j][i];
             if (UP) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = silu_mul(v[c], acc[(j + 2) & 3][i][c]);
+                for (int k = 0; k < 4; ++k) v[k] = silu_mul(v[k], acc[(j + 2) & 3][i][k]);
             }
-            OUT* const o = y + (size_t)(begin + r) * N + n;
+            OUT* const o = y + (size_t)(c.begin + r) * N + n;
             if (n + 4 <= N) {
                 if (sizeof(OUT) == 4) *(float4_anywhere_t*)o = v;
                 else *(half4_anywhere_t*)o = half4_t{(half_t)v[0], (half_t)v[1], (half_t)v[2], (half_t)v[3]};
             } else {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (n + c < N) o[c] = (OUT)v[c];
+                for (int k = 0; k < 4; ++k)
+                    if (n + k < N) o[k] = (OUT)v[k];
             }
         }
     }
 }
 
-template <int MT, bool F8, bool UP, typename OUT>
-void launch(const Fp8Args& a, hipStream_t st) {
-    typedef Tile<MT> L;
-    static std::atomic<unsigned long long> configured{0};
-    const auto kernel = fp8_tile_kernel<MT, F8, UP, OUT>;
-    allow_lds((const void*)kernel, L::kLds, configured);
-    const int n_tiles = (a.N + (UP ? 127 : 255)) / (UP ? 128 : 256);
-    const long long total = (long long)n_tiles * most_chunks(a, L::kRows);
-    kernel<<<(unsigned)((total + 7) / 8 * 8), 512, L::kLds, st>>>(a, n_tiles);
+// Chunks of up to `per` rows of an expert; a chunk runs in the body for its number of tiles.
+template <bool F8, bool UP, typename OUT>
+__global__ __launch_bounds__(512, 2) void fp8_tile_kernel(Fp8Args a, int per, int n_tiles) {
+    extern __shared__ uint8_t lds[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    // Workgroups go to the 8 XCDs in turn: each XCD takes a run of neighbouring tiles, eight chunks side by side.
+    const Chunks chunks = count_chunks(a, per, lane);
+    const int n_chunks = chunks.total(), total = n_chunks * n_tiles, per_xcd = (total + 7) >> 3;
+    const int slot = blockIdx.x >> 3, t = (blockIdx.x & 7) * per_xcd + slot;
+    if (slot >= per_xcd || t >= total) return;
+    const int group = t / (8 * n_tiles), rest = t - group * 8 * n_tiles, in_group = min(8, n_chunks - group * 8);
+    const int tile = rest / in_group;
+    constexpr int kOut = UP ? kCols / 2 : kCols;             // results of a tile
+    TileWork c;
+    c.n0 = tile * kOut;
+    if (!chunks.find(group * 8 + rest - tile * in_group, c.expert, c.begin, c.rows)) return;
+    c.expert = __builtin_amdgcn_readfirstlane(c.expert);
+    const int todo = a.todo[c.expert], N = a.N;
+    if (todo == kFp8Skip) return;
+    if (todo == kFp8Missing) {
+        if (tid == 0 && tile == 0 && a.status) atomicOr(a.status, kStatusNotResident);
+        if (!UP)
+            for (int i = tid; i < c.rows * kOut; i += 512)
+                if (c.n0 + i % kOut < N) ((OUT*)a.y)[(size_t)(c.begin + i / kOut) * N + c.n0 + i % kOut] = (OUT)0.0f;
+        return;
+    }
+    switch ((c.rows + 31) >> 5) {
+#define MOEMIX_TILE_CASE(n) case n: tile_body<(n), F8, UP, OUT>(a, c, lds); break;
+        MOEMIX_TILE_CASE(1)
+        MOEMIX_TILE_CASE(2)
+        MOEMIX_TILE_CASE(3)
+        MOEMIX_TILE_CASE(4)
+#undef MOEMIX_TILE_CASE
+#define MOEMIX_TILE_CASE(n) case n: if constexpr (F8) tile_body<(n), F8, UP, OUT>(a, c, lds); break;
+        MOEMIX_TILE_CASE(5)
+        MOEMIX_TILE_CASE(6)
+        MOEMIX_TILE_CASE(7)
+        MOEMIX_TILE_CASE(8)
+#undef MOEMIX_TILE_CASE
+    }
 }
 
-template <int MT>
-void launch_any(const Fp8Args& a, bool up, bool half_out, hipStream_t st) {
-    if (up) launch<MT, true, true, half_t>(a, st);
-    else if (half_out) launch<MT, true, false, half_t>(a, st);
-    else launch<MT, true, false, float>(a, st);
+template <bool F8, bool UP, typename OUT>
+void launch(const Fp8Args& a, int per, hipStream_t st) {
+    static std::atomic<unsigned long long> configured{0};
+    const auto kernel = fp8_tile_kernel<F8, UP, OUT>;
+    allow_lds((const void*)kernel, kLds, configured);
+    constexpr int kOut = UP ? kCols / 2 : kCols;
+    const int n_tiles = (a.N + kOut - 1) / kOut;
+    const long long total = (long long)n_tiles * most_chunks(a, per);
+    kernel<<<(unsigned)((total + 7) / 8 * 8), 512, kLds, st>>>(a, per, n_tiles);
 }
 
 }  // namespace
 
-bool fp8_tile_serves(const Fp8Args& a) {
-    const int mean = (a.P + a.E - 1) / a.E;
-    // gathered rows are found by 32-bit offsets
-    return mean > 64 && a.K > 0 && (!a.perm || (size_t)a.x_rows * a.K < (1ull << 32) - 4096) && a.K <= 1 << 20;
+// Rows per chunk: the number (of 32s) whose rounds of workgroups over the chip cost least, a block of 128 columns costing
+// 2 + MT in a workgroup of 32 MT rows (measured, 4096 rows 4096 -> 14336: 0.88 us a block for MT = 2, 1.40 for 4, 1.81 for 6, 2.18 for 8).
+// Of several experts some have more rows than the mean: an eighth more is reckoned with (512 tokens, 8 experts, top-2,
+// 128 rows on average: chunks of 128 rows 449 us a block, of 160 425).
+static int rows_per_chunk(const Fp8Args& a, bool up, bool exact, long long* best_cost) {
+    const int out = up ? kCols / 2 : kCols, tiles = (a.N + out - 1) / out, most = exact ? 4 : 8;
+    const int with_rows = a.E < a.P ? a.E : a.P, mean = (a.P + with_rows - 1) / with_rows + (with_rows > 1 ? a.P / with_rows / 8 : 0);
+    int per = 32, best_chunks = 0;
+    for (int mt = 1; mt <= most; ++mt) {
+        const int chunks = (mean + 32 * mt - 1) / (32 * mt), rows = (mean + chunks - 1) / chunks;
+        const long long rounds = ((long long)tiles * chunks * with_rows + kComputeUnits - 1) / kComputeUnits, cost = rounds * (2 + (rows + 31) / 32);
+        if (mt == 1 || cost < *best_cost || (cost == *best_cost && chunks < best_chunks)) {     // (of equal ones fewer chunks, then shorter ones)
+            *best_cost = cost;
+            best_chunks = chunks;
+            per = 32 * mt;
+        }
+    }
+    return per;
+}
+
+// Gathered rows are found by 32-bit offsets.
+bool fp8_tile_can(const Fp8Args& a) { return a.K > 0 && (!a.perm || (size_t)a.x_rows * a.K < (1ull << 32) - 4096); }
+
+// Microseconds, roughly: the rounds at 0.22 us per block of 128 columns and unit of cost (0.32 with rows expanded to fp16), or 5 TB/s of weights.
+float fp8_tile_us(const Fp8Args& a, bool up, bool exact) {
+    long long cost = 0;
+    rows_per_chunk(a, up, exact, &cost);
+    const float with_rows = (float)(a.E < a.P ? a.E : a.P), mb = 1e-6f * (float)a.N * (float)a.K * (up ? 2.0f : 1.0f) * with_rows;
+    const float blocks = (float)((a.K + kFp8Block - 1) / kFp8Block), busy = (float)cost * blocks * (exact ? 0.32f : 0.22f);
+    return 4.0f + (busy > mb / 5.0f ? busy : mb / 5.0f);
 }
 
 void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st) {
-    const int mean = (a.P + a.E - 1) / a.E;
-    if (exact) launch<4, false, false, float>(a, st);
-    else if (mean > 192) launch_any<8>(a, up, half_out, st);
-    else launch_any<4>(a, up, half_out, st);
+    long long cost = 0;
+    const int per = rows_per_chunk(a, up, exact, &cost);
+    if (up) launch<true, true, half_t>(a, per, st);
+    else if (half_out) launch<true, false, half_t>(a, per, st);
+    else if (exact) launch<false, false, float>(a, per, st);
+    else launch<true, false, float>(a, per, st);
 }
 
 }  // namespace moemix

@@ -51,6 +51,25 @@ __device__ __forceinline__ float4_t load_logits(const float* __restrict__ logits
     return l;
 }
 
+// What a lane reads of a token, all of it asked for before anything is used: up to eight slots (past the k-th: the k-th again).
+struct Token {
+    float4_t logits;
+    int32_t idx[MOE_MAX_TOPK];
+    bool counts;
+};
+template <bool WIDE>
+__device__ __forceinline__ void load_token(Token& r, const float* __restrict__ logits, const int32_t* __restrict__ idx,
+                                           const uint8_t* __restrict__ valid, size_t t, int E, int k, int e0) {
+    r.logits = load_logits<WIDE>(logits, t, E, e0);
+    const int32_t* const p = idx + t * k;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) r.idx[s] = p[min(s, k - 1)];
+    if (k > 4)
+#pragma unroll
+        for (int s = 4; s < MOE_MAX_TOPK; ++s) r.idx[s] = p[min(s, k - 1)];
+    r.counts = !valid || valid[t];
+}
+
 // Softmax over the experts with weights: p[i] = m[i] exp(l[i] - most) / sum, most over the experts with m != 0.  All of those at
 // -infinity: zeros.  NaN and +infinity make NaN.
 template <int LANES, class M>
@@ -78,41 +97,68 @@ __device__ __forceinline__ void softmax(const float4_t l, M m, float (&p)[4]) {
 
 constexpr int kLossWaves = 4;
 
-// Partial sums over the workgroup's tokens.  A token's lanes count, each for its own four experts, the slots that chose them.
-template <int LANES, bool WIDE>
-__global__ __launch_bounds__(64 * kLossWaves) void balance_sums_kernel(const float* __restrict__ logits, const int32_t* __restrict__ idx,
-                                                                       const uint8_t* __restrict__ valid, int T, int E, int k,
-                                                                       float* __restrict__ sums, int32_t* __restrict__ counts,
-                                                                       int32_t* __restrict__ status) {
-    __shared__ float wave_sums[kLossWaves][32];
-    __shared__ int32_t wave_counts[kLossWaves][33];
-    constexpr int kTokens = 64 / LANES;
+// What is known at the end: counts, mean probabilities and the loss, from a lane's (e = lane, up to 31) sums over all tokens, by half a
+// wavefront; and the status of the call.
+__device__ __forceinline__ void finish_loss(int e, double sum, int32_t c, int32_t n, bool bad, int E, int k, int32_t* __restrict__ counts,
+                                            float* __restrict__ mean_prob, float* __restrict__ loss, int32_t* __restrict__ status) {
+    const double mean = n > 0 ? sum / n : 0.0;
+    double l = e < E ? mean * c : 0.0;
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) l += __shfl_xor(l, m, kWave);
+    if (e < E) {
+        counts[e] = c;
+        mean_prob[e] = (float)mean;
+    }
+    if (e == 0) {
+        counts[E] = n;
+        *loss = n > 0 ? (float)(l * E / ((double)n * k)) : 0.0f;
+        *status = bad ? kStatusBadIndex : 0;
+    }
+}
+
+// Sums over the workgroup's tokens.  A token's lanes count, each for its own four experts, the slots that chose them.  Few tokens: one
+// workgroup of 16 wavefronts finishes as well (ONE); else partial sums go to `sums` and `partial`.
+template <int LANES, bool WIDE, bool ONE>
+__global__ __launch_bounds__(ONE ? 1024 : 64 * kLossWaves) void balance_sums_kernel(
+    const float* __restrict__ logits, const int32_t* __restrict__ idx, const uint8_t* __restrict__ valid, int T, int E, int k,
+    float* __restrict__ sums, int32_t* __restrict__ partial, int32_t* __restrict__ counts, float* __restrict__ mean_prob,
+    float* __restrict__ loss, int32_t* __restrict__ status) {
+    constexpr int kWaves = ONE ? 16 : kLossWaves, kTokens = 64 / LANES;
+    __shared__ float wave_sums[kWaves][32];
+    __shared__ int32_t wave_counts[kWaves][34];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LANES, e0 = 4 * j;
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     int32_t n[4] = {0, 0, 0, 0}, tokens = 0;
     bool bad = false;
-    for (long long t = (long long)(blockIdx.x * kLossWaves + wave) * kTokens + lane / LANES; t < T;
-         t += (long long)gridDim.x * kLossWaves * kTokens) {
-        if (valid && !valid[t]) continue;             // (a token's lanes agree)
+    const long long step = (long long)gridDim.x * kWaves * kTokens;
+    long long t = (long long)(blockIdx.x * kWaves + wave) * kTokens + lane / LANES;
+    Token now, next;
+    if (t < T) load_token<WIDE>(next, logits, idx, valid, t, E, k, e0);
+    for (; t < T; t += step) {                        // (a token's lanes agree)
+        now = next;
+        if (t + step < T) load_token<WIDE>(next, logits, idx, valid, t + step, E, k, e0);
+        if (!now.counts) continue;
         float p[4];
-        softmax<LANES>(load_logits<WIDE>(logits, t, E, e0), [&](int i) { return e0 + i < E ? 1.0f : 0.0f; }, p);
+        softmax<LANES>(now.logits, [&](int i) { return e0 + i < E ? 1.0f : 0.0f; }, p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] += p[i];
-        for (int s = 0; s < k; ++s) {
-            const int e = idx[t * k + s];
+#pragma unroll
+        for (int s = 0; s < MOE_MAX_TOPK; ++s) {
+            if (s >= k) break;
+            const int e = now.idx[s];
             bad |= (unsigned)e >= (unsigned)E;
 #pragma unroll
             for (int i = 0; i < 4; ++i) n[i] += e == e0 + i ? 1 : 0;
         }
         tokens += j == 0 ? 1 : 0;
     }
-    if (bad && status) atomicOr(status, kStatusBadIndex);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         acc[i] = over_tokens<LANES>(acc[i]);
         n[i] = over_tokens<LANES>(n[i]);
     }
     tokens = over_tokens<1>(tokens);
+    const bool any_bad = __ballot(bad) != 0;
     if (lane < LANES) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -120,73 +166,89 @@ __global__ __launch_bounds__(64 * kLossWaves) void balance_sums_kernel(const flo
             wave_counts[wave][e0 + i] = n[i];
         }
     }
-    if (lane == 0) wave_counts[wave][32] = tokens;
+    if (lane == 0) {
+        wave_counts[wave][32] = tokens;
+        wave_counts[wave][33] = any_bad;
+    }
     __syncthreads();
-    if ((int)threadIdx.x <= E) {
-        const int e = threadIdx.x;
+    if (threadIdx.x >= 64) return;
+    const int at = lane < E ? lane : 32 + (lane - E);    // lane E: tokens, lane E + 1: an index out of range
+    if (ONE) {
+        int32_t c = 0, all = 0, flags = 0;
+        double v = 0.0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (lane < E) {
+                c += wave_counts[w][lane];
+                v += wave_sums[w][lane];
+            }
+            all += wave_counts[w][32];
+            flags |= wave_counts[w][33];
+        }
+        finish_loss(lane, v, c, all, flags != 0, E, k, counts, mean_prob, loss, status);
+    } else if (lane < E + 2) {
         int32_t c = 0;
-        for (int w = 0; w < kLossWaves; ++w) c += wave_counts[w][e < E ? e : 32];
-        counts[(size_t)blockIdx.x * (E + 1) + e] = c;
-        if (e < E) {
+        for (int w = 0; w < kWaves; ++w) c += wave_counts[w][at];
+        partial[(size_t)blockIdx.x * (E + 2) + lane] = c;
+        if (lane < E) {
             float v = 0.0f;
-            for (int w = 0; w < kLossWaves; ++w) v += wave_sums[w][e];
-            sums[(size_t)blockIdx.x * E + e] = v;
+            for (int w = 0; w < kWaves; ++w) v += wave_sums[w][lane];
+            sums[(size_t)blockIdx.x * E + lane] = v;
         }
     }
 }
 
-// One workgroup: adds the partial sums up (in 64 bits, in a fixed order) and forms the loss.
+// One workgroup: adds the partial sums of up to 32 ROWS workgroups up (in 64 bits, in a fixed order) and forms the loss.
+template <int ROWS>
 __global__ __launch_bounds__(1024) void balance_finish_kernel(const float* __restrict__ sums, const int32_t* __restrict__ partial, int blocks,
                                                               int E, int k, int32_t* __restrict__ counts, float* __restrict__ mean_prob,
-                                                              float* __restrict__ loss) {
+                                                              float* __restrict__ loss, int32_t* __restrict__ status) {
     __shared__ double part[32][33];
-    __shared__ int32_t part_n[32][33];
+    __shared__ int32_t part_n[32][35];
     const int e = threadIdx.x & 31, g = threadIdx.x >> 5;
     double v = 0.0;
-    int32_t c = 0;
-    if (e < E)
-        for (int b = g; b < blocks; b += 32) {
-            v += sums[(size_t)b * E + e];
-            c += partial[(size_t)b * (E + 1) + e];
+    int32_t c = 0, more = 0;
+    float s[ROWS];                                    // all of a thread's values are asked for before the first is added
+    int32_t cs[ROWS], ms[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const size_t b = min(g + 32 * i, blocks - 1);
+        s[i] = sums[b * E + min(e, E - 1)];
+        cs[i] = partial[b * (E + 2) + min(e, E - 1)];
+        ms[i] = partial[b * (E + 2) + E + (e & 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+        if (g + 32 * i < blocks) {
+            v += e < E ? s[i] : 0.0f;
+            c += e < E ? cs[i] : 0;
+            more += ms[i];
         }
     part[g][e] = v;
     part_n[g][e] = c;
-    if (e == 0) {
-        int32_t t = 0;
-        for (int b = g; b < blocks; b += 32) t += partial[(size_t)b * (E + 1) + E];
-        part_n[g][32] = t;
-    }
+    if (e < 2) part_n[g][32 + e] = more;
     __syncthreads();
-    if (threadIdx.x < 32) {
-        int32_t n = 0;
-        v = 0.0;
-        c = 0;
-        for (int i = 0; i < 32; ++i) {
-            n += part_n[i][32];
+    if (threadIdx.x >= 64) return;
+    int32_t n = 0, flags = 0;
+    v = 0.0;
+    c = 0;
+    for (int i = 0; i < 32; ++i) {
+        n += part_n[i][32];
+        flags |= part_n[i][33];
+        if (threadIdx.x < 32) {
             v += part[i][e];
             c += part_n[i][e];
         }
-        const double mean = n > 0 ? v / n : 0.0;
-        double l = e < E ? mean * c : 0.0;
-#pragma unroll
-        for (int m = 16; m >= 1; m >>= 1) l += __shfl_xor(l, m, kWave);
-        if (e < E) {
-            counts[e] = c;
-            mean_prob[e] = (float)mean;
-        }
-        if (e == 0) {
-            counts[E] = n;
-            *loss = n > 0 ? (float)(l * E / ((double)n * k)) : 0.0f;
-        }
     }
+    finish_loss(threadIdx.x, v, c, n, flags != 0, E, k, counts, mean_prob, loss, status);
 }
 
 // ---------------------------------------------------------------- backward
 
 // d_logits, and partial sums of them over the workgroup's tokens for the bias.
 template <int LANES, bool WIDE>
-__global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradArgs a, float* __restrict__ sums, int32_t* __restrict__ status) {
+__global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradArgs a, float* __restrict__ sums, int32_t* __restrict__ flags) {
     __shared__ float wave_sums[kLossWaves][32];
+    __shared__ int32_t wave_bad[kLossWaves];
     constexpr int kTokens = 64 / LANES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LANES, e0 = 4 * j, E = a.E;
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, c[4] = {0.0f, 0.0f, 0.0f, 0.0f}, coef = 0.0f;
@@ -197,11 +259,29 @@ __global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradA
         for (int i = 0; i < 4; ++i) c[i] = e0 + i < E ? (float)a.counts[e0 + i] : 0.0f;
     }
     bool bad = false;
-    for (long long t = (long long)(blockIdx.x * kLossWaves + wave) * kTokens + lane / LANES; t < a.T;
-         t += (long long)gridDim.x * kLossWaves * kTokens) {
+    const long long step = (long long)gridDim.x * kLossWaves * kTokens;
+    long long t = (long long)(blockIdx.x * kLossWaves + wave) * kTokens + lane / LANES;
+    Token now, next;
+    float dgs[MOE_MAX_TOPK], dgs_next[MOE_MAX_TOPK];
+    auto ask = [&](long long at) {
+        load_token<WIDE>(next, a.logits, a.idx, a.valid, at, E, a.k, e0);
+        if (!a.d_gate) return;
+        const float* const p = a.d_gate + at * a.k;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) dgs_next[s] = p[min(s, a.k - 1)];
+        if (a.k > 4)
+#pragma unroll
+            for (int s = 4; s < MOE_MAX_TOPK; ++s) dgs_next[s] = p[min(s, a.k - 1)];
+    };
+    if (t < a.T) ask(t);
+    for (; t < a.T; t += step) {
+        now = next;
+#pragma unroll
+        for (int s = 0; s < MOE_MAX_TOPK; ++s) dgs[s] = dgs_next[s];
+        if (t + step < a.T) ask(t + step);
         float dl[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (!a.valid || a.valid[t]) {
-            const float4_t l = load_logits<WIDE>(a.logits, t, E, e0);
+        if (now.counts) {
+            const float4_t l = now.logits;
             if (a.d_loss) {
                 float p[4], mean = 0.0f;
                 softmax<LANES>(l, [&](int i) { return e0 + i < E ? 1.0f : 0.0f; }, p);
@@ -214,9 +294,11 @@ __global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradA
             if (a.d_gate) {
                 // the chosen experts with how often they were chosen (an expert chosen twice has two gates)
                 float times[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dg[4] = {0.0f, 0.0f, 0.0f, 0.0f}, g[4], dot = 0.0f;
-                for (int s = 0; s < a.k; ++s) {
-                    const int e = a.idx[t * a.k + s];
-                    const float d = a.d_gate[t * a.k + s];
+#pragma unroll
+                for (int s = 0; s < MOE_MAX_TOPK; ++s) {
+                    if (s >= a.k) break;
+                    const int e = now.idx[s];
+                    const float d = dgs[s];
                     bad |= (unsigned)e >= (unsigned)E;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -248,35 +330,64 @@ __global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradA
                 if (e0 + i < E) out[i] = dl[i];
         }
     }
-    if (bad && status) atomicOr(status, kStatusBadIndex);
-    if (!a.d_bias) return;
+    const bool any_bad = __ballot(bad) != 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] = over_tokens<LANES>(acc[i]);
     if (lane < LANES) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) wave_sums[wave][e0 + i] = acc[i];
     }
+    if (lane == 0) wave_bad[wave] = any_bad;
     __syncthreads();
     if ((int)threadIdx.x < E) {
         float v = 0.0f;
         for (int w = 0; w < kLossWaves; ++w) v += wave_sums[w][threadIdx.x];
         sums[(size_t)blockIdx.x * E + threadIdx.x] = v;
     }
+    if (threadIdx.x == 0) {
+        int32_t f = 0;
+        for (int w = 0; w < kLossWaves; ++w) f |= wave_bad[w];
+        flags[blockIdx.x] = f;
+    }
 }
 
-__global__ __launch_bounds__(1024) void gate_dbias_kernel(const float* __restrict__ sums, int blocks, int E, float* __restrict__ d_bias) {
-    __shared__ double part[32][33];
+// Workgroup 0: d_bias (in 64 bits, in a fixed order, of up to 8 ROWS workgroups) and the status of the call from what gate_dlogits_kernel left; the others: d_w from its
+// partial sums, in order, four values per thread.
+template <int ROWS>
+__global__ __launch_bounds__(256) void gate_finish_kernel(const float* __restrict__ sums, const int32_t* __restrict__ flags, int blocks, int E,
+                                                          float* __restrict__ d_bias, int32_t* __restrict__ status,
+                                                          const float* __restrict__ dw, int splits, size_t n, float* __restrict__ d_w) {
+    if (blockIdx.x) {
+        const size_t i = ((size_t)(blockIdx.x - 1) * 256 + threadIdx.x) * 4;
+        if (i >= n) return;                              // (n = E d is a multiple of 64)
+        float4_t v = *(const float4_t*)(dw + i);
+#pragma unroll 8
+        for (int s = 1; s < splits; ++s) v += *(const float4_t*)(dw + s * n + i);
+        *(float4_anywhere_t*)(d_w + i) = v;
+        return;
+    }
+    __shared__ double part[8][33];
+    __shared__ int32_t bad;
     const int e = threadIdx.x & 31, g = threadIdx.x >> 5;
+    if (threadIdx.x == 0) bad = 0;
     double v = 0.0;
-    if (e < E)
-        for (int b = g; b < blocks; b += 32) v += sums[(size_t)b * E + e];
+    float r[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) r[i] = sums[(size_t)min(g + 8 * i, blocks - 1) * E + min(e, E - 1)];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) v += e < E && g + 8 * i < blocks ? r[i] : 0.0f;
     part[g][e] = v;
+    int32_t f = 0;
+    for (int b = threadIdx.x; b < blocks; b += 256) f |= flags[b];
     __syncthreads();
-    if ((int)threadIdx.x < E) {
+    if (f) atomicOr(&bad, 1);
+    __syncthreads();
+    if (d_bias && (int)threadIdx.x < E) {
         v = 0.0;
-        for (int i = 0; i < 32; ++i) v += part[i][e];
+        for (int i = 0; i < 8; ++i) v += part[i][e];
         d_bias[e] = (float)v;
     }
+    if (threadIdx.x == 0) *status = bad ? kStatusBadIndex : 0;
 }
 
 // ---- d_x = d_logits W and d_w = d_logits^T x in one pass over x, on the matrix cores
@@ -504,6 +615,9 @@ void by_lanes(int E, F f) {
 
 bool wide_rows(const void* p, int E) { return E % 4 == 0 && (uintptr_t)p % 16 == 0; }
 
+// Up to so many workgroups' tokens one workgroup of four times the wavefronts takes alone.
+constexpr int kOneBlock = 8;
+
 int token_blocks(int T, int E) {
     const int lanes = E <= 4 ? 1 : E <= 8 ? 2 : E <= 16 ? 4 : 8, per = 64 / lanes * kLossWaves;
     const int blocks = (T - 1) / per + 1;
@@ -515,15 +629,25 @@ int token_blocks(int T, int E) {
 void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* valid, int T, int E, int k, int32_t* counts,
                          float* mean_prob, float* loss, const GateWorkspace& w, hipStream_t st) {
     const int blocks = token_blocks(T, E);
-    launch_zero_words(w.status, 1, st);
+    const bool one = blocks <= kOneBlock;
     by_lanes(E, [&](auto lanes) {
         constexpr int LANES = decltype(lanes)::value;
-        if (wide_rows(logits, E))
-            balance_sums_kernel<LANES, true><<<blocks, 64 * kLossWaves, 0, st>>>(logits, idx, valid, T, E, k, w.sums, w.counts, w.status);
-        else
-            balance_sums_kernel<LANES, false><<<blocks, 64 * kLossWaves, 0, st>>>(logits, idx, valid, T, E, k, w.sums, w.counts, w.status);
+        const auto go = [&](auto wide) {
+            constexpr bool WIDE = decltype(wide)::value;
+            if (one)
+                balance_sums_kernel<LANES, WIDE, true><<<1, 1024, 0, st>>>(logits, idx, valid, T, E, k, w.sums, w.counts, counts, mean_prob,
+                                                                           loss, w.status);
+            else
+                balance_sums_kernel<LANES, WIDE, false><<<blocks, 64 * kLossWaves, 0, st>>>(logits, idx, valid, T, E, k, w.sums, w.counts,
+                                                                                            counts, mean_prob, loss, w.status);
+        };
+        if (wide_rows(logits, E)) go(std::true_type{});
+        else go(std::false_type{});
     });
-    balance_finish_kernel<<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss);
+    static_assert(kGateBlocks == 32 * 16, "rows");
+    if (one) return;
+    if (blocks <= 64) balance_finish_kernel<2><<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss, w.status);
+    else balance_finish_kernel<16><<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss, w.status);
 }
 
 // A compute unit per workgroup, as far as every wavefront has a tile of 32 tokens.
@@ -535,16 +659,24 @@ int gate_dw_splits(int T, int d, int) {
 
 void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStream_t st) {
     const int blocks = token_blocks(a.T, a.E);
-    launch_zero_words(w.status, 1, st);
     by_lanes(a.E, [&](auto lanes) {
         constexpr int LANES = decltype(lanes)::value;
         if (wide_rows(a.logits, a.E) && wide_rows(a.d_logits, a.E))
-            gate_dlogits_kernel<LANES, true><<<blocks, 64 * kLossWaves, 0, st>>>(a, w.sums, w.status);
+            gate_dlogits_kernel<LANES, true><<<blocks, 64 * kLossWaves, 0, st>>>(a, w.sums, w.counts);
         else
-            gate_dlogits_kernel<LANES, false><<<blocks, 64 * kLossWaves, 0, st>>>(a, w.sums, w.status);
+            gate_dlogits_kernel<LANES, false><<<blocks, 64 * kLossWaves, 0, st>>>(a, w.sums, w.counts);
     });
-    if (a.d_bias) gate_dbias_kernel<<<1, 1024, 0, st>>>(w.sums, blocks, a.E, a.d_bias);
-    if (!a.d_x && !a.d_w) return;
+    const auto finish = [&](int splits) {
+        const size_t n = splits > 1 ? (size_t)a.E * a.d : 0;
+        const unsigned grid = 1 + (unsigned)((n / 4 + 255) / 256);
+        static_assert(kGateBlocks == 8 * 64, "rows");
+        if (blocks <= 64) gate_finish_kernel<8><<<grid, 256, 0, st>>>(w.sums, w.counts, blocks, a.E, a.d_bias, w.status, w.dw, splits, n, a.d_w);
+        else gate_finish_kernel<64><<<grid, 256, 0, st>>>(w.sums, w.counts, blocks, a.E, a.d_bias, w.status, w.dw, splits, n, a.d_w);
+    };
+    if (!a.d_x && !a.d_w) {
+        finish(1);
+        return;
+    }
     const int splits = w.dw_splits, tiles_per_split = ((a.T + 31) / 32 - 1) / splits + 1;
     float* const dw = splits > 1 ? w.dw : a.d_w;
     const dim3 grid((a.d + 127) / 128, splits);
@@ -555,8 +687,7 @@ void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStr
     };
     if (a.E <= 16) go(std::integral_constant<int, 1>{});
     else go(std::integral_constant<int, 2>{});
-    const size_t n = (size_t)a.E * a.d;
-    if (a.d_w && splits > 1) launch_reduce_splits(w.dw, splits, n, n, a.d_w, st);
+    finish(a.d_w ? splits : 1);
 }
 
 }  // namespace moemix

@@ -10,7 +10,7 @@ constexpr int kGateBlocks = 512;       // most workgroups that leave partial sum
 struct GateWorkspace {
     int32_t* status;    // [64] first word is the status word
     float* sums;        // [kGateBlocks][E]  partial sums over tokens: probabilities, or d_logits
-    int32_t* counts;    // [kGateBlocks][E + 1]
+    int32_t* counts;    // [kGateBlocks][E + 2]  pairs per expert, valid tokens, and whether an index was out of range
     float* dl;          // [T, E]  d_logits where the caller does not ask for them
     float* dw;          // [dw_splits][E, d]  partial d_w_gate
     int dw_splits;
@@ -29,7 +29,7 @@ inline GateWorkspace carve_gate_workspace(void* base, int T, int d, int E) {
     };
     w.status = (int32_t*)take(64 * sizeof(int32_t));
     w.sums = (float*)take((size_t)kGateBlocks * E * sizeof(float));
-    w.counts = (int32_t*)take((size_t)kGateBlocks * (E + 1) * sizeof(int32_t));
+    w.counts = (int32_t*)take((size_t)kGateBlocks * (E + 2) * sizeof(int32_t));
     w.dl = (float*)take((size_t)T * E * sizeof(float));
     w.dw_splits = gate_dw_splits(T, d, E);
     w.dw = (float*)take(w.dw_splits > 1 ? (size_t)w.dw_splits * E * d * sizeof(float) : 0);

@@ -209,7 +209,7 @@ def test_backward(T, E, k, d, padded, half):
     assert np.all(np.abs(got["d_x"].astype(np.float64) - ref) <= dx_bound)
     xv = xf * (valid[:, None] > 0)
     mag = np.abs(want).T @ np.abs(xv)
-    dw_bound = np.broadcast_to(dl_bound, want.shape).T @ np.abs(xv) + mag * (T / 8 + 32) * EPS
+    dw_bound = dl_bound.T @ np.abs(xv) + mag * (T / 8 + 32) * EPS            # (dl_bound is the same for all experts)
     err = np.abs(got["d_w_gate"] - want.T @ xv)
     assert np.all(err <= dw_bound)
     assert np.linalg.norm(err) <= 2.0 ** -18 * np.linalg.norm(want.T @ xv) + 2.0 ** -30 * np.linalg.norm(mag)
