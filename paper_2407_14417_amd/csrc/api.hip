@@ -210,7 +210,9 @@ void run_fp8(const DevExperts& table, int E, const RowMap& rows, const half_t* x
     launch_quantize_fp8_rows(x, x_rows, d, w.x8, w.xs, st);
     {
         TraceScope trace(kKernelUp, st);
-        launch_fp8_matmul(a, true, true, false, st);
+        // (exact sums: hidden values that come out a trifle off are rounded to other codes now and then, steps of 2^-4 of a value.  512 tokens, Mixtral shape,
+        // deviation from 64 bits with sums of the instructions for 8-bit operands 1.3e-3, with exact ones 2.4e-4)
+        launch_fp8_matmul(a, true, true, true, st);
     }
     launch_quantize_fp8_rows(w.h, P, f, w.h8, w.hs, st);
     for (int e = 0; e < a.E; ++e) a.w[e] = fp8_mat(table.e[alone ? rows.direct_expert : e].w2);

@@ -149,11 +149,16 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
     }
     uint32_t at = 0;
     read_first(0);
+    // F8: codes go to the matrix cores as they are; else expanded to fp16.
+    half8_t wf[F8 ? 1 : 4][4], xf[4];
+    auto expand = [](const uint4_t (&v)[2], half8_t (&o)[4]) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) o[p] = fp8_expand(v[p >> 1][2 * (p & 1)], v[p >> 1][2 * (p & 1) + 1]);
+    };
     for (int b = 0; b < blocks; ++b) {
         const uint32_t next = at == (L::kStages - 1) * L::kStage ? 0u : at + L::kStage;
         const float* const sx = (const float*)(lds + at + L::kX + L::kW) + wm * 16 * MT + r16;
         float4_t part[2][2];
-        half8_t wf[F8 ? 1 : 4][4];
         const float scale_w0 = w0, scale_w1 = w1;
         float s_now = 0.0f, s_before = 0.0f;
         auto add = [&](int i, int h, float s) {              // half h of tile i (up: 0 is w1's, 1 w3's)
@@ -165,6 +170,19 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
                 asm volatile("" : "+v"(acc[2 * h + j][i]));  // added here: sinking it to the end of the block would keep all products alive
             }
         };
+        auto products = [&](int h) {
+            if constexpr (F8) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    part[h][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(join(w[2 * h + j][0], w[2 * h + j][1]), join(x[0], x[1]),
+                                                                                  float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) part[h][j] = mfma16(wf[2 * h + j][p], xf[p], p ? part[h][j] : float4_t{0.0f, 0.0f, 0.0f, 0.0f});
+            }
+        };
         read_w(at, 2, w[2]);
         read_w(at, 3, w[3]);
 #pragma unroll
@@ -173,29 +191,16 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
             x[1] = x_next[1];
             if (i + 1 < MT) read_x(at, i + 1, x_next);
             s_now = sx[16 * i];
-            half8_t xf[4];
-            if (!F8)
-#pragma unroll
-                for (int p = 0; p < 4; ++p) xf[p] = fp8_expand(x[p >> 1][2 * (p & 1)], x[p >> 1][2 * (p & 1) + 1]);
+            if constexpr (!F8) expand(x, xf);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (!F8 && i == 0)
-#pragma unroll
-                    for (int j = 2 * h; j < 2 * h + 2; ++j)
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) wf[F8 ? 0 : j][p] = fp8_expand(w[j][p >> 1][2 * (p & 1)], w[j][p >> 1][2 * (p & 1) + 1]);
-                if (F8) {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        part[h][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(join(w[2 * h + j][0], w[2 * h + j][1]), join(x[0], x[1]),
-                                                                                      float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int p = 0; p < 4; ++p)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            part[h][j] = mfma16(wf[F8 ? 0 : 2 * h + j][p], xf[p], p ? part[h][j] : float4_t{0.0f, 0.0f, 0.0f, 0.0f});
+                if constexpr (!F8) {
+                    if (i == 0) {
+                        expand(w[2 * h], wf[2 * h]);
+                        expand(w[2 * h + 1], wf[2 * h + 1]);
+                    }
                 }
+                products(h);
                 pin_schedule();
                 if (i == MT - 1 && h == 0) {                 // (past the last block: whatever lies there, never used)
                     meet(b + 1, next);
@@ -271,9 +276,9 @@ __global__ __launch_bounds__(512, 2) void fp8_tile_kernel(Fp8Args a, int per, in
         MOEMIX_TILE_CASE(2)
         MOEMIX_TILE_CASE(3)
         MOEMIX_TILE_CASE(4)
+        MOEMIX_TILE_CASE(5)
 #undef MOEMIX_TILE_CASE
 #define MOEMIX_TILE_CASE(n) case n: if constexpr (F8) tile_body<(n), F8, UP, OUT>(a, c, lds); break;
-        MOEMIX_TILE_CASE(5)
         MOEMIX_TILE_CASE(6)
         MOEMIX_TILE_CASE(7)
         MOEMIX_TILE_CASE(8)
@@ -299,7 +304,7 @@ void launch(const Fp8Args& a, int per, hipStream_t st) {
 // Of several experts some have more rows than the mean: an eighth more is reckoned with (512 tokens, 8 experts, top-2,
 // 128 rows on average: chunks of 128 rows 449 us a block, of 160 425).
 static int rows_per_chunk(const Fp8Args& a, bool up, bool exact, long long* best_cost) {
-    const int out = up ? kCols / 2 : kCols, tiles = (a.N + out - 1) / out, most = exact ? 4 : 8;
+    const int out = up ? kCols / 2 : kCols, tiles = (a.N + out - 1) / out, most = exact ? 5 : 8;
     const int with_rows = a.E < a.P ? a.E : a.P, mean = (a.P + with_rows - 1) / with_rows + (with_rows > 1 ? a.P / with_rows / 8 : 0);
     int per = 32, best_chunks = 0;
     for (int mt = 1; mt <= most; ++mt) {
@@ -329,7 +334,7 @@ float fp8_tile_us(const Fp8Args& a, bool up, bool exact) {
 void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st) {
     long long cost = 0;
     const int per = rows_per_chunk(a, up, exact, &cost);
-    if (up) launch<true, true, half_t>(a, per, st);
+    if (up) launch<false, true, half_t>(a, per, st);
     else if (half_out) launch<true, false, half_t>(a, per, st);
     else if (exact) launch<false, false, float>(a, per, st);
     else launch<true, false, float>(a, per, st);
