@@ -201,20 +201,15 @@ void run_fp8(const DevExperts& table, int E, const RowMap& rows, const half_t* x
     a.offsets = rows.offsets;
     a.perm = rows.perm;
     a.status = w.status;
-    a.y = w.h;
     a.P = P;
     a.top_k = rows.top_k;
     a.x_rows = x_rows;
     a.N = f;
     a.K = d;
     launch_quantize_fp8_rows(x, x_rows, d, w.x8, w.xs, st);
-    {
-        TraceScope trace(kKernelUp, st);
-        // (exact sums: hidden values that come out a trifle off are rounded to other codes now and then, steps of 2^-4 of a value.  512 tokens, Mixtral shape,
-        // deviation from 64 bits with sums of the instructions for 8-bit operands 1.3e-3, with exact ones 2.4e-4)
-        launch_fp8_matmul(a, true, true, true, st);
-    }
-    launch_quantize_fp8_rows(w.h, P, f, w.h8, w.hs, st);
+    // (exact sums: hidden values that come out a trifle off are rounded to other codes now and then, steps of 2^-4 of a value.  512 tokens, Mixtral shape,
+    // deviation from 64 bits with sums of the instructions for 8-bit operands 1.3e-3, with exact ones 2.4e-4)
+    launch_fp8_up(a, w.h, w.h8, w.hs, st);
     for (int e = 0; e < a.E; ++e) a.w[e] = fp8_mat(table.e[alone ? rows.direct_expert : e].w2);
     a.x = w.h8;
     a.xs = w.hs;
@@ -224,7 +219,7 @@ void run_fp8(const DevExperts& table, int E, const RowMap& rows, const half_t* x
     a.N = d;
     a.K = f;
     TraceScope trace(kKernelDown, st);
-    launch_fp8_matmul(a, false, false, false, st);
+    launch_fp8_matmul(a, false, false, st);
 }
 
 // One token, all experts in e4m3: gating, then two launches that quantize the rows they multiply.
@@ -833,7 +828,7 @@ int matmul_fp8(const char* who, const moe_mat* w, int n_experts, int out, int in
     a.x_rows = n_rows;
     a.N = out;
     a.K = in;
-    launch_fp8_matmul(a, false, y_type == MOE_OUT_F16, y_type != MOE_OUT_F16, st);
+    launch_fp8_matmul(a, y_type == MOE_OUT_F16, y_type != MOE_OUT_F16, st);
     return check_hip(st);
 }
 

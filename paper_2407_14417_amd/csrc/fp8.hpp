@@ -28,12 +28,16 @@ struct Fp8Args {
     const int32_t* perm;          // [P] or null; row r reads x row perm[r] / top_k (null: r)
     int32_t* status;              // or null
     void* y;                      // [P, N]
+    float* y_scale;               // up, tile kernel: [ceil(N/128), P], y are codes
     int E, P, top_k, x_rows, N, K;
 };
 
-// up: y[r, :] = fp16( silu(W1 x) * (W3 x) ); else fp32 or fp16 (half_out) rows of W x.  exact: sums as exact as 32 bits allow (else they
+// Up-projection: hidden rows fp16( silu(W1 x) * (W3 x) ) quantized into codes [P, N] and scale [ceil(N/128), P]; h [P, N]: room for the rows in fp16.
+// Sums are exact.
+void launch_fp8_up(const Fp8Args& a, half_t* h, uint8_t* codes, float* scale, hipStream_t st);
+// Rows of W x, fp32 or fp16 (half_out).  exact: sums as exact as 32 bits allow (else they
 // may come from the matrix instructions for 8-bit operands, see fp8_tile.hip).
-void launch_fp8_matmul(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st);
+void launch_fp8_matmul(const Fp8Args& a, bool half_out, bool exact, hipStream_t st);
 bool fp8_tile_can(const Fp8Args& a);
 float fp8_tile_us(const Fp8Args& a, bool up, bool exact);
 void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st);

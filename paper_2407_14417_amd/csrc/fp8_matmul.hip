@@ -322,18 +322,37 @@ void launch_fp8_one(const Fp8OneArgs& a, bool up, hipStream_t st) {
     else fp8_one_kernel<false><<<tiles, 64 * kFewWaves, fp8_one_lds(a.k, a.K, false), st>>>(a);
 }
 
-void launch_fp8_matmul(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st) {
-    if (a.P == 0 || a.N == 0) return;
-    if (fp8_tile_can(a) && fp8_tile_us(a, up, exact) < few_us(a, up)) {
-        launch_fp8_tile(a, up, half_out, exact, st);
-        return;
-    }
+static void launch_few_any(const Fp8Args& a, bool up, bool half_out, hipStream_t st) {
     const int ct = few_rows16(a), nt = few_tiles(a, ct, up);
     if (ct == 1) launch_few<1, 1>(a, up, half_out, st);
     else if (ct == 2 && nt == 1) launch_few<2, 1>(a, up, half_out, st);
     else if (ct == 2) launch_few<2, 2>(a, up, half_out, st);
     else if (nt == 1) launch_few<4, 1>(a, up, half_out, st);
     else launch_few<4, 2>(a, up, half_out, st);
+}
+
+void launch_fp8_matmul(const Fp8Args& a, bool half_out, bool exact, hipStream_t st) {
+    if (a.P == 0 || a.N == 0) return;
+    if (fp8_tile_can(a) && fp8_tile_us(a, false, exact) < few_us(a, false)) launch_fp8_tile(a, false, half_out, exact, st);
+    else launch_few_any(a, false, half_out, st);
+}
+
+// The tile kernel holds a row's whole block of 128 hidden values and quantizes it; after the other kernel that is a launch of its own.
+void launch_fp8_up(const Fp8Args& args, half_t* h, uint8_t* codes, float* scale, hipStream_t st) {
+    Fp8Args a = args;
+    if (fp8_tile_can(a) && fp8_tile_us(a, true, true) < few_us(a, true)) {
+        a.y = codes;
+        a.y_scale = scale;
+        TraceScope trace(kKernelUp, st);
+        launch_fp8_tile(a, true, false, true, st);
+        return;
+    }
+    a.y = h;
+    {
+        TraceScope trace(kKernelUp, st);
+        launch_few_any(a, true, true, st);
+    }
+    launch_quantize_fp8_rows(h, a.P, a.N, codes, scale, st);
 }
 
 }  // namespace moemix

@@ -218,19 +218,64 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
         at = next;
     }
     // ---- lane: row r16 of a tile of x, results 4 q .. 4 q + 3 of a tile of w
+    if constexpr (UP) {
+        // The tile's 128 hidden values of a row are a block: rounded to fp16 as everywhere, then quantized here.  The largest magnitude of a row
+        // goes over the four lanes that hold it and, through LDS, over the four wavefronts.
+        uint32_t* const tops = (uint32_t*)lds;               // [4][32 MT]
+        half4_t h[MT][2];
+        __syncthreads();                                     // (the stages have been read)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const half_t v = n0 + wn * 32 + j * 16 + 4 * q + k < N ? (half_t)silu_mul(acc[j][i][k], acc[j + 2][i][k]) : (half_t)0.0f;
+                    const uint32_t bits = __builtin_bit_cast(uint16_t, v) & 0x7FFFu;
+                    h[i][j][k] = v;
+                    top = top > bits ? top : bits;
+                }
+#pragma unroll
+            for (int m = 16; m <= 32; m <<= 1) {
+                const uint32_t o = __shfl_xor(top, m, kWave);
+                top = top > o ? top : o;
+            }
+            if (q == 0) tops[wn * (32 * MT) + (wm * MT + i) * 16 + r16] = top;
+        }
+        __syncthreads();
+        uint8_t* const codes = (uint8_t*)a.y;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int r = (wm * MT + i) * 16 + r16;
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t o = tops[k * (32 * MT) + r];
+                top = top > o ? top : o;
+            }
+            const float m = magnitude_value(top), f = fp8_factor(m);
+            if (r >= rows) continue;
+            if (wn == 0 && q == 0) a.y_scale[(size_t)(n0 / kFp8Block) * a.P + c.begin + r] = fp8_scale(m);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int n = n0 + wn * 32 + j * 16 + 4 * q;     // (N is a multiple of 64)
+                const half4_t v = h[i][j];
+                if (n < N)
+                    *(uint32_t*)(codes + (size_t)(c.begin + r) * N + n) = fp8_pack((float)v[0] * f, (float)v[1] * f, (float)v[2] * f, (float)v[3] * f);
+            }
+        }
+        return;
+    }
     OUT* const y = (OUT*)a.y;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int r = (wm * MT + i) * 16 + r16;
         if (r >= rows) continue;
 #pragma unroll
-        for (int j = 0; j < (UP ? 2 : 4); ++j) {
-            const int n = n0 + (UP ? wn * 32 : wn * 64) + j * 16 + 4 * q;
-            float4_t v = acc[j][i];
-            if (UP) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = silu_mul(v[k], acc[(j + 2) & 3][i][k]);
-            }
+        for (int j = 0; j < 4; ++j) {
+            const int n = n0 + wn * 64 + j * 16 + 4 * q;
+            const float4_t v = acc[j][i];
             OUT* const o = y + (size_t)(c.begin + r) * N + n;
             if (n + 4 <= N) {
                 if (sizeof(OUT) == 4) *(float4_anywhere_t*)o = v;
@@ -334,7 +379,7 @@ float fp8_tile_us(const Fp8Args& a, bool up, bool exact) {
 void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st) {
     long long cost = 0;
     const int per = rows_per_chunk(a, up, exact, &cost);
-    if (up) launch<false, true, half_t>(a, per, st);
+    if (up) launch<false, true, uint8_t>(a, per, st);
     else if (half_out) launch<true, false, half_t>(a, per, st);
     else if (exact) launch<false, false, float>(a, per, st);
     else launch<true, false, float>(a, per, st);
