@@ -306,24 +306,38 @@ def moe_quantize_int8(w_fp16, codes, scale, zero) -> None:
 # Shapes, types and places of the tensors are looked at before a call (MoeError with MOE_EINVAL or MOE_ESHAPE): the kernels read and write what they
 # are told to.  Tensors have to be contiguous and on the current device.
 
-def _need(t, what: str, dtypes, shape) -> int:
-    """Pointer of tensor ``t``, which has to be contiguous, of one of ``dtypes`` and of ``shape``, on the current device."""
+# Types of tensors, filled in by _device(): f16, f32, i32, e4m3 codes, masks
+_F16 = _F32 = _I32 = _CODES = _MASK = _BYTES = ()
+
+
+def _device() -> int:
+    """The current GPU, on which the tensors of a call have to be (-1: there is none)."""
+    global _F16, _F32, _I32, _CODES, _MASK, _BYTES
     import torch
-    if not isinstance(t, torch.Tensor):
-        raise MoeError(MOE_EINVAL, f"{what}: a tensor is needed")
+    if not _F16:
+        _F32, _I32, _CODES = (torch.float32,), (torch.int32,), (torch.uint8, torch.float8_e4m3fn)
+        _MASK, _BYTES, _F16 = (torch.uint8, torch.bool), (torch.uint8,), (torch.float16,)
+    return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
+
+
+def _stream_on(dev: int) -> int:
+    """The current stream's handle, a small part of the time that torch.cuda.current_stream() takes (2.9 us a call)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _need(t, what: str, dtypes, shape, dev: int) -> int:
+    """Pointer of tensor ``t``, which has to be contiguous, of one of ``dtypes`` and of ``shape``, on GPU ``dev``."""
+    try:
+        if t.dtype in dtypes and t.shape == shape and t.is_contiguous() and t.get_device() == dev and dev >= 0:
+            return t.data_ptr()
+    except AttributeError:
+        raise MoeError(MOE_EINVAL, f"{what}: a tensor is needed") from None
     if t.dtype not in dtypes or not t.is_contiguous():
         raise MoeError(MOE_EINVAL, f"{what}: {t.dtype}, strides {t.stride()}: contiguous {dtypes} is needed")
     if t.shape != shape:
         raise MoeError(MOE_ESHAPE, f"{what}: {tuple(t.shape)}, {tuple(shape)} is needed")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise MoeError(MOE_EINVAL, f"{what}: on {t.device}, which is not the current GPU")
-    return t.data_ptr()
-
-
-def _types():
-    import torch
-    return ((torch.float16,), (torch.float32,), (torch.int32,), (torch.uint8, torch.float8_e4m3fn),
-            (torch.uint8, torch.bool))
+    raise MoeError(MOE_EINVAL, f"{what}: on {t.device}, which is not the current GPU")
 
 
 def _rows_cols(t, what: str):
@@ -336,97 +350,95 @@ def _blocks(n: int) -> int:
     return (n + FP8_BLOCK - 1) // FP8_BLOCK
 
 
-def _need_fp8(m: Mat, what: str):
-    """(out, in) of an e4m3 matrix whose tensors fit each other."""
-    _, f32, _, codes, _ = _types()
+def _need_fp8(m: Mat, what: str, dev: int) -> CMat:
+    """C descriptor of an e4m3 matrix whose tensors fit each other."""
     out, inn = _rows_cols(m.data, what)
-    _need(m.data, what, codes, (out, inn))
-    _need(m.scale, what + " scale", f32, (_blocks(out), _blocks(inn)))
-    return out, inn
+    return CMat(_need(m.data, what, _CODES, (out, inn), dev), _need(m.scale, "scale of " + what, _F32, (_blocks(out), _blocks(inn)), dev), None)
 
 
 def _out_type(t, what: str) -> int:
-    import torch
-    if t.dtype == torch.float32:
+    if t.dtype in _F32:
         return OUT_F32
-    if t.dtype == torch.float16:
+    if t.dtype in _F16:
         return OUT_F16
     raise MoeError(MOE_EINVAL, f"{what}: {t.dtype}: float32 or float16 is needed")
 
 
 def moe_quantize_fp8(w_fp16, codes, scale) -> None:
-    f16, f32, _, c8, _ = _types()
+    dev = _device()
     out, inn = _rows_cols(w_fp16, "w_fp16")
-    _check(lib().moe_quantize_fp8(_need(w_fp16, "w_fp16", f16, (out, inn)), out, inn, _need(codes, "codes", c8, (out, inn)),
-                                  _need(scale, "scale", f32, (_blocks(out), _blocks(inn))), _stream()))
+    _check(lib().moe_quantize_fp8(_need(w_fp16, "w_fp16", _F16, (out, inn), dev), out, inn, _need(codes, "codes", _CODES, (out, inn), dev),
+                                  _need(scale, "scale", _F32, (_blocks(out), _blocks(inn)), dev), _stream_on(dev)))
 
 
 def moe_dequant_fp8(m: Mat, out: int, inn: int, w_fp16) -> None:
-    f16 = _types()[0]
-    if _need_fp8(m, "m") != (out, inn):
+    dev = _device()
+    cm = _need_fp8(m, "m", dev)
+    if m.data.shape != (out, inn):
         raise MoeError(MOE_ESHAPE, f"m: {tuple(m.data.shape)}, {(out, inn)} is needed")
-    cm = m.c()
-    _check(lib().moe_dequant_fp8(ctypes.byref(cm), out, inn, _need(w_fp16, "w_fp16", f16, (out, inn)), _stream()))
+    _check(lib().moe_dequant_fp8(ctypes.byref(cm), out, inn, _need(w_fp16, "w_fp16", _F16, (out, inn), dev), _stream_on(dev)))
 
 
 def moe_quantize_fp8_rows(x, codes, scale) -> None:
-    f16, f32, _, c8, _ = _types()
+    dev = _device()
     n, inn = _rows_cols(x, "x")
-    _check(lib().moe_quantize_fp8_rows(_need(x, "x", f16, (n, inn)), n, inn, _need(codes, "codes", c8, (n, inn)),
-                                       _need(scale, "scale", f32, (_blocks(inn), n)), _stream()))
+    _check(lib().moe_quantize_fp8_rows(_need(x, "x", _F16, (n, inn), dev), n, inn, _need(codes, "codes", _CODES, (n, inn), dev),
+                                       _need(scale, "scale", _F32, (_blocks(inn), n), dev), _stream_on(dev)))
 
 
 def moe_transpose_fp8(m: Mat, codes_t, scale_t) -> None:
-    _, f32, _, c8, _ = _types()
-    out, inn = _need_fp8(m, "m")
-    cm = m.c()
-    _check(lib().moe_transpose_fp8(ctypes.byref(cm), out, inn, _need(codes_t, "codes_t", c8, (inn, out)),
-                                   _need(scale_t, "scale_t", f32, (_blocks(inn), _blocks(out))), _stream()))
+    dev = _device()
+    cm = _need_fp8(m, "m", dev)
+    out, inn = m.data.shape
+    _check(lib().moe_transpose_fp8(ctypes.byref(cm), out, inn, _need(codes_t, "codes_t", _CODES, (inn, out), dev),
+                                   _need(scale_t, "scale_t", _F32, (_blocks(inn), _blocks(out)), dev), _stream_on(dev)))
 
 
 def moe_matmul_fp8(w: Mat, x_codes, x_scale, y) -> None:
     """y = x W^T: ``x_codes`` [n,in] and ``x_scale`` [ceil(in/128),n] of moe_quantize_fp8_rows, ``y`` [n,out] float32 or float16."""
-    _, f32, _, c8, _ = _types()
-    out, inn = _need_fp8(w, "w")
+    dev = _device()
+    cm = _need_fp8(w, "w", dev)
+    out, inn = w.data.shape
     n = _rows_cols(x_codes, "x_codes")[0]
-    cm = w.c()
-    _check(lib().moe_matmul_fp8(ctypes.byref(cm), out, inn, _need(x_codes, "x_codes", c8, (n, inn)),
-                                _need(x_scale, "x_scale", f32, (_blocks(inn), n)), n, _need(y, "y", (y.dtype,), (n, out)),
-                                _out_type(y, "y"), _stream()))
+    _check(lib().moe_matmul_fp8(cm, out, inn, _need(x_codes, "x_codes", _CODES, (n, inn), dev),
+                                _need(x_scale, "x_scale", _F32, (_blocks(inn), n), dev), n, _need(y, "y", _F32 + _F16, (n, out), dev),
+                                _out_type(y, "y"), _stream_on(dev)))
 
 
 class MatGroup:
     """Host array of e4m3 matrices of one shape for moe_matmul_fp8_grouped, built once; keeps their tensors alive."""
 
     def __init__(self, mats: Sequence[Mat]):
-        self.mats = list(mats)
+        self.mats, dev = list(mats), _device()
         if not 1 <= len(self.mats) <= MAX_EXPERTS:
             raise MoeError(MOE_ESHAPE, f"{len(self.mats)} matrices, 1 to {MAX_EXPERTS} are possible")
-        self.shape = _need_fp8(self.mats[0], "matrix 0")
+        self.c = (CMat * len(self.mats))(*[_need_fp8(m, f"matrix {i}", dev) for i, m in enumerate(self.mats)])
+        self.shape, self.device = tuple(self.mats[0].data.shape), dev
         for i, m in enumerate(self.mats):
-            if _need_fp8(m, f"matrix {i}") != self.shape:
-                raise MoeError(MOE_ESHAPE, f"matrix {i}: {tuple(m.data.shape)}, {tuple(self.shape)} is needed")
-        self.c = (CMat * len(self.mats))(*[m.c() for m in self.mats])
+            if m.data.shape != self.shape:
+                raise MoeError(MOE_ESHAPE, f"matrix {i}: {tuple(m.data.shape)}, {self.shape} is needed")
 
 
 def moe_matmul_fp8_grouped(group: MatGroup, x_codes, x_scale, offsets, perm, top_k: int, y) -> None:
     """``perm`` None: rows of x in order."""
-    _, f32, i32, c8, _ = _types()
+    dev = _device()
+    if group.device != dev:
+        raise MoeError(MOE_EINVAL, f"matrices on GPU {group.device}, the current one is {dev}")
     (out, inn), E = group.shape, len(group.mats)
     n, P = _rows_cols(x_codes, "x_codes")[0], _rows_cols(y, "y")[0]
-    _check(lib().moe_matmul_fp8_grouped(group.c, E, out, inn, _need(x_codes, "x_codes", c8, (n, inn)),
-                                        _need(x_scale, "x_scale", f32, (_blocks(inn), n)), n,
-                                        _need(offsets, "offsets", i32, (E + 1,)),
-                                        None if perm is None else _need(perm.view(-1), "perm", i32, (P,)), top_k, P,
-                                        _need(y, "y", (y.dtype,), (P, out)), _out_type(y, "y"), _stream()))
+    _check(lib().moe_matmul_fp8_grouped(group.c, E, out, inn, _need(x_codes, "x_codes", _CODES, (n, inn), dev),
+                                        _need(x_scale, "x_scale", _F32, (_blocks(inn), n), dev), n,
+                                        _need(offsets, "offsets", _I32, (E + 1,), dev),
+                                        None if perm is None else _need(perm, "perm", _I32, (P,), dev), top_k, P,
+                                        _need(y, "y", _F32 + _F16, (P, out), dev), _out_type(y, "y"), _stream_on(dev)))
 
 
 def moe_route_logits(layer: Layer, x, logits, topk_idx, topk_gate) -> None:
-    f16, f32, i32, _, _ = _types()
+    dev = _device()
     T, E, k = _rows_cols(x, "x")[0], layer.n_experts, layer.top_k
-    _check(lib().moe_route_logits(ctypes.byref(layer.c), _need(x, "x", f16, (T, layer.d_model)), T,
-                                  _need(logits, "logits", f32, (T, E)), _need(topk_idx, "topk_idx", i32, (T, k)),
-                                  _need(topk_gate, "topk_gate", f32, (T, k)), _stream()))
+    _check(lib().moe_route_logits(layer.c, _need(x, "x", _F16, (T, layer.d_model), dev), T, _need(logits, "logits", _F32, (T, E), dev),
+                                  _need(topk_idx, "topk_idx", _I32, (T, k), dev), _need(topk_gate, "topk_gate", _F32, (T, k), dev),
+                                  _stream_on(dev)))
 
 
 def gate_workspace_bytes(layer: Layer, n_tokens: int) -> int:
@@ -441,39 +453,32 @@ def alloc_gate_workspace(layer: Layer, n_tokens: int):
     return torch.empty(n, dtype=torch.uint8, device="cuda")
 
 
-def _need_ws(ws):
-    import torch
-    if ws is None:
-        return None, 0
-    return _need(ws, "ws", (torch.uint8,), ws.shape), ws.numel()
-
-
 def moe_balance_loss(layer: Layer, logits, topk_idx, counts, mean_prob, loss, ws, valid=None) -> None:
-    _, f32, i32, _, u8 = _types()
+    dev = _device()
     T, E, k = _rows_cols(logits, "logits")[0], layer.n_experts, layer.top_k
-    p, nbytes = _need_ws(ws)
-    _check(lib().moe_balance_loss(ctypes.byref(layer.c), _need(logits, "logits", f32, (T, E)), _need(topk_idx, "topk_idx", i32, (T, k)),
-                                  None if valid is None else _need(valid, "valid", u8, (T,)), T,
-                                  _need(counts, "counts", i32, (E + 1,)), _need(mean_prob, "mean_prob", f32, (E,)),
-                                  _need(loss, "loss", f32, (1,)), p, nbytes, _stream()))
+    _check(lib().moe_balance_loss(layer.c, _need(logits, "logits", _F32, (T, E), dev), _need(topk_idx, "topk_idx", _I32, (T, k), dev),
+                                  None if valid is None else _need(valid, "valid", _MASK, (T,), dev), T,
+                                  _need(counts, "counts", _I32, (E + 1,), dev), _need(mean_prob, "mean_prob", _F32, (E,), dev),
+                                  _need(loss, "loss", _F32, (1,), dev), None if ws is None else _need(ws, "ws", _BYTES, ws.shape, dev),
+                                  0 if ws is None else ws.numel(), _stream_on(dev)))
 
 
 def moe_route_backward(layer: Layer, x, logits, topk_idx, ws, valid=None, counts=None, d_gate=None, d_loss=None, d_logits=None,
                        d_x=None, d_w_gate=None, d_bias=None) -> None:
     """The gradients that are not None are written; ``d_x`` float32 or float16."""
-    f16, f32, i32, _, u8 = _types()
+    dev = _device()
     T, E, k, d = _rows_cols(logits, "logits")[0], layer.n_experts, layer.top_k, layer.d_model
-
-    def opt(t, what, dtypes, shape):
-        return None if t is None else _need(t, what, dtypes, shape)
-
-    p, nbytes = _need_ws(ws)
     _check(lib().moe_route_backward(
-        ctypes.byref(layer.c), opt(x, "x", f16, (T, d)), _need(logits, "logits", f32, (T, E)),
-        _need(topk_idx, "topk_idx", i32, (T, k)), opt(valid, "valid", u8, (T,)), T, opt(counts, "counts", i32, (E + 1,)),
-        opt(d_gate, "d_gate", f32, (T, k)), opt(d_loss, "d_loss", f32, (1,)), opt(d_logits, "d_logits", f32, (T, E)),
-        opt(d_x, "d_x", f16 + f32, (T, d)), OUT_F32 if d_x is None else _out_type(d_x, "d_x"),
-        opt(d_w_gate, "d_w_gate", f32, (E, d)), opt(d_bias, "d_bias", f32, (E,)), p, nbytes, _stream()))
+        layer.c, None if x is None else _need(x, "x", _F16, (T, d), dev), _need(logits, "logits", _F32, (T, E), dev),
+        _need(topk_idx, "topk_idx", _I32, (T, k), dev), None if valid is None else _need(valid, "valid", _MASK, (T,), dev), T,
+        None if counts is None else _need(counts, "counts", _I32, (E + 1,), dev),
+        None if d_gate is None else _need(d_gate, "d_gate", _F32, (T, k), dev),
+        None if d_loss is None else _need(d_loss, "d_loss", _F32, (1,), dev),
+        None if d_logits is None else _need(d_logits, "d_logits", _F32, (T, E), dev),
+        None if d_x is None else _need(d_x, "d_x", _F32 + _F16, (T, d), dev), OUT_F32 if d_x is None else _out_type(d_x, "d_x"),
+        None if d_w_gate is None else _need(d_w_gate, "d_w_gate", _F32, (E, d), dev),
+        None if d_bias is None else _need(d_bias, "d_bias", _F32, (E,), dev),
+        None if ws is None else _need(ws, "ws", _BYTES, ws.shape, dev), 0 if ws is None else ws.numel(), _stream_on(dev)))
 
 
 def moe_synth_fill_f16(dst, first: int, seed: int, stream_id: int, scale: float, kind: int) -> None:
