@@ -351,43 +351,49 @@ __global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradA
     }
 }
 
-// Workgroup 0: d_bias (in 64 bits, in a fixed order, of up to 8 ROWS workgroups) and the status of the call from what gate_dlogits_kernel left; the others: d_w from its
-// partial sums, in order, four values per thread.
-template <int ROWS>
-__global__ __launch_bounds__(256) void gate_finish_kernel(const float* __restrict__ sums, const int32_t* __restrict__ flags, int blocks, int E,
-                                                          float* __restrict__ d_bias, int32_t* __restrict__ status,
-                                                          const float* __restrict__ dw, int splits, size_t n, float* __restrict__ d_w) {
-    if (blockIdx.x) {
-        const size_t i = ((size_t)(blockIdx.x - 1) * 256 + threadIdx.x) * 4;
-        if (i >= n) return;                              // (n = E d is a multiple of 64)
-        float4_t v = *(const float4_t*)(dw + i);
-#pragma unroll 8
-        for (int s = 1; s < splits; ++s) v += *(const float4_t*)(dw + s * n + i);
-        *(float4_anywhere_t*)(d_w + i) = v;
-        return;
-    }
-    __shared__ double part[8][33];
+// One workgroup of 32 GROUPS threads: d_bias (in 64 bits, in a fixed order, of up to GROUPS ROWS workgroups' sums) and the status of the call, from
+// what gate_dlogits_kernel left.
+template <int GROUPS, int ROWS>
+__device__ __forceinline__ void finish_bias(const float* __restrict__ sums, const int32_t* __restrict__ flags, int blocks, int E,
+                                            float* __restrict__ d_bias, int32_t* __restrict__ status) {
+    __shared__ double part[GROUPS][33];
     __shared__ int32_t bad;
     const int e = threadIdx.x & 31, g = threadIdx.x >> 5;
     if (threadIdx.x == 0) bad = 0;
     double v = 0.0;
-    float r[ROWS];
+    float r[ROWS];                                       // all of a thread's values are asked for before the first is added
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) r[i] = sums[(size_t)min(g + 8 * i, blocks - 1) * E + min(e, E - 1)];
+    for (int i = 0; i < ROWS; ++i) r[i] = sums[(size_t)min(g + GROUPS * i, blocks - 1) * E + min(e, E - 1)];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) v += e < E && g + 8 * i < blocks ? r[i] : 0.0f;
+    for (int i = 0; i < ROWS; ++i) v += e < E && g + GROUPS * i < blocks ? r[i] : 0.0f;
     part[g][e] = v;
     int32_t f = 0;
-    for (int b = threadIdx.x; b < blocks; b += 256) f |= flags[b];
+    for (int b = threadIdx.x; b < blocks; b += 32 * GROUPS) f |= flags[b];
     __syncthreads();
     if (f) atomicOr(&bad, 1);
     __syncthreads();
     if (d_bias && (int)threadIdx.x < E) {
         v = 0.0;
-        for (int i = 0; i < 8; ++i) v += part[i][e];
+        for (int i = 0; i < GROUPS; ++i) v += part[i][e];
         d_bias[e] = (float)v;
     }
     if (threadIdx.x == 0) *status = bad ? kStatusBadIndex : 0;
+}
+
+// Workgroup 0: d_bias and the status; the others: d_w from its partial sums, in order, four values per thread.
+__global__ __launch_bounds__(256) void gate_finish_kernel(const float* __restrict__ sums, const int32_t* __restrict__ flags, int blocks, int E,
+                                                          float* __restrict__ d_bias, int32_t* __restrict__ status,
+                                                          const float* __restrict__ dw, int splits, size_t n, float* __restrict__ d_w) {
+    if (blockIdx.x == 0) {
+        finish_bias<8, kGateBlocks / 8>(sums, flags, blocks, E, d_bias, status);
+        return;
+    }
+    const size_t i = ((size_t)(blockIdx.x - 1) * 256 + threadIdx.x) * 4;
+    if (i >= n) return;                                  // (n = E d is a multiple of 64)
+    float4_t v = *(const float4_t*)(dw + i);
+#pragma unroll 8
+    for (int s = 1; s < splits; ++s) v += *(const float4_t*)(dw + s * n + i);
+    *(float4_anywhere_t*)(d_w + i) = v;
 }
 
 // ---- d_x = d_logits W and d_w = d_logits^T x in one pass over x, on the matrix cores
@@ -423,9 +429,21 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
     return m;
 }
 
-// ET: tiles of 16 experts.  Workgroup (x, y): columns 128 x .., the y-th share of the units' token tiles, its wavefronts in turn.
+// ET: tiles of 16 experts.  Workgroup (x, y): columns 128 x .., the y-th share of the units' token tiles, its wavefronts in turn.  One share alone: the
+// workgroup behind the last column finishes what gate_dlogits_kernel left.
+struct GradRest {
+    const float* sums;
+    const int32_t* flags;
+    int blocks;
+    int32_t* status;
+};
 template <int ET, typename OUT>
-__global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGradArgs a, int tiles_per_split, float* __restrict__ dw) {
+__global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGradArgs a, int tiles_per_split, float* __restrict__ dw, GradRest rest) {
+    if ((int)blockIdx.x * 128 >= a.d) {
+        if (rest.blocks <= 64) finish_bias<2 * kGradWaves, 4>(rest.sums, rest.flags, rest.blocks, a.E, a.d_bias, rest.status);
+        else finish_bias<2 * kGradWaves, kGateBlocks / (2 * kGradWaves)>(rest.sums, rest.flags, rest.blocks, a.E, a.d_bias, rest.status);
+        return;
+    }
     __shared__ float4_t sums[kGradWaves / 2][16][64];
     const int lane = threadIdx.x & 63, r16 = lane & 15, q = lane >> 4, E = a.E, d = a.d;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -650,11 +668,12 @@ void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t*
     else balance_finish_kernel<16><<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss, w.status);
 }
 
-// A compute unit per workgroup, as far as every wavefront has a tile of 32 tokens.
+// A compute unit per workgroup, as far as every wavefront has a tile of 32 tokens; up to two tiles a wavefront one share takes alone, which saves the
+// launch that adds shares up.
 int gate_dw_splits(int T, int d, int) {
     const int by_work = ((T + 31) / 32 + kGradWaves - 1) / kGradWaves, by_chip = 256 / ((d + 127) / 128);
     const int s = by_work < by_chip ? by_work : by_chip;
-    return s < 1 ? 1 : s;
+    return by_work <= 2 || s < 1 ? 1 : s;
 }
 
 void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStream_t st) {
@@ -668,10 +687,8 @@ void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStr
     });
     const auto finish = [&](int splits) {
         const size_t n = splits > 1 ? (size_t)a.E * a.d : 0;
-        const unsigned grid = 1 + (unsigned)((n / 4 + 255) / 256);
-        static_assert(kGateBlocks == 8 * 64, "rows");
-        if (blocks <= 64) gate_finish_kernel<8><<<grid, 256, 0, st>>>(w.sums, w.counts, blocks, a.E, a.d_bias, w.status, w.dw, splits, n, a.d_w);
-        else gate_finish_kernel<64><<<grid, 256, 0, st>>>(w.sums, w.counts, blocks, a.E, a.d_bias, w.status, w.dw, splits, n, a.d_w);
+        gate_finish_kernel<<<1 + (unsigned)((n / 4 + 255) / 256), 256, 0, st>>>(w.sums, w.counts, blocks, a.E, a.d_bias, w.status, w.dw, splits, n,
+                                                                                a.d_w);
     };
     if (!a.d_x && !a.d_w) {
         finish(1);
@@ -679,15 +696,16 @@ void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStr
     }
     const int splits = w.dw_splits, tiles_per_split = ((a.T + 31) / 32 - 1) / splits + 1;
     float* const dw = splits > 1 ? w.dw : a.d_w;
-    const dim3 grid((a.d + 127) / 128, splits);
+    const GradRest rest{w.sums, w.counts, blocks, w.status};
+    const dim3 grid((a.d + 127) / 128 + (splits == 1), splits);
     const auto go = [&](auto tiles) {
         constexpr int ET = decltype(tiles)::value;
-        if (a.d_x_half) gate_dx_dw_kernel<ET, half_t><<<grid, 64 * kGradWaves, 0, st>>>(a, tiles_per_split, dw);
-        else gate_dx_dw_kernel<ET, float><<<grid, 64 * kGradWaves, 0, st>>>(a, tiles_per_split, dw);
+        if (a.d_x_half) gate_dx_dw_kernel<ET, half_t><<<grid, 64 * kGradWaves, 0, st>>>(a, tiles_per_split, dw, rest);
+        else gate_dx_dw_kernel<ET, float><<<grid, 64 * kGradWaves, 0, st>>>(a, tiles_per_split, dw, rest);
     };
     if (a.E <= 16) go(std::integral_constant<int, 1>{});
     else go(std::integral_constant<int, 2>{});
-    finish(a.d_w ? splits : 1);
+    if (splits > 1) finish(a.d_w ? splits : 1);
 }
 
 }  // namespace moemix
