@@ -122,8 +122,8 @@ struct Chunks {
         expert = __builtin_ctzll(past);
         const int first = i - (__builtin_amdgcn_readlane(end, expert) - __builtin_amdgcn_readlane(mine, expert));
         const int from = __builtin_amdgcn_readlane(lo, expert), to = __builtin_amdgcn_readlane(hi, expert);
-        // an expert's chunks are of equal length, to a whole number of 32 rows
-        const int even = (to - from - 1) / __builtin_amdgcn_readlane(mine, expert) + 1, size = min(per, (even + 31) & ~31);
+        // an expert's chunks are of equal length, to a whole number of 16 rows
+        const int even = (to - from - 1) / __builtin_amdgcn_readlane(mine, expert) + 1, size = min(per, (even + 15) & ~15);
         begin = from + first * size;
         rows = min(size, to - begin);
         return rows > 0;

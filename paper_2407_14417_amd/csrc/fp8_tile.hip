@@ -1,5 +1,6 @@
 // Products of e4m3 rows and matrices where a matrix has many rows: tiles that stay in LDS and registers.
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "fp8.hpp"
@@ -21,15 +22,16 @@ __device__ __forceinline__ int8v_t join(uint4_t a, uint4_t b) {
 constexpr int kLds = 163840;             // of a compute unit
 constexpr int kCols = 256;               // rows of w per tile (up: 128 of w1 and 128 of w3)
 
-// A chunk of 32 MT rows of x: 8 wavefronts = 2 (rows of x) x 4 (rows of w), each multiplies 16 MT rows of x with 64 of w.  A stage of LDS holds
-// a block of 128 columns: x [32 MT][128], w [256][128], scales [8][64].
-template <int MT>
+// A chunk of TT tiles of 16 rows of x: 8 wavefronts = 2 (rows of x) x 4 (rows of w).  A wavefront multiplies half of the tiles (an odd one is the first
+// half's) with 64 rows of w; the two that share a SIMD are one of each half.  A stage of LDS holds a block of 128 columns: x [16 TT][128], w [256][128],
+// scales [8][64].
+template <int TT>
 struct Tile {
-    static constexpr int kX = MT * 4096, kW = kCols * 128, kScales = 2048;
+    static constexpr int kX = TT * 2048, kW = kCols * 128, kScales = 2048;
     static constexpr int kStage = kX + kW + kScales;
-    static constexpr int kStages = 3 * kStage <= kLds ? 3 : 2;
+    static constexpr int kStages = 4 * kStage <= kLds ? 4 : 3 * kStage <= kLds ? 3 : 2;
     static_assert(kStages * kStage <= kLds, "LDS");
-    static constexpr int kRuns = 4 * MT;                     // runs of 8 rows (1 KB) of x; the first kRuns % 8 wavefronts (0: all) bring one more
+    static constexpr int kRuns = 2 * TT;                     // runs of 8 rows (1 KB) of x; the first kRuns % 8 wavefronts (0: all) bring one more
     static constexpr int kMost = (kRuns + 7) / 8, kMore = kRuns % 8;
 };
 
@@ -37,11 +39,12 @@ struct TileWork {
     int expert, n0, begin, rows;         // rows [begin, begin + rows) of y, results from n0 on
 };
 
-template <int MT, bool F8, bool UP, typename OUT>
-__device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, uint8_t* lds) {
-    typedef Tile<MT> L;
+// MT tiles of the chunk, those from `tile0` on, are the wavefront's.
+template <int TT, int MT, bool F8, bool UP, typename OUT>
+__device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, uint8_t* lds, int tile0) {
+    typedef Tile<TT> L;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave & 3;
     const int N = a.N, K = a.K, e = c.expert, n0 = c.n0, rows = c.rows;
     const int blocks = (K + kFp8Block - 1) / kFp8Block, tail = K - (blocks - 1) * kFp8Block;   // bytes of the last block
     const bool more = !L::kMore || wave < L::kMore;
@@ -88,6 +91,16 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
         sb += scales_of_block;
         put = put == lds0 + (L::kStages - 1) * L::kStage ? lds0 : put + L::kStage;
     };
+    // Up to `later` stages may be under way.
+    auto wait = [&](int later) {
+        if (later <= 0) wait_and_meet<0>();
+        else if (later == 1 && more) wait_and_meet<L::kMost + 5>();
+        else if (later == 1) wait_and_meet<L::kMost + 4>();
+        else if (later == 2 && more) wait_and_meet<2 * (L::kMost + 5)>();
+        else if (later == 2) wait_and_meet<2 * (L::kMost + 4)>();
+        else if (more) wait_and_meet<3 * (L::kMost + 5)>();
+        else wait_and_meet<3 * (L::kMost + 4)>();
+    };
     // Stage b is there, and nobody reads stage b - 1 any more.  The pieces past the end of the rows are cleared by who brought them.
     auto meet = [&](int b, uint32_t at) {
         if (b == blocks - 1 && tail < kFp8Block) {
@@ -100,9 +113,7 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
                 for (int k = 0; k < 4; ++k) *(uint4_t*)(lds + at + L::kX + (wave + 8 * k) * 1024 + lane * 16) = uint4_t{0u, 0u, 0u, 0u};
             }
         }
-        if (L::kStages == 2 || b + 1 >= blocks) wait_and_meet<0>();
-        else if (more) wait_and_meet<L::kMost + 5>();
-        else wait_and_meet<L::kMost + 4>();
+        wait(min(L::kStages - 2, blocks - 1 - b));
     };
     // ---- what it reads: lane l row r16 of 16, bytes 32 q .. 32 q + 31
     uint32_t off[2];
@@ -116,9 +127,9 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
     };
     auto read_x = [&](uint32_t at, int i, uint4_t (&v)[2]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) v[h] = *(const uint4_t*)(lds + at + (wm * MT + i) * 2048 + off[h]);
+        for (int h = 0; h < 2; ++h) v[h] = *(const uint4_t*)(lds + at + (tile0 + i) * 2048 + off[h]);
     };
-    float4_t acc[4][MT];
+    float4_t acc[4][MT ? MT : 1];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -137,18 +148,11 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
         if (UP) w1 = sw[64];
     };
     for (int b = 0; b < L::kStages && b < blocks; ++b) bring_stage(b == blocks - 1);
-    // (all stages asked for: the first one is there when those after it may be under way)
-    if (blocks > 2 && L::kStages == 3) {
-        if (more) wait_and_meet<2 * (L::kMost + 5)>();
-        else wait_and_meet<2 * (L::kMost + 4)>();
-    } else if (blocks > 1) {
-        if (more) wait_and_meet<L::kMost + 5>();
-        else wait_and_meet<L::kMost + 4>();
-    } else {
-        meet(0, 0);
-    }
+    if (blocks == 1) meet(0, 0);
+    else wait(min(L::kStages, blocks) - 1);
     uint32_t at = 0;
-    read_first(0);
+    if constexpr (MT > 0) read_first(0);
+    else w0 = 0.0f;
     // F8: codes go to the matrix cores as they are; else expanded to fp16.
     half8_t wf[F8 ? 1 : 4][4], xf[4];
     auto expand = [](const uint4_t (&v)[2], half8_t (&o)[4]) {
@@ -157,7 +161,7 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
     };
     for (int b = 0; b < blocks; ++b) {
         const uint32_t next = at == (L::kStages - 1) * L::kStage ? 0u : at + L::kStage;
-        const float* const sx = (const float*)(lds + at + L::kX + L::kW) + wm * 16 * MT + r16;
+        const float* const sx = (const float*)(lds + at + L::kX + L::kW) + 16 * tile0 + r16;
         float4_t part[2][2];
         const float scale_w0 = w0, scale_w1 = w1;
         float s_now = 0.0f, s_before = 0.0f;
@@ -183,8 +187,10 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
                     for (int j = 0; j < 2; ++j) part[h][j] = mfma16(wf[2 * h + j][p], xf[p], p ? part[h][j] : float4_t{0.0f, 0.0f, 0.0f, 0.0f});
             }
         };
-        read_w(at, 2, w[2]);
-        read_w(at, 3, w[3]);
+        if constexpr (MT > 0) {
+            read_w(at, 2, w[2]);
+            read_w(at, 3, w[3]);
+        }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             x[0] = x_next[0];
@@ -214,15 +220,20 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
             }
             s_before = s_now;
         }
-        add(MT - 1, 1, s_before);
+        if constexpr (MT > 0) {
+            add(MT - 1, 1, s_before);
+        } else {
+            meet(b + 1, next);
+            if (b + L::kStages < blocks) bring_stage(b + L::kStages == blocks - 1);
+        }
         at = next;
     }
     // ---- lane: row r16 of a tile of x, results 4 q .. 4 q + 3 of a tile of w
     if constexpr (UP) {
         // The tile's 128 hidden values of a row are a block: rounded to fp16 as everywhere, then quantized here.  The largest magnitude of a row
         // goes over the four lanes that hold it and, through LDS, over the four wavefronts.
-        uint32_t* const tops = (uint32_t*)lds;               // [4][32 MT]
-        half4_t h[MT][2];
+        uint32_t* const tops = (uint32_t*)lds;               // [4][16 TT]
+        half4_t h[MT ? MT : 1][2];
         __syncthreads();                                     // (the stages have been read)
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -241,17 +252,17 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
                 const uint32_t o = __shfl_xor(top, m, kWave);
                 top = top > o ? top : o;
             }
-            if (q == 0) tops[wn * (32 * MT) + (wm * MT + i) * 16 + r16] = top;
+            if (q == 0) tops[wn * (16 * TT) + (tile0 + i) * 16 + r16] = top;
         }
         __syncthreads();
         uint8_t* const codes = (uint8_t*)a.y;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const int r = (wm * MT + i) * 16 + r16;
+            const int r = (tile0 + i) * 16 + r16;
             uint32_t top = 0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const uint32_t o = tops[k * (32 * MT) + r];
+                const uint32_t o = tops[k * (16 * TT) + r];
                 top = top > o ? top : o;
             }
             const float m = magnitude_value(top), f = fp8_factor(m);
@@ -270,7 +281,7 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
     OUT* const y = (OUT*)a.y;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int r = (wm * MT + i) * 16 + r16;
+        const int r = (tile0 + i) * 16 + r16;
         if (r >= rows) continue;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -286,6 +297,17 @@ __device__ __forceinline__ void tile_body(const Fp8Args& a, const TileWork& c, u
                     if (n + k < N) o[k] = (OUT)v[k];
             }
         }
+    }
+}
+
+constexpr int most_tiles(bool f8) { return f8 ? 16 : 10; }   // (operands expanded to fp16 need more registers)
+
+template <int TT, bool F8, bool UP, typename OUT>
+__device__ __forceinline__ void tile_halves(const Fp8Args& a, const TileWork& c, uint8_t* lds) {
+    if constexpr (TT <= most_tiles(F8)) {
+        if (TT % 2 == 0) tile_body<TT, TT / 2, F8, UP, OUT>(a, c, lds, __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) * (TT / 2));
+        else if (threadIdx.x < 256) tile_body<TT, (TT + 1) / 2, F8, UP, OUT>(a, c, lds, 0);
+        else tile_body<TT, TT / 2, F8, UP, OUT>(a, c, lds, (TT + 1) / 2);
     }
 }
 
@@ -315,18 +337,24 @@ __global__ __launch_bounds__(512, 2) void fp8_tile_kernel(Fp8Args a, int per, in
                 if (c.n0 + i % kOut < N) ((OUT*)a.y)[(size_t)(c.begin + i / kOut) * N + c.n0 + i % kOut] = (OUT)0.0f;
         return;
     }
-    switch ((c.rows + 31) >> 5) {
-#define MOEMIX_TILE_CASE(n) case n: tile_body<(n), F8, UP, OUT>(a, c, lds); break;
+    switch ((c.rows + 15) >> 4) {
+#define MOEMIX_TILE_CASE(n) case n: tile_halves<(n), F8, UP, OUT>(a, c, lds); break;
         MOEMIX_TILE_CASE(1)
         MOEMIX_TILE_CASE(2)
         MOEMIX_TILE_CASE(3)
         MOEMIX_TILE_CASE(4)
         MOEMIX_TILE_CASE(5)
-#undef MOEMIX_TILE_CASE
-#define MOEMIX_TILE_CASE(n) case n: if constexpr (F8) tile_body<(n), F8, UP, OUT>(a, c, lds); break;
         MOEMIX_TILE_CASE(6)
         MOEMIX_TILE_CASE(7)
         MOEMIX_TILE_CASE(8)
+        MOEMIX_TILE_CASE(9)
+        MOEMIX_TILE_CASE(10)
+        MOEMIX_TILE_CASE(11)
+        MOEMIX_TILE_CASE(12)
+        MOEMIX_TILE_CASE(13)
+        MOEMIX_TILE_CASE(14)
+        MOEMIX_TILE_CASE(15)
+        MOEMIX_TILE_CASE(16)
 #undef MOEMIX_TILE_CASE
     }
 }
@@ -344,21 +372,23 @@ void launch(const Fp8Args& a, int per, hipStream_t st) {
 
 }  // namespace
 
-// Rows per chunk: the number (of 32s) whose rounds of workgroups over the chip cost least, a block of 128 columns costing
-// 2 + MT in a workgroup of 32 MT rows (measured, 4096 rows 4096 -> 14336: 0.88 us a block for MT = 2, 1.40 for 4, 1.81 for 6, 2.18 for 8).
-// Of several experts some have more rows than the mean: an eighth more is reckoned with (512 tokens, 8 experts, top-2,
-// 128 rows on average: chunks of 128 rows 449 us a block, of 160 425).
+// Rows per chunk: the number (of 16s) whose rounds of workgroups over the chip cost least, a block of 128 columns costing
+// 4 + TT in a workgroup of TT tiles (measured, 4096 rows 4096 -> 14336: 0.88 us a block for TT = 4, 1.40 for 8, 1.81 for 12, 2.18 for 16).
+// Of several experts some have more rows than the mean: an eighth or two standard deviations more is reckoned with (16 experts of 1024 x 4096, 128 rows
+// on average: chunks of 144 rows, which some experts exceed, 37.5 us, of 160 24.7).
 static int rows_per_chunk(const Fp8Args& a, bool up, bool exact, long long* best_cost) {
-    const int out = up ? kCols / 2 : kCols, tiles = (a.N + out - 1) / out, most = exact ? 5 : 8;
-    const int with_rows = a.E < a.P ? a.E : a.P, mean = (a.P + with_rows - 1) / with_rows + (with_rows > 1 ? a.P / with_rows / 8 : 0);
-    int per = 32, best_chunks = 0;
-    for (int mt = 1; mt <= most; ++mt) {
-        const int chunks = (mean + 32 * mt - 1) / (32 * mt), rows = (mean + chunks - 1) / chunks;
-        const long long rounds = ((long long)tiles * chunks * with_rows + kComputeUnits - 1) / kComputeUnits, cost = rounds * (2 + (rows + 31) / 32);
-        if (mt == 1 || cost < *best_cost || (cost == *best_cost && chunks < best_chunks)) {     // (of equal ones fewer chunks, then shorter ones)
+    const int out = up ? kCols / 2 : kCols, tiles = (a.N + out - 1) / out;
+    const int with_rows = a.E < a.P ? a.E : a.P, even = (a.P + with_rows - 1) / with_rows;
+    const float eighth = (float)even / 8.0f, deviations = 2.0f * sqrtf((float)even);
+    const int mean = even + (with_rows > 1 ? (int)(eighth > deviations ? eighth : deviations) : 0);
+    int per = 16, best_chunks = 0;
+    for (int tt = 1; tt <= most_tiles(!exact); ++tt) {
+        const int chunks = (mean + 16 * tt - 1) / (16 * tt), rows = (mean + chunks - 1) / chunks;
+        const long long rounds = ((long long)tiles * chunks * with_rows + kComputeUnits - 1) / kComputeUnits, cost = rounds * (4 + (rows + 15) / 16);
+        if (tt == 1 || cost < *best_cost || (cost == *best_cost && chunks < best_chunks)) {     // (of equal ones fewer chunks, then shorter ones)
             *best_cost = cost;
             best_chunks = chunks;
-            per = 32 * mt;
+            per = 16 * tt;
         }
     }
     return per;
@@ -367,12 +397,12 @@ static int rows_per_chunk(const Fp8Args& a, bool up, bool exact, long long* best
 // Gathered rows are found by 32-bit offsets.
 bool fp8_tile_can(const Fp8Args& a) { return a.K > 0 && (!a.perm || (size_t)a.x_rows * a.K < (1ull << 32) - 4096); }
 
-// Microseconds, roughly: the rounds at 0.22 us per block of 128 columns and unit of cost (0.32 with rows expanded to fp16), or 5 TB/s of weights.
+// Microseconds, roughly: the rounds at 0.11 us per block of 128 columns and unit of cost (0.16 with rows expanded to fp16), or 5 TB/s of weights.
 float fp8_tile_us(const Fp8Args& a, bool up, bool exact) {
     long long cost = 0;
     rows_per_chunk(a, up, exact, &cost);
     const float with_rows = (float)(a.E < a.P ? a.E : a.P), mb = 1e-6f * (float)a.N * (float)a.K * (up ? 2.0f : 1.0f) * with_rows;
-    const float blocks = (float)((a.K + kFp8Block - 1) / kFp8Block), busy = (float)cost * blocks * (exact ? 0.32f : 0.22f);
+    const float blocks = (float)((a.K + kFp8Block - 1) / kFp8Block), busy = (float)cost * blocks * (exact ? 0.16f : 0.11f);
     return 4.0f + (busy > mb / 5.0f ? busy : mb / 5.0f);
 }
 
