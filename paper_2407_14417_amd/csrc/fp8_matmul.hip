@@ -295,16 +295,17 @@ int few_rows16(const Fp8Args& a) {
     return mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
 }
 
-// Microseconds of the kernel above, roughly: 4.2 TB/s of weights, 10 TB/s of rows (every workgroup reads its chunk's), and 3 us for every round of
-// workgroups (two per compute unit with one tile of rows, else one).  Beside fp8_tile_us this says which kernel serves a product: 4096 -> 14336, fp16
-// results, few and tile: 16 rows 19.7, 21.7 us; 48 rows 31.1, 22.5; fp32 results 32 rows 23.9, 31.7; 96 rows 76, 33; 14336 -> 4096: 64 rows 36.7, 61.3;
-// 192 rows 104, 61.6; 8 experts 4096 -> 14336 with a row each 105, 86; 32 experts of 2048 x 1408 with 2 each 24.4, 16.4.
+// Microseconds of the kernel above, roughly: 4.2 TB/s of weights, 10 TB/s of rows (every workgroup reads its chunk's), and 3 us (4 with more than one
+// tile of rows) for every round of workgroups, two per compute unit with one tile of rows, else one.  Beside fp8_tile_us this says which kernel serves
+// a product.  Few and tile, us: 4096 -> 14336, fp16 results, 16 rows 19.7 and 21.7, 48 rows 31.1 and 18.9; fp32 results, 32 rows 23.9 and 24.9, 96 rows 76 and 33;
+// 14336 -> 4096, 64 rows 36.7 and 61.3, 192 rows 104 and 50; 8 experts 4096 -> 14336 with a row each 105 and 86; 32 experts of 2048 x 1408 with two
+// each 24.4 and 16.3.
 float few_us(const Fp8Args& a, bool up) {
     const int ct = few_rows16(a), cols = up ? 16 : 16 * few_tiles(a, ct, up), with_rows = a.E < a.P ? a.E : a.P;
     const int mean = (a.P + with_rows - 1) / with_rows, chunks = with_rows * ((mean + 16 * ct - 1) / (16 * ct));
     const float tiles = (float)((a.N + cols - 1) / cols), mb = 1e-6f * (float)a.N * (float)a.K * (up ? 2.0f : 1.0f);
     const float rounds = ceilf(tiles * (float)chunks / (ct == 1 ? 512.0f : 256.0f));
-    return 3.0f * rounds + mb * (float)chunks / 4.2f + 1e-6f * tiles * (float)a.P * (float)a.K / 10.0f;
+    return (ct == 1 ? 3.0f : 4.0f) * rounds + mb * (float)chunks / 4.2f + 1e-6f * tiles * (float)a.P * (float)a.K / 10.0f;
 }
 
 }  // namespace
