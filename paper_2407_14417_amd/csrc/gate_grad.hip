@@ -95,7 +95,7 @@ __device__ __forceinline__ void softmax(const float4_t l, M m, float (&p)[4]) {
 
 // ---------------------------------------------------------------- loss
 
-constexpr int kLossWaves = 4;
+constexpr int kLossWaves = 16;    // (so that few workgroups leave partial sums for the finish)
 
 // What is known at the end: counts, mean probabilities and the loss, from a lane's (e = lane, up to 31) sums over all tokens, by half a
 // wavefront; and the status of the call.
@@ -117,13 +117,13 @@ __device__ __forceinline__ void finish_loss(int e, double sum, int32_t c, int32_
 }
 
 // Sums over the workgroup's tokens.  A token's lanes count, each for its own four experts, the slots that chose them.  Few tokens: one
-// workgroup of 16 wavefronts finishes as well (ONE); else partial sums go to `sums` and `partial`.
+// workgroup finishes as well (ONE); else partial sums go to `sums` and `partial`.
 template <int LANES, bool WIDE, bool ONE>
-__global__ __launch_bounds__(ONE ? 1024 : 64 * kLossWaves) void balance_sums_kernel(
+__global__ __launch_bounds__(64 * kLossWaves) void balance_sums_kernel(
     const float* __restrict__ logits, const int32_t* __restrict__ idx, const uint8_t* __restrict__ valid, int T, int E, int k,
     float* __restrict__ sums, int32_t* __restrict__ partial, int32_t* __restrict__ counts, float* __restrict__ mean_prob,
     float* __restrict__ loss, int32_t* __restrict__ status) {
-    constexpr int kWaves = ONE ? 16 : kLossWaves, kTokens = 64 / LANES;
+    constexpr int kWaves = kLossWaves, kTokens = 64 / LANES;
     __shared__ float wave_sums[kWaves][32];
     __shared__ int32_t wave_counts[kWaves][34];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LANES, e0 = 4 * j;
@@ -244,11 +244,13 @@ __global__ __launch_bounds__(1024) void balance_finish_kernel(const float* __res
 
 // ---------------------------------------------------------------- backward
 
+constexpr int kGradTokenWaves = 4;   // (16: 333 tokens 14.4 -> 16.1 us a backward pass)
+
 // d_logits, and partial sums of them over the workgroup's tokens for the bias.
 template <int LANES, bool WIDE>
-__global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradArgs a, float* __restrict__ sums, int32_t* __restrict__ flags) {
-    __shared__ float wave_sums[kLossWaves][32];
-    __shared__ int32_t wave_bad[kLossWaves];
+__global__ __launch_bounds__(64 * kGradTokenWaves) void gate_dlogits_kernel(GateGradArgs a, float* __restrict__ sums, int32_t* __restrict__ flags) {
+    __shared__ float wave_sums[kGradTokenWaves][32];
+    __shared__ int32_t wave_bad[kGradTokenWaves];
     constexpr int kTokens = 64 / LANES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane % LANES, e0 = 4 * j, E = a.E;
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, c[4] = {0.0f, 0.0f, 0.0f, 0.0f}, coef = 0.0f;
@@ -259,8 +261,8 @@ __global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradA
         for (int i = 0; i < 4; ++i) c[i] = e0 + i < E ? (float)a.counts[e0 + i] : 0.0f;
     }
     bool bad = false;
-    const long long step = (long long)gridDim.x * kLossWaves * kTokens;
-    long long t = (long long)(blockIdx.x * kLossWaves + wave) * kTokens + lane / LANES;
+    const long long step = (long long)gridDim.x * kGradTokenWaves * kTokens;
+    long long t = (long long)(blockIdx.x * kGradTokenWaves + wave) * kTokens + lane / LANES;
     Token now, next;
     float dgs[MOE_MAX_TOPK], dgs_next[MOE_MAX_TOPK];
     auto ask = [&](long long at) {
@@ -341,12 +343,12 @@ __global__ __launch_bounds__(64 * kLossWaves) void gate_dlogits_kernel(GateGradA
     __syncthreads();
     if ((int)threadIdx.x < E) {
         float v = 0.0f;
-        for (int w = 0; w < kLossWaves; ++w) v += wave_sums[w][threadIdx.x];
+        for (int w = 0; w < kGradTokenWaves; ++w) v += wave_sums[w][threadIdx.x];
         sums[(size_t)blockIdx.x * E + threadIdx.x] = v;
     }
     if (threadIdx.x == 0) {
         int32_t f = 0;
-        for (int w = 0; w < kLossWaves; ++w) f |= wave_bad[w];
+        for (int w = 0; w < kGradTokenWaves; ++w) f |= wave_bad[w];
         flags[blockIdx.x] = f;
     }
 }
@@ -633,27 +635,27 @@ void by_lanes(int E, F f) {
 
 bool wide_rows(const void* p, int E) { return E % 4 == 0 && (uintptr_t)p % 16 == 0; }
 
-// Up to so many workgroups' tokens one workgroup of four times the wavefronts takes alone.
-constexpr int kOneBlock = 8;
+// Up to so many workgroups' tokens one workgroup takes alone.
+constexpr int kOneBlock = 2;
 
-int token_blocks(int T, int E) {
-    const int lanes = E <= 4 ? 1 : E <= 8 ? 2 : E <= 16 ? 4 : 8, per = 64 / lanes * kLossWaves;
+int token_blocks(int T, int E, int waves, int most) {
+    const int lanes = E <= 4 ? 1 : E <= 8 ? 2 : E <= 16 ? 4 : 8, per = 64 / lanes * waves;
     const int blocks = (T - 1) / per + 1;
-    return blocks < kGateBlocks ? blocks : kGateBlocks;
+    return blocks < most ? blocks : most;
 }
 
 }  // namespace
 
 void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t* valid, int T, int E, int k, int32_t* counts,
                          float* mean_prob, float* loss, const GateWorkspace& w, hipStream_t st) {
-    const int blocks = token_blocks(T, E);
+    const int blocks = token_blocks(T, E, kLossWaves, kGateBlocks / 2);
     const bool one = blocks <= kOneBlock;
     by_lanes(E, [&](auto lanes) {
         constexpr int LANES = decltype(lanes)::value;
         const auto go = [&](auto wide) {
             constexpr bool WIDE = decltype(wide)::value;
             if (one)
-                balance_sums_kernel<LANES, WIDE, true><<<1, 1024, 0, st>>>(logits, idx, valid, T, E, k, w.sums, w.counts, counts, mean_prob,
+                balance_sums_kernel<LANES, WIDE, true><<<1, 64 * kLossWaves, 0, st>>>(logits, idx, valid, T, E, k, w.sums, w.counts, counts, mean_prob,
                                                                            loss, w.status);
             else
                 balance_sums_kernel<LANES, WIDE, false><<<blocks, 64 * kLossWaves, 0, st>>>(logits, idx, valid, T, E, k, w.sums, w.counts,
@@ -662,10 +664,10 @@ void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t*
         if (wide_rows(logits, E)) go(std::true_type{});
         else go(std::false_type{});
     });
-    static_assert(kGateBlocks == 32 * 16, "rows");
+    static_assert(kGateBlocks / 2 == 32 * 8, "rows");
     if (one) return;
     if (blocks <= 64) balance_finish_kernel<2><<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss, w.status);
-    else balance_finish_kernel<16><<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss, w.status);
+    else balance_finish_kernel<8><<<1, 1024, 0, st>>>(w.sums, w.counts, blocks, E, k, counts, mean_prob, loss, w.status);
 }
 
 // A compute unit per workgroup, as far as every wavefront has a tile of 32 tokens; up to two tiles a wavefront one share takes alone, which saves the
@@ -677,13 +679,13 @@ int gate_dw_splits(int T, int d, int) {
 }
 
 void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStream_t st) {
-    const int blocks = token_blocks(a.T, a.E);
+    const int blocks = token_blocks(a.T, a.E, kGradTokenWaves, kGateBlocks);
     by_lanes(a.E, [&](auto lanes) {
         constexpr int LANES = decltype(lanes)::value;
         if (wide_rows(a.logits, a.E) && wide_rows(a.d_logits, a.E))
-            gate_dlogits_kernel<LANES, true><<<blocks, 64 * kLossWaves, 0, st>>>(a, w.sums, w.counts);
+            gate_dlogits_kernel<LANES, true><<<blocks, 64 * kGradTokenWaves, 0, st>>>(a, w.sums, w.counts);
         else
-            gate_dlogits_kernel<LANES, false><<<blocks, 64 * kLossWaves, 0, st>>>(a, w.sums, w.counts);
+            gate_dlogits_kernel<LANES, false><<<blocks, 64 * kGradTokenWaves, 0, st>>>(a, w.sums, w.counts);
     });
     const auto finish = [&](int splits) {
         const size_t n = splits > 1 ? (size_t)a.E * a.d : 0;
