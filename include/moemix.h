@@ -183,7 +183,8 @@ int moe_layer_forward_static(const moe_layer* layer, const void* x, int T, void*
  * swap space on `copy_stream` while the resident experts of the same call already compute on `stream`, then the
  * swapped-in experts run and their contribution is added.  The result equals moe_layer_forward on the same
  * layer with every expert resident, bit for bit, except at T == 1 with d_model and d_ff both multiples of 2048, where
- * the output is rounded to fp16 once more between the two passes.
+ * the output is rounded to fp16 once more between the two passes, and at T == 1 with all experts of MOE_PREC_FP8B128, whose
+ * sums moe_layer_forward adds in another order.
  *   host_experts: HOST array [n_experts]; entry e is read only if layer->experts[e].resident == 0 and then
  *                 names the expert's matrices (same layouts, `prec` as in the layer) in pinned host memory;
  *                 a missed expert whose entry has no data keeps the behaviour of moe_layer_forward (left out,
@@ -277,7 +278,10 @@ int moe_transpose_fp8(const moe_mat* m, int out, int in, void* codes_t, float* s
  *   outside [offsets[0], offsets[n_experts]) are left as they were.  (Whatever offsets and perm hold, nothing outside the arrays is read or
  *   written.)
  * x_codes: device [n,in], 16-byte aligned; x_scale: device fp32 [ceil(in/128), n]; y: device, fp32 (MOE_OUT_F32) or fp16 (MOE_OUT_F16, rounded once).
- * in: a multiple of 16; out: any.  n, n_rows and n_pairs: at most 2^20, 0 does nothing.  Sums are fp32.
+ * in: a multiple of 16; out: any.  n, n_rows and n_pairs: at most 2^20; n or n_pairs 0 does nothing.
+ * Sums are fp32 and, for MOE_OUT_F32, as exact as that allows.  MOE_OUT_F16 with many rows: within a block the products of eight neighbouring
+ * columns (8 i .. 8 i + 7) are added by the matrix instructions for 8-bit operands, which drop of each what lies more than 13 binary places below the
+ * largest of the eight (1.5e-5 of a result for normally distributed operands, a fifteenth of the rounding to fp16).
  */
 typedef enum { MOE_OUT_F32 = 0, MOE_OUT_F16 = 1 } moe_out;
 int moe_matmul_fp8(const moe_mat* w, int out, int in, const void* x_codes, const float* x_scale, int n, void* y, int y_type,
@@ -320,7 +324,7 @@ int moe_balance_loss(const moe_layer* layer, const float* logits, const int32_t*
  * d_gate: device fp32 [T, top_k] or NULL; d_loss: device fp32 [1] with counts, or both NULL; one of the two gradients has to be given.
  * Each result may be NULL, at least one has to be asked for: d_logits: device fp32 [T, n_experts]; d_x: device fp32 or fp16 (d_x_type, a moe_out) [T, d_model];
  * d_w_gate: device fp32 [n_experts, d_model]; d_bias: device fp32 [n_experts].  x: device fp16 [T, d_model], needed for d_w_gate only.
- * All are overwritten; the same inputs give the same bits.
+ * All are overwritten, d_x must not be x; the same inputs give the same bits.
  */
 int moe_route_backward(const moe_layer* layer, const void* x, const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T,
                        const int32_t* counts, const float* d_gate, const float* d_loss, float* d_logits, void* d_x, int d_x_type,

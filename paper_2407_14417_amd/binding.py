@@ -436,6 +436,7 @@ def moe_matmul_fp8_grouped(group: MatGroup, x_codes, x_scale, offsets, perm, top
 def moe_route_logits(layer: Layer, x, logits, topk_idx, topk_gate) -> None:
     dev = _device()
     T, E, k = _rows_cols(x, "x")[0], layer.n_experts, layer.top_k
+    _need(layer.w_gate, "w_gate", _F16, (E, layer.d_model), dev)
     _check(lib().moe_route_logits(layer.c, _need(x, "x", _F16, (T, layer.d_model), dev), T, _need(logits, "logits", _F32, (T, E), dev),
                                   _need(topk_idx, "topk_idx", _I32, (T, k), dev), _need(topk_gate, "topk_gate", _F32, (T, k), dev),
                                   _stream_on(dev)))
@@ -468,6 +469,8 @@ def moe_route_backward(layer: Layer, x, logits, topk_idx, ws, valid=None, counts
     """The gradients that are not None are written; ``d_x`` float32 or float16."""
     dev = _device()
     T, E, k, d = _rows_cols(logits, "logits")[0], layer.n_experts, layer.top_k, layer.d_model
+    if d_x is not None:
+        _need(layer.w_gate, "w_gate", _F16, (E, d), dev)
     _check(lib().moe_route_backward(
         layer.c, None if x is None else _need(x, "x", _F16, (T, d), dev), _need(logits, "logits", _F32, (T, E), dev),
         _need(topk_idx, "topk_idx", _I32, (T, k), dev), None if valid is None else _need(valid, "valid", _MASK, (T,), dev), T,

@@ -803,6 +803,7 @@ int matmul_fp8(const char* who, const moe_mat* w, int n_experts, int out, int in
     if (n_rows < 0 || n_pairs < 0) return fail(MOE_EINVAL, "%s: negative size", who);
     if (n_rows > kFp8MaxDim || n_pairs > kFp8MaxDim) return fail(MOE_ESHAPE, "%s: %d rows, %d pairs past %d", who, n_rows, n_pairs, kFp8MaxDim);
     if (y_type != MOE_OUT_F32 && y_type != MOE_OUT_F16) return fail(MOE_EINVAL, "%s: y_type=%d", who, y_type);
+    if (n_pairs == 0 || out == 0) return MOE_OK;
     if (!w) return fail(MOE_EINVAL, "%s: NULL argument", who);
     Fp8Args a;
     memset(&a, 0, sizeof(a));
@@ -811,7 +812,6 @@ int matmul_fp8(const char* who, const moe_mat* w, int n_experts, int out, int in
         a.w[e] = Fp8Mat{(const uint8_t*)w[e].data, (const float*)w[e].scale};
         a.todo[e] = kFp8Run;
     }
-    if (n_pairs == 0 || out == 0) return MOE_OK;
     if (!y || (in && (!x_codes || !x_scale))) return fail(MOE_EINVAL, "%s: NULL argument", who);
     if (n_rows < 1) return fail(MOE_ESHAPE, "%s: %d pairs of no rows", who, n_pairs);
     if (!perm && n_rows < n_pairs) return fail(MOE_ESHAPE, "%s: %d rows for %d rows of y", who, n_rows, n_pairs);
@@ -836,6 +836,7 @@ int matmul_fp8(const char* who, const moe_mat* w, int n_experts, int out, int in
 
 int moe_quantize_fp8(const void* w_fp16, int out, int in, void* codes, float* scale, moe_stream_t stream) {
     if (int rc = check_fp8_shape("moe_quantize_fp8", out, in)) return rc;
+    if (out == 0 || in == 0) return MOE_OK;
     if (!w_fp16 || !codes || !scale) return fail(MOE_EINVAL, "moe_quantize_fp8: NULL argument");
     if ((uintptr_t)codes % 16) return fail(MOE_EINVAL, "moe_quantize_fp8: codes must be 16-byte aligned");
     launch_quantize_fp8((const half_t*)w_fp16, out, in, (uint8_t*)codes, scale, (hipStream_t)stream);
@@ -844,6 +845,7 @@ int moe_quantize_fp8(const void* w_fp16, int out, int in, void* codes, float* sc
 
 int moe_dequant_fp8(const moe_mat* m, int out, int in, void* w_fp16, moe_stream_t stream) {
     if (int rc = check_fp8_shape("moe_dequant_fp8", out, in)) return rc;
+    if (out == 0 || in == 0) return MOE_OK;
     if (!m || !w_fp16) return fail(MOE_EINVAL, "moe_dequant_fp8: NULL argument");
     if (int rc = check_fp8_mat("moe_dequant_fp8", *m)) return rc;
     if ((uintptr_t)w_fp16 % 16) return fail(MOE_EINVAL, "moe_dequant_fp8: w_fp16 must be 16-byte aligned");
@@ -855,6 +857,7 @@ int moe_quantize_fp8_rows(const void* x, int n, int in, void* codes, float* scal
     if (int rc = check_fp8_shape("moe_quantize_fp8_rows", 0, in)) return rc;
     if (n < 0) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: negative size");
     if (n > kFp8MaxRows) return fail(MOE_ESHAPE, "moe_quantize_fp8_rows: n=%d past %d", n, kFp8MaxRows);
+    if (n == 0 || in == 0) return MOE_OK;
     if (!x || !codes || !scale) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: NULL argument");
     if ((uintptr_t)codes % 16) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: codes must be 16-byte aligned");
     launch_quantize_fp8_rows((const half_t*)x, n, in, (uint8_t*)codes, scale, (hipStream_t)stream);
@@ -864,6 +867,7 @@ int moe_quantize_fp8_rows(const void* x, int n, int in, void* codes, float* scal
 int moe_transpose_fp8(const moe_mat* m, int out, int in, void* codes_t, float* scale_t, moe_stream_t stream) {
     if (int rc = check_fp8_shape("moe_transpose_fp8", out, in)) return rc;
     if (out % 16) return fail(MOE_ESHAPE, "moe_transpose_fp8: out=%d not a multiple of 16", out);
+    if (out == 0 || in == 0) return MOE_OK;
     if (!m || !codes_t || !scale_t) return fail(MOE_EINVAL, "moe_transpose_fp8: NULL argument");
     if (int rc = check_fp8_mat("moe_transpose_fp8", *m)) return rc;
     if ((uintptr_t)codes_t % 16) return fail(MOE_EINVAL, "moe_transpose_fp8: codes_t must be 16-byte aligned");
@@ -885,6 +889,21 @@ int moe_matmul_fp8_grouped(const moe_mat* w, int n_experts, int out, int in, con
     if (perm && top_k < 1) return fail(MOE_ESHAPE, "moe_matmul_fp8_grouped: top_k=%d < 1", top_k);
     return matmul_fp8("moe_matmul_fp8_grouped", w, n_experts, out, in, x_codes, x_scale, n_rows, offsets, perm, top_k, n_pairs, y, y_type,
                       (hipStream_t)stream);
+}
+
+// For the tests, host-only: rows per chunk of the tile kernel for such a product (up: of the up-projection of a block), 0 if the kernel for few rows
+// serves it.
+int moemix_fp8_rows_per_chunk(int n_experts, int n_rows, int n_pairs, int out, int in, int gathered, int exact, int up) {
+    Fp8Args a;
+    memset(&a, 0, sizeof(a));
+    a.E = n_experts;
+    a.offsets = n_experts > 1 ? (const int32_t*)16 : nullptr;
+    a.perm = gathered ? (const int32_t*)16 : nullptr;
+    a.x_rows = n_rows;
+    a.P = n_pairs;
+    a.N = out;
+    a.K = in;
+    return fp8_rows_per_chunk(a, up != 0, exact != 0);
 }
 
 // ---------------------------------------------------------------- training the gate

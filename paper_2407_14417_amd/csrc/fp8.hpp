@@ -40,6 +40,9 @@ void launch_fp8_up(const Fp8Args& a, half_t* h, uint8_t* codes, float* scale, hi
 void launch_fp8_matmul(const Fp8Args& a, bool half_out, bool exact, hipStream_t st);
 bool fp8_tile_can(const Fp8Args& a);
 float fp8_tile_us(const Fp8Args& a, bool up, bool exact);
+int fp8_tile_rows(const Fp8Args& a, bool up, bool exact);
+// Rows per chunk of the tile kernel, 0: the kernel for few rows.
+int fp8_rows_per_chunk(const Fp8Args& a, bool up, bool exact);
 void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st);
 
 // One token: up (y: [k, N] hidden rows of the slots, x: the token) or down (y: [N] the block's output, x: the hidden rows), rows quantized on the way.

@@ -332,16 +332,20 @@ static void launch_few_any(const Fp8Args& a, bool up, bool half_out, hipStream_t
     else launch_few<4, 2>(a, up, half_out, st);
 }
 
+int fp8_rows_per_chunk(const Fp8Args& a, bool up, bool exact) {
+    return fp8_tile_can(a) && fp8_tile_us(a, up, exact) < few_us(a, up) ? fp8_tile_rows(a, up, exact) : 0;
+}
+
 void launch_fp8_matmul(const Fp8Args& a, bool half_out, bool exact, hipStream_t st) {
     if (a.P == 0 || a.N == 0) return;
-    if (fp8_tile_can(a) && fp8_tile_us(a, false, exact) < few_us(a, false)) launch_fp8_tile(a, false, half_out, exact, st);
+    if (fp8_rows_per_chunk(a, false, exact)) launch_fp8_tile(a, false, half_out, exact, st);
     else launch_few_any(a, false, half_out, st);
 }
 
 // The tile kernel holds a row's whole block of 128 hidden values and quantizes it; after the other kernel that is a launch of its own.
 void launch_fp8_up(const Fp8Args& args, half_t* h, uint8_t* codes, float* scale, hipStream_t st) {
     Fp8Args a = args;
-    if (fp8_tile_can(a) && fp8_tile_us(a, true, true) < few_us(a, true)) {
+    if (fp8_rows_per_chunk(a, true, true)) {
         a.y = codes;
         a.y_scale = scale;
         TraceScope trace(kKernelUp, st);

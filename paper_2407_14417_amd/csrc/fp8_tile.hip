@@ -406,9 +406,13 @@ float fp8_tile_us(const Fp8Args& a, bool up, bool exact) {
     return 4.0f + (busy > mb / 5.0f ? busy : mb / 5.0f);
 }
 
-void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st) {
+int fp8_tile_rows(const Fp8Args& a, bool up, bool exact) {
     long long cost = 0;
-    const int per = rows_per_chunk(a, up, exact, &cost);
+    return rows_per_chunk(a, up, exact, &cost);
+}
+
+void launch_fp8_tile(const Fp8Args& a, bool up, bool half_out, bool exact, hipStream_t st) {
+    const int per = fp8_tile_rows(a, up, exact);
     if (up) launch<false, true, uint8_t>(a, per, st);
     else if (half_out) launch<true, false, half_t>(a, per, st);
     else if (exact) launch<false, false, float>(a, per, st);

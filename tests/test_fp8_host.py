@@ -85,6 +85,9 @@ def test_products_refuse(L):
     assert call(one, 16, 32, 4096 + 8, 4096, 1, 4096, 0, None) == mm.MOE_EINVAL      # alignment
     assert call(one, 16, 32, None, 4096, 1, 4096, 0, None) == mm.MOE_EINVAL
     assert call(None, 16, 32, 4096, 4096, 1, 4096, 0, None) == mm.MOE_EINVAL
+    assert call(one, 16, 32, None, None, 0, None, 0, None) == mm.MOE_OK              # nothing to do
+    assert L.moe_quantize_fp8_rows(None, 0, 32, None, None, None) == mm.MOE_OK
+    assert L.moe_quantize_fp8(None, 0, 32, None, None, None) == mm.MOE_OK
     assert call(ctypes.byref(mm.CMat(4096, None, None)), 16, 32, 4096, 4096, 1, 4096, 0, None) == mm.MOE_EINVAL
     assert call(ctypes.byref(mm.CMat(4104, 4096, None)), 16, 32, 4096, 4096, 1, 4096, 0, None) == mm.MOE_EINVAL
     group = L.moe_matmul_fp8_grouped

@@ -195,15 +195,77 @@ def test_infinities_and_nan_stay_in_their_rows(n):
 
 def test_product_of_nothing():
     wq = on_device(quantized_matrix(rng_of(8), 32, 64))
-    empty = torch.empty(0, 64, dtype=torch.uint8, device="cuda")
-    mm.moe_quantize_fp8_rows(torch.empty(0, 64, dtype=torch.float16, device="cuda"), empty, torch.empty(1, 0, device="cuda")) \
-        if empty.data_ptr() else None
-    y = spoiled((5, 32), torch.float32)
+    new = lambda *shape, t=torch.float32: torch.empty(*shape, dtype=t, device="cuda")  # noqa: E731
+    codes, scale = new(0, 64, t=torch.uint8), new(1, 0)
+    mm.moe_quantize_fp8_rows(new(0, 64, t=torch.float16), codes, scale)
+    mm.moe_matmul_fp8(wq, codes, scale, new(0, 32))
+    offsets = torch.zeros(3, dtype=torch.int32, device="cuda")
+    mm.moe_matmul_fp8_grouped(mm.MatGroup([wq, wq]), codes, scale, offsets, new(0, t=torch.int32), 2, new(0, 32))
+    y = spoiled((5, 32), torch.float32)                  # pairs, but none of an expert's
+    mm.moe_matmul_fp8_grouped(mm.MatGroup([wq, wq]), new(5, 64, t=torch.uint8).zero_(), torch.ones(1, 5, device="cuda"), offsets, None, 1, y)
+    assert bool(y.isnan().all())
+    nothing = mm.Mat(new(32, 0, t=torch.uint8), new(1, 0))
     m = mm.CMat(wq.data.data_ptr(), wq.scale.data_ptr(), None)
     import ctypes
-    assert mm.lib().moe_matmul_fp8(ctypes.byref(m), 32, 64, None, None, 0, None, 0, None) == mm.MOE_OK
     assert mm.lib().moe_matmul_fp8(ctypes.byref(m), 32, 0, None, None, 5, y.data_ptr(), 0, torch.cuda.current_stream().cuda_stream) == mm.MOE_OK
-    assert torch.equal(y, torch.zeros_like(y))           # a sum over no columns
+    assert torch.equal(y, torch.zeros_like(y)) and nothing.nbytes() == 0           # a sum over no columns
+
+
+def rows_per_chunk(P, out, inn, E=1, T=None, gathered=False, exact=False, up=False):
+    return mm.lib().moemix_fp8_rows_per_chunk(E, T or P, P, out, inn, int(gathered), int(exact), int(up))
+
+
+def tiles_of(n, per):
+    """Tiles of 16 rows of the chunks that n rows of one expert make."""
+    chunks = -(-n // per)
+    size = min(per, -(-(-(-n // chunks)) // 16) * 16)
+    return [-(-min(size, n - i * size) // 16) for i in range(chunks) if n > i * size]
+
+
+@pytest.mark.parametrize("half", [True, False])
+def test_chunks_of_every_number_of_tiles(half):
+    """Products whose chunks have 1 to 16 (fp32 results: 10) tiles of 16 rows, most of them not full, and a block that ends early."""
+    inn, out, seen = 400, 13000, set()
+    wq = quantized_matrix(rng_of(15), out, inn)
+    wv, m = fp8_ref.matrix_values(*wq), on_device(wq)
+    some = np.r_[0:40, 250:262, 6000:6040, out - 40:out]
+    for n in list(range(5, 300, 13)) + list(range(300, 4300, 61)):
+        per = rows_per_chunk(n, out, inn, exact=not half)
+        tiles = set(tiles_of(n, per)) if per else set()
+        if tiles <= seen:
+            continue
+        seen |= tiles
+        print(f"n={n} chunks of {per}: {sorted(tiles)}", flush=True)
+        x = normal(rng_of(n, 16), n, inn)
+        codes, scale = fp8_ref.quantize_rows(x)
+        y = spoiled((n, out), torch.float16 if half else torch.float32)
+        mm.moe_matmul_fp8(m, dev(codes), dev(scale), y)
+        assert bool(y.isfinite().all())
+        rows = np.unique(np.r_[0:min(n, 20), n - min(n, 40):n, rng_of(n).integers(0, n, 40)])
+        check_product(y[torch.from_numpy(rows).cuda()][:, torch.from_numpy(some).cuda()].cpu().numpy(),
+                      fp8_ref.row_values(codes, scale)[rows], wv[some], inn, half, n)
+    assert seen == set(range(1, 17 if half else 11)), seen
+
+
+@pytest.mark.parametrize("T,E,k,d,f", [(700, 6, 2, 256, 1984), (420, 4, 1, 192, 2112), (1500, 16, 2, 128, 1088), (260, 3, 3, 320, 4032)])
+def test_hidden_rows_quantized_by_the_tile_kernel(T, E, k, d, f):
+    """Bit for bit the quantizer's codes of what the block's parts give, so the block equals the chain of its parts up to sums of fp32."""
+    assert rows_per_chunk(T * k, f, d, E, T, True, True, True) > 0
+    rng = rng_of(T, E, 21)
+    new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+    experts = [mm.Expert(mm.PREC_FP8B128, *[on_device(quantized_matrix(rng, o, i, 0.05)) for o, i in ((f, d), (f, d), (d, f))]) for _ in range(E)]
+    layer = mm.Layer(d, f, k, dev(normal(rng, E, d, scale=0.05)), experts)
+    x = dev(normal(rng, T, d))
+    out, ws = new(T, d, t=torch.float16), mm.alloc_workspace(layer, T)
+    idx, gate = new(T, k, t=torch.int32), new(T, k)
+    mm.moe_layer_forward(layer, x, out, ws, idx, gate)
+    i, g, xh = idx.cpu().numpy(), gate.cpu().numpy().astype(np.float64), x.cpu().numpy()
+    ref = np.zeros((T, d))
+    for e, ex in enumerate(experts):
+        t, s = np.nonzero(i == e)
+        if len(t):
+            ref[t] += g[t, s][:, None] * fp8_ffn(xh[t], [fp8_ref.matrix_values(m.data.cpu().numpy(), m.scale.cpu().numpy()) for m in (ex.w1, ex.w3, ex.w2)])
+    assert_ffn_close(out.cpu().numpy(), ref, "block")
 
 
 @pytest.mark.parametrize("n,inn,out,half", [(5, 256, 272, False), (200, 1024, 512, True), (150, 384, 144, False)])
@@ -486,6 +548,41 @@ def test_experts_that_are_not_there(orc):
         mm.moe_layer_forward(layer, x[t:t + 1], want, mm.alloc_workspace(layer, 1))
         torch.cuda.synchronize()
         assert torch.equal(one, want), t
+
+
+def test_one_token_with_a_missing_expert(orc):
+    wl = common.build_workload(FP8_BLOCK, orc)
+    layer, values = with_fp8(device_layer(wl), wl, range(8))
+    _, idx, gate = orc.layer_forward(wl.x, wl.wg, wl.experts, 2, None)
+    gone = [mm.Expert(e.prec, None, None, None, resident=False) if i == 3 else e for i, e in enumerate(layer.experts)]
+    part = mm.Layer(layer.d_model, layer.d_ff, 2, layer.w_gate, gone)
+    ws, out = mm.alloc_workspace(part, 1), spoiled((1, layer.d_model), torch.float16)
+    hit = 0
+    for t in range(FP8_BLOCK.T):
+        x = np.ascontiguousarray(wl.x[t:t + 1])
+        mm.moe_layer_forward(part, dev(x), out, ws)
+        missing = 3 in idx[t]
+        hit += missing
+        assert mm.moe_read_status(ws) == (mm.STATUS_NOT_RESIDENT if missing else 0)
+        ref = sum(float(g) * fp8_ffn(x, values[e]) for e, g in zip(idx[t], gate[t]) if e != 3)
+        assert_ffn_close(out.cpu().numpy(), ref, f"token {t}")
+    assert 0 < hit < FP8_BLOCK.T
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_one_token_of_many_wide_experts(T):
+    """Eight slots of 16384 hidden columns: more pieces than the one-token launches keep in LDS."""
+    rng, d, f, E, k = rng_of(22), 128, 16384, 8, 8
+    mats = [[on_device(quantized_matrix(rng, o, i, 0.05)) for o, i in ((f, d), (f, d), (d, f))] for _ in range(E)]
+    layer = mm.Layer(d, f, k, dev(normal(rng, E, d, scale=0.05)), [mm.Expert(mm.PREC_FP8B128, *m) for m in mats])
+    x = normal(rng, T, d)
+    out, idx, gate = spoiled((T, d), torch.float16), torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda")
+    mm.moe_layer_forward(layer, dev(x), out, mm.alloc_workspace(layer, T), idx, gate)
+    i, g, ref = idx.cpu().numpy(), gate.cpu().numpy().astype(np.float64), np.zeros((T, d))
+    for t in range(T):
+        for e, w in zip(i[t], g[t]):
+            ref[t] += w * fp8_ffn(x[t:t + 1], [fp8_ref.matrix_values(m.data.cpu().numpy(), m.scale.cpu().numpy()) for m in mats[e]])[0]
+    assert_ffn_close(out.cpu().numpy(), ref, "block")
 
 
 @pytest.mark.parametrize("T", [1, 12])
