@@ -144,20 +144,23 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_kernel(Fp8Args a) {
     }
 }
 
-// One token: workgroup (tile of 16 weight rows, slot) of the up-projection, or tile of the down-projection with all slots, whose outputs it adds
-// weighted.  Rows come as fp16 and every wavefront quantizes what it multiplies (the same operations as quantize_fp8_rows_kernel), so a block of one
+// One token: workgroup (tile of 16 rows of w1 and of w3, slot) of the up-projection, or tile of 16 rows of the down-projection with all slots, whose
+// outputs it adds weighted.  Rows come as fp16 and every wavefront quantizes what it multiplies (the same operations as quantize_fp8_rows_kernel), so a block of one
 // token is three launches: gating, up, down.  Mixtral shape, top-2: 101 us a block with grouping, quantizers and average as launches of their own.
+constexpr size_t one_sums(bool up) { return kFewWaves * (up ? 2 : 1) * 16 * sizeof(float); }
+
 template <bool UP>
 __global__ __launch_bounds__(64 * kFewWaves) void fp8_one_kernel(Fp8OneArgs a) {
-    constexpr int T = UP ? 2 : 1, DEPTH = UP ? 4 : 6;
-    extern __shared__ uint8_t lds[];                          // [8][T][256] sums; per wavefront its quantized pieces [steps][128] and their scales
+    constexpr int NT = 1, T = UP ? 2 * NT : 1, DEPTH = UP ? 4 : 6;
+    extern __shared__ uint8_t lds[];                          // sums [8][T][16]; per wavefront its quantized pieces [most][128], then scales [most]
     float* const sums = (float*)lds;
-    const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4, n0 = blockIdx.x * 16, K = a.K;
+    const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4, n0 = blockIdx.x * (16 * NT), K = a.K;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int blocks = (K + kFp8Block - 1) / kFp8Block, total = UP ? blocks : a.k * blocks;
     const int steps = (total - wave + kFewWaves - 1) / kFewWaves, most = (total + kFewWaves - 1) / kFewWaves;
-    uint8_t* const codes = lds + kFewWaves * T * 1024 + wave * most * kFp8Block;
-    float* const scales = (float*)(lds + kFewWaves * T * 1024 + kFewWaves * most * kFp8Block) + wave * most;
+    uint8_t* const codes = lds + one_sums(UP) + wave * most * kFp8Block;
+    float* const scales = (float*)(lds + one_sums(UP) + kFewWaves * most * kFp8Block) + wave * most;
+    static_assert(kFewWaves * T * 16 * sizeof(float) == one_sums(UP), "LDS");
     // step s of the wavefront: block and slot
     auto place = [&](int s, int& slot, int& b) {
         const int g = wave + s * kFewWaves;
@@ -178,11 +181,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_one_kernel(Fp8OneArgs a) {
         const int col = b * kFp8Block + q * 32;
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            const Fp8Mat& m = UP && t ? a.w3[e] : a.w[e];
-            const uint8_t* const row = m.data + (size_t)min(n0 + r16, a.N - 1) * K + col;
+            const Fp8Mat& m = UP && t >= NT ? a.w3[e] : a.w[e];
+            const int first = min(n0 + 16 * (t % NT), a.N - 1);
+            const uint8_t* const row = m.data + (size_t)min(first + r16, a.N - 1) * K + col;
 #pragma unroll
             for (int h = 0; h < 2; ++h) r.w[t][h] = *(const uint4_t*)(run && col + 16 * h < K ? row + 16 * h : (const uint8_t*)zeros);
-            const float* const f = m.scale + (size_t)(n0 / kFp8Block) * blocks + b;
+            const float* const f = m.scale + (size_t)(first / kFp8Block) * blocks + b;
             r.f[t] = *(run ? f : (const float*)zeros);
         }
     };
@@ -262,16 +266,17 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_one_kernel(Fp8OneArgs a) {
 #pragma unroll
         for (int t = 0; t < T; ++t) *(float4_t*)(sums + (wave * T + t) * 16 + 4 * q) = acc[t];
     __syncthreads();
-    const int n = n0 + tid;
-    if (tid >= 16 || n >= a.N) return;
-    float v[T];
+    const int n = n0 + tid, tile = tid >> 4;
+    if (tid >= 16 * NT || n >= a.N) return;
+    float v[2];
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-        v[t] = sums[t * 16 + tid];
+    for (int t = 0; t < (UP ? 2 : 1); ++t) {
+        const float* const from = sums + (t * NT + tile) * 16 + (tid & 15);
+        v[t] = from[0];
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) v[t] += sums[(w * T + t) * 16 + tid];
+        for (int w = 1; w < kFewWaves; ++w) v[t] += from[w * T * 16];
     }
-    if (UP) a.y[(size_t)blockIdx.y * a.N + n] = (half_t)silu_mul(v[0], v[T - 1]);
+    if (UP) a.y[(size_t)blockIdx.y * a.N + n] = (half_t)silu_mul(v[0], v[UP ? 1 : 0]);
     else a.y[n] = (half_t)(v[0] + (a.residual ? (float)a.residual[n] : 0.0f));
     if (!UP && blockIdx.x == 0 && tid < a.k && a.todo[expert_of(tid)] == kFp8Missing) atomicOr(a.status, kStatusNotResident);
 }
@@ -312,7 +317,7 @@ float few_us(const Fp8Args& a, bool up) {
 
 size_t fp8_one_lds(int k, int K, bool up) {
     const int total = (up ? 1 : k) * ((K + kFp8Block - 1) / kFp8Block), most = (total + kFewWaves - 1) / kFewWaves;
-    return (size_t)kFewWaves * ((up ? 2 : 1) * 1024 + most * (kFp8Block + 4));
+    return one_sums(up) + (size_t)kFewWaves * most * (kFp8Block + sizeof(float));
 }
 bool fp8_one_serves(int k, int d, int f) { return fp8_one_lds(k, d, true) <= 65536 && fp8_one_lds(k, f, false) <= 65536; }
 
