@@ -147,23 +147,25 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_kernel(Fp8Args a) {
 // One token: workgroup (tile of 16 rows of w1 and of w3, slot) of the up-projection, or tile of 16 rows of the down-projection with all slots, whose
 // outputs it adds weighted.  Rows come as fp16 and every wavefront quantizes what it multiplies (the same operations as quantize_fp8_rows_kernel), so a block of one
 // token is three launches: gating, up, down.  Mixtral shape, top-2: 101 us a block with grouping, quantizers and average as launches of their own.
-constexpr size_t one_sums(bool up) { return kFewWaves * (up ? 2 : 1) * 16 * sizeof(float); }
+// Down: at 4096 columns a workgroup per compute unit, which needs 16 wavefronts to have enough on its way (Mixtral shape, block 79.5 us with 8, 76.5 with 16).
+constexpr int one_waves(bool up) { return up ? 8 : 16; }
+constexpr size_t one_sums(bool up) { return one_waves(up) * (up ? 2 : 1) * 16 * sizeof(float); }
 
 template <bool UP>
-__global__ __launch_bounds__(64 * kFewWaves) void fp8_one_kernel(Fp8OneArgs a) {
-    constexpr int NT = 1, T = UP ? 2 * NT : 1, DEPTH = UP ? 4 : 6;
+__global__ __launch_bounds__(64 * one_waves(UP)) void fp8_one_kernel(Fp8OneArgs a) {
+    constexpr int kWaves = one_waves(UP), NT = 1, T = UP ? 2 * NT : 1, DEPTH = UP ? 4 : 3;
     extern __shared__ uint8_t lds[];                          // sums [8][T][16]; per wavefront its quantized pieces [most][128], then scales [most]
     float* const sums = (float*)lds;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4, n0 = blockIdx.x * (16 * NT), K = a.K;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int blocks = (K + kFp8Block - 1) / kFp8Block, total = UP ? blocks : a.k * blocks;
-    const int steps = (total - wave + kFewWaves - 1) / kFewWaves, most = (total + kFewWaves - 1) / kFewWaves;
+    const int steps = (total - wave + kWaves - 1) / kWaves, most = (total + kWaves - 1) / kWaves;
     uint8_t* const codes = lds + one_sums(UP) + wave * most * kFp8Block;
-    float* const scales = (float*)(lds + one_sums(UP) + kFewWaves * most * kFp8Block) + wave * most;
-    static_assert(kFewWaves * T * 16 * sizeof(float) == one_sums(UP), "LDS");
+    float* const scales = (float*)(lds + one_sums(UP) + kWaves * most * kFp8Block) + wave * most;
+    static_assert(kWaves * T * 16 * sizeof(float) == one_sums(UP), "LDS");
     // step s of the wavefront: block and slot
     auto place = [&](int s, int& slot, int& b) {
-        const int g = wave + s * kFewWaves;
+        const int g = wave + s * kWaves;
         slot = UP ? (int)blockIdx.y : g / blocks;
         b = UP ? g : g - slot * blocks;
     };
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_one_kernel(Fp8OneArgs a) {
         const float* const from = sums + (t * NT + tile) * 16 + (tid & 15);
         v[t] = from[0];
 #pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) v[t] += from[w * T * 16];
+        for (int w = 1; w < kWaves; ++w) v[t] += from[w * T * 16];
     }
     if (UP) a.y[(size_t)blockIdx.y * a.N + n] = (half_t)silu_mul(v[0], v[UP ? 1 : 0]);
     else a.y[n] = (half_t)(v[0] + (a.residual ? (float)a.residual[n] : 0.0f));
@@ -300,7 +302,7 @@ int few_rows16(const Fp8Args& a) {
     return mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
 }
 
-// Microseconds of the kernel above, roughly: 4.2 TB/s of weights, 10 TB/s of rows (every workgroup reads its chunk's), and 3 us (4 with more than one
+// Microseconds of the kernel above, roughly: 4.2 TB/s of weights, 10 TB/s of rows (every workgroup reads its chunk's), and 2 us (4 with more than one
 // tile of rows) for every round of workgroups, two per compute unit with one tile of rows, else one.  Beside fp8_tile_us this says which kernel serves
 // a product.  Few and tile, us: 4096 -> 14336, fp16 results, 16 rows 19.7 and 21.7, 48 rows 31.1 and 18.9; fp32 results, 32 rows 23.9 and 24.9, 96 rows 76 and 33;
 // 14336 -> 4096, 64 rows 36.7 and 61.3, 192 rows 104 and 50; 8 experts 4096 -> 14336 with a row each 105 and 86; 32 experts of 2048 x 1408 with two
@@ -310,22 +312,22 @@ float few_us(const Fp8Args& a, bool up) {
     const int mean = (a.P + with_rows - 1) / with_rows, chunks = with_rows * ((mean + 16 * ct - 1) / (16 * ct));
     const float tiles = (float)((a.N + cols - 1) / cols), mb = 1e-6f * (float)a.N * (float)a.K * (up ? 2.0f : 1.0f);
     const float rounds = ceilf(tiles * (float)chunks / (ct == 1 ? 512.0f : 256.0f));
-    return (ct == 1 ? 3.0f : 4.0f) * rounds + mb * (float)chunks / 4.2f + 1e-6f * tiles * (float)a.P * (float)a.K / 10.0f;
+    return (ct == 1 ? 2.0f : 4.0f) * rounds + mb * (float)chunks / 4.2f + 1e-6f * tiles * (float)a.P * (float)a.K / 10.0f;
 }
 
 }  // namespace
 
 size_t fp8_one_lds(int k, int K, bool up) {
-    const int total = (up ? 1 : k) * ((K + kFp8Block - 1) / kFp8Block), most = (total + kFewWaves - 1) / kFewWaves;
-    return one_sums(up) + (size_t)kFewWaves * most * (kFp8Block + sizeof(float));
+    const int waves = one_waves(up), total = (up ? 1 : k) * ((K + kFp8Block - 1) / kFp8Block), most = (total + waves - 1) / waves;
+    return one_sums(up) + (size_t)waves * most * (kFp8Block + sizeof(float));
 }
 bool fp8_one_serves(int k, int d, int f) { return fp8_one_lds(k, d, true) <= 65536 && fp8_one_lds(k, f, false) <= 65536; }
 
 void launch_fp8_one(const Fp8OneArgs& a, bool up, hipStream_t st) {
     TraceScope trace(up ? kKernelUp : kKernelDown, st);
     const unsigned tiles = (unsigned)((a.N + 15) / 16);
-    if (up) fp8_one_kernel<true><<<dim3(tiles, a.k), 64 * kFewWaves, fp8_one_lds(a.k, a.K, true), st>>>(a);
-    else fp8_one_kernel<false><<<tiles, 64 * kFewWaves, fp8_one_lds(a.k, a.K, false), st>>>(a);
+    if (up) fp8_one_kernel<true><<<dim3(tiles, a.k), 64 * one_waves(true), fp8_one_lds(a.k, a.K, true), st>>>(a);
+    else fp8_one_kernel<false><<<tiles, 64 * one_waves(false), fp8_one_lds(a.k, a.K, false), st>>>(a);
 }
 
 static void launch_few_any(const Fp8Args& a, bool up, bool half_out, hipStream_t st) {
