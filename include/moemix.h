@@ -1,6 +1,7 @@
 /*
  * moemix -- one Mixture-of-Experts feed-forward block in which every expert is
- * held either in 16-bit or in 4-bit form, for AMD MI355X (gfx950).
+ * held either in 16-bit or in 4-bit form (or in one of two 8-bit forms), for AMD
+ * MI355X (gfx950).
  *
  * Method: "Mixture of Experts with Mixture of Precisions for Tuning Quality of
  * Service" (arXiv 2407.14417).  The paper serves an MoE model whose experts are
@@ -351,7 +352,8 @@ int moe_read_status(void* ws, moe_stream_t stream, int* status_bits);
  * arm again for the next launch).  Events are hipEvent_t created by the caller with timing enabled.
  * Both events NULL: a bracket that has been armed and not used yet is dropped.  A call on one token launches no
  * separate gating, grouping or averaging kernel (they run inside the two projections' launches): MOE_KERNEL_ROUTE,
- * MOE_KERNEL_PERMUTE and MOE_KERNEL_COMBINE then never fire (nor do they drop: they stay armed for a later call).
+ * MOE_KERNEL_PERMUTE and MOE_KERNEL_COMBINE then never fire (nor do they drop: they stay armed for a later call); with a layer that has e4m3
+ * experts such a call launches gating, but neither grouping nor averaging, or, if it has experts of other precisions too, all of them.
  * A call with few (token, slot) pairs works out the grouping inside the other launches.  Arming MOE_KERNEL_PERMUTE makes
  * it launch the grouping kernel all the same, and the projections and the weighted average then read its result: the
  * outputs are the same bits, but brackets around those kernels in the same call time the variants that go with a
