@@ -144,7 +144,7 @@ int moe_permute(const moe_layer* layer, const int32_t* topk_idx, int T, int32_t*
  * ws: at least moe_workspace_bytes(layer, ceil(n / top_k)) bytes (the hidden rows live there).
  * Fails with MOE_ENOTRESIDENT on the host if the expert is not resident.
  * n == 1 runs the same one-token kernels as moe_layer_forward with T == 1, n > 1 the multi-token kernels, so
- * each can be checked alone, before gating and weighted average.
+ * each can be checked alone, before gating and weighted average.  An e4m3 expert runs the kernels of moe_matmul_fp8's kind for any n.
  */
 int moe_expert_ffn_mixed(const moe_layer* layer, int expert, const void* x_rows, int n, float* y, void* ws,
                          size_t ws_bytes, moe_stream_t stream);
@@ -342,7 +342,8 @@ int moe_synth_fill_f16(void* dst, size_t n, size_t first, uint64_t seed, uint64_
 
 /* Waits for `stream`, then reads the status word of `ws` (NULL: of the library's own scratch on the current GPU,
  * as used by moe_layer_forward_static): OR of (1 << -code) over the device-side conditions
- * raised by the most recent moe_layer_forward / moe_chain_forward / moe_permute call that used `ws`
+ * raised by the most recent moe_layer_forward / moe_chain_forward / moe_permute / moe_balance_loss / moe_route_backward call
+ * that used `ws`
  * (bit 3: a routed expert was not resident; bit 1: an expert index outside [0, n_experts)). */
 int moe_read_status(void* ws, moe_stream_t stream, int* status_bits);
 
