@@ -2,8 +2,9 @@
 //   y[m, n] = sum_b xs[b, m] ws[n/128, b] sum_{k in block b} x[m, k] w[n, k]
 // over one matrix or over the experts of a grouping (rows offsets[e] .. offsets[e+1] belong to expert e).  Here: few rows, and the choice between the kernels.
 //
-// Few rows are bound by the bytes of the matrix: a wavefront has up to four blocks of 16 rows x 128 codes on their way in registers.  One
-// row, 4096 -> 14336: 15.4 us, 3.8 TB/s (59 MB; a copy of 1 GiB reads and writes 5.2 TB/s), of which 4 us are the kernel's beginning and end.
+// Few rows are bound by the bytes of the matrix: 16 to 24 wavefronts a compute unit have one or two blocks of 16 rows x 128 codes each on their way.  One
+// row, 4096 -> 14336: 14.9 us, 3.9 TB/s (59 MB; a copy of 1 GiB reads and writes 5.2 TB/s), of which 4 us are the kernel's beginning and end;
+// 8 matrices of 14336 -> 4096 with a row each: 83 us, 5.0 TB/s.
 #include <cmath>
 
 #include "fp8.hpp"
@@ -20,11 +21,13 @@ __device__ const uint32_t zeros[4] __attribute__((aligned(16))) = {0u, 0u, 0u, 0
 // Few rows: one workgroup = 16 weight rows (up: of w1 and of w3) and up to 16 CT rows; its wavefronts take the blocks of 128
 // columns in turn and their sums are added at the end, in order.  Codes go from memory to registers, DEPTH blocks ahead, are
 // expanded to fp16 (exact) and multiplied by v_mfma_f32_16x16x32_f16, so a block's sum is as exact as 32 bits allow.
+// Wavefronts side by side hide the way to memory better than blocks under way in one, whose registers they would take: one row 4096 -> 14336 with four
+// ahead 16.0 us, with two 14.9 (one 15.1; 14336 -> 4096 13.2, 12.3, 15.3); 40 rows 4096 -> 4096 with two 12.0, with one 11.1.
 constexpr int kFewWaves = 8;
 
 template <int CT, int NT, bool UP, typename OUT>
 __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_kernel(Fp8Args a) {
-    constexpr int T = UP ? 2 : NT, DEPTH = CT * T <= 2 ? 4 : 2, kCols = UP ? 16 : 16 * NT;
+    constexpr int T = UP ? 2 : NT, DEPTH = CT * T == 1 ? 2 : 1, kCols = UP ? 16 : 16 * NT;
     __shared__ float sums[kFewWaves][T * CT][256];
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -306,17 +309,18 @@ int few_rows16(const Fp8Args& a) {
     return mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
 }
 
-// Microseconds of the kernel above, roughly: 4.2 TB/s of weights, 10 TB/s of rows (every workgroup reads its chunk's), and 2 us (4 with more than one
-// tile of rows) for every round of workgroups, two per compute unit with one tile of rows, else one.  Beside fp8_tile_us this says which kernel serves
-// a product.  Few and tile, us: 4096 -> 14336, fp16 results, 16 rows 19.7 and 21.7, 48 rows 31.1 and 18.9; fp32 results, 32 rows 23.9 and 24.9, 96 rows 76 and 33;
-// 14336 -> 4096, 64 rows 36.7 and 61.3, 192 rows 104 and 50; 8 experts 4096 -> 14336 with a row each 105 and 86; 32 experts of 2048 x 1408 with two
-// each 24.4 and 16.3.
+// Microseconds of the kernel above, roughly: 7.6 TB/s of weights and 7 TB/s of rows (every workgroup reads its chunk's) on top of 1.65 us (2.6 with more than
+// one tile of rows) for every round of workgroups, two per compute unit with one tile of rows, else one.  Beside fp8_tile_us this says which kernel serves
+// a product; both were fitted to 290 products of 1 to 256 rows and 1 to 32 matrices, where the choice costs 0.5 % over the better kernel (a fifth at worst).
+// Few and tile, us: 4096 -> 14336, fp16 results, 8 rows 16.7 and 18.6, 48 rows 25.0 and 18.9; fp32 results, 32 rows 21.3 and 24.5; 14336 -> 4096, fp32, 64 rows
+// 37.4 and 61; 8 experts 14336 -> 4096 with a row each 83 and 106; 32 experts 1408 -> 2048, 8 rows in all 6.3 and 9.1; a block of two tokens of the Mixtral
+// shape, both projections, 149 and 193, of 16 tokens 286 and 302.
 float few_us(const Fp8Args& a, bool up) {
     const int ct = few_rows16(a), cols = up ? 16 : 16 * few_tiles(a, ct, up), with_rows = a.E < a.P ? a.E : a.P;
     const int mean = (a.P + with_rows - 1) / with_rows, chunks = with_rows * ((mean + 16 * ct - 1) / (16 * ct));
     const float tiles = (float)((a.N + cols - 1) / cols), mb = 1e-6f * (float)a.N * (float)a.K * (up ? 2.0f : 1.0f);
     const float rounds = ceilf(tiles * (float)chunks / (ct == 1 ? 512.0f : 256.0f));
-    return (ct == 1 ? 2.0f : 4.0f) * rounds + mb * (float)chunks / 4.2f + 1e-6f * tiles * (float)a.P * (float)a.K / 10.0f;
+    return 1.0f + (ct == 1 ? 1.65f : 2.6f) * rounds + mb * (float)chunks / 7.6f + 1e-6f * tiles * (float)a.P * (float)a.K / 7.0f;
 }
 
 }  // namespace

@@ -414,13 +414,13 @@ static int rows_per_chunk(const Fp8Args& a, bool up, bool exact, long long* best
 // Gathered rows are found by 32-bit offsets.
 bool fp8_tile_can(const Fp8Args& a) { return a.K > 0 && (!a.perm || (size_t)a.x_rows * a.K < (1ull << 32) - 4096); }
 
-// Microseconds, roughly: the rounds at 0.10 us per block of 128 columns and unit of cost (0.14 with rows expanded to fp16), or 5 TB/s of weights.
+// Microseconds, roughly: the rounds at 0.087 us per block of 128 columns and unit of cost (0.123 with rows expanded to fp16), or 6 TB/s of weights.
 float fp8_tile_us(const Fp8Args& a, bool up, bool exact) {
     long long cost = 0;
     rows_per_chunk(a, up, exact, &cost);
     const float with_rows = (float)(a.E < a.P ? a.E : a.P), mb = 1e-6f * (float)a.N * (float)a.K * (up ? 2.0f : 1.0f) * with_rows;
-    const float blocks = (float)((a.K + kFp8Block - 1) / kFp8Block), busy = (float)cost * blocks * (exact ? 0.14f : 0.10f);
-    return 4.0f + (busy > mb / 5.0f ? busy : mb / 5.0f);
+    const float blocks = (float)((a.K + kFp8Block - 1) / kFp8Block), busy = (float)cost * blocks * (exact ? 0.123f : 0.087f);
+    return 4.5f + (busy > mb / 6.0f ? busy : mb / 6.0f);
 }
 
 int fp8_tile_rows(const Fp8Args& a, bool up, bool exact) {
