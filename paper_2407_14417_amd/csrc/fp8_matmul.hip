@@ -152,15 +152,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void fp8_few_kernel(Fp8Args a) {
 
 // One token: workgroup (tile of 16 rows of w1 and of w3, slot) of the up-projection, or tile of 16 rows of the down-projection with all slots, whose
 // outputs it adds weighted.  Rows come as fp16 and every wavefront quantizes what it multiplies (the same operations as quantize_fp8_rows_kernel), so a block of one
-// token is three launches: gating, up, down.  Mixtral shape, top-2: 76.5 us, 4.6 TB/s of weights over the three (up 41 us, 5.7 TB/s; down 29, 4.0), and 101 with grouping,
+// token is three launches: gating, up, down.  Mixtral shape, top-2: 75 us, 4.7 TB/s of weights over the three (up 41 us, 5.7 TB/s; down 27, 4.3), and 101 with grouping,
 // quantizers and average as launches of their own.
-// Down: at 4096 columns a workgroup per compute unit, which needs 16 wavefronts to have enough on its way (Mixtral shape, block 79.5 us with 8, 76.5 with 16).
+// Down: at 4096 columns a workgroup per compute unit, which needs 16 wavefronts to have enough on its way (Mixtral shape, block 79.5 us with 8, 76.5 with 16);
+// of 16 one block each is enough (three ahead 76.9, two 74.9, one 74.6; up, 8 wavefronts: one 78.5, two 79.4, three and four 76.4 and 77.0).
 constexpr int one_waves(bool up) { return up ? 8 : 16; }
 constexpr size_t one_sums(bool up) { return one_waves(up) * (up ? 2 : 1) * 16 * sizeof(float); }
 
 template <bool UP>
 __global__ __launch_bounds__(64 * one_waves(UP)) void fp8_one_kernel(Fp8OneArgs a) {
-    constexpr int kWaves = one_waves(UP), NT = 1, T = UP ? 2 * NT : 1, DEPTH = UP ? 4 : 3;
+    constexpr int kWaves = one_waves(UP), NT = 1, T = UP ? 2 * NT : 1, DEPTH = UP ? 4 : 1;
     extern __shared__ uint8_t lds[];                          // sums [8][T][16]; per wavefront its quantized pieces [most][128], then scales [most]
     float* const sums = (float*)lds;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4, n0 = blockIdx.x * (16 * NT), K = a.K;
@@ -300,7 +301,7 @@ void launch_few(const Fp8Args& a, bool up, bool half_out, hipStream_t st) {
 }
 
 // Two tiles of 16 weight rows per wavefront halve what is read of x: with more than 16 rows, where that still leaves every compute unit a workgroup
-// (4096 -> 14336: 32 rows 33.4 -> 23.9 us, 64 rows 49.3 -> 34.6; 14336 -> 4096: 24.1 and 30.5, 36.7 and 44.5).
+// (4096 -> 14336, 32 rows, 448 workgroups: 24.1 -> 20.6 us; 14336 -> 4096, 128 workgroups: 32 rows 23.0 and 29.7, 64 rows 36.3 and 44.5).
 int few_tiles(const Fp8Args& a, int ct, bool up) {
     return !up && ct > 1 && (long long)((a.N + 31) / 32) * most_chunks(a, 16 * ct) >= 256 ? 2 : 1;
 }
