@@ -161,10 +161,10 @@ constexpr size_t one_sums(bool up) { return one_waves(up) * (up ? 2 : 1) * 16 * 
 
 template <bool UP>
 __global__ __launch_bounds__(64 * one_waves(UP)) void fp8_one_kernel(Fp8OneArgs a) {
-    constexpr int kWaves = one_waves(UP), NT = 1, T = UP ? 2 * NT : 1, DEPTH = UP ? 4 : 1;
-    extern __shared__ uint8_t lds[];                          // sums [8][T][16]; per wavefront its quantized pieces [most][128], then scales [most]
+    constexpr int kWaves = one_waves(UP), T = UP ? 2 : 1, DEPTH = UP ? 4 : 1;
+    extern __shared__ uint8_t lds[];                          // sums [wavefronts][T][16]; per wavefront its quantized pieces [most][128], then scales [most]
     float* const sums = (float*)lds;
-    const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4, n0 = blockIdx.x * (16 * NT), K = a.K;
+    const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4, n0 = blockIdx.x * 16, K = a.K;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int blocks = (K + kFp8Block - 1) / kFp8Block, total = UP ? blocks : a.k * blocks;
     const int steps = (total - wave + kWaves - 1) / kWaves, most = (total + kWaves - 1) / kWaves;
@@ -191,12 +191,11 @@ __global__ __launch_bounds__(64 * one_waves(UP)) void fp8_one_kernel(Fp8OneArgs 
         const int col = b * kFp8Block + q * 32;
 #pragma unroll
         for (int t = 0; t < T; ++t) {
-            const Fp8Mat& m = UP && t >= NT ? a.w3[e] : a.w[e];
-            const int first = min(n0 + 16 * (t % NT), a.N - 1);
-            const uint8_t* const row = m.data + (size_t)min(first + r16, a.N - 1) * K + col;
+            const Fp8Mat& m = UP && t ? a.w3[e] : a.w[e];
+            const uint8_t* const row = m.data + (size_t)min(n0 + r16, a.N - 1) * K + col;
 #pragma unroll
             for (int h = 0; h < 2; ++h) r.w[t][h] = *(const uint4_t*)(run && col + 16 * h < K ? row + 16 * h : (const uint8_t*)zeros);
-            const float* const f = m.scale + (size_t)(first / kFp8Block) * blocks + b;
+            const float* const f = m.scale + (size_t)(n0 / kFp8Block) * blocks + b;
             r.f[t] = *(run ? f : (const float*)zeros);
         }
     };
@@ -276,12 +275,12 @@ __global__ __launch_bounds__(64 * one_waves(UP)) void fp8_one_kernel(Fp8OneArgs 
 #pragma unroll
         for (int t = 0; t < T; ++t) *(float4_t*)(sums + (wave * T + t) * 16 + 4 * q) = acc[t];
     __syncthreads();
-    const int n = n0 + tid, tile = tid >> 4;
-    if (tid >= 16 * NT || n >= a.N) return;
+    const int n = n0 + tid;
+    if (tid >= 16 || n >= a.N) return;
     float v[2];
 #pragma unroll
     for (int t = 0; t < (UP ? 2 : 1); ++t) {
-        const float* const from = sums + (t * NT + tile) * 16 + (tid & 15);
+        const float* const from = sums + t * 16 + tid;
         v[t] = from[0];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) v[t] += from[w * T * 16];
