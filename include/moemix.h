@@ -144,7 +144,8 @@ int moe_permute(const moe_layer* layer, const int32_t* topk_idx, int T, int32_t*
  * ws: at least moe_workspace_bytes(layer, ceil(n / top_k)) bytes (the hidden rows live there).
  * Fails with MOE_ENOTRESIDENT on the host if the expert is not resident.
  * n == 1 runs the same one-token kernels as moe_layer_forward with T == 1, n > 1 the multi-token kernels, so
- * each can be checked alone, before gating and weighted average.  An e4m3 expert runs the kernels of moe_matmul_fp8's kind for any n.
+ * each can be checked alone, before gating and weighted average.  An e4m3 expert runs the kernels of moe_matmul_fp8's kind for any n,
+ * with sums as exact as 32 bits allow.
  */
 int moe_expert_ffn_mixed(const moe_layer* layer, int expert, const void* x_rows, int n, float* y, void* ws,
                          size_t ws_bytes, moe_stream_t stream);
@@ -153,6 +154,8 @@ int moe_expert_ffn_mixed(const moe_layer* layer, int expert, const void* x_rows,
  * The whole block on T tokens: gating, top-k, grouping, every selected expert in its own precision,
  * weighted average (§1, §2.1, §3):
  *   out[t,:] = fp16_rne( sum_s topk_gate[t,s] * FFN_{topk_idx[t,s]}(x[t,:]) )
+ * FFN as in moe_expert_ffn_mixed, but for the down-projection of an e4m3 expert with many rows: there products are cut as moe_matmul_fp8 says for
+ * MOE_OUT_F16, out being rounded to fp16.
  * x: device fp16 [T, d_model]; out: device fp16 [T, d_model];
  * topk_idx_out / topk_gate_out: device [T, top_k], nullable.
  * Routing happens on the device, so a routed expert that is not resident cannot fail the call on the
