@@ -109,8 +109,9 @@ typedef void* moe_stream_t; /* hipStream_t; NULL = the default stream */
  * stays within MOE_STATIC_SCRATCH_BYTES (so they may fall where T grows past that).  A smaller workspace that holds the
  * unsplit call is accepted as well and split less, so that one sized for more tokens always serves fewer; the fp32 sums
  * are then added in another order.
- * Layers with experts of MOE_PREC_FP8B128 also keep quantized rows there: `layer->experts` has to be filled in when this is
- * asked.  (If it is NULL the bytes are those of a layer without such experts.) */
+ * Layers with experts of MOE_PREC_FP8B128 also keep quantized rows there.  So the bytes are those of the precisions in `layer->experts`; if it is NULL, or
+ * holds a precision that there is none of (not filled in yet), they are enough for every table of the shape: a workspace
+ * for experts that are planned anew into or out of that precision is sized so.  (A table of zeros is one of 16-bit experts.) */
 size_t moe_workspace_bytes(const moe_layer* layer, int n_tokens);
 
 /*
@@ -222,7 +223,7 @@ int moe_layer_forward_swap(const moe_layer* layer, const moe_swap* swap, const v
  * layers: host array [n_layers]; rms_gain: host array of n_layers device pointers to fp16 [d_model];
  * h: device fp16 [T, d_model], updated in place; topk_idx_out: device int32 [n_layers, T, top_k] or NULL.
  * All layers must share d_model, d_ff, n_experts, top_k.  ws sized by moe_workspace_bytes(&layers[0], T), or of a layer with an
- * expert of MOE_PREC_FP8B128 where there is one.
+ * expert of MOE_PREC_FP8B128 where there is one (or of the shape with `experts` NULL).
  */
 int moe_chain_forward(const moe_layer* layers, const void* const* rms_gain, int n_layers, float eps, void* h,
                       int T, int32_t* topk_idx_out, void* ws, size_t ws_bytes, moe_stream_t stream);

@@ -195,13 +195,17 @@ class Layer:
         return len(self.experts)
 
 
-def workspace_bytes(layer: Layer, n_tokens: int) -> int:
-    return int(lib().moe_workspace_bytes(ctypes.byref(layer.c), n_tokens))
+def workspace_bytes(layer: Layer, n_tokens: int, any_precision: bool = False) -> int:
+    """``any_precision``: enough for every table of experts of the layer's shape, not for the one it has alone."""
+    c = layer.c
+    if any_precision:
+        c = CLayer(c.d_model, c.d_ff, c.n_experts, c.top_k, c.w_gate, c.gate_bias, None)
+    return int(lib().moe_workspace_bytes(ctypes.byref(c), n_tokens))
 
 
-def alloc_workspace(layer: Layer, n_tokens: int):
+def alloc_workspace(layer: Layer, n_tokens: int, any_precision: bool = False):
     import torch
-    n = workspace_bytes(layer, n_tokens)
+    n = workspace_bytes(layer, n_tokens, any_precision)
     if n == 0:
         raise MoeError(MOE_EINVAL, "moe_workspace_bytes rejected the arguments")
     return torch.empty(n, dtype=torch.uint8, device="cuda")

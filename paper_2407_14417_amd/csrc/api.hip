@@ -74,7 +74,8 @@ constexpr int kDecodeUpBlocks = 1024;
 
 // Which kernels serve T tokens of a block: T == 1 the batch-1 kernels, otherwise the matrix-core path when
 // the shape allows it, else the shape-agnostic kernels.
-// Layers with an e4m3 expert take no one-token kernels: those of the e4m3 products read a grouping.
+// A layer with an e4m3 expert takes the launches for several tokens (with e4m3 experts alone: one_token_fp8): the batch-1 kernels
+// know no such experts.
 bool any_fp8(const moe_layer* L) {
     if (!L->experts || L->n_experts > MOE_MAX_EXPERTS) return false;
     for (int e = 0; e < L->n_experts; ++e)
@@ -82,6 +83,14 @@ bool any_fp8(const moe_layer* L) {
     return false;
 }
 bool use_decode(const moe_layer* L, int T) { return T == 1 && !any_fp8(L); }
+
+// Is the table there, with precisions that there are?  (Sizes may be asked for before it is filled in.)
+bool known_precisions(const moe_layer* L) {
+    if (!L->experts || L->n_experts > MOE_MAX_EXPERTS) return false;
+    for (int e = 0; e < L->n_experts; ++e)
+        if (L->experts[e].prec < MOE_PREC_FP16 || L->experts[e].prec > MOE_PREC_FP8B128) return false;
+    return true;
+}
 bool use_mfma(const moe_layer* L, int rows) {
     return rows > 1 && mfma_shape_ok(L->d_model, L->d_ff) && mfma_rows_ok(rows, L->d_model, L->d_ff);
 }
@@ -110,7 +119,7 @@ bool copies_tokens(const DevExperts& table, int E, const RowMap& rows, int P, co
 }
 
 int y_splits_for(const moe_layer* L, int T) {
-    if (!use_mfma(L, T * L->top_k) || any_fp8(L)) return 1;     // (the e4m3 products write whole sums)
+    if (!use_mfma(L, T * L->top_k)) return 1;
     // (of the shape alone: the experts need not be known when a workspace is sized)
     return plan_mfma(T * L->top_k, L->d_model, L->d_ff, L->n_experts, L->top_k, false).down_splits;
 }
@@ -364,8 +373,13 @@ int moe_trace_kernel(int kernel, void* start_event, void* stop_event) {
 size_t moe_workspace_bytes(const moe_layer* layer, int n_tokens) {
     if (!layer || n_tokens < 1 || layer->d_model < 1 || layer->d_ff < 1 || layer->n_experts < 1 || layer->top_k < 1)
         return 0;
-    return carve_workspace(nullptr, n_tokens, layer->d_model, layer->d_ff, layer->n_experts, layer->top_k, asked_splits(layer, n_tokens),
-                           any_fp8(layer)).bytes;
+    const auto bytes = [&](int splits, bool fp8) {
+        return carve_workspace(nullptr, n_tokens, layer->d_model, layer->d_ff, layer->n_experts, layer->top_k, splits, fp8).bytes;
+    };
+    const bool known = known_precisions(layer);
+    const size_t others = known && any_fp8(layer) ? 0 : bytes(asked_splits(layer, n_tokens), false);
+    const size_t fp8 = known && !any_fp8(layer) ? 0 : bytes(1, true);       // (the e4m3 products write whole sums)
+    return others > fp8 ? others : fp8;
 }
 
 int moe_route(const moe_layer* layer, const void* x, int T, int32_t* topk_idx, float* topk_gate, moe_stream_t stream) {
