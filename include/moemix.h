@@ -46,7 +46,8 @@
  *     all 0 where most == 0;  value = fp32(code) * scale.  A block that holds an infinity or a NaN makes every result
  *     that depends on it NaN.  An expert of this precision multiplies quantized rows: the block's input rows, and the
  *     hidden rows (rounded to fp16 as everywhere), are brought into this form, 128 columns to a scale, on the fly.
- *   - d_model and d_ff must be multiples of 64, d_model <= 8192, d_ff <= 16384 (else MOE_ESHAPE);
+ *   - d_model and d_ff must be multiples of 64, d_model <= 8192, d_ff <= 16384 (else MOE_ESHAPE); with an expert of MOE_PREC_FP8B128
+ *     T * top_k <= 63 * 2^16;
  *     n_experts <= MOE_MAX_EXPERTS; 1 <= top_k <= min(n_experts, MOE_MAX_TOPK).
  */
 #ifndef MOEMIX_H
@@ -259,13 +260,14 @@ int moe_quantize_int8(const void* w_fp16, int out, int in, void* codes, void* sc
  * The hooks of the e4m3 form: a matrix quantized with a scale per block of 128 x 128, and back
  * (w_fp16[r,c] = fp16_rne( fp32(code[r,c]) * scale[r/128,c/128] )).  w_fp16: device fp16 [out,in]; codes: device uint8 [out,in],
  * 16-byte aligned; scale: device fp32 [ceil(out/128), ceil(in/128)].  in: a multiple of 16 (MOE_ESHAPE otherwise).  Both are bit-exact
- * against the definition above.  out and in: at most 2^20.
+ * against the definition above.  out and in: at most 2^20; of moe_dequant_fp8 out * in: less than 2^35 - 2047.
  */
 int moe_quantize_fp8(const void* w_fp16, int out, int in, void* codes, float* scale, moe_stream_t stream);
 int moe_dequant_fp8(const moe_mat* m, int out, int in, void* w_fp16, moe_stream_t stream);
 
 /* Rows for the products below: codes: device uint8 [n,in], 16-byte aligned; scale: device fp32 [ceil(in/128), n], the scales of all rows
- * for one block of columns side by side.  x: device fp16 [n,in].  in: a multiple of 16.  n up to 2^22, 0 does nothing. */
+ * for one block of columns side by side.  x: device fp16 [n,in].  in: a multiple of 16.  n up to 2^22, 0 does nothing; n * ceil(in/128) up to
+ * 2^29 - 32. */
 int moe_quantize_fp8_rows(const void* x, int n, int in, void* codes, float* scale, moe_stream_t stream);
 
 /* The transposed matrix: codes_t: device uint8 [in,out], 16-byte aligned, scale_t: device fp32 [ceil(in/128), ceil(out/128)].  A block of 128 x 128
@@ -297,7 +299,7 @@ int moe_matmul_fp8_grouped(const moe_mat* w, int n_experts, int out, int in, con
 
 /* ---------------------------------------------------------------- training the gate
  *
- * moe_route that also keeps the logits [T, n_experts] (device fp32), which the calls below take.  Same bits as moe_route.
+ * moe_route that also keeps the logits [T, n_experts] (device fp32), which the calls below take.  Same bits as moe_route.  T: less than 2^24.
  */
 int moe_route_logits(const moe_layer* layer, const void* x, int T, float* logits, int32_t* topk_idx, float* topk_gate,
                      moe_stream_t stream);
@@ -313,7 +315,7 @@ size_t moe_gate_workspace_bytes(const moe_layer* layer, int T);
  * valid: device uint8 [T], 0 marks padding whose logits and indices are not looked at; NULL: all tokens are valid.
  * A token whose logits are all -infinity has p = 0.  An index outside [0, n_experts) is left out and sets the MOE_EINVAL bit of the status.
  * logits: device fp32 [T, n_experts]; topk_idx: device int32 [T, top_k]; counts: device int32 [n_experts + 1];
- * mean_prob: device fp32 [n_experts]; loss: device fp32 [1].  The same inputs give the same bits.
+ * mean_prob: device fp32 [n_experts]; loss: device fp32 [1].  T * top_k: less than 2^31.  The same inputs give the same bits.
  */
 int moe_balance_loss(const moe_layer* layer, const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T, int32_t* counts,
                      float* mean_prob, float* loss, void* ws, size_t ws_bytes, moe_stream_t stream);

@@ -146,10 +146,16 @@ DevExperts device_table(const moe_layer* L) {
     return t;
 }
 
+// (token, slot) pairs of a layer with e4m3 experts: chunks of 64 rows are less than 2^16 workgroups of a launch's second dimension, and eight threads for
+// each 128 of up to 16384 columns less than 2^32.
+constexpr int kFp8MaxPairs = 63 << 16;
+
 // fp8: room for quantized rows, and no split contractions
 int check_ws(const moe_layer* L, int T, void* ws, size_t ws_bytes, Workspace* out, bool fp8) {
     if (!ws) return fail(MOE_EWORKSPACE, "workspace is NULL");
     if ((uintptr_t)ws % 256) return fail(MOE_EWORKSPACE, "workspace must be 256-byte aligned");
+    if (fp8 && (long long)T * L->top_k > kFp8MaxPairs)
+        return fail(MOE_ESHAPE, "T=%d, top_k=%d: more than %d pairs in a layer with e4m3 experts", T, L->top_k, kFp8MaxPairs);
     int splits = fp8 ? 1 : y_splits_for(L, T);
     *out = carve_workspace(ws, T, L->d_model, L->d_ff, L->n_experts, L->top_k, splits, fp8);
     // (at these widths every workspace that holds the unsplit call has always been enough)
@@ -799,6 +805,9 @@ namespace {
 
 constexpr int kFp8MaxDim = 1 << 20, kFp8MaxRows = 1 << 22;
 
+// A launch has less than 2^32 threads along its first dimension, in whole workgroups of 256.
+bool too_many_threads(size_t threads) { return threads > (1ull << 32) - 256; }
+
 int check_fp8_shape(const char* who, int out, int in) {
     if (out < 0 || in < 0) return fail(MOE_EINVAL, "%s: negative size", who);
     if (in % 16) return fail(MOE_ESHAPE, "%s: in=%d not a multiple of 16", who, in);
@@ -861,6 +870,7 @@ int moe_quantize_fp8(const void* w_fp16, int out, int in, void* codes, float* sc
 
 int moe_dequant_fp8(const moe_mat* m, int out, int in, void* w_fp16, moe_stream_t stream) {
     if (int rc = check_fp8_shape("moe_dequant_fp8", out, in)) return rc;
+    if (too_many_threads((size_t)out * in / 8)) return fail(MOE_ESHAPE, "moe_dequant_fp8: out=%d, in=%d are too many for a call", out, in);
     if (out == 0 || in == 0) return MOE_OK;
     if (!m || !w_fp16) return fail(MOE_EINVAL, "moe_dequant_fp8: NULL argument");
     if (int rc = check_fp8_mat("moe_dequant_fp8", *m)) return rc;
@@ -873,6 +883,8 @@ int moe_quantize_fp8_rows(const void* x, int n, int in, void* codes, float* scal
     if (int rc = check_fp8_shape("moe_quantize_fp8_rows", 0, in)) return rc;
     if (n < 0) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: negative size");
     if (n > kFp8MaxRows) return fail(MOE_ESHAPE, "moe_quantize_fp8_rows: n=%d past %d", n, kFp8MaxRows);
+    if (too_many_threads((size_t)n * ((in + MOE_FP8_BLOCK - 1) / MOE_FP8_BLOCK) * 8))
+        return fail(MOE_ESHAPE, "moe_quantize_fp8_rows: n=%d rows of in=%d are too many for a call", n, in);
     if (n == 0 || in == 0) return MOE_OK;
     if (!x || !codes || !scale) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: NULL argument");
     if ((uintptr_t)codes % 16) return fail(MOE_EINVAL, "moe_quantize_fp8_rows: codes must be 16-byte aligned");
@@ -928,7 +940,7 @@ int moe_route_logits(const moe_layer* layer, const void* x, int T, float* logits
                      moe_stream_t stream) {
     if (int rc = check_layer(layer)) return rc;
     if (!x || !logits || !topk_idx || !topk_gate) return fail(MOE_EINVAL, "moe_route_logits: NULL argument");
-    if (T < 1) return fail(MOE_ESHAPE, "moe_route_logits: T=%d < 1", T);
+    if (T < 1 || T >= 1 << 24) return fail(MOE_ESHAPE, "moe_route_logits: T=%d outside [1, 2^24)", T);   // (256 threads per token)
     launch_route_logits((const half_t*)x, (const half_t*)layer->w_gate, layer->gate_bias, T, layer->d_model, layer->n_experts, layer->top_k,
                         topk_idx, topk_gate, logits, (hipStream_t)stream);
     return check_hip((hipStream_t)stream);
@@ -952,6 +964,7 @@ int moe_balance_loss(const moe_layer* layer, const float* logits, const int32_t*
     if (int rc = check_layer(layer)) return rc;
     if (!logits || !topk_idx || !counts || !mean_prob || !loss) return fail(MOE_EINVAL, "moe_balance_loss: NULL argument");
     if (T < 1) return fail(MOE_ESHAPE, "moe_balance_loss: T=%d < 1", T);
+    if ((long long)T * layer->top_k > INT32_MAX) return fail(MOE_ESHAPE, "moe_balance_loss: T=%d, top_k=%d: past 32-bit counts", T, layer->top_k);
     GateWorkspace w;
     if (int rc = check_gate_ws(layer, T, ws, ws_bytes, &w)) return rc;
     launch_balance_loss(logits, topk_idx, valid, T, layer->n_experts, layer->top_k, counts, mean_prob, loss, w, (hipStream_t)stream);

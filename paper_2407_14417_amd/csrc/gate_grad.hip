@@ -478,7 +478,7 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGrad
     for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int s = 0; s < ET; ++s) acc[j][s] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int tiles = (a.T + 31) / 32;
+    const int tiles = (a.T - 1) / 32 + 1;
     const int first = blockIdx.y * tiles_per_split, end = min(first + tiles_per_split, tiles);
     float* const dl = (float*)sums + wave * 1024;        // the unit's d_logits, [32][E]
     // What the next unit needs is asked for between the two products of this one.  Tokens past the last one: the last one again; their d_logits are 0.
@@ -678,7 +678,7 @@ void launch_balance_loss(const float* logits, const int32_t* idx, const uint8_t*
 // A compute unit per workgroup, as far as every wavefront has a tile of 32 tokens; up to two tiles a wavefront one share takes alone, which saves the
 // launch that adds shares up.
 int gate_dw_splits(int T, int d, int) {
-    const int by_work = ((T + 31) / 32 + kGradWaves - 1) / kGradWaves, by_chip = 256 / ((d + 127) / 128);
+    const int by_work = ((T - 1) / 32 + kGradWaves) / kGradWaves, by_chip = 256 / ((d + 127) / 128);
     const int s = by_work < by_chip ? by_work : by_chip;
     return by_work <= 2 || s < 1 ? 1 : s;
 }
@@ -701,7 +701,7 @@ void launch_route_backward(const GateGradArgs& a, const GateWorkspace& w, hipStr
         finish(1);
         return;
     }
-    const int splits = w.dw_splits, tiles_per_split = ((a.T + 31) / 32 - 1) / splits + 1;
+    const int splits = w.dw_splits, tiles_per_split = (a.T - 1) / 32 / splits + 1;
     float* const dw = splits > 1 ? w.dw : a.d_w;
     const GradRest rest{w.sums, w.counts, blocks, w.status};
     const dim3 grid((a.d + 127) / 128 + (splits == 1), splits);

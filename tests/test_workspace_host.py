@@ -41,3 +41,24 @@ def test_binding_asks_for_any_precision():
     for T in (1, 40):
         plain, most = mm.workspace_bytes(layer, T), mm.workspace_bytes(layer, T, any_precision=True)
         assert most == max(plain, mm.workspace_bytes(later, T)) == mm.workspace_bytes(later, T, any_precision=True)
+
+
+def test_sizes_past_one_launch_are_refused(L):
+    """A launch has less than 2^32 threads along its first dimension and 2^16 workgroups along its second: larger calls are refused before it."""
+    most = 2 ** 29 - 32                                      # blocks of 128 columns of all rows, eight threads each
+    n = most // 8192 + 1
+    assert L.moe_quantize_fp8_rows(4096, n, 1 << 20, 4096, 4096, None) == mm.MOE_ESHAPE and b"moe_quantize_fp8_rows" in L.moe_last_error()
+    assert L.moe_quantize_fp8_rows(4096, 1 << 22, 128 * 128, 4096, 4096, None) == mm.MOE_ESHAPE
+    m = ctypes.byref(mm.CMat(4096, 4096, None))
+    assert L.moe_dequant_fp8(m, 1 << 18, 1 << 17, 4096, None) == mm.MOE_ESHAPE and b"moe_dequant_fp8" in L.moe_last_error()
+    assert L.moe_dequant_fp8(m, 1 << 20, 1 << 20, 4096, None) == mm.MOE_ESHAPE
+    lay = layer_of([mm.PREC_FP8B128] * 8, 64, 64, 8)
+    p, T = ctypes.byref(lay), (63 << 16) // 8 + 1            # (token, slot) pairs of a block with e4m3 experts
+    assert L.moe_layer_forward(p, 4096, T, 4096, None, None, 4096, 1 << 62, None) == mm.MOE_ESHAPE
+    assert L.moe_layer_forward(p, 4096, T - 1, 4096, None, None, 4096, 4096, None) == mm.MOE_EWORKSPACE
+    assert L.moe_route_logits(p, 4096, 1 << 24, 4096, 4096, 4096, None) == mm.MOE_ESHAPE
+    ws = 1 << 62
+    assert L.moe_balance_loss(p, 4096, 4096, None, 1 << 28, 4096, 4096, 4096, 4096, ws, None) == mm.MOE_ESHAPE    # 2^31 pairs
+    # tokens up to the last int: as many shares of d_w, one float per expert and token more (64 tokens are 2048 bytes)
+    assert 0 < L.moe_gate_workspace_bytes(p, 2 ** 31 - 1) < ws
+    assert L.moe_gate_workspace_bytes(p, 2 ** 31 - 1) - L.moe_gate_workspace_bytes(p, 2 ** 31 - 64) == 64 * 8 * 4
