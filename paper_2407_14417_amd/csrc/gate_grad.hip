@@ -491,10 +491,10 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGrad
         if (a.d_w) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = *(const uint4_anywhere_t*)(a.x + (t0 + min(8 * q + k, left - 1)) * d + (in ? col : 0));
-            if (a.valid)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) valid[k] = a.valid[t0 + min(8 * q + k, left - 1)];
         }
+        if (a.valid)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) valid[k] = a.valid[t0 + min(8 * q + k, left - 1)];
         const int n = min(left, 32) * E;
         const float* const src = a.d_logits + t0 * E;
 #pragma unroll
@@ -519,6 +519,14 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGrad
         for (int i = 0; i < 4; ++i)
             if (256 * i < 32 * E) *(float4_t*)(dl + 256 * i + 4 * lane) = part[i];
         wave_lds_handover();
+        uint32_t live = ~0u;                             // bit t: token t of the unit is no padding (its d_x is 0 whatever W holds)
+        if (a.valid) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) m |= (valid[k] ? 1u : 0u) << k;
+            live = __builtin_amdgcn_readlane(m, 0) | __builtin_amdgcn_readlane(m, 16) << 8 | __builtin_amdgcn_readlane(m, 32) << 16 |
+                   __builtin_amdgcn_readlane(m, 48) << 24;
+        }
         if (a.d_w) {
             if (a.valid) {                               // padding may hold anything
 #pragma unroll
@@ -580,7 +588,7 @@ __global__ __launch_bounds__(64 * kGradWaves, 2) void gate_dx_dw_kernel(GateGrad
                         o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], lo, float4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
                         o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[2 * p + c], hi, o[c], 0, 0, 0);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[c][i] *= back;
+                        for (int i = 0; i < 4; ++i) o[c][i] = live >> t & 1 ? o[c][i] * back : 0.0f;
                     }
                     const int c = col0 + 32 * p + 8 * q;
                     if (t >= left || c >= d) continue;
