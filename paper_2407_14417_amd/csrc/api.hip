@@ -984,6 +984,11 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
     if (T < 1) return fail(MOE_ESHAPE, "moe_route_backward: T=%d < 1", T);
     GateWorkspace w;
     if (int rc = check_gate_ws(layer, T, ws, ws_bytes, &w)) return rc;
+    if (d_x && d_w_gate) {   // rows of x are read while others of d_x are written
+        const size_t n = (size_t)T * layer->d_model, bytes = n * (d_x_type == MOE_OUT_F16 ? 2 : 4);
+        if ((uintptr_t)d_x < (uintptr_t)x + n * 2 && (uintptr_t)x < (uintptr_t)d_x + bytes)
+            return fail(MOE_EINVAL, "moe_route_backward: d_x overlaps x");
+    }
     const GateGradArgs a{(const half_t*)x, (const half_t*)layer->w_gate, logits, topk_idx, valid, counts, d_gate, d_loss,
                          d_logits ? d_logits : w.dl, d_x, d_w_gate, d_bias, T, layer->d_model, layer->n_experts, layer->top_k,
                          d_x_type == MOE_OUT_F16};

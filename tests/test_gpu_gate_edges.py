@@ -30,3 +30,29 @@ def test_rows_of_padding_get_zeros_whatever_the_gate_holds(T, E, k, d, half, wan
     assert np.array_equal(np.delete(got["d_x"], cols, 1), np.delete(clean["d_x"], cols, 1))
     for n in set(want) - {"d_x"}:
         assert np.array_equal(got[n], clean[n]), n
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_d_x_next_to_x_and_in_its_place(half):
+    """d_x right behind x, and over x where no d_w_gate is asked for; over x with it is refused."""
+    T, E, k, d = 70, 8, 2, 128
+    rng = np.random.default_rng(21)
+    z, idx, _ = case(rng, T, E, k, 0.0)
+    x, w = rng.standard_normal((T, d)).astype(np.float16), (rng.standard_normal((E, d)) * 0.05).astype(np.float16)
+    dg, layer = rng.standard_normal((T, k)).astype(np.float32), gate_layer(E, k, d, cuda(w))
+    kind = torch.float16 if half else torch.float32
+    want = run_backward(layer, x, z, idx, None, None, dg, None, ("d_x", "d_w_gate"), kind)
+    room = torch.empty(3 * T * d, dtype=torch.float16, device="cuda")
+    xs = room[: T * d].view(T, d)
+    xs.copy_(cuda(x))
+    dx = (room[T * d: 2 * T * d] if half else room[T * d:].view(torch.float32)).view(T, d)
+    dw, ws = torch.empty(E, d, device="cuda"), mm.alloc_gate_workspace(layer, T)
+    call = lambda at, **k: mm.moe_route_backward(layer, xs, cuda(z), cuda(idx), ws, d_gate=cuda(dg), d_x=at, **k)  # noqa: E731
+    call(dx, d_w_gate=dw)
+    assert np.array_equal(dx.cpu().numpy(), want["d_x"]) and np.array_equal(dw.cpu().numpy(), want["d_w_gate"])
+    over = (room[: T * d] if half else room[: 2 * T * d].view(torch.float32)).view(T, d)
+    with pytest.raises(mm.MoeError) as refused:
+        call(over, d_w_gate=dw)
+    assert refused.value.code == mm.MOE_EINVAL
+    call(over)
+    assert np.array_equal(over.cpu().numpy(), want["d_x"])

@@ -62,3 +62,15 @@ def test_sizes_past_one_launch_are_refused(L):
     # tokens up to the last int: as many shares of d_w, one float per expert and token more (64 tokens are 2048 bytes)
     assert 0 < L.moe_gate_workspace_bytes(p, 2 ** 31 - 1) < ws
     assert L.moe_gate_workspace_bytes(p, 2 ** 31 - 1) - L.moe_gate_workspace_bytes(p, 2 ** 31 - 64) == 64 * 8 * 4
+
+
+def test_d_x_on_x_is_refused(L):
+    """Tokens are read for d_w_gate while rows of d_x are written: not in place, nor with a part of the rows."""
+    lay = layer_of([mm.PREC_FP16] * 4, 64, 64, 2)
+    p, T, d, x = ctypes.byref(lay), 9, 64, 1 << 20
+
+    ws = L.moe_gate_workspace_bytes(p, T)
+    for kind, size in ((mm.OUT_F16, 2), (mm.OUT_F32, 4)):
+        for dx in (x, x + T * d * 2 - 2, x - T * d * size + 2):
+            rc = L.moe_route_backward(p, x, 4096, 4096, None, T, None, 4096, None, None, dx, kind, 4096, None, 4096, ws, None)
+            assert rc == mm.MOE_EINVAL and b"d_x" in L.moe_last_error()
