@@ -181,13 +181,36 @@ class Expert:
         return sum(m.nbytes() for m in (self.w1, self.w3, self.w2) if m is not None)
 
 
+def _fits_fp8(m: Optional[Mat], what: str, out: int, inn: int) -> None:
+    """The kernels read what an e4m3 expert's descriptor and its layer's shape say: codes [out,in], fp32 scales per block of 128 x 128."""
+    import torch
+    blocks = ((out + FP8_BLOCK - 1) // FP8_BLOCK, (inn + FP8_BLOCK - 1) // FP8_BLOCK)
+    for t, part, types, shape in ((m and m.data, "codes", (torch.uint8, torch.float8_e4m3fn), (out, inn)), (m and m.scale, "scales", (torch.float32,), blocks)):
+        if t is None:
+            raise MoeError(MOE_EINVAL, f"{what}: no {part}")
+        if t.dtype not in types or not t.is_contiguous():
+            raise MoeError(MOE_EINVAL, f"{part} of {what}: {t.dtype}, strides {t.stride()}: contiguous {types} is needed")
+        if tuple(t.shape) != shape:
+            raise MoeError(MOE_ESHAPE, f"{part} of {what}: {tuple(t.shape)}, {shape} is needed")
+
+
+def _fitting_expert(e: Expert, prec: int, i: int, d: int, f: int, on_gpu: bool) -> CExpert:
+    """C descriptor of expert ``i``, whose matrices fit its layer if they are e4m3 (a missing expert may have none)."""
+    if prec == PREC_FP8B128 and (on_gpu or e.w1 or e.w3 or e.w2):
+        for m, name, out, inn in ((e.w1, "w1", f, d), (e.w3, "w3", f, d), (e.w2, "w2", d, f)):
+            _fits_fp8(m, f"expert {i}, {name}", out, inn)
+        if on_gpu and not all(t.is_cuda for m in (e.w1, e.w3, e.w2) for t in (m.data, m.scale)):
+            raise MoeError(MOE_EINVAL, f"expert {i} is resident, and not on a GPU")
+    return e.c()
+
+
 class Layer:
     """Host descriptor of one MoE block; keeps the tensors alive that its device pointers name."""
 
     def __init__(self, d_model: int, d_ff: int, top_k: int, w_gate, experts: Sequence[Expert], gate_bias=None):
         self.d_model, self.d_ff, self.top_k = d_model, d_ff, top_k
         self.w_gate, self.gate_bias, self.experts = w_gate, gate_bias, list(experts)
-        self._arr = (CExpert * len(self.experts))(*[e.c() for e in self.experts])
+        self._arr = (CExpert * len(self.experts))(*[_fitting_expert(e, e.prec, i, d_model, d_ff, e.resident) for i, e in enumerate(self.experts)])
         self.c = CLayer(d_model, d_ff, len(self.experts), top_k, _ptr(w_gate), _ptr(gate_bias), self._arr)
 
     @property
@@ -249,7 +272,8 @@ class Swap:
         import torch
         self.layer, self.host_experts, self.n_slots = layer, list(host_experts), n_slots
         null = CExpert(PREC_FP16, 0, CMat(None, None, None), CMat(None, None, None), CMat(None, None, None))
-        self._arr = (CExpert * layer.n_experts)(*[e.c() if e is not None else null for e in self.host_experts])
+        self._arr = (CExpert * layer.n_experts)(*[null if e is None else _fitting_expert(e, layer.experts[i].prec, i, layer.d_model, layer.d_ff, False)
+                                                  for i, e in enumerate(self.host_experts)])
         self.slot_bytes = int(lib().moe_swap_slot_bytes(ctypes.byref(layer.c)))
         self.space = torch.empty(max(1, n_slots * self.slot_bytes), dtype=torch.uint8, device="cuda")
         self.host_idx = torch.empty(n_tokens * layer.top_k, dtype=torch.int32).pin_memory()
