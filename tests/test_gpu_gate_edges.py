@@ -5,6 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2407_14417_amd import binding as mm
+from tests.test_gpu_fp8_many_rows import behind_work
 from tests.test_gpu_gate_grad import ALL, case, cuda, gate_layer, loss_of, run_backward
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +57,33 @@ def test_d_x_next_to_x_and_in_its_place(half):
     assert refused.value.code == mm.MOE_EINVAL
     call(over)
     assert np.array_equal(over.cpu().numpy(), want["d_x"])
+
+
+def test_training_of_the_gate_on_another_stream():
+    """Tokens and gradients come into being on the stream of the calls, behind work: calls on another stream would see what was there before."""
+    T, E, k, d = 1500, 32, 4, 512
+    rng = np.random.default_rng(22)
+    layer = gate_layer(E, k, d, cuda((rng.standard_normal((E, d)) * 0.05).astype(np.float16)))
+    new = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device="cuda")  # noqa: E731
+    x, logits, idx, gate, dg = new(T, d, t=torch.float16), new(T, E), new(T, k, t=torch.int32), new(T, k), new(T, k)
+    res = dict(counts=new(E + 1, t=torch.int32), mean=new(E), loss=new(1), d_logits=new(T, E), d_x=new(T, d), d_w_gate=new(E, d), d_bias=new(E))
+    one, ws = torch.full((1,), 2.0, device="cuda"), mm.alloc_gate_workspace(layer, T)
+    x_new, dg_new = cuda(rng.standard_normal((T, d)).astype(np.float16)), cuda(rng.standard_normal((T, k)).astype(np.float32))
+
+    def step():
+        mm.moe_route_logits(layer, x, logits, idx, gate)
+        mm.moe_balance_loss(layer, logits, idx, res["counts"], res["mean"], res["loss"], ws)
+        mm.moe_route_backward(layer, x, logits, idx, ws, counts=res["counts"], d_gate=dg, d_loss=one, **{n: res[n] for n in ALL})
+    side = torch.cuda.Stream()
+    behind_work(side, x, x_new)
+    with torch.cuda.stream(side):
+        dg.copy_(dg_new)
+        step()
+        got = {n: t.clone() for n, t in res.items()}
+    torch.cuda.synchronize()
+    for t in res.values():
+        t.zero_()
+    step()
+    torch.cuda.synchronize()
+    for n, t in res.items():
+        assert torch.equal(t, got[n]) and float(t.double().abs().max()) > 0, n
