@@ -5,6 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2407_14417_amd import binding as mm
+from tests.common import assert_ffn_close
 from tests.test_gpu_fp8_many_rows import behind_work
 from tests.test_gpu_gate_grad import ALL, case, cuda, gate_layer, loss_of, run_backward
 
@@ -87,3 +88,42 @@ def test_training_of_the_gate_on_another_stream():
     torch.cuda.synchronize()
     for n, t in res.items():
         assert torch.equal(t, got[n]) and float(t.double().abs().max()) > 0, n
+
+
+def test_gates_of_a_block_are_trained_through_its_experts():
+    """f = sum(g * out) of a block with e4m3 experts: d_gate from the rows of the experts alone, the rest from the backward pass, against differences of
+    the 64-bit formula with those rows held."""
+    T, E, k, d, f = 48, 4, 2, 256, 384
+    rng = np.random.default_rng(23)
+    half = lambda *s, scale=1.0: (rng.standard_normal(s) * scale).astype(np.float16)  # noqa: E731
+    x, w, g = half(T, d), half(E, d, scale=0.1), rng.standard_normal((T, d))
+    experts = [mm.Expert(mm.PREC_FP8B128, *[mm.quantize_mat_fp8(cuda(half(o, i, scale=0.1))) for o, i in ((f, d), (f, d), (d, f))]) for _ in range(E)]
+    layer = mm.Layer(d, f, k, cuda(w), experts)
+    new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+    logits, idx, gate, out = new(T, E), new(T, k, t=torch.int32), new(T, k), new(T, d, t=torch.float16)
+    mm.moe_route_logits(layer, cuda(x), logits, idx, gate)
+    ws = mm.alloc_workspace(layer, T)
+    rows = new(E, T, d)
+    for e in range(E):
+        mm.moe_expert_ffn_mixed(layer, e, cuda(x), rows[e], ws)
+    pick, y = idx.cpu().numpy().astype(np.int64), rows.cpu().numpy().astype(np.float64)
+    slots = y[pick, np.arange(T)[:, None]]                                  # [T, k, d]
+    mm.moe_layer_forward(layer, cuda(x), out, ws)
+    assert_ffn_close(out.cpu().numpy(), (gate.cpu().numpy().astype(np.float64)[:, :, None] * slots).sum(1), "block")
+    d_gate = (slots * g[:, None]).sum(2).astype(np.float32)
+    got = run_backward(layer, x, logits.cpu().numpy(), pick.astype(np.int32), None, None, d_gate, None, ALL)
+
+    def value(xf, wf):
+        z = np.take_along_axis(xf @ wf.T, pick, 1)
+        z = np.exp(z - z.max(1, keepdims=True))
+        return (z / z.sum(1, keepdims=True) * (slots * g[:, None]).sum(2)).sum()
+    xf, wf, h = x.astype(np.float64), w.astype(np.float64), 1e-5
+    for _ in range(24):
+        t, e, c = rng.integers(T), rng.integers(E), rng.integers(d)
+        for name, at, step in (("d_x", (t, c), 0), ("d_w_gate", (e, c), 1)):
+            lo, hi = [xf.copy(), wf.copy()], [xf.copy(), wf.copy()]
+            lo[step][at] -= h
+            hi[step][at] += h
+            diff = (value(*hi) - value(*lo)) / (2 * h)
+            # a difference quotient of 64-bit values of this size over 2e-5, its third derivative, and the backward pass's own roundings
+            assert abs(diff - got[name][at]) <= 1e-4 * max(np.abs(got[name]).max(), 1.0), (name, at)
