@@ -326,6 +326,8 @@ int moe_balance_loss(const moe_layer* layer, const float* logits, const int32_t*
  *                 + d_loss * n_experts / (n top_k) * 1/n * p[t,j] * (counts[j] - sum_e counts[e] p[t,e])
  *   d_x = d_logits W_gate,   d_w_gate = d_logits^T x,   d_bias = sum_t d_logits[t,:]
  * g = topk_gate, worked out again from the logits; counts as moe_balance_loss gives them (no gradient flows through them).
+ * Of a block with out[t,:] = sum_s topk_gate[t,s] y[t,s,:] the caller has d_gate[t,s] = sum_c d_out[t,c] y[t,s,c], y being the rows that
+ * moe_expert_ffn_mixed gives.
  * Rows of padding get zeros and count nowhere, whatever they hold; so does a token's gate term if its chosen logits are all
  * -infinity, and its loss term if all its logits are.
  * d_gate: device fp32 [T, top_k] or NULL; d_loss: device fp32 [1] with counts, or both NULL; one of the two gradients has to be given.

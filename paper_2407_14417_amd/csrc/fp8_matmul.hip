@@ -329,6 +329,9 @@ size_t fp8_one_lds(int k, int K, bool up) {
     const int waves = one_waves(up), total = (up ? 1 : k) * ((K + kFp8Block - 1) / kFp8Block), most = (total + waves - 1) / waves;
     return one_sums(up) + (size_t)waves * most * (kFp8Block + sizeof(float));
 }
+// Up to 64 KB of LDS, so that two workgroups share a compute unit; past that the launches for several tokens serve one as well (us, these launches and those:
+// 8 experts of 4096 x 14336, two slots 73 and 85, four 131 and 143; 4096 x 7168, eight 128 and 141; past the line, with as much LDS as there is, 4096 x 14336,
+// eight 249 and 258, 1024 x 16384, eight 144 and 106, 16 experts of 2048 x 8192, eight 96 and 94).
 bool fp8_one_serves(int k, int d, int f) { return fp8_one_lds(k, d, true) <= 65536 && fp8_one_lds(k, f, false) <= 65536; }
 
 void launch_fp8_one(const Fp8OneArgs& a, bool up, hipStream_t st) {

@@ -15,7 +15,7 @@
 //
 // Why this tile: 256 rows of w and up to 256 of x are 128 results per lane, what the registers hold without a spill at two wavefronts per SIMD; and two are
 // needed, since the scaling of one wavefront's products has to run beside the matrix instructions of the other (2.1 PFLOP/s in registers with one, 4.1 with two).
-// Every code brought into LDS serves 256 results then; a stage is 64 KB at most, so two to four are under way.
+// Every code brought into LDS serves 256 results then; a stage is 66 KB at most (256 rows of x), so two to four are under way.
 #include <atomic>
 #include <cmath>
 #include <type_traits>

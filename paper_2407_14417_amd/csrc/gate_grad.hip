@@ -5,8 +5,8 @@
 // reductions over them on the DPP network; sums over tokens stay in the lane, which always sees the same experts.
 //
 // Bound: the loss by its launches and the way to memory and back (65536 tokens, 32 experts, four slots: 9.5 MB, 1.8 us of a copy's rate; 7.3 us and a finish of
-// 4.1; few tokens: one launch, 4.7).  The backward pass by x read and d_x written once (16384 tokens, 4096 columns, 32 experts, fp16: 272 MB, 52 us; 67-69 us,
-// 4.0 TB/s, beside 6.7 for d_logits and 4.8 for the sums of d_w).  d_x and d_w share the one pass over x's tokens and columns, since both
+// 4.1; few tokens: one launch, 4.7).  The backward pass by x read and d_x written once (16384 tokens, 4096 columns, 32 experts, fp16: 272 MB, 52 us; 69-71 us,
+// 3.9 TB/s, beside 6.8 for d_logits and 4.9 for the sums of d_w).  d_x and d_w share the one pass over x's tokens and columns, since both
 // need a tile's d_logits.
 #include <type_traits>
 
