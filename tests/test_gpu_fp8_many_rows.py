@@ -451,3 +451,38 @@ def test_block_of_the_mixtral_shape(T):
             y = values(*quantized_rows(h), True) @ values(ex.w2.data, ex.w2.scale, False).t()
             want.index_add_(0, p // k, y * gate.reshape(-1)[p].double()[:, None])
     assert_ffn_close(out.cpu().numpy(), want.cpu().numpy(), f"{T} tokens")
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_gathered_rows_past_32_bit_offsets(half):
+    """Rows of x that lie past 2^32 bytes: the kernel for few rows serves them, however many there are."""
+    n, inn, out, E, P = 524_400, 8192, 96, 3, 5000
+    assert n * inn > 1 << 32 and rows_per_chunk(P, out, inn, E, n, True, not half) == 0
+    g = generator(7)
+    codes, scale = torch.zeros(n, inn, dtype=torch.uint8, device="cuda"), torch.zeros(inn // 128, n, device="cuda")
+    far = torch.arange(n - 300, n, device="cuda")
+    codes[far], scale[:, far] = quantized_rows(random_half(g, 300, inn))
+    rows = far[torch.randint(0, 300, (P,), generator=g, device="cuda")]
+    rows[::7] = 0
+    ws = [mm.quantize_mat_fp8(random_half(g, out, inn, scale=0.02)) for _ in range(E)]
+    off = [0, 1700, 1700, P]
+    y, around = result(P, out, half)
+    mm.moe_matmul_fp8_grouped(mm.MatGroup(ws), codes, scale, dev(np.array(off, dtype=np.int32)), (rows * 2 + 1).int(), 2, y)
+    for e in (0, 2):
+        at = rows[off[e]: off[e + 1]]
+        check_on_device(y[off[e]: off[e + 1]], values(codes[at], scale[:, at].contiguous(), True), values(ws[e].data, ws[e].scale, False), half, e)
+    assert all(bool(a.isnan().all()) for a in around)
+
+
+def test_block_of_more_than_65536_tokens():
+    T, d, f, E, k = 70_001, 64, 128, 4, 2
+    g = generator(8)
+    layer = mm.Layer(d, f, k, random_half(g, E, d, scale=0.2), [expert_on_device(g, d, f, 0.1) for _ in range(E)])
+    x, out = random_half(g, T, d), spoiled((T, d), torch.float16)
+    ws = mm.alloc_workspace(layer, T)
+    mm.moe_layer_forward(layer, x, out, ws)
+    assert mm.moe_read_status(ws) == 0
+    for lo, hi in ((0, 20_000), (50_000, T)):
+        part = spoiled((hi - lo, d), torch.float16)
+        mm.moe_layer_forward(layer, x[lo:hi], part, ws)
+        assert_ffn_close(out[lo:hi].cpu().numpy(), part.cpu().numpy(), (lo, hi))
