@@ -333,7 +333,7 @@ int moe_balance_loss(const moe_layer* layer, const float* logits, const int32_t*
  * d_gate: device fp32 [T, top_k] or NULL; d_loss: device fp32 [1] with counts, or both NULL; one of the two gradients has to be given.
  * Each result may be NULL, at least one has to be asked for: d_logits: device fp32 [T, n_experts]; d_x: device fp32 or fp16 (d_x_type, a moe_out) [T, d_model];
  * d_w_gate: device fp32 [n_experts, d_model]; d_bias: device fp32 [n_experts].  x: device fp16 [T, d_model], needed for d_w_gate only.
- * All are overwritten; with d_w_gate d_x must not overlap x (MOE_EINVAL); the same inputs give the same bits.
+ * All are overwritten; with d_w_gate d_x must not overlap x (MOE_EINVAL); d_logits may be logits; the same inputs give the same bits.
  */
 int moe_route_backward(const moe_layer* layer, const void* x, const float* logits, const int32_t* topk_idx, const uint8_t* valid, int T,
                        const int32_t* counts, const float* d_gate, const float* d_loss, float* d_logits, void* d_x, int d_x_type,

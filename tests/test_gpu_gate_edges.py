@@ -127,3 +127,19 @@ def test_gates_of_a_block_are_trained_through_its_experts():
             diff = (value(*hi) - value(*lo)) / (2 * h)
             # a difference quotient of 64-bit values of this size over 2e-5, its third derivative, and the backward pass's own roundings
             assert abs(diff - got[name][at]) <= 1e-4 * max(np.abs(got[name]).max(), 1.0), (name, at)
+
+
+@pytest.mark.parametrize("T,E,k,d", [(20_001, 32, 4, 64), (17_000, 6, 2, 64)])
+def test_d_logits_in_the_place_of_the_logits(T, E, k, d):
+    rng = np.random.default_rng([T, E])
+    z, idx, valid = case(rng, T, E, k, 0.2)
+    x, dg = rng.standard_normal((T, d)).astype(np.float16), rng.standard_normal((T, k)).astype(np.float32)
+    counts, _, _ = loss_of(z.astype(np.float64), idx, valid, E, k)
+    layer = gate_layer(E, k, d, cuda((rng.standard_normal((E, d)) * 0.05).astype(np.float16)))
+    want = run_backward(layer, x, z, idx, valid, counts, dg, 5.0, ALL)
+    logits, out = cuda(z), {n: torch.empty(s, device="cuda") for n, s in (("d_x", (T, d)), ("d_w_gate", (E, d)), ("d_bias", (E,)))}
+    mm.moe_route_backward(layer, cuda(x), logits, cuda(idx), mm.alloc_gate_workspace(layer, T), valid=cuda(valid),
+                          counts=cuda(np.concatenate([counts, [int(valid.sum())]]).astype(np.int32)), d_gate=cuda(dg),
+                          d_loss=torch.full((1,), 5.0, device="cuda"), d_logits=logits, **out)
+    for n, t in (out | {"d_logits": logits}).items():
+        assert np.array_equal(t.cpu().numpy(), want[n]), n
