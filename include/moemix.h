@@ -339,6 +339,59 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
                        const int32_t* counts, const float* d_gate, const float* d_loss, float* d_logits, void* d_x, int d_x_type,
                        float* d_w_gate, float* d_bias, void* ws, size_t ws_bytes, moe_stream_t stream);
 
+/* ---------------------------------------------------------------- training the experts
+ *
+ * Forward and backward pass of the experts of a grouping (moe_permute's), all of them held in 16 bits and resident (else MOE_EINVAL,
+ * MOE_ENOTRESIDENT).  Grouped row r of expert e stands for pair p = perm[r], token t = p / top_k, with gate g = topk_gate[p]; P = T top_k.
+ *   moe_experts_forward:   a[r,:] = W1 x[t,:],  u[r,:] = W3 x[t,:],  h = silu(a) * u,  out[t,:] = sum over the token's rows of g W2 h[r,:]
+ *     a and u are kept for the backward pass, rounded to fp16; h, of the unrounded values, is rounded to fp16 as everywhere.
+ *   moe_experts_backward:  with q[r,:] = W2^T d_out[t,:] and s = 1 / (1 + exp(-a)), from the kept a and u:
+ *     d_gate[p] = sum_f q h,   d_a = g q u s (1 + a (1 - s)),   d_u = g q a s        (d_a, d_u and g h are rounded to fp16)
+ *     d_x[t,:] = sum over the token's rows of W1^T d_a[r,:] + W3^T d_u[r,:]          (without what flows through the gates: moe_route_backward)
+ *     d_w1 = sum_r d_a[r,:]^T x[t,:],   d_w3 = sum_r d_u[r,:]^T x[t,:],   d_w2 = sum_r d_out[t,:]^T (g h[r,:])      over the rows of the expert
+ * Sums are fp32.  Gradients carry the caller's loss scale: what passes 65504 on the way is an infinity, which moe_clip_gradients then finds.
+ * A pair in no group (moe_permute drops indices outside [0, n_experts), so that is how tokens of padding are left out, whatever they hold) adds nothing
+ * to its token and gets a d_gate of 0; grouped rows outside [offsets[0], offsets[n_experts]) of a and u are left as they were.  An expert without rows gets
+ * gradients of zeros.
+ * x, d_out: device fp16 [T, d_model]; a, u: device fp16 [P, d_ff]; out: device fp16 [T, d_model]; topk_gate: device fp32 [T, top_k], NULL: all gates are 1;
+ * offsets: device int32 [n_experts + 1], NULL (one expert only): all P rows are its; perm: device int32 [P], NULL: row r is pair r.  (Whatever offsets and perm
+ * hold, nothing outside the arrays is read or written.)
+ * d_x: device, fp32 or fp16 (d_x_type, a moe_out) [T, d_model]; d_gate: device fp32 [T, top_k]; d_w: HOST array [n_experts] of the matrices' gradients,
+ * device, all fp32 or all fp16 (d_w_type), of the matrices' shapes, a NULL entry is not asked for.  Each of d_x, d_gate and d_w may be NULL, not all.  accumulate != 0:
+ * the gradients of the matrices are added to what is there (and an expert without rows leaves its as they are).  The same inputs give the same bits.
+ * Tensors start on 16-byte boundaries (d_gate, topk_gate, offsets and perm: 4).  layer->w_gate and gate_bias are not looked at.
+ * T >= 1, T * d_model <= 2^31 - 2048, T * top_k <= 2^22 (MOE_ESHAPE otherwise).  ws: at least moe_experts_workspace_bytes(layer, T); it carries nothing from one
+ * call to the next.  Neither call sets a status that moe_read_status reads.
+ */
+typedef struct {
+    void *w1, *w3, *w2;
+} moe_expert_grads;
+size_t moe_experts_workspace_bytes(const moe_layer* layer, int T);
+int moe_experts_forward(const moe_layer* layer, const void* x, int T, const float* topk_gate, const int32_t* offsets, const int32_t* perm, void* a,
+                        void* u, void* out, void* ws, size_t ws_bytes, moe_stream_t stream);
+int moe_experts_backward(const moe_layer* layer, const void* x, int T, const float* topk_gate, const int32_t* offsets, const int32_t* perm,
+                         const void* a, const void* u, const void* d_out, void* d_x, int d_x_type, float* d_gate, const moe_expert_grads* d_w,
+                         int d_w_type, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/*
+ * Global norm over the elements v of n_tensors gradients, and clipping:
+ *   norm = unscale * sqrt( sum v^2 ),   out = v * c  with  c = unscale * min(1, max_norm / (norm + 1e-6))
+ * Sums are held in 64 bits.  unscale: finite, > 0, 1 / loss scale; max_norm: >= 0, INFINITY: no limit.  If norm is not finite in 32 bits (a gradient was
+ * not) only norm is written: the caller leaves out the step.
+ * grads: HOST array of at most MOE_MAX_GRADS entries.  grad, out: device, fp32 or fp16 (a moe_out), on the boundary of their type, n elements (n < 2^40, 0: none);
+ * out may be grad (with the same type); apart from that no out may overlap another out or a grad (MOE_EINVAL).
+ * norm: device fp32 [1].  ws: at least moe_clip_workspace_bytes(n_tensors).  The same inputs give the same bits.
+ */
+#define MOE_MAX_GRADS 1024
+typedef struct {
+    const void* grad;
+    void* out;
+    size_t n;
+    int32_t grad_type, out_type;
+} moe_grad;
+size_t moe_clip_workspace_bytes(int n_tensors);
+int moe_clip_gradients(const moe_grad* grads, int n_tensors, float max_norm, float unscale, float* norm, void* ws, size_t ws_bytes, moe_stream_t stream);
+
 /*
  * Seeded synthetic tensors written directly in device memory (stand-ins for trained weights and real
  * activations): element i of the stream is a pure function of (seed, stream_id, first + i).

@@ -20,6 +20,7 @@ GROUP = 64
 FP8_BLOCK = 128
 OUT_F32, OUT_F16 = 0, 1
 MAX_EXPERTS = 32
+MAX_GRADS = 1024
 STATUS_BAD_INDEX = 1 << 1
 STATUS_NOT_RESIDENT = 1 << 3
 
@@ -30,7 +31,8 @@ EXPORTS = (
     "moe_stream_read", "moe_static_scratch_bytes", "moe_layer_forward_static",
     "moe_dequant_int8", "moe_quantize_int8", "moe_quantize_fp8", "moe_dequant_fp8", "moe_quantize_fp8_rows",
     "moe_transpose_fp8", "moe_matmul_fp8", "moe_matmul_fp8_grouped", "moe_route_logits", "moe_gate_workspace_bytes",
-    "moe_balance_loss", "moe_route_backward",
+    "moe_balance_loss", "moe_route_backward", "moe_experts_workspace_bytes", "moe_experts_forward", "moe_experts_backward",
+    "moe_clip_workspace_bytes", "moe_clip_gradients",
 )
 
 
@@ -69,6 +71,15 @@ class CSwap(ctypes.Structure):
     _fields_ = [("host_experts", ctypes.POINTER(CExpert)), ("swap", ctypes.c_void_p), ("slot_bytes", ctypes.c_size_t),
                 ("n_slots", ctypes.c_int32), ("host_idx", ctypes.c_void_p), ("copy_stream", ctypes.c_void_p),
                 ("copied_event", ctypes.c_void_p), ("computed_event", ctypes.c_void_p)]
+
+
+class CExpertGrads(ctypes.Structure):
+    _fields_ = [("w1", ctypes.c_void_p), ("w3", ctypes.c_void_p), ("w2", ctypes.c_void_p)]
+
+
+class CGrad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_size_t), ("grad_type", ctypes.c_int32),
+                ("out_type", ctypes.c_int32)]
 
 
 PREFER_THROUGHPUT, PREFER_QUALITY = 0, 1
@@ -111,6 +122,13 @@ def lib():
         L.moe_gate_workspace_bytes.restype = sz
         L.moe_balance_loss.argtypes = [LP, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         L.moe_route_backward.argtypes = [LP, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.moe_experts_workspace_bytes.argtypes = [LP, i32]
+        L.moe_experts_workspace_bytes.restype = sz
+        L.moe_experts_forward.argtypes = [LP, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.moe_experts_backward.argtypes = [LP, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, ctypes.POINTER(CExpertGrads), i32, i32, vp, sz, vp]
+        L.moe_clip_workspace_bytes.argtypes = [i32]
+        L.moe_clip_workspace_bytes.restype = sz
+        L.moe_clip_gradients.argtypes = [ctypes.POINTER(CGrad), i32, ctypes.c_float, ctypes.c_float, vp, vp, sz, vp]
         L.moe_synth_fill_f16.argtypes = [vp, sz, sz, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_float, i32, vp]
         L.moe_read_status.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_int)]
         L.moe_trace_kernel.argtypes = [i32, vp, vp]
@@ -127,7 +145,8 @@ def lib():
         L.moe_version.restype = i32
         for name in EXPORTS:
             if name not in ("moe_workspace_bytes", "moe_last_error", "moe_version", "moe_swap_slot_bytes",
-                            "moe_static_scratch_bytes", "moe_gate_workspace_bytes"):
+                            "moe_static_scratch_bytes", "moe_gate_workspace_bytes", "moe_experts_workspace_bytes",
+                            "moe_clip_workspace_bytes"):
                 getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -510,6 +529,133 @@ def moe_route_backward(layer: Layer, x, logits, topk_idx, ws, valid=None, counts
         None if d_w_gate is None else _need(d_w_gate, "d_w_gate", _F32, (E, d), dev),
         None if d_bias is None else _need(d_bias, "d_bias", _F32, (E,), dev),
         None if ws is None else _need(ws, "ws", _BYTES, ws.shape, dev), 0 if ws is None else ws.numel(), _stream_on(dev)))
+
+
+# ---------------------------------------------------------------- training the experts
+
+def experts_workspace_bytes(layer: Layer, n_tokens: int) -> int:
+    return int(lib().moe_experts_workspace_bytes(layer.c, n_tokens))
+
+
+def alloc_experts_workspace(layer: Layer, n_tokens: int):
+    import torch
+    n = experts_workspace_bytes(layer, n_tokens)
+    if n == 0:
+        raise MoeError(MOE_ESHAPE, "moe_experts_workspace_bytes rejected the arguments: " + lib().moe_last_error().decode())
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def _need_experts(layer: Layer, dev: int) -> None:
+    """The matrices are 16-bit ones of the layer's shape on the current GPU.  (Looked at once per layer and GPU: a Layer keeps its experts.)"""
+    if getattr(layer, "_trained_on", None) == dev:
+        return
+    d, f = layer.d_model, layer.d_ff
+    for i, e in enumerate(layer.experts):
+        if e.prec != PREC_FP16:
+            raise MoeError(MOE_EINVAL, f"expert {i} is not held in 16 bits")
+        if not e.resident or e.w1 is None or e.w3 is None or e.w2 is None:
+            raise MoeError(MOE_ENOTRESIDENT, f"expert {i} is not resident")
+        for m, name, shape in ((e.w1, "w1", (f, d)), (e.w3, "w3", (f, d)), (e.w2, "w2", (d, f))):
+            _need(m.data, f"expert {i}, {name}", _F16, shape, dev)
+    layer._trained_on = dev
+
+
+def _grouping(layer: Layer, T: int, topk_gate, offsets, perm, dev: int):
+    E, k = layer.n_experts, layer.top_k
+    return (None if topk_gate is None else _need(topk_gate, "topk_gate", _F32, (T, k), dev),
+            None if offsets is None else _need(offsets, "offsets", _I32, (E + 1,), dev),
+            None if perm is None else _need(perm, "perm", _I32, (T * k,), dev))
+
+
+def moe_experts_forward(layer: Layer, x, topk_gate, offsets, perm, a, u, out, ws) -> None:
+    """``topk_gate`` None: gates of 1; ``offsets`` None: one expert has all rows; ``perm`` None: row r is pair r."""
+    dev = _device()
+    T, d, f = _rows_cols(x, "x")[0], layer.d_model, layer.d_ff
+    _need_experts(layer, dev)
+    kept = (T * layer.top_k, f)
+    _check(lib().moe_experts_forward(layer.c, _need(x, "x", _F16, (T, d), dev), T, *_grouping(layer, T, topk_gate, offsets, perm, dev),
+                                     _need(a, "a", _F16, kept, dev), _need(u, "u", _F16, kept, dev), _need(out, "out", _F16, (T, d), dev),
+                                     None if ws is None else _need(ws, "ws", _BYTES, ws.shape, dev), 0 if ws is None else ws.numel(), _stream_on(dev)))
+
+
+class ExpertGrads:
+    """Host array of the gradients of a block's matrices for moe_experts_backward, built once; keeps their tensors alive.  One (w1, w3, w2) per expert, all
+    float32 or all float16; None is not asked for."""
+
+    def __init__(self, grads: Sequence):
+        self.grads, dev = [tuple(g) if g is not None else (None, None, None) for g in grads], _device()
+        if not 1 <= len(self.grads) <= MAX_EXPERTS:
+            raise MoeError(MOE_ESHAPE, f"gradients of {len(self.grads)} experts, 1 to {MAX_EXPERTS} are possible")
+        self.device, self.type, self.shape, rows = dev, None, None, []
+        for i, g in enumerate(self.grads):
+            if len(g) != 3:
+                raise MoeError(MOE_EINVAL, f"expert {i}: three gradients are needed")
+            ptrs = []
+            for t, name in zip(g, ("w1", "w3", "w2")):
+                if t is None:
+                    ptrs.append(None)
+                    continue
+                shape = tuple(_rows_cols(t, f"expert {i}, {name}"))
+                as_w1 = shape[::-1] if name == "w2" else shape
+                if self.type is None:
+                    self.type, self.shape = t.dtype, as_w1
+                    _out_type(t, f"expert {i}, {name}")
+                if as_w1 != self.shape:
+                    raise MoeError(MOE_ESHAPE, f"expert {i}, {name}: {shape}")
+                ptrs.append(_need(t, f"expert {i}, {name}", (self.type,), shape, dev))
+            rows.append(CExpertGrads(*ptrs))
+        self.c = (CExpertGrads * len(rows))(*rows)
+
+
+def moe_experts_backward(layer: Layer, x, topk_gate, offsets, perm, a, u, d_out, ws, d_x=None, d_gate=None, d_w: Optional[ExpertGrads] = None,
+                         accumulate: bool = False) -> None:
+    """The gradients that are not None are written; ``d_x`` float32 or float16."""
+    dev = _device()
+    T, d, f, E, k = _rows_cols(x, "x")[0], layer.d_model, layer.d_ff, layer.n_experts, layer.top_k
+    _need_experts(layer, dev)
+    kept = (T * k, f)
+    if d_w is not None:
+        if d_w.device != dev:
+            raise MoeError(MOE_EINVAL, f"gradients on GPU {d_w.device}, the current one is {dev}")
+        if len(d_w.grads) != E or d_w.shape not in (None, (f, d)):
+            raise MoeError(MOE_ESHAPE, f"gradients of {len(d_w.grads)} experts of {d_w.shape}, {E} of {(f, d)} are needed")
+    _check(lib().moe_experts_backward(
+        layer.c, _need(x, "x", _F16, (T, d), dev), T, *_grouping(layer, T, topk_gate, offsets, perm, dev), _need(a, "a", _F16, kept, dev),
+        _need(u, "u", _F16, kept, dev), _need(d_out, "d_out", _F16, (T, d), dev),
+        None if d_x is None else _need(d_x, "d_x", _F32 + _F16, (T, d), dev), OUT_F32 if d_x is None else _out_type(d_x, "d_x"),
+        None if d_gate is None else _need(d_gate, "d_gate", _F32, (T, k), dev), None if d_w is None else d_w.c,
+        OUT_F16 if d_w is not None and d_w.type in _F16 else OUT_F32, int(accumulate),
+        None if ws is None else _need(ws, "ws", _BYTES, ws.shape, dev), 0 if ws is None else ws.numel(), _stream_on(dev)))
+
+
+class GradList:
+    """Host array of gradients for moe_clip_gradients, built once; keeps their tensors alive.  ``outs`` None: clipped in place."""
+
+    def __init__(self, grads: Sequence, outs: Optional[Sequence] = None):
+        self.grads, dev = list(grads), _device()
+        self.outs = self.grads if outs is None else list(outs)
+        if len(self.grads) > MAX_GRADS or len(self.outs) != len(self.grads):
+            raise MoeError(MOE_ESHAPE, f"{len(self.grads)} gradients, {len(self.outs)} outs: as many are needed, at most {MAX_GRADS}")
+        self.device = dev
+        self.c = (CGrad * max(1, len(self.grads)))(*[
+            CGrad(_need(g, f"gradient {i}", _F32 + _F16, g.shape, dev), _need(o, f"out {i}", _F32 + _F16, g.shape, dev), g.numel(),
+                  _out_type(g, f"gradient {i}"), _out_type(o, f"out {i}")) for i, (g, o) in enumerate(zip(self.grads, self.outs))])
+
+
+def alloc_clip_workspace(n_tensors: int):
+    import torch
+    n = int(lib().moe_clip_workspace_bytes(n_tensors))
+    if n == 0:
+        raise MoeError(MOE_ESHAPE, "moe_clip_workspace_bytes rejected the argument")
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def moe_clip_gradients(grads: GradList, max_norm: float, norm, ws, unscale: float = 1.0) -> None:
+    dev = _device()
+    if grads.device != dev:
+        raise MoeError(MOE_EINVAL, f"gradients on GPU {grads.device}, the current one is {dev}")
+    _check(lib().moe_clip_gradients(grads.c, len(grads.grads), max_norm, unscale, _need(norm, "norm", _F32, (1,), dev),
+                                    None if ws is None else _need(ws, "ws", _BYTES, ws.shape, dev), 0 if ws is None else ws.numel(), _stream_on(dev)))
 
 
 def moe_synth_fill_f16(dst, first: int, seed: int, stream_id: int, scale: float, kind: int) -> None:

@@ -1,13 +1,17 @@
 // C-ABI entry points of libmoemix (declared and documented in include/moemix.h): argument
 // checks, workspace carving, kernel sequencing.  No allocation, no synchronization except in
 // moe_read_status.
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 
+#include "clip.hpp"
 #include "common.hpp"
+#include "experts_train.hpp"
 #include "fp8.hpp"
 #include "gate_grad.hpp"
 #include "kernels.hpp"
@@ -994,6 +998,284 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
                          d_x_type == MOE_OUT_F16};
     launch_route_backward(a, w, (hipStream_t)stream);
     return check_hip((hipStream_t)stream);
+}
+
+// ---------------------------------------------------------------- training the experts
+
+namespace {
+
+constexpr int kTrainMaxPairs = 1 << 22;             // of a call: its launches have less than 2^32 threads
+constexpr long long kTrainMaxRows = 2147483647 - 2047;   // T d_model: rows of tokens are found by 32-bit offsets in bytes
+
+bool misaligned(const void* p, int to) { return (uintptr_t)p % to != 0; }
+
+bool overlap(const void* a, size_t n, const void* b, size_t m) { return (uintptr_t)a < (uintptr_t)b + m && (uintptr_t)b < (uintptr_t)a + n; }
+
+int check_train_shape(const char* who, const moe_layer* L, int T) {
+    if (!L) return fail(MOE_EINVAL, "%s: layer is NULL", who);
+    if (L->d_model < 64 || L->d_ff < 64 || L->d_model % MOE_GROUP || L->d_ff % MOE_GROUP || L->d_model > 8192 || L->d_ff > 16384)
+        return fail(MOE_ESHAPE, "%s: d_model=%d, d_ff=%d: multiples of %d up to 8192 and 16384 are needed", who, L->d_model, L->d_ff, MOE_GROUP);
+    if (L->n_experts < 1 || L->n_experts > MOE_MAX_EXPERTS || L->top_k < 1 || L->top_k > L->n_experts || L->top_k > MOE_MAX_TOPK)
+        return fail(MOE_ESHAPE, "%s: n_experts=%d, top_k=%d", who, L->n_experts, L->top_k);
+    if (T < 1) return fail(MOE_ESHAPE, "%s: T=%d < 1", who, T);
+    if ((long long)T * L->d_model > kTrainMaxRows || (long long)T * L->top_k > kTrainMaxPairs)
+        return fail(MOE_ESHAPE, "%s: T=%d, d_model=%d, top_k=%d: too many for a call", who, T, L->d_model, L->top_k);
+    return MOE_OK;
+}
+
+// Experts, grouping and workspace of a call.
+int check_train(const char* who, const moe_layer* L, int T, const float* topk_gate, const int32_t* offsets, const int32_t* perm, void* ws, size_t ws_bytes,
+                TrainWorkspace* w, TrainPlan* plan) {
+    if (int rc = check_train_shape(who, L, T)) return rc;
+    if (!L->experts) return fail(MOE_EINVAL, "%s: layer.experts is NULL", who);
+    for (int e = 0; e < L->n_experts; ++e) {
+        const moe_expert& x = L->experts[e];
+        if (x.prec != MOE_PREC_FP16) return fail(MOE_EINVAL, "%s: expert %d is not held in 16 bits", who, e);
+        if (!expert_resident(x)) return fail(MOE_ENOTRESIDENT, "%s: expert %d is not resident", who, e);
+        if (misaligned(x.w1.data, 16) || misaligned(x.w3.data, 16) || misaligned(x.w2.data, 16))
+            return fail(MOE_EINVAL, "%s: expert %d: data must be 16-byte aligned", who, e);
+    }
+    if (!offsets && L->n_experts > 1) return fail(MOE_EINVAL, "%s: offsets is NULL with %d experts", who, L->n_experts);
+    if (misaligned(offsets, 4) || misaligned(perm, 4) || misaligned(topk_gate, 4)) return fail(MOE_EINVAL, "%s: offsets, perm and topk_gate must be 4-byte aligned", who);
+    if (!ws) return fail(MOE_EWORKSPACE, "workspace is NULL");
+    if (misaligned(ws, 256)) return fail(MOE_EWORKSPACE, "workspace must be 256-byte aligned");
+    *plan = plan_train(T * L->top_k, L->d_model, L->d_ff, L->n_experts);
+    const int splits = plan->splits_down > plan->splits_dx ? plan->splits_down : plan->splits_dx;
+    *w = carve_train_workspace(ws, T, L->d_model, L->d_ff, L->n_experts, L->top_k, splits);
+    if (ws_bytes < w->bytes) return fail(MOE_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, w->bytes);
+    return MOE_OK;
+}
+
+TrainRows train_rows(const moe_layer* L, const TrainWorkspace& w, const TrainPlan& plan, int T) {
+    TrainRows a;
+    memset(&a, 0, sizeof(a));
+    a.h = w.h;
+    a.d_a = w.d_a;
+    a.d_u = w.d_u;
+    a.y = w.y;
+    a.part = w.part;
+    a.meta = w.meta;
+    a.chunks = w.chunks;
+    a.tok = w.tok;
+    a.gate = w.gate;
+    a.P = T * L->top_k;
+    a.per = plan.per;
+    a.splits = 1;
+    a.most_chunks = train_most_chunks(a.P, L->n_experts, plan.per);
+    return a;
+}
+
+}  // namespace
+
+size_t moe_experts_workspace_bytes(const moe_layer* layer, int T) {
+    if (check_train_shape("moe_experts_workspace_bytes", layer, T)) return 0;
+    const TrainPlan p = plan_train(T * layer->top_k, layer->d_model, layer->d_ff, layer->n_experts);
+    return carve_train_workspace(nullptr, T, layer->d_model, layer->d_ff, layer->n_experts, layer->top_k,
+                                 p.splits_down > p.splits_dx ? p.splits_down : p.splits_dx).bytes;
+}
+
+int moe_experts_forward(const moe_layer* layer, const void* x, int T, const float* topk_gate, const int32_t* offsets, const int32_t* perm, void* a,
+                        void* u, void* out, void* ws, size_t ws_bytes, moe_stream_t stream) {
+    const char* const who = "moe_experts_forward";
+    TrainWorkspace w;
+    TrainPlan plan;
+    if (int rc = check_train(who, layer, T, topk_gate, offsets, perm, ws, ws_bytes, &w, &plan)) return rc;
+    if (!x || !a || !u || !out) return fail(MOE_EINVAL, "%s: NULL argument", who);
+    if (misaligned(x, 16) || misaligned(a, 16) || misaligned(u, 16) || misaligned(out, 16)) return fail(MOE_EINVAL, "%s: x, a, u and out must be 16-byte aligned", who);
+    const int d = layer->d_model, f = layer->d_ff, E = layer->n_experts, k = layer->top_k;
+    const size_t kept = (size_t)T * k * f * 2, rows = (size_t)T * d * 2;
+    if (overlap(a, kept, u, kept) || overlap(a, kept, x, rows) || overlap(u, kept, x, rows) || overlap(a, kept, out, rows) || overlap(u, kept, out, rows))
+        return fail(MOE_EINVAL, "%s: a and u must not overlap each other, x or out", who);
+    hipStream_t st = (hipStream_t)stream;
+    const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
+    launch_train_group(g, w, plan.per, st);
+    TrainRows r = train_rows(layer, w, plan, T);
+    for (int e = 0; e < E; ++e) {
+        r.w[e] = (const half_t*)layer->experts[e].w1.data;
+        r.w3[e] = (const half_t*)layer->experts[e].w3.data;
+    }
+    r.in = (const half_t*)x;
+    r.a = (half_t*)a;
+    r.u = (half_t*)u;
+    r.N = f;
+    r.K = d;
+    launch_train_up(r, st);
+    for (int e = 0; e < E; ++e) r.w[e] = (const half_t*)layer->experts[e].w2.data;
+    r.in = w.h;
+    r.N = d;
+    r.K = f;
+    w.splits = r.splits = plan.splits_down;
+    launch_train_down(r, st);
+    launch_train_gather(g, w, true, d, out, true, nullptr, 0, st);
+    return check_hip(st);
+}
+
+int moe_experts_backward(const moe_layer* layer, const void* x, int T, const float* topk_gate, const int32_t* offsets, const int32_t* perm,
+                         const void* a, const void* u, const void* d_out, void* d_x, int d_x_type, float* d_gate, const moe_expert_grads* d_w,
+                         int d_w_type, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream) {
+    const char* const who = "moe_experts_backward";
+    TrainWorkspace w;
+    TrainPlan plan;
+    if (int rc = check_train(who, layer, T, topk_gate, offsets, perm, ws, ws_bytes, &w, &plan)) return rc;
+    if (!x || !a || !u || !d_out) return fail(MOE_EINVAL, "%s: NULL argument", who);
+    if (!d_x && !d_gate && !d_w) return fail(MOE_EINVAL, "%s: no gradient asked for", who);
+    if ((d_x_type != MOE_OUT_F32 && d_x_type != MOE_OUT_F16) || (d_w_type != MOE_OUT_F32 && d_w_type != MOE_OUT_F16))
+        return fail(MOE_EINVAL, "%s: d_x_type=%d, d_w_type=%d", who, d_x_type, d_w_type);
+    if (misaligned(x, 16) || misaligned(a, 16) || misaligned(u, 16) || misaligned(d_out, 16) || misaligned(d_x, 16) || misaligned(d_gate, 4))
+        return fail(MOE_EINVAL, "%s: x, a, u, d_out and d_x must be 16-byte aligned, d_gate 4-byte", who);
+    const int d = layer->d_model, f = layer->d_ff, E = layer->n_experts, k = layer->top_k;
+    TrainWeights g_w;
+    memset(&g_w, 0, sizeof(g_w));
+    bool any = false;
+    for (int e = 0; d_w && e < E; ++e) {
+        if (misaligned(d_w[e].w1, 16) || misaligned(d_w[e].w3, 16) || misaligned(d_w[e].w2, 16))
+            return fail(MOE_EINVAL, "%s: the gradients of expert %d must be 16-byte aligned", who, e);
+        g_w.w1[e] = d_w[e].w1;
+        g_w.w3[e] = d_w[e].w3;
+        g_w.w2[e] = d_w[e].w2;
+        any |= d_w[e].w1 || d_w[e].w3 || d_w[e].w2;
+    }
+    hipStream_t st = (hipStream_t)stream;
+    const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
+    launch_train_group(g, w, plan.per, st);
+    TrainRows r = train_rows(layer, w, plan, T);
+    for (int e = 0; e < E; ++e) r.w[e] = (const half_t*)layer->experts[e].w2.data;
+    r.in = (const half_t*)d_out;
+    r.a = (half_t*)a;      // (read only here)
+    r.u = (half_t*)u;
+    r.N = f;
+    r.K = d;
+    launch_train_d_hidden(r, st);
+    if (any) {
+        g_w.x = (const half_t*)x;
+        g_w.d_out = (const half_t*)d_out;
+        g_w.h = w.h;
+        g_w.d_a = w.d_a;
+        g_w.d_u = w.d_u;
+        g_w.meta = w.meta;
+        g_w.tok = w.tok;
+        g_w.d = d;
+        g_w.f = f;
+        g_w.E = E;
+        g_w.accumulate = accumulate != 0;
+        launch_train_d_weights(g_w, d_w_type == MOE_OUT_F16, st);
+    }
+    if (d_x) {
+        for (int e = 0; e < E; ++e) {
+            r.w[e] = (const half_t*)layer->experts[e].w1.data;
+            r.w3[e] = (const half_t*)layer->experts[e].w3.data;
+        }
+        r.in = w.d_a;
+        r.in2 = w.d_u;
+        r.N = d;
+        r.K = f;
+        w.splits = r.splits = plan.splits_dx;
+        launch_train_d_rows(r, st);
+    }
+    if (d_x || d_gate) launch_train_gather(g, w, false, d, d_x, d_x_type == MOE_OUT_F16, d_gate, (f + kTrainCols - 1) / kTrainCols, st);
+    return check_hip(st);
+}
+
+// ---------------------------------------------------------------- global norm and clipping
+
+namespace {
+
+int clip_launches(int n_tensors) { return (n_tensors + kClipMost - 1) / kClipMost; }
+
+struct Interval {
+    uintptr_t begin, end;
+    int tensor;
+    bool written;
+};
+
+// Does an out overlap another out, or a gradient that is not its own at the same place and of the same type?
+bool outs_overlap(const moe_grad* g, int n) {
+    Interval v[2 * MOE_MAX_GRADS];
+    int count = 0;
+    for (int i = 0; i < n; ++i) {
+        if (!g[i].n) continue;
+        const uintptr_t r = (uintptr_t)g[i].grad, w = (uintptr_t)g[i].out;
+        if (r == w && g[i].grad_type != g[i].out_type) return true;
+        v[count++] = Interval{r, r + g[i].n * (g[i].grad_type == MOE_OUT_F16 ? 2 : 4), i, false};
+        v[count++] = Interval{w, w + g[i].n * (g[i].out_type == MOE_OUT_F16 ? 2 : 4), i, true};
+    }
+    std::sort(v, v + count, [](const Interval& a, const Interval& b) { return a.begin < b.begin || (a.begin == b.begin && a.tensor < b.tensor); });
+    // the interval of each kind that reaches furthest, and of the gradients the one of another tensor that does
+    const Interval none{0, 0, -1, false};
+    Interval write = none, read = none, other = none;
+    auto meets = [](const Interval& before, const Interval& i) {
+        return before.end > i.begin && !(before.tensor == i.tensor && before.begin == i.begin && before.written != i.written);
+    };
+    for (int i = 0; i < count; ++i) {
+        if (meets(write, v[i]) || (v[i].written && (meets(read, v[i]) || meets(other, v[i])))) return true;
+        if (v[i].written) {
+            if (v[i].end > write.end) write = v[i];
+        } else if (v[i].end > read.end) {
+            other = read;
+            read = v[i];
+        } else if (v[i].end > other.end) {
+            other = v[i];
+        }
+    }
+    return false;
+}
+
+}  // namespace
+
+size_t moe_clip_workspace_bytes(int n_tensors) {
+    if (n_tensors < 0 || n_tensors > MOE_MAX_GRADS) return 0;
+    return (size_t)(n_tensors ? clip_launches(n_tensors) : 1) * kClipBlocks * sizeof(double);
+}
+
+int moe_clip_gradients(const moe_grad* grads, int n_tensors, float max_norm, float unscale, float* norm, void* ws, size_t ws_bytes, moe_stream_t stream) {
+    const char* const who = "moe_clip_gradients";
+    if (n_tensors < 0) return fail(MOE_EINVAL, "%s: negative size", who);
+    if (n_tensors > MOE_MAX_GRADS) return fail(MOE_ESHAPE, "%s: %d tensors, at most %d are possible", who, n_tensors, MOE_MAX_GRADS);
+    if ((n_tensors && !grads) || !norm) return fail(MOE_EINVAL, "%s: NULL argument", who);
+    if (misaligned(norm, 4)) return fail(MOE_EINVAL, "%s: norm must be 4-byte aligned", who);
+    if (!(max_norm >= 0.0f)) return fail(MOE_EINVAL, "%s: max_norm=%g", who, (double)max_norm);
+    if (!(unscale > 0.0f) || std::isinf(unscale)) return fail(MOE_EINVAL, "%s: unscale=%g", who, (double)unscale);
+    for (int i = 0; i < n_tensors; ++i) {
+        const moe_grad& g = grads[i];
+        if ((g.grad_type != MOE_OUT_F32 && g.grad_type != MOE_OUT_F16) || (g.out_type != MOE_OUT_F32 && g.out_type != MOE_OUT_F16))
+            return fail(MOE_EINVAL, "%s: tensor %d: grad_type=%d, out_type=%d", who, i, g.grad_type, g.out_type);
+        if (g.n >= 1ull << 40) return fail(MOE_ESHAPE, "%s: tensor %d: %zu elements", who, i, g.n);
+        if (!g.n) continue;
+        if (!g.grad || !g.out) return fail(MOE_EINVAL, "%s: tensor %d is NULL", who, i);
+        if (misaligned(g.grad, g.grad_type == MOE_OUT_F16 ? 2 : 4) || misaligned(g.out, g.out_type == MOE_OUT_F16 ? 2 : 4))
+            return fail(MOE_EINVAL, "%s: tensor %d is not aligned to its type", who, i);
+    }
+    if (outs_overlap(grads, n_tensors)) return fail(MOE_EINVAL, "%s: an out overlaps another tensor", who);
+    if (!ws) return fail(MOE_EWORKSPACE, "workspace is NULL");
+    if (misaligned(ws, 256)) return fail(MOE_EWORKSPACE, "workspace must be 256-byte aligned");
+    if (ws_bytes < moe_clip_workspace_bytes(n_tensors))
+        return fail(MOE_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, moe_clip_workspace_bytes(n_tensors));
+    hipStream_t st = (hipStream_t)stream;
+    // tables of up to kClipMost tensors, each with at most 2^31 chunks
+    auto table = [&](int first, ClipTable& t) {
+        memset(&t, 0, sizeof(t));
+        for (int i = first; i < n_tensors && i < first + kClipMost; ++i) {
+            const moe_grad& g = grads[i];
+            const int j = t.n++;
+            t.grad[j] = g.grad;
+            t.out[j] = g.out;
+            t.size[j] = (unsigned long long)g.n | (g.grad_type == MOE_OUT_F16 ? kClipGradHalf : 0) | (g.out_type == MOE_OUT_F16 ? kClipOutHalf : 0);
+            t.first[j + 1] = t.first[j] + (uint32_t)((g.n + kClipChunk - 1) / kClipChunk);
+        }
+    };
+    ClipTable t;
+    double* const part = (double*)ws;
+    int n_part = 0;
+    for (int i = 0; i < n_tensors; i += kClipMost) {
+        table(i, t);
+        launch_clip_sums(t, part + n_part, st);
+        n_part += clip_blocks(t);
+    }
+    for (int i = 0; i < n_tensors || i == 0; i += kClipMost) {
+        if (n_tensors > kClipMost || n_tensors == 0) table(i, t);
+        launch_clip_scale(t, part, n_part, max_norm, unscale, i == 0 ? norm : nullptr, st);
+    }
+    return check_hip(st);
 }
 
 int moe_synth_fill_f16(void* dst, size_t n, size_t first, uint64_t seed, uint64_t stream_id, float scale, int kind,

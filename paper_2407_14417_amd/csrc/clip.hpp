@@ -1,0 +1,28 @@
+// Global norm over many gradients, and clipping (clip.hip).
+#pragma once
+
+#include "common.hpp"
+
+namespace moemix {
+
+constexpr int kClipMost = 96;                  // tensors of one launch: their table travels as a kernel argument (2.8 KB)
+constexpr int kClipChunk = 16384;              // elements that a workgroup takes at a time
+constexpr int kClipBlocks = 2048;              // most workgroups of a launch, eight per compute unit
+
+struct ClipTable {
+    const void* grad[kClipMost];
+    void* out[kClipMost];
+    unsigned long long size[kClipMost];        // elements; bit 62: the gradient is fp16, bit 63: out is
+    uint32_t first[kClipMost + 1];             // chunks of the tensors before
+    int n;
+};
+constexpr unsigned long long kClipGradHalf = 1ull << 62, kClipOutHalf = 1ull << 63, kClipSize = kClipGradHalf - 1;
+
+inline int clip_blocks(const ClipTable& t) { return t.first[t.n] < kClipBlocks ? (int)t.first[t.n] : kClipBlocks; }
+
+// part[0 .. clip_blocks(t)) = sums of squares
+void launch_clip_sums(const ClipTable& t, double* part, hipStream_t st);
+// From n_part sums: norm (written if norm != null), and out = c * grad unless the norm is not finite.
+void launch_clip_scale(const ClipTable& t, const double* part, int n_part, float max_norm, float unscale, float* norm, hipStream_t st);
+
+}  // namespace moemix

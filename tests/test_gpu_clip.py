@@ -1,0 +1,172 @@
+"""Global norm and clipping of gradients against their definition in 64 bits."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2407_14417_amd import binding as mm
+
+pytestmark = pytest.mark.gpu
+
+
+def tensors(seed, sizes, dtype=torch.float32, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [(torch.randn(n, generator=g, device="cuda") * scale).to(dtype) for n in sizes]
+
+
+def clip(grads, outs=None, max_norm=1.0, unscale=1.0):
+    norm = torch.full((1,), -3.0, device="cuda")
+    mm.moe_clip_gradients(mm.GradList(grads, outs), max_norm, norm, mm.alloc_clip_workspace(len(grads)), unscale=unscale)
+    return norm
+
+
+def length(grads):
+    return math.sqrt(math.fsum(float(g.double().square().sum()) for g in grads))
+
+
+def check(before, after, norm, max_norm, unscale=1.0):
+    """norm: rounded once to 32 bits (and sums in 64): 2^-24 of its value, or below the normal range half the smallest step, 2^-149 / 2.  Products: the factor and the product are rounded to 32 bits each, then to the type of out, which is at
+    least half its smallest step off."""
+    want = length(before) * unscale
+    assert abs(float(norm) - want) <= (2.0 ** -24 + 1e-12) * want + 2.0 ** -150
+    c = unscale * min(1.0, max_norm / (want + 1e-6))
+    for p, q in zip(before, after):
+        if not p.numel():
+            continue
+        v = p.double() * c
+        half = q.dtype == torch.float16
+        assert float(((q.double() - v).abs() - v.abs() * (2.0 ** -23 * 1.01 + (2.0 ** -11 if half else 0)) - (2.0 ** -25 if half else 2.0 ** -149)).max()) <= 0
+
+
+SIZES = [[1], [3, 0, 255], [16384], [16385, 16383, 1], [100003, 7, 32768, 64], [5] * 50, [1 << 22, 12345]]
+
+
+@pytest.mark.parametrize("sizes", SIZES)
+@pytest.mark.parametrize("kinds", [(torch.float32, None), (torch.float16, None), (torch.float32, torch.float16), (torch.float16, torch.float32)])
+@pytest.mark.parametrize("max_norm", [0.5, 1e9])
+def test_norm_and_clipping(sizes, kinds, max_norm):
+    grads = tensors(len(sizes), sizes, kinds[0])
+    before = [g.clone() for g in grads]
+    outs = None if kinds[1] is None else [torch.full_like(g, 7.0, dtype=kinds[1]) for g in grads]
+    norm = clip(grads, outs, max_norm, 0.25)
+    check(before, grads if outs is None else outs, norm, max_norm, 0.25)
+    if outs is not None:
+        assert all(torch.equal(p, q) for p, q in zip(before, grads))
+
+
+@pytest.mark.parametrize("count", [95, 96, 97, 193, 1024])
+def test_more_tensors_than_one_launch_takes(count):
+    grads = tensors(count, [1 + i % 700 for i in range(count)])
+    for i in range(0, count, 3):
+        grads[i] = grads[i].half()
+    before = [g.clone() for g in grads]
+    check(before, grads, clip(grads, max_norm=0.1), 0.1)
+
+
+def test_within_the_limit_nothing_is_written():
+    grads = tensors(1, [1000, 33])
+    before = [g.clone() for g in grads]
+    norm = clip(grads, max_norm=float("inf"))
+    check(before, grads, norm, float("inf"))
+    assert all(torch.equal(p, q) for p, q in zip(before, grads))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_a_gradient_that_is_not_finite(bad, dtype):
+    grads = tensors(2, [70000, 5], dtype)
+    grads[0][69999] = bad
+    before = [g.clone() for g in grads]
+    outs = [torch.full_like(g, 7.0) for g in grads]
+    assert not math.isfinite(float(clip(grads, outs)))
+    assert all((o == 7).all() for o in outs)
+    assert not math.isfinite(float(clip(grads)))
+    assert all(torch.equal(p.nan_to_num(1), q.nan_to_num(1)) for p, q in zip(before, grads))
+
+
+@pytest.mark.parametrize("scale", [1e30, 1e-30, 3e-42])
+def test_squares_outside_the_range_of_32_bits(scale):
+    grads = tensors(3, [5000, 17], scale=scale)
+    before = [g.clone() for g in grads]
+    norm = clip(grads, max_norm=1.0)
+    check(before, grads, norm, 1.0)
+    assert float(norm) > 0
+
+
+def test_a_norm_past_32_bits_is_not_finite():
+    grads = [torch.full((100,), 3e38, device="cuda")]
+    assert float(clip(grads)) == float("inf") and (grads[0] == torch.tensor(3e38)).all()
+
+
+def test_limit_of_zero_and_zero_gradients():
+    grads = tensors(4, [100])
+    clip(grads, max_norm=0.0)
+    assert float(grads[0].abs().max()) == 0
+    norm = clip(grads, max_norm=1.0)
+    assert float(norm) == 0 and float(grads[0].abs().max()) == 0
+    assert float(clip([])) == 0
+
+
+@pytest.mark.parametrize("at", [1, 2, 3, 5])
+@pytest.mark.parametrize("kinds", [(torch.float32, torch.float32), (torch.float16, torch.float16), (torch.float16, torch.float32), (torch.float32, torch.float16)])
+def test_tensors_that_start_anywhere(at, kinds):
+    (src,) = tensors(at, [40000], kinds[0])
+    dst = torch.full((40000,), 7.0, dtype=kinds[1], device="cuda")
+    g, o = src[at: at + 33333], dst[2 * at: 2 * at + 33333]
+    check([g.clone()], [o], clip([g], [o]), 1.0)
+    assert (dst[: 2 * at] == 7).all() and (dst[2 * at + 33333:] == 7).all()
+
+
+def test_neighbours_and_overlaps():
+    """Parts of one buffer side by side are fine; what overlaps is refused, and nothing is done."""
+    (buf,) = tensors(5, [1000])
+    before = buf.clone()
+    check([before[:400], before[400:]], [buf[:400], buf[400:]], clip([buf[:400], buf[400:]]), 1.0)
+    other = torch.empty(1000, device="cuda")
+    keep = buf.clone()
+    for grads, outs in (([buf, buf], None), ([buf[:500], buf[499:]], None), ([buf[:500], buf[500:]], [buf[500:], other[:500]]), ([buf[:500]], [buf[1:501]]),
+                        ([buf[:300], buf[:200]], [other[:300], other[299:499]]), ([buf, buf[100:200], buf[300:350]], [other, buf[150:250], other[:50]])):
+        with pytest.raises(mm.MoeError) as e:
+            clip(grads, outs)
+        assert e.value.code == mm.MOE_EINVAL
+    assert torch.equal(buf, keep)
+    check([keep, keep[:500]], [other, torch.empty(500, device="cuda")][:1], clip([keep, keep[:500]], [other, torch.empty(500, device="cuda")]), 1.0)
+
+
+def test_the_same_bits_eager_and_in_graphs():
+    sizes = [50000, 3, 70001, 1 << 20]
+    grads = tensors(6, sizes)
+    outs = [torch.empty_like(g) for g in grads]
+    lists, norm, ws = mm.GradList(grads, outs), torch.empty(1, device="cuda"), mm.alloc_clip_workspace(4)
+    mm.moe_clip_gradients(lists, 2.0, norm, ws)
+    want = [norm.clone()] + [o.clone() for o in outs]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mm.moe_clip_gradients(lists, 2.0, norm, ws)
+    for turn in range(3):
+        ws.random_(0, 255)
+        norm.fill_(turn)
+        for o in outs:
+            o.fill_(turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip([norm] + outs, want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        norm.zero_()
+        mm.moe_clip_gradients(lists, 2.0, norm, ws)
+    side.synchronize()
+    assert torch.equal(norm, want[0])
+
+
+def test_more_than_2_32_elements():
+    n = (1 << 32) + 5
+    g = torch.full((n,), 0.5, dtype=torch.float16, device="cuda")
+    norm = clip([g], max_norm=1.0)
+    want = 0.5 * math.sqrt(n)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    c = torch.tensor(0.5 / (want + 1e-6), dtype=torch.float32).half()
+    assert (g == c.cuda()).all()
