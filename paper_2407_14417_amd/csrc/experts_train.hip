@@ -64,10 +64,65 @@ __device__ __forceinline__ gptr_t uniform_ptr(const void* p) {
 
 __device__ __forceinline__ float sigmoid(float a) { return 1.0f / (1.0f + __expf(-a)); }
 
+// ---- who does what when
+//
+// The 8 wavefronts of a workgroup are two groups of four, one of each per SIMD.  A step of the contraction (64 elements) takes each group two phases: it reads the
+// operands of the step from LDS into registers, then it multiplies them.  The groups are one phase apart, so that in every phase one of them feeds the matrix cores and
+// the other reads, and all meet at its end.  Group 0 brings the matrix's side into LDS while it reads, group 1 the other side:
+//   phase 2k:     group 0 reads step k and asks for B of step k + nB - 1; group 1 multiplies step k - 1
+//   phase 2k + 1: group 1 reads step k and asks for A of step k + nA - 1; group 0 multiplies step k
+// A ring of nA (nB) units holds them: the unit that is written was read last in phase 2k - 1.  What is read from phase 2k + 2 on has been waited for by who
+// brought it before the end of phase 2k + 1.
+
+// The wavefront's own transfers but the last `later` stages of RUNS each are done.
+template <int RUNS>
+__device__ __forceinline__ void wait_stages(int later) {
+    if (later <= 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RUNS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * RUNS) : "memory");
+}
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// TILE: kRunsA, kRunsB (transfers of a wavefront per stage), kStagesA, kStagesB (units of the rings, at most 4), bring() (the next stage of the wavefront's side),
+// landed(step) (after its transfers have ended, before others read them), read() (the next step), multiply().
+template <typename TILE>
+__device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
+    const int ahead = group ? TILE::kStagesA - 1 : TILE::kStagesB - 1;     // stages asked for before step k's
+    auto wait = [&](int step) {                                            // step's stage is there
+        const int later = min(ahead - 1, n - 1 - step);
+        if (group) wait_stages<TILE::kRunsA>(later);
+        else wait_stages<TILE::kRunsB>(later);
+        t.landed(step);
+    };
+    for (int k = 0; k < ahead && k < n; ++k) t.bring();
+    {
+        const int later = min(ahead, n) - 1;
+        if (group) wait_stages<TILE::kRunsA>(later);
+        else wait_stages<TILE::kRunsB>(later);
+        t.landed(0);
+    }
+    meet();
+    if (group) meet();
+    for (int k = 0; k < n; ++k) {
+        if (k + ahead < n) t.bring();
+        t.read();
+        if (group && k + 1 < n) wait(k + 1);
+        pin_schedule();
+        meet();
+        pin_schedule();
+        __builtin_amdgcn_s_setprio(1);
+        t.multiply();
+        __builtin_amdgcn_s_setprio(0);
+        pin_schedule();
+        if (!group && k + 1 < n) wait(k + 1);
+        if (!group || k + 1 < n) meet();
+    }
+}
+
 // ---- products of rows
 
-// What a workgroup of 8 wavefronts = 2 (rows) x 4 (columns) works on: a chunk of up to 32 MT rows, 256 columns from n0 on (up: 128 of each matrix), contraction
-// steps [s0, s1).
+// What a workgroup works on: a chunk of up to 32 MT rows (group g the tiles of 16 rows MT g .. MT g + MT - 1), 256 columns from n0 on (up: 128 of each matrix; wavefront
+// w of a group a quarter), contraction steps [s0, s1).
 struct RowsWork {
     int expert, begin, rows, n0, s0, s1, split;
 };
@@ -76,13 +131,17 @@ template <int FORM, int MT>
 struct RowsTile {
     static constexpr bool kColumns = FORM == kDHidden || FORM == kDRows;     // how the matrix lies
     static constexpr int kA = MT * 4096;                                    // bytes of a unit of rows
+    static constexpr int kRunsA = MT, kRunsB = 8;
+    static constexpr int kStagesA = MT > 4 ? 3 : 4, kStagesB = MT > 4 ? 2 : MT > 2 ? 3 : 4;
+    static_assert(kStagesA * kA + kStagesB * kUnit <= kLdsBytes, "LDS");
+    static constexpr int kRingB = kStagesA * kA;                            // where the matrix's ring begins
     const TrainRows& a;
     const RowsWork& c;
-    uint32_t lds0;
-    int lane, wave, wm, wn;
-    gptr_t ab, bb[2];
-    int left;                    // d_rows: steps before the second half
-    uint32_t av[(MT + 1) / 2], bv[4];
+    uint32_t lds0, put, get_a, get_b;    // LDS addresses: the ring of what the wavefront brings, where its next stage goes; the next step to read
+    int lane, group, wn;
+    gptr_t base[2];
+    uint32_t v[8];
+    int left;                            // d_rows: stages before the second half
     uint32_t ra[2], rb[kColumns ? 4 : 2];
     float4_t acc[4][MT];
     half8_t fa[2][MT], fb[2][4];
@@ -90,33 +149,31 @@ struct RowsTile {
     __device__ __forceinline__ RowsTile(const TrainRows& a_, const RowsWork& c_, uint8_t* lds) : a(a_), c(c_) {
         lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
         lane = threadIdx.x & 63;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        wm = wave >> 2;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        group = wave >> 2;
         wn = wave & 3;
         const int N = a.N, K = a.K, row_in_run = lane >> 3;
-        const int piece = ((lane & 7) ^ swizzle128(8 * (wave & 1) + row_in_run)) * 16;
+        const int piece = ((lane & 7) ^ swizzle128(8 * (wn & 1) + row_in_run)) * 16;
         const bool gathered = FORM == kUp || FORM == kDHidden;
+        // run k of the wavefront: rows: 8 rows of 64 elements, run wn + 4 k of the unit; columns: two rows of 256, run 8 wn + k
 #pragma unroll
-        for (int k = 0; k < (MT + 1) / 2; ++k) {
-            const int row = min(run_of(k) * 8 + row_in_run, c.rows - 1);     // (past the last row: the last one again)
-            av[k] = (uint32_t)(gathered ? a.tok[c.begin + row] : row) * (uint32_t)K * 2 + piece;
+        for (int k = 0; k < 8; ++k) {
+            if (group) {
+                const int row = min((wn + 4 * k) * 8 + row_in_run, c.rows - 1);     // (past the last row: the last one again)
+                v[k] = k < MT ? (uint32_t)(gathered ? a.tok[c.begin + row] : row) * (uint32_t)K * 2 + piece : 0;
+            } else if (kColumns) {
+                const int row = 16 * wn + 2 * k + (lane >> 5), p = lane & 31;
+                const int col = ((((p >> 1) ^ slab_swizzle(row)) << 1) | (p & 1)) * 8;
+                v[k] = (uint32_t)row * (uint32_t)N * 2 + (uint32_t)min(col, N - 8 - c.n0) * 2;
+            } else {
+                const int row = (wn + 4 * (FORM == kUp ? k & 3 : k)) * 8 + row_in_run;
+                v[k] = (uint32_t)min(row, N - 1 - c.n0) * (uint32_t)K * 2 + piece;
+            }
         }
         if (kColumns) {
-            // wavefront w brings rows 8 w .. 8 w + 7 of the 64, two at a time
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int row = 8 * wave + 2 * k + (lane >> 5), p = lane & 31;
-                const int col = ((((p >> 1) ^ slab_swizzle(row)) << 1) | (p & 1)) * 8;
-                bv[k] = (uint32_t)row * (uint32_t)N * 2 + (uint32_t)min(col, N - 8 - c.n0) * 2;
-            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) rb[j] = columns_at(lane, 4 * wn + j);
         } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int row = (wave + 8 * (FORM == kUp ? k & 1 : k)) * 8 + row_in_run;
-                bv[k] = (uint32_t)min(row, N - 1 - c.n0) * (uint32_t)K * 2 + piece;
-            }
             rb[0] = rows_at(lane, 0);
             rb[1] = rows_at(lane, 1);
         }
@@ -126,11 +183,11 @@ struct RowsTile {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < MT; ++i) acc[j][i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        put = group ? lds0 : lds0 + kRingB;
+        get_a = lds0;
+        get_b = lds0 + kRingB;
         seek(c.s0);
     }
-
-    // run k of the wavefront's runs of 8 rows (where there are fewer runs than wavefronts, two bring the same one)
-    __device__ __forceinline__ int run_of(int k) const { return 8 * k + ((MT & 1) && k == MT / 2 ? wave & 3 : wave); }
 
     // The next stage to bring is step s.  (d_rows: the second half of the steps is d_u's and W3's.)
     __device__ __forceinline__ void seek(int s) {
@@ -138,50 +195,54 @@ struct RowsTile {
         const int e = c.expert, half = FORM == kDRows ? a.K / kTrainStep : 0;
         const bool second = FORM == kDRows && s >= half;
         const size_t k0 = (size_t)(second ? s - half : s) * kTrainStep;
-        const half_t* const in = second ? a.in2 : a.in;
-        ab = uniform_ptr((FORM == kDown || FORM == kDRows ? in + (size_t)c.begin * K : in) + k0);
-        if (kColumns) {
-            bb[0] = uniform_ptr((second ? a.w3[e] : a.w[e]) + k0 * N + c.n0);
+        const half_t* p[2];
+        if (group) {
+            p[0] = p[1] = (second ? a.in2 : a.in) + (FORM == kDown || FORM == kDRows ? (size_t)c.begin * K : 0) + k0;
+        } else if (kColumns) {
+            p[0] = p[1] = (second ? a.w3[e] : a.w[e]) + k0 * N + c.n0;
         } else {
-            bb[0] = uniform_ptr(a.w[e] + (size_t)c.n0 * K + k0);
-            if (FORM == kUp) bb[1] = uniform_ptr(a.w3[e] + (size_t)c.n0 * K + k0);
+            p[0] = a.w[e] + (size_t)c.n0 * K + k0;
+            p[1] = (FORM == kUp ? a.w3[e] : a.w[e]) + (size_t)c.n0 * K + k0;
         }
+        base[0] = uniform_ptr(p[0]);
+        base[1] = FORM == kUp ? uniform_ptr(p[1]) : base[0];
         left = second || FORM != kDRows ? 1 << 30 : half - s;
     }
-    __device__ __forceinline__ void advance() {
+
+    __device__ __forceinline__ void bring() {
+        const uint32_t first = group ? put + wn * 1024 : put + wn * (kColumns ? 8192 : 1024);
+        const uint32_t apart = group || !kColumns ? 4096 : 1024;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < MT || !group) moemix::bring<0>(first + k * apart, base[FORM == kUp && k >= 4], v[k]);
+        if (group) put = put == lds0 + (kStagesA - 1) * kA ? lds0 : put + kA;
+        else put = put == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : put + kUnit;
         if (FORM == kDRows && --left == 0) {
             seek(a.K / kTrainStep);
             return;
         }
-        ab += kTrainStep * 2;
-        bb[0] += kColumns ? (size_t)a.N * (kTrainStep * 2) : kTrainStep * 2;
-        if (FORM == kUp) bb[1] += kTrainStep * 2;
+        const size_t step = !group && kColumns ? (size_t)a.N * (kTrainStep * 2) : kTrainStep * 2;
+        base[0] += step;
+        if (FORM == kUp) base[1] += step;
     }
+    __device__ __forceinline__ void landed(int) {}
 
-    __device__ __forceinline__ void bring_a(uint32_t at) {
-#pragma unroll
-        for (int k = 0; k < (MT + 1) / 2; ++k) bring<0>(at + run_of(k) * 1024, ab, av[k]);
-    }
-    __device__ __forceinline__ void bring_b(uint32_t at) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            bring<0>(at + (kColumns ? wave * 4 + k : wave + 8 * k) * 1024, bb[FORM == kUp && k >= 2], bv[k]);
-    }
-
-    __device__ __forceinline__ void read(uint32_t at_a, uint32_t at_b) {
+    __device__ __forceinline__ void read() {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (kColumns) fb[kk][j] = read_columns(at_b + rb[j], kk);
+                if (kColumns) fb[kk][j] = read_columns(get_b + rb[j], kk);
                 else {
                     const uint32_t row0 = FORM == kUp ? (j >> 1) * 128 + wn * 32 + (j & 1) * 16 : wn * 64 + j * 16;
-                    fb[kk][j] = read_rows(at_b + row0 * 128 + rb[kk]);
+                    fb[kk][j] = read_rows(get_b + row0 * 128 + rb[kk]);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < MT; ++i) fa[kk][i] = read_rows(at_a + (wm * MT + i) * 2048 + ra[kk]);
+            for (int i = 0; i < MT; ++i) fa[kk][i] = read_rows(get_a + (group * MT + i) * 2048 + ra[kk]);
         }
+        get_a = get_a == lds0 + (kStagesA - 1) * kA ? lds0 : get_a + kA;
+        get_b = get_b == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
     }
     __device__ __forceinline__ void multiply() {
 #pragma unroll
@@ -192,24 +253,12 @@ struct RowsTile {
                 for (int j = 0; j < 4; ++j) acc[j][i] = mfma16(fb[kk][j], fa[kk][i], acc[j][i]);
     }
 
-    __device__ __forceinline__ void run() {
-        for (int s = c.s0; s < c.s1; ++s) {
-            bring_a(lds0);
-            bring_b(lds0 + kA);
-            advance();
-            wait_and_meet<0>();
-            read(lds0, lds0 + kA);
-            multiply();
-            wait_and_meet<0>();
-        }
-    }
-
     // lane: row r16 of a tile of rows, columns 4 q .. 4 q + 3 of a tile of the matrix
     __device__ __forceinline__ void write(uint8_t* lds) {
         const int r16 = lane & 15, q = lane >> 4, N = a.N;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const int r = (wm * MT + i) * 16 + r16;
+            const int r = (group * MT + i) * 16 + r16;
             const bool there = r < c.rows;
             const size_t row = (size_t)(c.begin + (there ? r : 0));
             if (FORM == kUp) {
@@ -276,7 +325,8 @@ struct RowsTile {
 template <int FORM, int MT>
 __device__ __forceinline__ void rows_body(const TrainRows& a, const RowsWork& c, uint8_t* lds) {
     RowsTile<FORM, MT> t(a, c, lds);
-    t.run();
+    run_steps(t, c.s1 - c.s0, t.group);
+    __syncthreads();                     // (LDS is read no more)
     t.write(lds);
 }
 
@@ -330,29 +380,50 @@ struct WeightsWork {
 
 template <typename OUT>
 struct WeightsTile {
+    static constexpr int kRunsA = 8, kRunsB = 8, kStagesA = 3, kStagesB = 2;
+    static constexpr int kRingB = kStagesA * kUnit;
     const TrainWeights& a;
     const WeightsWork& c;
-    uint32_t lds0;
-    int lane, wave, wm, wn;
-    uint32_t col_m[2], col_n[2];     // by parity of the run: what the lane brings of a row, in bytes
+    uint8_t* lds;
+    uint32_t lds0, put, get_a, get_b;
+    int lane, group, wn;
+    bool gather;
+    gptr_t base;
+    uint32_t ld;                         // bytes of a row of what the wavefront brings
+    const_ints_t tok;                    // tokens of the rows that it brings next
+    uint32_t v[8];                       // run k: rows 16 wn + 2 k, + 1 of a stage; gathered: what the lane brings of a row (v[0 .. 3])
     uint32_t at_m, at_n;
     float4_t acc[4][8];
     half8_t fm[2][8], fn[2][4];
 
-    __device__ __forceinline__ WeightsTile(const TrainWeights& a_, const WeightsWork& c_, uint8_t* lds) : a(a_), c(c_) {
+    __device__ __forceinline__ WeightsTile(const TrainWeights& a_, const WeightsWork& c_, uint8_t* lds_) : a(a_), c(c_), lds(lds_) {
         lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
         lane = threadIdx.x & 63;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        wm = wave >> 2;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        group = wave >> 2;
         wn = wave & 3;
+        gather = group ? c.gather_m : c.gather_n;
+        const int width = group ? c.lm : c.ln, col0 = group ? c.m0 : c.n0;
+        ld = (uint32_t)width * 2;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int row = 8 * wave + 2 * k + (lane >> 5), p = lane & 31;
+        for (int k = 0; k < 8; ++k) {
+            const int row = 16 * wn + 2 * k + (lane >> 5), p = lane & 31;
             const int col = ((((p >> 1) ^ slab_swizzle(row)) << 1) | (p & 1)) * 8;
-            col_m[k] = (uint32_t)(c.m0 + min(col, c.lm - 8 - c.m0)) * 2;
-            col_n[k] = (uint32_t)(c.n0 + min(col, c.ln - 8 - c.n0)) * 2;
+            v[k] = (uint32_t)(col0 + min(col, width - 8 - col0)) * 2;
         }
-        at_m = columns_at(lane, 8 * wm);
+        if (gather) {                    // (the pattern of a run depends on k & 1 and k >> 2)
+            v[2] = v[4];
+            v[3] = v[5];
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += (uint32_t)(16 * wn + 2 * k + (lane >> 5)) * ld;
+        }
+        tok = (const_ints_t)(uintptr_t)uniform_ptr(a.tok + c.begin + 16 * wn);
+        base = uniform_ptr((group ? c.m : c.n) + (gather ? 0 : (size_t)c.begin * width));
+        put = group ? lds0 : lds0 + kRingB;
+        get_a = lds0;
+        get_b = lds0 + kRingB;
+        at_m = columns_at(lane, 8 * group);
         at_n = columns_at(lane, 4 * wn);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -360,39 +431,43 @@ struct WeightsTile {
             for (int i = 0; i < 8; ++i) acc[j][i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    // Rows 64 s + 8 wave .. + 7 of the expert, two at a time.  (Past its last row: other rows, cleared before they are used.)
-    __device__ __forceinline__ void bring_stage(int s, uint32_t at) {
-        const int r0 = c.begin + s * kTrainStep + 8 * wave;
-        const const_ints_t tok = (const_ints_t)(uintptr_t)(a.tok + r0);
-        const int most = c.rows - 1 - s * kTrainStep - 8 * wave;             // last row that there is, seen from r0
-        gptr_t pm = uniform_ptr(c.gather_m ? c.m : c.m + (size_t)max(min(r0, c.begin + c.rows - 1), 0) * c.lm);
-        gptr_t pn = uniform_ptr(c.gather_n ? c.n : c.n + (size_t)max(min(r0, c.begin + c.rows - 1), 0) * c.ln);
+    // (Past the last row of the expert: other rows, cleared before they are read.)
+    __device__ __forceinline__ void bring() {
+        const uint32_t first = put + wn * 8192;
+        if (gather) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int t0 = tok[2 * k], t1 = tok[2 * k + 1];
-            const uint32_t t = (uint32_t)(lane < 32 ? t0 : t1), r = (uint32_t)max(min(2 * k + (lane >> 5), most), 0);
-            bring<0>(at + (wave * 4 + k) * 1024, pm, (c.gather_m ? t : r) * (uint32_t)c.lm * 2 + col_m[k & 1]);
-            bring<0>(at + kUnit + (wave * 4 + k) * 1024, pn, (c.gather_n ? t : r) * (uint32_t)c.ln * 2 + col_n[k & 1]);
-        }
-    }
-    __device__ __forceinline__ void clear_tail(int s, uint32_t at, uint8_t* lds) {
-        const int left = c.rows - s * kTrainStep;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (8 * wave + 2 * k + (lane >> 5) >= left) {
-                const uint32_t o = at - lds0 + (wave * 4 + k) * 1024 + lane * 16;
-                *(uint4_t*)(lds + o) = uint4_t{0u, 0u, 0u, 0u};
-                *(uint4_t*)(lds + o + kUnit) = uint4_t{0u, 0u, 0u, 0u};
+            for (int k = 0; k < 8; ++k) {
+                const int t0 = tok[2 * k], t1 = tok[2 * k + 1];
+                moemix::bring<0>(first + k * 1024, base, (uint32_t)(lane < 32 ? t0 : t1) * ld + v[(k >> 2) * 2 + (k & 1)]);
             }
+            tok += kTrainStep;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) moemix::bring<0>(first + k * 1024, base, v[k]);
+            base += (size_t)ld * kTrainStep;
+        }
+        if (group) put = put == lds0 + (kStagesA - 1) * kUnit ? lds0 : put + kUnit;
+        else put = put == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : put + kUnit;
     }
-    __device__ __forceinline__ void read(uint32_t at) {
+    // Rows past the expert's last one, whatever they hold, are zeros on both sides.
+    __device__ __forceinline__ void landed(int step) {
+        const int there = c.rows - step * kTrainStep;
+        if (there >= kTrainStep) return;
+        uint8_t* const at = lds + (group ? step % kStagesA * kUnit : kRingB + step % kStagesB * kUnit) + wn * 8192 + lane * 16;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (16 * wn + 2 * k + (lane >> 5) >= there) *(uint4_t*)(at + k * 1024) = uint4_t{0u, 0u, 0u, 0u};
+    }
+    __device__ __forceinline__ void read() {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) fn[kk][j] = read_columns((at + kUnit + at_n) ^ (j << 5), kk);
+            for (int j = 0; j < 4; ++j) fn[kk][j] = read_columns((get_b + at_n) ^ (j << 5), kk);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) fm[kk][i] = read_columns((at + at_m) ^ (i << 5), kk);
+            for (int i = 0; i < 8; ++i) fm[kk][i] = read_columns((get_a + at_m) ^ (i << 5), kk);
         }
+        get_a = get_a == lds0 + (kStagesA - 1) * kUnit ? lds0 : get_a + kUnit;
+        get_b = get_b == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
     }
     __device__ __forceinline__ void multiply() {
 #pragma unroll
@@ -402,27 +477,13 @@ struct WeightsTile {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[j][i] = mfma16(fn[kk][j], fm[kk][i], acc[j][i]);
     }
-    __device__ __forceinline__ void run(uint8_t* lds) {
-        const int steps = (c.rows + kTrainStep - 1) / kTrainStep;
-        for (int s = 0; s < steps; ++s) {
-            bring_stage(s, lds0);
-            if (s == steps - 1) {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                clear_tail(s, lds0, lds);
-            }
-            wait_and_meet<0>();
-            read(lds0);
-            multiply();
-            wait_and_meet<0>();
-        }
-    }
     __device__ __forceinline__ void write() {
         typedef OUT out4_t __attribute__((ext_vector_type(4)));
         const int r16 = lane & 15, q = lane >> 4;
         OUT* const out = (OUT*)c.out;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int m = c.m0 + (wm * 8 + i) * 16 + r16;
+            const int m = c.m0 + (group * 8 + i) * 16 + r16;
             if (m >= c.lm) continue;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -470,7 +531,7 @@ __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights
     c.m0 = tm * kTrainCols;
     c.n0 = tn * kTrainCols;
     WeightsTile<OUT> w(a, c, lds);
-    w.run(lds);
+    if (c.rows) run_steps(w, (c.rows + kTrainStep - 1) / kTrainStep, w.group);
     w.write();
 }
 

@@ -25,9 +25,9 @@ struct TrainWorkspace {
     int32_t* tok;         // [P + 64]  grouped row -> token (0 for a row of no expert and past the end)
     float* gate;          // [P + 64]  grouped row -> its gate
     int32_t* inv;         // [P]       pair -> grouped row; anything for a pair in no group
-    half_t* h;            // [P, f]    hidden rows; backward: times the gate
-    half_t* d_a;          // [P, f]
-    half_t* d_u;          // [P, f]
+    half_t* h;            // [P + 64, f]  hidden rows; backward: times the gate (d_weights reads whole steps of 64 rows)
+    half_t* d_a;          // [P + 64, f]
+    half_t* d_u;          // [P + 64, f]
     float* y;             // [splits][P, d]  rows of the down-projection; backward: of d_x
     float* part;          // [ceil(f / 256)][P]  shares of d_gate
     int splits;
@@ -48,9 +48,9 @@ inline TrainWorkspace carve_train_workspace(void* base, int T, int d, int f, int
     w.tok = (int32_t*)take((P + 64) * sizeof(int32_t));
     w.gate = (float*)take((P + 64) * sizeof(float));
     w.inv = (int32_t*)take(P * sizeof(int32_t));
-    w.h = (half_t*)take(P * f * sizeof(half_t));
-    w.d_a = (half_t*)take(P * f * sizeof(half_t));
-    w.d_u = (half_t*)take(P * f * sizeof(half_t));
+    w.h = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
+    w.d_a = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
+    w.d_u = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
     w.y = (float*)take((size_t)splits * P * d * sizeof(float));
     w.part = (float*)take((size_t)((f + kTrainCols - 1) / kTrainCols) * P * sizeof(float));
     w.splits = splits;
