@@ -44,13 +44,15 @@ __device__ __forceinline__ uint32_t columns_at(int lane, int slab) {
     const int r16 = lane & 15, q = lane >> 4, row = 8 * q + (r16 >> 2);
     return row * 512 + (r16 & 3) * 8 + ((slab ^ slab_swizzle(row)) << 5);
 }
-// "Rows": 16-byte pieces of row r at piece ^ swizzle128(r).
+// "Rows": 16-byte pieces of row r at piece ^ rows_swizzle(r).  A 16-byte read serves lanes 0-3, 12-15 and 20-27 together, then 4-11, 16-19 and 28-31, and so on: of the
+// operand's 16 rows each time some of one piece and the others of its neighbour, in 16 different places of 256 bytes.
+__device__ __forceinline__ int rows_swizzle(int r) { return (r >> 1) & 7; }
 __device__ __forceinline__ half8_t read_rows(uint32_t at) {
     return *(const half8_t __attribute__((address_space(3)))*)(uintptr_t)at;
 }
 __device__ __forceinline__ uint32_t rows_at(int lane, int kk) {
     const int r16 = lane & 15, q = lane >> 4;
-    return r16 * 128 + (((4 * kk + q) ^ swizzle128(r16)) << 4);
+    return r16 * 128 + (((4 * kk + q) ^ rows_swizzle(r16)) << 4);
 }
 
 // A pointer that is the same in every lane, whatever the compiler knows about it.
@@ -153,7 +155,7 @@ struct RowsTile {
         group = wave >> 2;
         wn = wave & 3;
         const int N = a.N, K = a.K, row_in_run = lane >> 3;
-        const int piece = ((lane & 7) ^ swizzle128(8 * (wn & 1) + row_in_run)) * 16;
+        const int piece = ((lane & 7) ^ rows_swizzle(8 * (wn & 1) + row_in_run)) * 16;
         const bool gathered = FORM == kUp || FORM == kDHidden;
         // run k of the wavefront: rows: 8 rows of 64 elements, run wn + 4 k of the unit; columns: two rows of 256, run 8 wn + k
 #pragma unroll
