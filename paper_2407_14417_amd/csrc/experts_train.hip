@@ -8,6 +8,8 @@
 //
 // An operand whose contraction runs along memory ("rows") lies in LDS as rows of 64 elements, one whose contraction runs across it
 // ("columns") as 64 rows of 256 columns, and ds_read_b64_tr_b16 hands its columns to the lanes: no transposed copy of a matrix is made.
+#include <type_traits>
+
 #include "experts_train.hpp"
 #include "kernels.hpp"
 #include "mfma_common.hpp"
@@ -34,9 +36,10 @@ typedef __attribute__((address_space(3))) short4v_t* lds_short4_t;
 __device__ __forceinline__ int slab_swizzle(int r) { return (r & 3) | (((r >> 3) & 3) << 2); }
 
 // 8 consecutive contraction elements (kk: 32 kk + 8 q ..) of column r16 of a slab; at: the lane's address for it (columns_at) in the unit.
+template <int ROW = 512>   // bytes of a row
 __device__ __forceinline__ half8_t read_columns(uint32_t at, int kk) {
-    const short4v_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(uintptr_t)(at + kk * 16384));
-    const short4v_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(uintptr_t)(at + kk * 16384 + 2048));
+    const short4v_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(uintptr_t)(at + kk * 32 * ROW));
+    const short4v_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(uintptr_t)(at + kk * 32 * ROW + 4 * ROW));
     const half4_t l = __builtin_bit_cast(half4_t, lo), h = __builtin_bit_cast(half4_t, hi);
     return half8_t{l[0], l[1], l[2], l[3], h[0], h[1], h[2], h[3]};
 }
@@ -68,47 +71,54 @@ __device__ __forceinline__ float sigmoid(float a) { return 1.0f / (1.0f + __expf
 
 // ---- who does what when
 //
-// The 8 wavefronts of a workgroup are two groups of four, one of each per SIMD.  A step of the contraction (64 elements) takes each group two phases: it reads the
-// operands of the step from LDS into registers, then it multiplies them.  The groups are one phase apart, so that in every phase one of them feeds the matrix cores and
-// the other reads, and all meet at its end.  Group 0 brings the matrix's side into LDS while it reads, group 1 the other side:
-//   phase 2k:     group 0 reads step k and asks for B of step k + nB - 1; group 1 multiplies step k - 1
-//   phase 2k + 1: group 1 reads step k and asks for A of step k + nA - 1; group 0 multiplies step k
-// A ring of nA (nB) units holds them: the unit that is written was read last in phase 2k - 1.  What is read from phase 2k + 2 on has been waited for by who
-// brought it before the end of phase 2k + 1.
+// The 8 wavefronts of a workgroup are two groups of four, one of each per SIMD; group g multiplies half g of the tile's rows.  A step of the contraction (64 elements)
+// takes each group two phases: it reads the operands of the step from LDS into registers, then it multiplies them.  The groups are one phase apart, so that in
+// every phase one of them feeds the matrix cores and the other reads, and all meet at its end.  In the phase in which a group reads it also asks for 8 KB per
+// wavefront, always of a step that lies ahead, straight into LDS:
+//   phase 2k:      group 0 reads step k, asks for rows' half 1 of step k + nA - 1 and the first half of the matrix's unit of step k + nB - 1;  group 1 multiplies step k - 1
+//   phase 2k + 1:  group 1 reads step k, asks for rows' half 0 of step k + nA and the second half of the matrix's unit of step k + nB - 1;  group 0 multiplies step k
+// Each half of the rows has a ring of nA units, the matrix one of nB; what is written then was read last in the phase before, or earlier.  A transfer has three phases or more
+// to arrive (nA = 2, nB = 3, 160 KB of LDS; with two phases for the matrix's side a step took 2400 cycles in place of 2048).
+// Past the last step the last one is asked for again, so that the waits can count.
 
-// The wavefront's own transfers but the last `later` stages of RUNS each are done.
-template <int RUNS>
-__device__ __forceinline__ void wait_stages(int later) {
-    if (later <= 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(RUNS) : "memory");
-    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * RUNS) : "memory");
+// Up to COUNT of the wavefront's own transfers are under way.
+template <int COUNT>
+__device__ __forceinline__ void wait_transfers() {
+    static_assert(COUNT < 64, "six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
 }
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// TILE: kRunsA, kRunsB (transfers of a wavefront per stage), kStagesA, kStagesB (units of the rings, at most 4), bring() (the next stage of the wavefront's side),
-// landed(step) (after its transfers have ended, before others read them), read() (the next step), multiply().
+// TILE: kA, kB (units of the rings), kRuns (transfers of a wavefront for its half of the rows; for its half of the matrix's unit it is four), bring_rows(), bring_matrix() (the next
+// stage), look_up() (asks for what those will need), rows_there(step), matrix_there(step) (what the wavefront brought of a step has arrived and nobody reads it yet), read() (the next step), multiply() (which
+// looks up).
 template <typename TILE>
 __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
-    const int ahead = group ? TILE::kStagesA - 1 : TILE::kStagesB - 1;     // stages asked for before step k's
-    auto wait = [&](int step) {                                            // step's stage is there
-        const int later = min(ahead - 1, n - 1 - step);
-        if (group) wait_stages<TILE::kRunsA>(later);
-        else wait_stages<TILE::kRunsB>(later);
-        t.landed(step);
-    };
-    for (int k = 0; k < ahead && k < n; ++k) t.bring();
-    {
-        const int later = min(ahead, n) - 1;
-        if (group) wait_stages<TILE::kRunsA>(later);
-        else wait_stages<TILE::kRunsB>(later);
-        t.landed(0);
+    constexpr int kA = TILE::kA, kB = TILE::kB, kPer = TILE::kRuns + 4;
+    static_assert(kA <= kB && kB <= kA + 1, "what follows counts on it");
+    constexpr int kRowsLate = 4 + (kA - 1) * kPer, kMatrixLate = (kB - 2) * kPer;     // transfers after those of the step that is read next
+    for (int k = -kB; k < 0; ++k) {
+        if (k + kA - 1 + group >= 0) t.bring_rows();
+        if (k + kB - 1 >= 0) t.bring_matrix();
+        t.look_up();
     }
+    wait_transfers<kMatrixLate>();
+    if (group) t.rows_there(0);
+    t.matrix_there(0);
     meet();
     if (group) meet();
     for (int k = 0; k < n; ++k) {
-        if (k + ahead < n) t.bring();
+        t.bring_rows();
+        t.bring_matrix();
         t.read();
-        if (group && k + 1 < n) wait(k + 1);
+        if (group) {
+            wait_transfers<kRowsLate < kMatrixLate ? kRowsLate : kMatrixLate>();
+            t.rows_there(k + 1);
+            t.matrix_there(k + 1);
+        } else {
+            wait_transfers<kRowsLate>();
+            t.rows_there(k);
+        }
         pin_schedule();
         meet();
         pin_schedule();
@@ -116,9 +126,13 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
         t.multiply();
         __builtin_amdgcn_s_setprio(0);
         pin_schedule();
-        if (!group && k + 1 < n) wait(k + 1);
+        if (!group) {
+            wait_transfers<kMatrixLate>();
+            t.matrix_there(k + 1);
+        }
         if (!group || k + 1 < n) meet();
     }
+    wait_transfers<0>();
 }
 
 // ---- products of rows
@@ -132,18 +146,18 @@ struct RowsWork {
 template <int FORM, int MT>
 struct RowsTile {
     static constexpr bool kColumns = FORM == kDHidden || FORM == kDRows;     // how the matrix lies
-    static constexpr int kA = MT * 4096;                                    // bytes of a unit of rows
-    static constexpr int kRunsA = MT, kRunsB = 8;
-    static constexpr int kStagesA = MT > 4 ? 3 : 4, kStagesB = MT > 4 ? 2 : MT > 2 ? 3 : 4;
-    static_assert(kStagesA * kA + kStagesB * kUnit <= kLdsBytes, "LDS");
-    static constexpr int kRingB = kStagesA * kA;                            // where the matrix's ring begins
+    static constexpr int kA = MT > 4 ? 2 : MT > 2 ? 3 : 4, kB = MT > 2 ? 3 : 4;
+    static constexpr int kHalf = MT * 2048;                                 // bytes of a unit of half of the rows
+    static constexpr int kRuns = MT > 1 ? MT / 2 : 1;                       // (one tile: two wavefronts bring the same run)
+    static constexpr int kRingB = 2 * kA * kHalf;                           // where the matrix's ring begins
+    static_assert(kRingB + kB * kUnit <= kLdsBytes, "LDS");
     const TrainRows& a;
     const RowsWork& c;
-    uint32_t lds0, put, get_a, get_b;    // LDS addresses: the ring of what the wavefront brings, where its next stage goes; the next step to read
+    uint32_t lds0, put_a, put_b, get_a, get_b;      // LDS addresses: units that are filled next, units that are read next
     int lane, group, wn;
-    gptr_t base[2];
-    uint32_t v[8];
-    int left;                            // d_rows: stages before the second half
+    gptr_t base_a, base_b;
+    uint32_t va[kRuns], vb[4];
+    int left_a, left_b;                             // steps to bring after the next one
     uint32_t ra[2], rb[kColumns ? 4 : 2];
     float4_t acc[4][MT];
     half8_t fa[2][MT], fb[2][4];
@@ -157,19 +171,22 @@ struct RowsTile {
         const int N = a.N, K = a.K, row_in_run = lane >> 3;
         const int piece = ((lane & 7) ^ rows_swizzle(8 * (wn & 1) + row_in_run)) * 16;
         const bool gathered = FORM == kUp || FORM == kDHidden;
-        // run k of the wavefront: rows: 8 rows of 64 elements, run wn + 4 k of the unit; columns: two rows of 256, run 8 wn + k
+        // half 1 - group of the rows, runs wn, wn + 4 .. of 8 rows
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (group) {
-                const int row = min((wn + 4 * k) * 8 + row_in_run, c.rows - 1);     // (past the last row: the last one again)
-                v[k] = k < MT ? (uint32_t)(gathered ? a.tok[c.begin + row] : row) * (uint32_t)K * 2 + piece : 0;
-            } else if (kColumns) {
-                const int row = 16 * wn + 2 * k + (lane >> 5), p = lane & 31;
+        for (int k = 0; k < kRuns; ++k) {
+            const int row = min((1 - group) * 16 * MT + run_of(k) * 8 + row_in_run, c.rows - 1);     // (past the last row: the last one again)
+            va[k] = (uint32_t)(gathered ? a.tok[c.begin + row] : row) * (uint32_t)K * 2 + piece;
+        }
+        // half `group` of the matrix's unit: 128 rows of 64 elements (up: of W1, of W3), or 32 rows of 256, runs of two
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (kColumns) {
+                const int row = 32 * group + 8 * wn + 2 * k + (lane >> 5), p = lane & 31;
                 const int col = ((((p >> 1) ^ slab_swizzle(row)) << 1) | (p & 1)) * 8;
-                v[k] = (uint32_t)row * (uint32_t)N * 2 + (uint32_t)min(col, N - 8 - c.n0) * 2;
+                vb[k] = (uint32_t)row * (uint32_t)N * 2 + (uint32_t)min(col, N - 8 - c.n0) * 2;
             } else {
-                const int row = (wn + 4 * (FORM == kUp ? k & 3 : k)) * 8 + row_in_run;
-                v[k] = (uint32_t)min(row, N - 1 - c.n0) * (uint32_t)K * 2 + piece;
+                const int row = (FORM == kUp ? 0 : 128 * group) + (wn + 4 * k) * 8 + row_in_run;
+                vb[k] = (uint32_t)min(row, N - 1 - c.n0) * (uint32_t)K * 2 + piece;
             }
         }
         if (kColumns) {
@@ -185,49 +202,54 @@ struct RowsTile {
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < MT; ++i) acc[j][i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        put = group ? lds0 : lds0 + kRingB;
-        get_a = lds0;
-        get_b = lds0 + kRingB;
-        seek(c.s0);
+        put_a = lds0 + (1 - group) * kA * kHalf;
+        get_a = lds0 + group * kA * kHalf;
+        put_b = get_b = lds0 + kRingB;
+        left_a = left_b = c.s1 - c.s0 - 1;
+        seek_rows(c.s0);
+        seek_matrix(c.s0);
     }
 
-    // The next stage to bring is step s.  (d_rows: the second half of the steps is d_u's and W3's.)
-    __device__ __forceinline__ void seek(int s) {
-        const size_t N = a.N, K = a.K;
-        const int e = c.expert, half = FORM == kDRows ? a.K / kTrainStep : 0;
-        const bool second = FORM == kDRows && s >= half;
-        const size_t k0 = (size_t)(second ? s - half : s) * kTrainStep;
-        const half_t* p[2];
-        if (group) {
-            p[0] = p[1] = (second ? a.in2 : a.in) + (FORM == kDown || FORM == kDRows ? (size_t)c.begin * K : 0) + k0;
-        } else if (kColumns) {
-            p[0] = p[1] = (second ? a.w3[e] : a.w[e]) + k0 * N + c.n0;
-        } else {
-            p[0] = a.w[e] + (size_t)c.n0 * K + k0;
-            p[1] = (FORM == kUp ? a.w3[e] : a.w[e]) + (size_t)c.n0 * K + k0;
-        }
-        base[0] = uniform_ptr(p[0]);
-        base[1] = FORM == kUp ? uniform_ptr(p[1]) : base[0];
-        left = second || FORM != kDRows ? 1 << 30 : half - s;
+    __device__ __forceinline__ int run_of(int k) const { return MT == 1 ? wn & 1 : wn + 4 * k; }
+    // d_rows: the second half of the steps is d_u's and W3's.
+    __device__ __forceinline__ int steps_of_one() const { return a.K / kTrainStep; }
+
+    // The next step to bring is s.
+    __device__ __forceinline__ void seek_rows(int s) {
+        const bool second = FORM == kDRows && s >= steps_of_one();
+        const size_t k0 = (size_t)(second ? s - steps_of_one() : s) * kTrainStep;
+        base_a = uniform_ptr((second ? a.in2 : a.in) + (FORM == kDown || FORM == kDRows ? (size_t)c.begin * a.K : 0) + k0);
+    }
+    __device__ __forceinline__ void seek_matrix(int s) {
+        const bool second = FORM == kDRows ? s >= steps_of_one() : FORM == kUp && group;
+        const size_t k0 = (size_t)(FORM == kDRows && second ? s - steps_of_one() : s) * kTrainStep;
+        const half_t* const w = second ? a.w3[c.expert] : a.w[c.expert];
+        base_b = uniform_ptr(kColumns ? w + k0 * a.N + c.n0 : w + (size_t)c.n0 * a.K + k0);
     }
 
-    __device__ __forceinline__ void bring() {
-        const uint32_t first = group ? put + wn * 1024 : put + wn * (kColumns ? 8192 : 1024);
-        const uint32_t apart = group || !kColumns ? 4096 : 1024;
+    __device__ __forceinline__ void bring_rows() {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < MT || !group) moemix::bring<0>(first + k * apart, base[FORM == kUp && k >= 4], v[k]);
-        if (group) put = put == lds0 + (kStagesA - 1) * kA ? lds0 : put + kA;
-        else put = put == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : put + kUnit;
-        if (FORM == kDRows && --left == 0) {
-            seek(a.K / kTrainStep);
-            return;
-        }
-        const size_t step = !group && kColumns ? (size_t)a.N * (kTrainStep * 2) : kTrainStep * 2;
-        base[0] += step;
-        if (FORM == kUp) base[1] += step;
+        for (int k = 0; k < kRuns; ++k) moemix::bring<0>(put_a + run_of(k) * 1024, base_a, va[k]);
+        const uint32_t ring = lds0 + (1 - group) * kA * kHalf;
+        put_a = put_a == ring + (kA - 1) * kHalf ? ring : put_a + kHalf;
+        if (left_a <= 0) return;
+        --left_a;
+        if (FORM == kDRows && c.s1 - 1 - left_a == steps_of_one()) seek_rows(steps_of_one());
+        else base_a += kTrainStep * 2;
     }
-    __device__ __forceinline__ void landed(int) {}
+    __device__ __forceinline__ void bring_matrix() {
+        const uint32_t first = put_b + group * (kUnit / 2) + wn * (kColumns ? 4096 : 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) moemix::bring<0>(first + k * (kColumns ? 1024 : 4096), base_b, vb[k]);
+        put_b = put_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : put_b + kUnit;
+        if (left_b <= 0) return;
+        --left_b;
+        if (FORM == kDRows && c.s1 - 1 - left_b == steps_of_one()) seek_matrix(steps_of_one());
+        else base_b += kColumns ? (size_t)a.N * (kTrainStep * 2) : kTrainStep * 2;
+    }
+    __device__ __forceinline__ void look_up() {}
+    __device__ __forceinline__ void rows_there(int) {}
+    __device__ __forceinline__ void matrix_there(int) {}
 
     __device__ __forceinline__ void read() {
 #pragma unroll
@@ -241,10 +263,11 @@ struct RowsTile {
                 }
             }
 #pragma unroll
-            for (int i = 0; i < MT; ++i) fa[kk][i] = read_rows(get_a + (group * MT + i) * 2048 + ra[kk]);
+            for (int i = 0; i < MT; ++i) fa[kk][i] = read_rows(get_a + i * 2048 + ra[kk]);
         }
-        get_a = get_a == lds0 + (kStagesA - 1) * kA ? lds0 : get_a + kA;
-        get_b = get_b == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
+        const uint32_t ring = lds0 + group * kA * kHalf;
+        get_a = get_a == ring + (kA - 1) * kHalf ? ring : get_a + kHalf;
+        get_b = get_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
     }
     __device__ __forceinline__ void multiply() {
 #pragma unroll
@@ -375,28 +398,34 @@ void launch_rows(const TrainRows& a, hipStream_t st) {
 struct WeightsWork {
     int begin, rows;             // of the expert
     const half_t *m, *n;         // [., lm], [., ln]
-    bool gather_m, gather_n;
     int lm, ln, m0, n0;
     void* out;                   // [lm, ln]
 };
 
-template <typename OUT>
+// GM: the tokens' side is m (W2: d_out), else it is n (x).
+template <typename OUT, bool GM>
 struct WeightsTile {
-    static constexpr int kRunsA = 8, kRunsB = 8, kStagesA = 3, kStagesB = 2;
-    static constexpr int kRingB = kStagesA * kUnit;
+    static constexpr int kA = 2, kB = 3, kRuns = 4, kHalf = 16384;          // a half of m: 64 rows of 128 columns
+    static constexpr int kRingB = 2 * kA * kHalf;
     const TrainWeights& a;
     const WeightsWork& c;
     uint8_t* lds;
-    uint32_t lds0, put, get_a, get_b;
+    uint32_t lds0, put_a, put_b, get_a, get_b;
     int lane, group, wn;
-    bool gather;
-    gptr_t base;
-    uint32_t ld;                         // bytes of a row of what the wavefront brings
-    const_ints_t tok;                    // tokens of the rows that it brings next
-    uint32_t v[8];                       // run k: rows 16 wn + 2 k, + 1 of a stage; gathered: what the lane brings of a row (v[0 .. 3])
+    gptr_t base_a, base_b;
+    uint32_t ld_a, ld_b;                 // bytes of a row
+    const_ints_t tok;                    // tokens of the rows that are brought next of the gathered operand: 16 of m, 8 of n
+    int next[GM ? 16 : 8];               // the same, asked for a phase before they are used
+    uint32_t va[4], vb[4];               // gathered: what the lane brings of a row
+    int left_a, left_b;
     uint32_t at_m, at_n;
     float4_t acc[4][8];
     half8_t fm[2][8], fn[2][4];
+
+    // Half a unit of m: rows of 8 slabs.  One transposed read takes its 16 rows in two goes of 8.
+    __device__ __forceinline__ static int half_swizzle(int r) { return (r & 3) | (((r >> 3) & 1) << 2); }
+    __device__ __forceinline__ int row_a(int k) const { return 16 * wn + 4 * k + (lane >> 4); }
+    __device__ __forceinline__ int row_b(int k) const { return 32 * group + 8 * wn + 2 * k + (lane >> 5); }
 
     __device__ __forceinline__ WeightsTile(const TrainWeights& a_, const WeightsWork& c_, uint8_t* lds_) : a(a_), c(c_), lds(lds_) {
         lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
@@ -404,28 +433,26 @@ struct WeightsTile {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         group = wave >> 2;
         wn = wave & 3;
-        gather = group ? c.gather_m : c.gather_n;
-        const int width = group ? c.lm : c.ln, col0 = group ? c.m0 : c.n0;
-        ld = (uint32_t)width * 2;
+        ld_a = (uint32_t)c.lm * 2;
+        ld_b = (uint32_t)c.ln * 2;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int row = 16 * wn + 2 * k + (lane >> 5), p = lane & 31;
-            const int col = ((((p >> 1) ^ slab_swizzle(row)) << 1) | (p & 1)) * 8;
-            v[k] = (uint32_t)(col0 + min(col, width - 8 - col0)) * 2;
+        for (int k = 0; k < 4; ++k) {
+            const int pa = lane & 15, pb = lane & 31;
+            const int col_a = (1 - group) * 128 + ((((pa >> 1) ^ half_swizzle(row_a(k))) << 1) | (pa & 1)) * 8;
+            const int col_b = ((((pb >> 1) ^ slab_swizzle(row_b(k))) << 1) | (pb & 1)) * 8;
+            va[k] = (uint32_t)(c.m0 + min(col_a, c.lm - 8 - c.m0)) * 2 + (GM ? 0 : (uint32_t)row_a(k) * ld_a);
+            vb[k] = (uint32_t)(c.n0 + min(col_b, c.ln - 8 - c.n0)) * 2 + (!GM ? 0 : (uint32_t)row_b(k) * ld_b);
         }
-        if (gather) {                    // (the pattern of a run depends on k & 1 and k >> 2)
-            v[2] = v[4];
-            v[3] = v[5];
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += (uint32_t)(16 * wn + 2 * k + (lane >> 5)) * ld;
-        }
-        tok = (const_ints_t)(uintptr_t)uniform_ptr(a.tok + c.begin + 16 * wn);
-        base = uniform_ptr((group ? c.m : c.n) + (gather ? 0 : (size_t)c.begin * width));
-        put = group ? lds0 : lds0 + kRingB;
-        get_a = lds0;
-        get_b = lds0 + kRingB;
-        at_m = columns_at(lane, 8 * group);
+        tok = (const_ints_t)(uintptr_t)uniform_ptr(a.tok + c.begin + (GM ? 16 * wn : 32 * group + 8 * wn));
+        look_up();
+        base_a = uniform_ptr(c.m + (GM ? 0 : (size_t)c.begin * c.lm));
+        base_b = uniform_ptr(c.n + (!GM ? 0 : (size_t)c.begin * c.ln));
+        put_a = lds0 + (1 - group) * kA * kHalf;
+        get_a = lds0 + group * kA * kHalf;
+        put_b = get_b = lds0 + kRingB;
+        left_a = left_b = (c.rows + kTrainStep - 1) / kTrainStep - 1;
+        const int row = 8 * (lane >> 4) + ((lane & 15) >> 2);
+        at_m = row * 256 + (lane & 3) * 8 + (half_swizzle(row) << 5);
         at_n = columns_at(lane, 4 * wn);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -433,51 +460,98 @@ struct WeightsTile {
             for (int i = 0; i < 8; ++i) acc[j][i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    __device__ __forceinline__ void look_up() {
+#pragma unroll
+        for (int k = 0; k < (GM ? 16 : 8); ++k) next[k] = tok[k];
+    }
+    // Where a token's row begins, worked out by the scalar unit.
+    __device__ __forceinline__ uint32_t row_at(int i, uint32_t ld) const {
+        uint32_t v = (uint32_t)next[i] * ld;
+        asm volatile("" : "+s"(v));
+        return v;
+    }
     // (Past the last row of the expert: other rows, cleared before they are read.)
-    __device__ __forceinline__ void bring() {
-        const uint32_t first = put + wn * 8192;
-        if (gather) {
+    __device__ __forceinline__ void bring_rows() {
+        const uint32_t first = put_a + wn * 4096;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int t0 = tok[2 * k], t1 = tok[2 * k + 1];
-                moemix::bring<0>(first + k * 1024, base, (uint32_t)(lane < 32 ? t0 : t1) * ld + v[(k >> 2) * 2 + (k & 1)]);
+        for (int k = 0; k < 4; ++k) {
+            uint32_t v = va[k];
+            if (GM) {
+                const uint32_t r0 = row_at(4 * k, ld_a), r1 = row_at(4 * k + 1, ld_a), r2 = row_at(4 * k + 2, ld_a), r3 = row_at(4 * k + 3, ld_a);
+                const uint32_t lo = lane & 16 ? r1 : r0, hi = lane & 16 ? r3 : r2;
+                v += lane & 32 ? hi : lo;
             }
-            tok += kTrainStep;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) moemix::bring<0>(first + k * 1024, base, v[k]);
-            base += (size_t)ld * kTrainStep;
+            moemix::bring<0>(first + k * 1024, base_a, v);
         }
-        if (group) put = put == lds0 + (kStagesA - 1) * kUnit ? lds0 : put + kUnit;
-        else put = put == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : put + kUnit;
+        const uint32_t ring = lds0 + (1 - group) * kA * kHalf;
+        put_a = put_a == ring + (kA - 1) * kHalf ? ring : put_a + kHalf;
+        if (left_a <= 0) return;
+        --left_a;
+        if (GM) tok += kTrainStep;
+        else base_a += (size_t)ld_a * kTrainStep;
+    }
+    __device__ __forceinline__ void bring_matrix() {
+        const uint32_t first = put_b + group * (kUnit / 2) + wn * 4096;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t v = vb[k];
+            if (!GM) {
+                const uint32_t r0 = row_at(2 * k, ld_b), r1 = row_at(2 * k + 1, ld_b);
+                v += lane & 32 ? r1 : r0;
+            }
+            moemix::bring<0>(first + k * 1024, base_b, v);
+        }
+        put_b = put_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : put_b + kUnit;
+        if (left_b <= 0) return;
+        --left_b;
+        if (!GM) tok += kTrainStep;
+        else base_b += (size_t)ld_b * kTrainStep;
     }
     // Rows past the expert's last one, whatever they hold, are zeros on both sides.
-    __device__ __forceinline__ void landed(int step) {
+    __device__ __forceinline__ void rows_there(int step) {
         const int there = c.rows - step * kTrainStep;
-        if (there >= kTrainStep) return;
-        uint8_t* const at = lds + (group ? step % kStagesA * kUnit : kRingB + step % kStagesB * kUnit) + wn * 8192 + lane * 16;
+        if (there >= kTrainStep || there <= 0) return;
+        const int l = (int)fresh_offset(lane);      // (worked out here: hoisted, the addresses would cost registers in every step)
+        uint8_t* const at = lds + (1 - group) * kA * kHalf + step % kA * kHalf + wn * 4096 + l * 16;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (16 * wn + 2 * k + (lane >> 5) >= there) *(uint4_t*)(at + k * 1024) = uint4_t{0u, 0u, 0u, 0u};
+        for (int k = 0; k < 4; ++k)
+            if (16 * wn + 4 * k + (l >> 4) >= there) *(uint4_t*)(at + k * 1024) = uint4_t{0u, 0u, 0u, 0u};
+    }
+    __device__ __forceinline__ void matrix_there(int step) {
+        const int there = c.rows - step * kTrainStep;
+        if (there >= kTrainStep || there <= 0) return;
+        const int l = (int)fresh_offset(lane);
+        uint8_t* const at = lds + kRingB + step % kB * kUnit + group * (kUnit / 2) + wn * 4096 + l * 16;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (32 * group + 8 * wn + 2 * k + (l >> 5) >= there) *(uint4_t*)(at + k * 1024) = uint4_t{0u, 0u, 0u, 0u};
     }
     __device__ __forceinline__ void read() {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) fn[kk][j] = read_columns((get_b + at_n) ^ (j << 5), kk);
+            for (int kk = 0; kk < 2; ++kk) fn[kk][j] = read_columns<512>((get_b + at_n) ^ (j << 5), kk);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) fm[kk][i] = read_columns((get_a + at_m) ^ (i << 5), kk);
-        }
-        get_a = get_a == lds0 + (kStagesA - 1) * kUnit ? lds0 : get_a + kUnit;
-        get_b = get_b == lds0 + kRingB + (kStagesB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) fm[kk][i] = read_columns<256>((get_a + at_m) ^ (i << 5), kk);
+        const uint32_t ring = lds0 + group * kA * kHalf;
+        get_a = get_a == ring + (kA - 1) * kHalf ? ring : get_a + kHalf;
+        get_b = get_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
     }
     __device__ __forceinline__ void multiply() {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 8; ++i) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[j][i] = mfma16(fn[kk][j], fm[kk][i], acc[j][i]);
+                if (kk == 0 && i == 0) {     // (behind the first products: in front of them the wait for their operands would be one for the tokens too)
+                    pin_schedule();
+                    look_up();
+                    pin_schedule();
+                }
+            }
     }
     __device__ __forceinline__ void write() {
         typedef OUT out4_t __attribute__((ext_vector_type(4)));
@@ -526,15 +600,17 @@ __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights
     const int tn = rest / in_group, tm = group * 8 + rest - tn * in_group;
     c.m = which == 0 ? a.d_a : which == 1 ? a.d_u : a.d_out;
     c.n = which == 2 ? a.h : a.x;
-    c.gather_m = which == 2;
-    c.gather_n = which != 2;
     c.lm = which == 2 ? a.d : a.f;
     c.ln = which == 2 ? a.f : a.d;
     c.m0 = tm * kTrainCols;
     c.n0 = tn * kTrainCols;
-    WeightsTile<OUT> w(a, c, lds);
-    if (c.rows) run_steps(w, (c.rows + kTrainStep - 1) / kTrainStep, w.group);
-    w.write();
+    auto body = [&](auto gather_m) {
+        WeightsTile<OUT, decltype(gather_m)::value> w(a, c, lds);
+        if (c.rows) run_steps(w, (c.rows + kTrainStep - 1) / kTrainStep, w.group);
+        w.write();
+    };
+    if (which == 2) body(std::true_type{});
+    else body(std::false_type{});
 }
 
 template <typename OUT>
