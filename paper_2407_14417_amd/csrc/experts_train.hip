@@ -135,6 +135,22 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
     wait_transfers<0>();
 }
 
+// ---- results
+
+// A wavefront's sums: lane l of tile (j, i) holds row l & 15 of 16 i .., columns 16 j + 4 (l >> 4) .. + 3.  Written as they lie, rows would go to memory in pieces of 32 bytes (fp16), which
+// took 30 000 cycles for 128 KB of a workgroup; so they are spread out as rows of 64 columns in 20 KB of LDS that the wavefront has for itself, 64 rows at a time.
+constexpr int kRegion = kLdsBytes / 8, kSpreadRow = 272;
+
+template <int MT>
+__device__ __forceinline__ void spread(const float4_t (&acc)[4][MT], int i0, uint8_t* region, int lane) {
+#pragma unroll
+    for (int i = 0; i < (MT < 4 ? MT : 4); ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *(float4_t*)(region + (i * 16 + (lane & 15)) * kSpreadRow + (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i0 + i];
+    wave_lds_handover();
+}
+__device__ __forceinline__ float4_t spread_at(const uint8_t* region, int row, int col) { return *(const float4_t*)(region + row * kSpreadRow + col * 4); }
+
 // ---- products of rows
 
 // What a workgroup works on: a chunk of up to 32 MT rows (group g the tiles of 16 rows MT g .. MT g + MT - 1), 256 columns from n0 on (up: 128 of each matrix; wavefront
@@ -278,71 +294,130 @@ struct RowsTile {
                 for (int j = 0; j < 4; ++j) acc[j][i] = mfma16(fb[kk][j], fa[kk][i], acc[j][i]);
     }
 
-    // lane: row r16 of a tile of rows, columns 4 q .. 4 q + 3 of a tile of the matrix
     __device__ __forceinline__ void write(uint8_t* lds) {
-        const int r16 = lane & 15, q = lane >> 4, N = a.N;
+        if (FORM == kUp) write_up(lds);
+        else if (FORM == kDHidden) write_d_hidden(lds);
+        else write_rows(lds);
+    }
+
+    // a, u and then h of the tile go through LDS, so that a row's 128 columns are written at once.
+    __device__ __forceinline__ void write_up(uint8_t* lds) {
+        constexpr int kRow = 272, kTile = 32 * MT * kRow;
+        const int r16 = lane & 15, q = lane >> 4;
+        uint8_t* const at = lds + (group * 16 * MT + r16) * kRow + (wn * 32 + 4 * q) * 2;
+        const int row0 = threadIdx.x >> 4, col = (threadIdx.x & 15) * 8;
+        const bool mine = c.n0 + col < a.N;
+        auto out = [&](half_t* to, int tile) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int r = (group * MT + i) * 16 + r16;
-            const bool there = r < c.rows;
-            const size_t row = (size_t)(c.begin + (there ? r : 0));
-            if (FORM == kUp) {
+            for (int p = 0; p < MT; ++p) {
+                const int r = row0 + 32 * p;
+                if (r < c.rows && mine) *(half8_t*)(to + (size_t)(c.begin + r) * a.N + c.n0 + col) = *(const half8_t*)(lds + tile * kTile + r * kRow + col * 2);
+            }
+        };
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int n = c.n0 + wn * 32 + j * 16 + 4 * q;
-                    if (!there || n >= N) continue;
-                    half4_t va, vu, vh;
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        va[k] = (half_t)acc[j][i][k];
-                        vu[k] = (half_t)acc[j + 2][i][k];
-                        vh[k] = (half_t)silu_mul(acc[j][i][k], acc[j + 2][i][k]);
-                    }
-                    *(half4_t*)(a.a + row * N + n) = va;
-                    *(half4_t*)(a.u + row * N + n) = vu;
-                    *(half4_t*)(a.h + row * N + n) = vh;
+            for (int j = 0; j < 2; ++j) {
+                half4_t va, vu;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    va[k] = (half_t)acc[j][i][k];
+                    vu[k] = (half_t)acc[j + 2][i][k];
                 }
-            } else if (FORM == kDHidden) {
-                const float g = a.gate[row];
-                float share = 0.0f;
+                *(half4_t*)(at + i * 16 * kRow + j * 32) = va;
+                *(half4_t*)(at + i * 16 * kRow + j * 32 + kTile) = vu;
+            }
+        __syncthreads();
+        out(a.a, 0);
+        out(a.u, 1);
+        __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int col = c.n0 + wn * 64 + j * 16 + 4 * q, n = min(col, N - 4);
-                    const bool mine = there && col < N;
-                    const half4_t va = *(const half4_t*)(a.a + row * N + n), vu = *(const half4_t*)(a.u + row * N + n);
-                    half4_t da, du, gh;
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float x = (float)va[k], y = (float)vu[k], s = sigmoid(x), z = x * s, h = z * y, v = acc[j][i][k];
-                        share = mine ? fmaf(v, h, share) : share;
+            for (int j = 0; j < 2; ++j) {
+                half4_t vh;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) vh[k] = (half_t)silu_mul(acc[j][i][k], acc[j + 2][i][k]);
+                *(half4_t*)(at + i * 16 * kRow + j * 32) = vh;
+            }
+        __syncthreads();
+        out(a.h, 0);
+    }
+
+    // A wavefront turns its sums, up to 64 rows at a time, into whole lines of rows in LDS of its own: eight columns of eight rows per instruction.
+    __device__ __forceinline__ void write_d_hidden(uint8_t* lds) {
+        uint8_t* const region = lds + (4 * group + wn) * kRegion;
+        float* const shares = (float*)(region + 64 * kSpreadRow);            // of d_gate, for the wavefront's rows
+        const int N = a.N, col = c.n0 + wn * 64 + (lane & 7) * 8;
+        const bool any = c.n0 + wn * 64 < N;                                 // (64 divides N)
+        if (!any) {
+            for (int r = lane; r < 16 * MT; r += 64) shares[r] = 0.0f;
+        } else {
+#pragma unroll
+            for (int i0 = 0; i0 < MT; i0 += 4) {
+                constexpr int kMost = MT < 4 ? MT : 4;
+                half8_t va[2 * kMost], vu[2 * kMost];
+                float gate[2 * kMost];
+                const int r0 = (group * MT + i0) * 16 + (lane >> 3);
+#pragma unroll
+                for (int p = 0; p < 2 * kMost; ++p) {
+                    const size_t row = (size_t)(c.begin + (r0 + 8 * p < c.rows ? r0 + 8 * p : 0));
+                    va[p] = *(const half8_t*)(a.a + row * N + col);
+                    vu[p] = *(const half8_t*)(a.u + row * N + col);
+                    gate[p] = a.gate[row];
+                }
+                spread<MT>(acc, i0, region, lane);
+#pragma unroll
+                for (int p = 0; p < 2 * kMost; ++p) {
+                    const float4_t lo = spread_at(region, 8 * p + (lane >> 3), (lane & 7) * 8), hi = spread_at(region, 8 * p + (lane >> 3), (lane & 7) * 8 + 4);
+                    const float g = gate[p];
+                    half8_t da, du, gh;
+                    float share = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float x = (float)va[p][k], y = (float)vu[p][k], s = sigmoid(x), z = x * s, h = z * y, v = k < 4 ? lo[k & 3] : hi[k & 3];
+                        share = fmaf(v, h, share);
                         du[k] = (half_t)(g * v * z);
                         da[k] = (half_t)(g * v * y * (s * (1.0f + x * (1.0f - s))));
                         gh[k] = (half_t)(g * h);
                     }
-                    if (mine) {
-                        *(half4_t*)(a.d_a + row * N + n) = da;
-                        *(half4_t*)(a.d_u + row * N + n) = du;
-                        *(half4_t*)(a.h + row * N + n) = gh;
+                    const int r = r0 + 8 * p;
+                    if (r < c.rows) {
+                        const size_t at = (size_t)(c.begin + r) * N + col;
+                        *(half8_t*)(a.d_a + at) = da;
+                        *(half8_t*)(a.d_u + at) = du;
+                        *(half8_t*)(a.h + at) = gh;
                     }
-                }
-                share += __shfl_xor(share, 16, kWave);
-                share += __shfl_xor(share, 32, kWave);
-                if (q == 0) ((float*)lds)[wn * kTrainRows + r] = share;
-            } else {
-                float* const y = a.y + (size_t)c.split * a.P * N + row * N;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int n = c.n0 + wn * 64 + j * 16 + 4 * q;
-                    if (there && n < N) *(float4_t*)(y + n) = acc[j][i];
+                    for (int m = 1; m < 8; m <<= 1) share += __shfl_xor(share, m, kWave);
+                    if ((lane & 7) == 0) shares[i0 * 16 + 8 * p + (lane >> 3)] = share;
                 }
+                wave_lds_handover();
             }
         }
-        if (FORM == kDHidden) {
-            __syncthreads();
-            const float* const s = (const float*)lds;
-            for (int r = threadIdx.x; r < c.rows; r += kThreads)
-                a.part[(size_t)(c.n0 / kTrainCols) * a.P + c.begin + r] =
-                    (s[r] + s[kTrainRows + r]) + (s[2 * kTrainRows + r] + s[3 * kTrainRows + r]);
+        __syncthreads();
+        const int r = threadIdx.x;
+        if (r < c.rows) {
+            const int half = r / (16 * MT);
+            const float* const s = (const float*)(lds + 4 * half * kRegion + 64 * kSpreadRow) + r % (16 * MT);
+            constexpr int kNext = kRegion / 4;
+            a.part[(size_t)(c.n0 / kTrainCols) * a.P + c.begin + r] = (s[0] + s[kNext]) + (s[2 * kNext] + s[3 * kNext]);
+        }
+    }
+
+    __device__ __forceinline__ void write_rows(uint8_t* lds) {
+        if (c.n0 + wn * 64 >= a.N) return;
+        uint8_t* const region = lds + (4 * group + wn) * kRegion;
+        float* const y = a.y + (size_t)c.split * a.P * a.N + c.n0 + wn * 64 + (lane & 15) * 4;
+#pragma unroll
+        for (int i0 = 0; i0 < MT; i0 += 4) {
+            spread<MT>(acc, i0, region, lane);
+#pragma unroll
+            for (int p = 0; p < 4 * (MT < 4 ? MT : 4); ++p) {
+                const int r = (group * MT + i0) * 16 + 4 * p + (lane >> 4);
+                if (r < c.rows) *(float4_t*)(y + (size_t)(c.begin + r) * a.N) = spread_at(region, 4 * p + (lane >> 4), (lane & 15) * 4);
+            }
+            wave_lds_handover();
         }
     }
 };
@@ -554,29 +629,35 @@ struct WeightsTile {
             }
     }
     __device__ __forceinline__ void write() {
-        typedef OUT out4_t __attribute__((ext_vector_type(4)));
-        const int r16 = lane & 15, q = lane >> 4;
-        OUT* const out = (OUT*)c.out;
+        constexpr int W = 16 / sizeof(OUT), kLanes = 64 / W, kRows = 64 / kLanes;     // columns of a lane, lanes of a row, rows per instruction
+        typedef OUT wide_t __attribute__((ext_vector_type(W)));
+        if (c.n0 + wn * 64 >= c.ln) return;
+        uint8_t* const region = lds + (4 * group + wn) * kRegion;
+        const int row0 = lane / kLanes, col = lane % kLanes * W;
+        OUT* const out = (OUT*)c.out + c.n0 + wn * 64 + col;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int m = c.m0 + (group * 8 + i) * 16 + r16;
-            if (m >= c.lm) continue;
+        for (int i0 = 0; i0 < 8; i0 += 4) {
+            const int m0 = c.m0 + (group * 8 + i0) * 16 + row0;
+            wide_t before[64 / kRows];
+            if (a.accumulate)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = c.n0 + wn * 64 + j * 16 + 4 * q;
-                if (n >= c.ln) continue;
-                out4_t* const o = (out4_t*)(out + (size_t)m * c.ln + n);
-                float4_t v = acc[j][i];
-                if (a.accumulate) {
-                    const out4_t before = *o;
+                for (int p = 0; p < 64 / kRows; ++p) before[p] = *(const wide_t*)(out + (size_t)min(m0 + p * kRows, c.lm - 1) * c.ln);
+            spread<8>(acc, i0, region, lane);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] += (float)before[k];
+            for (int p = 0; p < 64 / kRows; ++p) {
+                wide_t w;
+#pragma unroll
+                for (int k = 0; k < W; k += 4) {
+                    float4_t v = spread_at(region, p * kRows + row0, col + k);
+                    if (a.accumulate)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] += (float)before[p][k + i];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[k + i] = (OUT)v[i];
                 }
-                out4_t w;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = (OUT)v[k];
-                *o = w;
+                if (m0 + p * kRows < c.lm) *(wide_t*)(out + (size_t)(m0 + p * kRows) * c.ln) = w;
             }
+            wave_lds_handover();
         }
     }
 };
@@ -607,6 +688,7 @@ __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights
     auto body = [&](auto gather_m) {
         WeightsTile<OUT, decltype(gather_m)::value> w(a, c, lds);
         if (c.rows) run_steps(w, (c.rows + kTrainStep - 1) / kTrainStep, w.group);
+        __syncthreads();                 // (LDS is read no more)
         w.write();
     };
     if (which == 2) body(std::true_type{});
