@@ -21,6 +21,13 @@ namespace {
 constexpr int kLdsBytes = 163840;        // of a compute unit
 constexpr int kUnit = 32768;             // 256 rows of 64 elements, or 64 rows of 256
 constexpr int kThreads = 512;
+#ifndef KS
+#define KS 8
+#endif
+#ifndef KR
+#define KR 8
+#endif
+constexpr int kSide = KS, kSideR = KR;
 
 enum Form { kUp, kDown, kDHidden, kDRows };
 
@@ -89,17 +96,25 @@ __device__ __forceinline__ void wait_transfers() {
 }
 __device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// TILE: kA, kB (units of the rings), kRuns (transfers of a wavefront for its half of the rows; for its half of the matrix's unit it is four), bring_rows(), bring_matrix() (the next
-// stage), look_up() (asks for what those will need), rows_there(step), matrix_there(step) (what the wavefront brought of a step has arrived and nobody reads it yet), read() (the next step), multiply() (which
-// looks up).
+// TILE: kA, kB (units of the rings), kRuns (transfers of a wavefront for its half of the rows; for its half of the matrix's unit it is four), kReads (operands of a step), bring_rows(k),
+// bring_matrix(k) (transfer k of the next stage), rows_asked(), matrix_asked() (all of a stage's have been made), look_up() (asks for what the next ones need), rows_there(step),
+// matrix_there(step) (what the wavefront brought of a step has arrived and nobody reads it yet), read(r) (operand r of the next step), step_read(), multiply() (which looks up).
 template <typename TILE>
 __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
     constexpr int kA = TILE::kA, kB = TILE::kB, kPer = TILE::kRuns + 4;
     static_assert(kA <= kB && kB <= kA + 1, "what follows counts on it");
     constexpr int kRowsLate = 4 + (kA - 1) * kPer, kMatrixLate = (kB - 2) * kPer;     // transfers after those of the step that is read next
     for (int k = -kB; k < 0; ++k) {
-        if (k + kA - 1 + group >= 0) t.bring_rows();
-        if (k + kB - 1 >= 0) t.bring_matrix();
+        if (k + kA - 1 + group >= 0) {
+#pragma unroll
+            for (int i = 0; i < TILE::kRuns; ++i) t.bring_rows(i);
+            t.rows_asked();
+        }
+        if (k + kB - 1 >= 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.bring_matrix(i);
+            t.matrix_asked();
+        }
         t.look_up();
     }
     wait_transfers<kMatrixLate>();
@@ -108,9 +123,18 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
     meet();
     if (group) meet();
     for (int k = 0; k < n; ++k) {
-        t.bring_rows();
-        t.bring_matrix();
-        t.read();
+        // Transfers and reads by turns: a transfer waits for its place in the compute unit's address path, 64 bytes per cycle for all wavefronts, and LDS delivers meanwhile.
+        // (One after the other 450 + 550 cycles, more than the other group's products take.)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (i < TILE::kRuns) t.bring_rows(i);
+            else t.bring_matrix(i - TILE::kRuns);
+#pragma unroll
+            for (int r = i * TILE::kReads / kPer; r < (i + 1) * TILE::kReads / kPer; ++r) t.read(r);
+        }
+        t.rows_asked();
+        t.matrix_asked();
+        t.step_read();
         if (group) {
             wait_transfers<kRowsLate < kMatrixLate ? kRowsLate : kMatrixLate>();
             t.rows_there(k + 1);
@@ -243,9 +267,8 @@ struct RowsTile {
         base_b = uniform_ptr(kColumns ? w + k0 * a.N + c.n0 : w + (size_t)c.n0 * a.K + k0);
     }
 
-    __device__ __forceinline__ void bring_rows() {
-#pragma unroll
-        for (int k = 0; k < kRuns; ++k) moemix::bring<0>(put_a + run_of(k) * 1024, base_a, va[k]);
+    __device__ __forceinline__ void bring_rows(int k) { moemix::bring<0>(put_a + run_of(k) * 1024, base_a, va[k]); }
+    __device__ __forceinline__ void rows_asked() {
         const uint32_t ring = lds0 + (1 - group) * kA * kHalf;
         put_a = put_a == ring + (kA - 1) * kHalf ? ring : put_a + kHalf;
         if (left_a <= 0) return;
@@ -253,10 +276,10 @@ struct RowsTile {
         if (FORM == kDRows && c.s1 - 1 - left_a == steps_of_one()) seek_rows(steps_of_one());
         else base_a += kTrainStep * 2;
     }
-    __device__ __forceinline__ void bring_matrix() {
-        const uint32_t first = put_b + group * (kUnit / 2) + wn * (kColumns ? 4096 : 1024);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) moemix::bring<0>(first + k * (kColumns ? 1024 : 4096), base_b, vb[k]);
+    __device__ __forceinline__ void bring_matrix(int k) {
+        moemix::bring<0>(put_b + group * (kUnit / 2) + wn * (kColumns ? 4096 : 1024) + k * (kColumns ? 1024 : 4096), base_b, vb[k]);
+    }
+    __device__ __forceinline__ void matrix_asked() {
         put_b = put_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : put_b + kUnit;
         if (left_b <= 0) return;
         --left_b;
@@ -267,20 +290,18 @@ struct RowsTile {
     __device__ __forceinline__ void rows_there(int) {}
     __device__ __forceinline__ void matrix_there(int) {}
 
-    __device__ __forceinline__ void read() {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (kColumns) fb[kk][j] = read_columns(get_b + rb[j], kk);
-                else {
-                    const uint32_t row0 = FORM == kUp ? (j >> 1) * 128 + wn * 32 + (j & 1) * 16 : wn * 64 + j * 16;
-                    fb[kk][j] = read_rows(get_b + row0 * 128 + rb[kk]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) fa[kk][i] = read_rows(get_a + i * 2048 + ra[kk]);
+    static constexpr int kReads = 2 * (4 + MT);
+    __device__ __forceinline__ void read(int r) {
+        if (r < 8) {
+            const int kk = r & 1, j = r >> 1;
+            if (kColumns) fb[kk][j] = read_columns(get_b + rb[j], kk);
+            else fb[kk][j] = read_rows(get_b + (FORM == kUp ? (j >> 1) * 128 + wn * 32 + (j & 1) * 16 : wn * 64 + j * 16) * 128 + rb[kk]);
+        } else {
+            const int kk = r & 1, i = (r - 8) >> 1;
+            fa[kk][i] = read_rows(get_a + i * 2048 + ra[kk]);
         }
+    }
+    __device__ __forceinline__ void step_read() {
         const uint32_t ring = lds0 + group * kA * kHalf;
         get_a = get_a == ring + (kA - 1) * kHalf ? ring : get_a + kHalf;
         get_b = get_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
@@ -441,9 +462,9 @@ __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, in
     RowsWork c;
     c.split = __builtin_amdgcn_readfirstlane(t0 / units);
     const int t = t0 - c.split * units;
-    const int group = t / (8 * n_tiles), rest = t - group * 8 * n_tiles, in_group = min(8, n_chunks - group * 8);
+    const int group = t / (kSideR * n_tiles), rest = t - group * kSideR * n_tiles, in_group = min(kSideR, n_chunks - group * kSideR);
     const int tile = __builtin_amdgcn_readfirstlane(rest / in_group);
-    const TrainChunk ch = a.chunks[group * 8 + rest - tile * in_group];
+    const TrainChunk ch = a.chunks[group * kSideR + rest - tile * in_group];
     c.expert = __builtin_amdgcn_readfirstlane(ch.expert);
     c.begin = __builtin_amdgcn_readfirstlane(ch.begin);
     c.rows = __builtin_amdgcn_readfirstlane(ch.rows);
@@ -546,18 +567,16 @@ struct WeightsTile {
         return v;
     }
     // (Past the last row of the expert: other rows, cleared before they are read.)
-    __device__ __forceinline__ void bring_rows() {
-        const uint32_t first = put_a + wn * 4096;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t v = va[k];
-            if (GM) {
-                const uint32_t r0 = row_at(4 * k, ld_a), r1 = row_at(4 * k + 1, ld_a), r2 = row_at(4 * k + 2, ld_a), r3 = row_at(4 * k + 3, ld_a);
-                const uint32_t lo = lane & 16 ? r1 : r0, hi = lane & 16 ? r3 : r2;
-                v += lane & 32 ? hi : lo;
-            }
-            moemix::bring<0>(first + k * 1024, base_a, v);
+    __device__ __forceinline__ void bring_rows(int k) {
+        uint32_t v = va[k];
+        if (GM) {
+            const uint32_t r0 = row_at(4 * k, ld_a), r1 = row_at(4 * k + 1, ld_a), r2 = row_at(4 * k + 2, ld_a), r3 = row_at(4 * k + 3, ld_a);
+            const uint32_t lo = lane & 16 ? r1 : r0, hi = lane & 16 ? r3 : r2;
+            v += lane & 32 ? hi : lo;
         }
+        moemix::bring<0>(put_a + wn * 4096 + k * 1024, base_a, v);
+    }
+    __device__ __forceinline__ void rows_asked() {
         const uint32_t ring = lds0 + (1 - group) * kA * kHalf;
         put_a = put_a == ring + (kA - 1) * kHalf ? ring : put_a + kHalf;
         if (left_a <= 0) return;
@@ -565,17 +584,15 @@ struct WeightsTile {
         if (GM) tok += kTrainStep;
         else base_a += (size_t)ld_a * kTrainStep;
     }
-    __device__ __forceinline__ void bring_matrix() {
-        const uint32_t first = put_b + group * (kUnit / 2) + wn * 4096;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            uint32_t v = vb[k];
-            if (!GM) {
-                const uint32_t r0 = row_at(2 * k, ld_b), r1 = row_at(2 * k + 1, ld_b);
-                v += lane & 32 ? r1 : r0;
-            }
-            moemix::bring<0>(first + k * 1024, base_b, v);
+    __device__ __forceinline__ void bring_matrix(int k) {
+        uint32_t v = vb[k];
+        if (!GM) {
+            const uint32_t r0 = row_at(2 * k, ld_b), r1 = row_at(2 * k + 1, ld_b);
+            v += lane & 32 ? r1 : r0;
         }
+        moemix::bring<0>(put_b + group * (kUnit / 2) + wn * 4096 + k * 1024, base_b, v);
+    }
+    __device__ __forceinline__ void matrix_asked() {
         put_b = put_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : put_b + kUnit;
         if (left_b <= 0) return;
         --left_b;
@@ -601,15 +618,12 @@ struct WeightsTile {
         for (int k = 0; k < 4; ++k)
             if (32 * group + 8 * wn + 2 * k + (l >> 5) >= there) *(uint4_t*)(at + k * 1024) = uint4_t{0u, 0u, 0u, 0u};
     }
-    __device__ __forceinline__ void read() {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) fn[kk][j] = read_columns<512>((get_b + at_n) ^ (j << 5), kk);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) fm[kk][i] = read_columns<256>((get_a + at_m) ^ (i << 5), kk);
+    static constexpr int kReads = 24;
+    __device__ __forceinline__ void read(int r) {
+        if (r < 8) fn[r & 1][r >> 1] = read_columns<512>((get_b + at_n) ^ ((r >> 1) << 5), r & 1);
+        else fm[r & 1][(r - 8) >> 1] = read_columns<256>((get_a + at_m) ^ (((r - 8) >> 1) << 5), r & 1);
+    }
+    __device__ __forceinline__ void step_read() {
         const uint32_t ring = lds0 + group * kA * kHalf;
         get_a = get_a == ring + (kA - 1) * kHalf ? ring : get_a + kHalf;
         get_b = get_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : get_b + kUnit;
@@ -677,8 +691,8 @@ __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights
     if (c.rows == 0 && a.accumulate) return;
     // eight tiles of m side by side
     const int tiles_m = which == 2 ? tiles_d : tiles_f, tiles_n = which == 2 ? tiles_f : tiles_d;
-    const int group = t / (8 * tiles_n), rest = t - group * 8 * tiles_n, in_group = min(8, tiles_m - group * 8);
-    const int tn = rest / in_group, tm = group * 8 + rest - tn * in_group;
+    const int group = t / (kSide * tiles_n), rest = t - group * kSide * tiles_n, in_group = min(kSide, tiles_m - group * kSide);
+    const int tn = rest / in_group, tm = group * kSide + rest - tn * in_group;
     c.m = which == 0 ? a.d_a : which == 1 ? a.d_u : a.d_out;
     c.n = which == 2 ? a.h : a.x;
     c.lm = which == 2 ? a.d : a.f;
