@@ -360,8 +360,8 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
  * device, all fp32 or all fp16 (d_w_type), of the matrices' shapes, a NULL entry is not asked for.  Each of d_x, d_gate and d_w may be NULL, not all.  accumulate != 0:
  * the gradients of the matrices are added to what is there (and an expert without rows leaves its as they are).  The same inputs give the same bits.
  * Tensors start on 16-byte boundaries (d_gate, topk_gate, offsets and perm: 4).  layer->w_gate and gate_bias are not looked at.
- * T >= 1, T * d_model <= 2^31 - 2048, T * top_k <= 2^22 (MOE_ESHAPE otherwise).  ws: at least moe_experts_workspace_bytes(layer, T); it carries nothing from one
- * call to the next.  Neither call sets a status that moe_read_status reads.
+ * T >= 1, T * d_model <= 2^31 - 2048, T * top_k <= 2^22 (MOE_ESHAPE otherwise).  ws: moe_experts_workspace_bytes(layer, T) bytes, or what these were for more tokens (a
+ * workspace that holds the call without partial results is enough; sums are then added in another order); it carries nothing from one call to the next.  Neither call sets a status that moe_read_status reads.
  */
 typedef struct {
     void *w1, *w3, *w2;

@@ -1025,7 +1025,7 @@ int check_train_shape(const char* who, const moe_layer* L, int T) {
 
 // Experts, grouping and workspace of a call.
 int check_train(const char* who, const moe_layer* L, int T, const float* topk_gate, const int32_t* offsets, const int32_t* perm, void* ws, size_t ws_bytes,
-                TrainWorkspace* w, TrainPlan* plan) {
+                TrainWorkspace* w) {
     if (int rc = check_train_shape(who, L, T)) return rc;
     if (!L->experts) return fail(MOE_EINVAL, "%s: layer.experts is NULL", who);
     for (int e = 0; e < L->n_experts; ++e) {
@@ -1039,14 +1039,14 @@ int check_train(const char* who, const moe_layer* L, int T, const float* topk_ga
     if (misaligned(offsets, 4) || misaligned(perm, 4) || misaligned(topk_gate, 4)) return fail(MOE_EINVAL, "%s: offsets, perm and topk_gate must be 4-byte aligned", who);
     if (!ws) return fail(MOE_EWORKSPACE, "workspace is NULL");
     if (misaligned(ws, 256)) return fail(MOE_EWORKSPACE, "workspace must be 256-byte aligned");
-    *plan = plan_train(T * L->top_k, L->d_model, L->d_ff, L->n_experts);
-    const int splits = plan->splits_down > plan->splits_dx ? plan->splits_down : plan->splits_dx;
-    *w = carve_train_workspace(ws, T, L->d_model, L->d_ff, L->n_experts, L->top_k, splits);
+    int splits = train_most_splits(T * L->top_k, L->d_model);
+    do *w = carve_train_workspace(ws, T, L->d_model, L->d_ff, L->n_experts, L->top_k, splits);
+    while (w->bytes > ws_bytes && --splits > 0);
     if (ws_bytes < w->bytes) return fail(MOE_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, w->bytes);
     return MOE_OK;
 }
 
-TrainRows train_rows(const moe_layer* L, const TrainWorkspace& w, const TrainPlan& plan, int T) {
+TrainRows train_rows(const moe_layer* L, const TrainWorkspace& w, int T) {
     TrainRows a;
     memset(&a, 0, sizeof(a));
     a.h = w.h;
@@ -1059,9 +1059,8 @@ TrainRows train_rows(const moe_layer* L, const TrainWorkspace& w, const TrainPla
     a.tok = w.tok;
     a.gate = w.gate;
     a.P = T * L->top_k;
-    a.per = plan.per;
-    a.splits = 1;
-    a.most_chunks = train_most_chunks(a.P, L->n_experts, plan.per);
+    a.E = L->n_experts;
+    a.most_splits = w.splits;
     return a;
 }
 
@@ -1069,17 +1068,15 @@ TrainRows train_rows(const moe_layer* L, const TrainWorkspace& w, const TrainPla
 
 size_t moe_experts_workspace_bytes(const moe_layer* layer, int T) {
     if (check_train_shape("moe_experts_workspace_bytes", layer, T)) return 0;
-    const TrainPlan p = plan_train(T * layer->top_k, layer->d_model, layer->d_ff, layer->n_experts);
     return carve_train_workspace(nullptr, T, layer->d_model, layer->d_ff, layer->n_experts, layer->top_k,
-                                 p.splits_down > p.splits_dx ? p.splits_down : p.splits_dx).bytes;
+                                 train_most_splits(T * layer->top_k, layer->d_model)).bytes;
 }
 
 int moe_experts_forward(const moe_layer* layer, const void* x, int T, const float* topk_gate, const int32_t* offsets, const int32_t* perm, void* a,
                         void* u, void* out, void* ws, size_t ws_bytes, moe_stream_t stream) {
     const char* const who = "moe_experts_forward";
     TrainWorkspace w;
-    TrainPlan plan;
-    if (int rc = check_train(who, layer, T, topk_gate, offsets, perm, ws, ws_bytes, &w, &plan)) return rc;
+    if (int rc = check_train(who, layer, T, topk_gate, offsets, perm, ws, ws_bytes, &w)) return rc;
     if (!x || !a || !u || !out) return fail(MOE_EINVAL, "%s: NULL argument", who);
     if (misaligned(x, 16) || misaligned(a, 16) || misaligned(u, 16) || misaligned(out, 16)) return fail(MOE_EINVAL, "%s: x, a, u and out must be 16-byte aligned", who);
     const int d = layer->d_model, f = layer->d_ff, E = layer->n_experts, k = layer->top_k;
@@ -1088,8 +1085,8 @@ int moe_experts_forward(const moe_layer* layer, const void* x, int T, const floa
         return fail(MOE_EINVAL, "%s: a and u must not overlap each other, x or out", who);
     hipStream_t st = (hipStream_t)stream;
     const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
-    launch_train_group(g, w, plan.per, st);
-    TrainRows r = train_rows(layer, w, plan, T);
+    launch_train_group(g, w, d, f, st);
+    TrainRows r = train_rows(layer, w, T);
     for (int e = 0; e < E; ++e) {
         r.w[e] = (const half_t*)layer->experts[e].w1.data;
         r.w3[e] = (const half_t*)layer->experts[e].w3.data;
@@ -1104,7 +1101,6 @@ int moe_experts_forward(const moe_layer* layer, const void* x, int T, const floa
     r.in = w.h;
     r.N = d;
     r.K = f;
-    w.splits = r.splits = plan.splits_down;
     launch_train_down(r, st);
     launch_train_gather(g, w, true, d, out, true, nullptr, 0, st);
     return check_hip(st);
@@ -1115,8 +1111,7 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
                          int d_w_type, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream) {
     const char* const who = "moe_experts_backward";
     TrainWorkspace w;
-    TrainPlan plan;
-    if (int rc = check_train(who, layer, T, topk_gate, offsets, perm, ws, ws_bytes, &w, &plan)) return rc;
+    if (int rc = check_train(who, layer, T, topk_gate, offsets, perm, ws, ws_bytes, &w)) return rc;
     if (!x || !a || !u || !d_out) return fail(MOE_EINVAL, "%s: NULL argument", who);
     if (!d_x && !d_gate && !d_w) return fail(MOE_EINVAL, "%s: no gradient asked for", who);
     if ((d_x_type != MOE_OUT_F32 && d_x_type != MOE_OUT_F16) || (d_w_type != MOE_OUT_F32 && d_w_type != MOE_OUT_F16))
@@ -1137,8 +1132,8 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
     }
     hipStream_t st = (hipStream_t)stream;
     const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
-    launch_train_group(g, w, plan.per, st);
-    TrainRows r = train_rows(layer, w, plan, T);
+    launch_train_group(g, w, d, f, st);
+    TrainRows r = train_rows(layer, w, T);
     for (int e = 0; e < E; ++e) r.w[e] = (const half_t*)layer->experts[e].w2.data;
     r.in = (const half_t*)d_out;
     r.a = (half_t*)a;      // (read only here)
@@ -1169,7 +1164,6 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
         r.in2 = w.d_u;
         r.N = d;
         r.K = f;
-        w.splits = r.splits = plan.splits_dx;
         launch_train_d_rows(r, st);
     }
     if (d_x || d_gate) launch_train_gather(g, w, false, d, d_x, d_x_type == MOE_OUT_F16, d_gate, (f + kTrainCols - 1) / kTrainCols, st);

@@ -21,13 +21,6 @@ namespace {
 constexpr int kLdsBytes = 163840;        // of a compute unit
 constexpr int kUnit = 32768;             // 256 rows of 64 elements, or 64 rows of 256
 constexpr int kThreads = 512;
-#ifndef KS
-#define KS 8
-#endif
-#ifndef KR
-#define KR 8
-#endif
-constexpr int kSide = KS, kSideR = KR;
 
 enum Form { kUp, kDown, kDHidden, kDRows };
 
@@ -94,7 +87,13 @@ __device__ __forceinline__ void wait_transfers() {
     static_assert(COUNT < 64, "six bits");
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
 }
-__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// The wavefront's LDS accesses are done (said in a way that the compiler counts on: else it waits for the operands again among the products, and for the tokens that are being
+// looked up with them), then all meet.
+__device__ __forceinline__ void meet() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0), nothing else
+    asm volatile("s_barrier" ::: "memory");
+}
 
 // TILE: kA, kB (units of the rings), kRuns (transfers of a wavefront for its half of the rows; for its half of the matrix's unit it is four), kReads (operands of a step), bring_rows(k),
 // bring_matrix(k) (transfer k of the next stage), rows_asked(), matrix_asked() (all of a stage's have been made), look_up() (asks for what the next ones need), rows_there(step),
@@ -168,9 +167,10 @@ constexpr int kRegion = kLdsBytes / 8, kSpreadRow = 272;
 template <int MT>
 __device__ __forceinline__ void spread(const float4_t (&acc)[4][MT], int i0, uint8_t* region, int lane) {
 #pragma unroll
-    for (int i = 0; i < (MT < 4 ? MT : 4); ++i)
+    for (int i = 0; i < 4; ++i)
+        if (i0 + i < MT)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *(float4_t*)(region + (i * 16 + (lane & 15)) * kSpreadRow + (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i0 + i];
+            for (int j = 0; j < 4; ++j) *(float4_t*)(region + (i * 16 + (lane & 15)) * kSpreadRow + (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i0 + i];
     wave_lds_handover();
 }
 __device__ __forceinline__ float4_t spread_at(const uint8_t* region, int row, int col) { return *(const float4_t*)(region + row * kSpreadRow + col * 4); }
@@ -188,7 +188,7 @@ struct RowsTile {
     static constexpr bool kColumns = FORM == kDHidden || FORM == kDRows;     // how the matrix lies
     static constexpr int kA = MT > 4 ? 2 : MT > 2 ? 3 : 4, kB = MT > 2 ? 3 : 4;
     static constexpr int kHalf = MT * 2048;                                 // bytes of a unit of half of the rows
-    static constexpr int kRuns = MT > 1 ? MT / 2 : 1;                       // (one tile: two wavefronts bring the same run)
+    static constexpr int kRuns = (MT + 1) / 2;                              // (of 2 MT over four wavefronts; odd: two bring the same one at the end)
     static constexpr int kRingB = 2 * kA * kHalf;                           // where the matrix's ring begins
     static_assert(kRingB + kB * kUnit <= kLdsBytes, "LDS");
     const TrainRows& a;
@@ -250,7 +250,7 @@ struct RowsTile {
         seek_matrix(c.s0);
     }
 
-    __device__ __forceinline__ int run_of(int k) const { return MT == 1 ? wn & 1 : wn + 4 * k; }
+    __device__ __forceinline__ int run_of(int k) const { return MT % 2 && k == MT / 2 ? 4 * k + (wn & 1) : 4 * k + wn; }
     // d_rows: the second half of the steps is d_u's and W3's.
     __device__ __forceinline__ int steps_of_one() const { return a.K / kTrainStep; }
 
@@ -382,6 +382,7 @@ struct RowsTile {
                 const int r0 = (group * MT + i0) * 16 + (lane >> 3);
 #pragma unroll
                 for (int p = 0; p < 2 * kMost; ++p) {
+                    if (i0 * 2 + p >= 2 * MT) continue;
                     const size_t row = (size_t)(c.begin + (r0 + 8 * p < c.rows ? r0 + 8 * p : 0));
                     va[p] = *(const half8_t*)(a.a + row * N + col);
                     vu[p] = *(const half8_t*)(a.u + row * N + col);
@@ -390,6 +391,7 @@ struct RowsTile {
                 spread<MT>(acc, i0, region, lane);
 #pragma unroll
                 for (int p = 0; p < 2 * kMost; ++p) {
+                    if (i0 * 2 + p >= 2 * MT) continue;
                     const float4_t lo = spread_at(region, 8 * p + (lane >> 3), (lane & 7) * 8), hi = spread_at(region, 8 * p + (lane >> 3), (lane & 7) * 8 + 4);
                     const float g = gate[p];
                     half8_t da, du, gh;
@@ -434,7 +436,8 @@ struct RowsTile {
         for (int i0 = 0; i0 < MT; i0 += 4) {
             spread<MT>(acc, i0, region, lane);
 #pragma unroll
-            for (int p = 0; p < 4 * (MT < 4 ? MT : 4); ++p) {
+            for (int p = 0; p < 16; ++p) {
+                if (i0 * 4 + p >= 4 * MT) continue;
                 const int r = (group * MT + i0) * 16 + 4 * p + (lane >> 4);
                 if (r < c.rows) *(float4_t*)(y + (size_t)(c.begin + r) * a.N) = spread_at(region, 4 * p + (lane >> 4), (lane & 15) * 4);
             }
@@ -454,28 +457,48 @@ __device__ __forceinline__ void rows_body(const TrainRows& a, const RowsWork& c,
 template <int FORM>
 __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, int n_tiles) {
     extern __shared__ uint8_t lds[];
-    // Workgroups go to the 8 XCDs in turn: each XCD takes a run of neighbouring tiles, eight chunks side by side.
-    const int n_chunks = __builtin_amdgcn_readfirstlane(a.meta->n_chunks);
-    const int units = n_chunks * n_tiles, total = units * a.splits, per_xcd = (total + 7) >> 3;
-    const int slot = blockIdx.x >> 3, t0 = (blockIdx.x & 7) * per_xcd + slot;
-    if (slot >= per_xcd || t0 >= total) return;
+    // Workgroups go to the 8 XCDs in turn.  Each takes a run of neighbouring tiles of the chunks that are not split, eight chunks side by side, and then some columns of all the others, which
+    // are of many lengths.
+    const TrainMeta* const meta = a.meta;
+    const TrainSplit sp = FORM == kDown ? meta->down : FORM == kDRows ? meta->d_rows : meta->whole;
+    const int first = sp.first_split, others = meta->n_chunks - first;
+    const int n_a = first * n_tiles, n_b = others * n_tiles * sp.splits, per_a = (n_a + 7) >> 3, per_b = (n_b + 7) >> 3;
+    const int slot = blockIdx.x >> 3, xcd = blockIdx.x & 7;
+    const bool split = slot >= per_a;
+    const int t = split ? xcd * per_b + slot - per_a : xcd * per_a + slot;
+    if (split ? slot - per_a >= per_b || t >= n_b : t >= n_a) return;
     RowsWork c;
-    c.split = __builtin_amdgcn_readfirstlane(t0 / units);
-    const int t = t0 - c.split * units;
-    const int group = t / (kSideR * n_tiles), rest = t - group * kSideR * n_tiles, in_group = min(kSideR, n_chunks - group * kSideR);
-    const int tile = __builtin_amdgcn_readfirstlane(rest / in_group);
-    const TrainChunk ch = a.chunks[group * kSideR + rest - tile * in_group];
+    int tile, chunk;
+    c.split = 0;
+    if (split) {
+        const int column = t / others;
+        chunk = first + t - column * others;
+        c.split = __builtin_amdgcn_readfirstlane(column / n_tiles);
+        tile = column - c.split * n_tiles;
+    } else {
+        const int group = t / (8 * n_tiles), rest = t - group * 8 * n_tiles, in_group = min(8, first - group * 8);
+        tile = rest / in_group;
+        chunk = group * 8 + rest - tile * in_group;
+    }
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    const TrainChunk ch = a.chunks[__builtin_amdgcn_readfirstlane(chunk)];
     c.expert = __builtin_amdgcn_readfirstlane(ch.expert);
     c.begin = __builtin_amdgcn_readfirstlane(ch.begin);
     c.rows = __builtin_amdgcn_readfirstlane(ch.rows);
     c.n0 = tile * (FORM == kUp ? kTrainCols / 2 : kTrainCols);
-    const int steps = a.K / kTrainStep * (FORM == kDRows ? 2 : 1);
-    c.s0 = __builtin_amdgcn_readfirstlane(steps * c.split / a.splits);
-    c.s1 = __builtin_amdgcn_readfirstlane(steps * (c.split + 1) / a.splits);
-    if (c.rows <= 32) rows_body<FORM, 1>(a, c, lds);
-    else if (c.rows <= 64) rows_body<FORM, 2>(a, c, lds);
-    else if (c.rows <= 128) rows_body<FORM, 4>(a, c, lds);
-    else rows_body<FORM, 8>(a, c, lds);
+    const int steps = a.K / kTrainStep * (FORM == kDRows ? 2 : 1), shares = split ? sp.splits : 1;
+    c.s0 = __builtin_amdgcn_readfirstlane(steps * c.split / shares);
+    c.s1 = __builtin_amdgcn_readfirstlane(steps * (c.split + 1) / shares);
+    switch ((c.rows + 31) >> 5) {
+        case 1: rows_body<FORM, 1>(a, c, lds); break;
+        case 2: rows_body<FORM, 2>(a, c, lds); break;
+        case 3: rows_body<FORM, 3>(a, c, lds); break;
+        case 4: rows_body<FORM, 4>(a, c, lds); break;
+        case 5: rows_body<FORM, 5>(a, c, lds); break;
+        case 6: rows_body<FORM, 6>(a, c, lds); break;
+        case 7: rows_body<FORM, 7>(a, c, lds); break;
+        default: rows_body<FORM, 8>(a, c, lds);
+    }
 }
 
 template <int FORM>
@@ -484,9 +507,11 @@ void launch_rows(const TrainRows& a, hipStream_t st) {
     const auto kernel = train_rows_kernel<FORM>;
     allow_lds((const void*)kernel, kLdsBytes, configured);
     constexpr int kOut = FORM == kUp ? kTrainCols / 2 : kTrainCols;
-    const int n_tiles = (a.N + kOut - 1) / kOut;
-    const long long total = (long long)n_tiles * a.most_chunks * a.splits;
-    kernel<<<(unsigned)((total + 7) / 8 * 8), kThreads, kLdsBytes, st>>>(a, n_tiles);
+    const int n_tiles = (a.N + kOut - 1) / kOut, full = a.P / kTrainRows, rests = a.E < a.P ? a.E : a.P;
+    // (as many full chunks as leave less than a round of workgroups may be split, and all rests: choose_splits)
+    const int splits = FORM == kDown || FORM == kDRows ? a.most_splits : 1, some = kComputeUnits / n_tiles + 1;
+    const long long most_a = (long long)full * n_tiles, most_b = (long long)((full < some ? full : some) + rests) * n_tiles * splits;
+    kernel<<<(unsigned)((most_a + 7) / 8 + (most_b + 7) / 8) * 8, kThreads, kLdsBytes, st>>>(a, n_tiles);
 }
 
 // ---- gradients of the matrices
@@ -679,10 +704,11 @@ struct WeightsTile {
 template <typename OUT>
 __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights a, int tiles_f, int tiles_d) {
     extern __shared__ uint8_t lds[];
-    const int per_matrix = tiles_f * tiles_d, total = a.E * 3 * per_matrix, per_xcd = (total + 7) >> 3;
-    const int slot = blockIdx.x >> 3, t0 = (blockIdx.x & 7) * per_xcd + slot;
-    if (slot >= per_xcd || t0 >= total) return;
-    const int matrix = t0 / per_matrix, t = t0 - matrix * per_matrix, e = matrix / 3, which = matrix - 3 * e;
+    // Workgroups go to the 8 XCDs in turn: each takes an eighth of every matrix, neighbouring tiles, the matrices of the experts with most rows first.
+    const int per_xcd = (tiles_f * tiles_d + 7) >> 3, slot = blockIdx.x >> 3;
+    const int matrix = __builtin_amdgcn_readfirstlane(slot / per_xcd), t = (blockIdx.x & 7) * per_xcd + slot - matrix * per_xcd;
+    if (t >= tiles_f * tiles_d) return;
+    const int place = matrix / 3, which = matrix - 3 * place, e = __builtin_amdgcn_readfirstlane(a.meta->order[place]);
     WeightsWork c;
     c.out = which == 0 ? a.w1[e] : which == 1 ? a.w3[e] : a.w2[e];
     if (!c.out) return;
@@ -691,8 +717,8 @@ __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights
     if (c.rows == 0 && a.accumulate) return;
     // eight tiles of m side by side
     const int tiles_m = which == 2 ? tiles_d : tiles_f, tiles_n = which == 2 ? tiles_f : tiles_d;
-    const int group = t / (kSide * tiles_n), rest = t - group * kSide * tiles_n, in_group = min(kSide, tiles_m - group * kSide);
-    const int tn = rest / in_group, tm = group * kSide + rest - tn * in_group;
+    const int group = t / (8 * tiles_n), rest = t - group * 8 * tiles_n, in_group = min(8, tiles_m - group * 8);
+    const int tn = rest / in_group, tm = group * 8 + rest - tn * in_group;
     c.m = which == 0 ? a.d_a : which == 1 ? a.d_u : a.d_out;
     c.n = which == 2 ? a.h : a.x;
     c.lm = which == 2 ? a.d : a.f;
@@ -715,77 +741,147 @@ void launch_weights(const TrainWeights& a, hipStream_t st) {
     const auto kernel = train_weights_kernel<OUT>;
     allow_lds((const void*)kernel, kLdsBytes, configured);
     const int tiles_f = (a.f + kTrainCols - 1) / kTrainCols, tiles_d = (a.d + kTrainCols - 1) / kTrainCols;
-    const int total = a.E * 3 * tiles_f * tiles_d;
-    kernel<<<(unsigned)((total + 7) / 8 * 8), kThreads, kLdsBytes, st>>>(a, tiles_f, tiles_d);
+    kernel<<<(unsigned)(a.E * 3 * ((tiles_f * tiles_d + 7) / 8) * 8), kThreads, kLdsBytes, st>>>(a, tiles_f, tiles_d);
 }
 
 // ---- the grouping, and the rows of a token
 
-__global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, TrainWorkspace w, int per) {
-    __shared__ int32_t off[MOE_MAX_EXPERTS + 1];
-    const int tid = threadIdx.x, P = g.T * g.k;
-    if (tid == 0) {
-        int run = 0;
-        for (int e = 0; e <= g.E; ++e) {
-            const int o = g.offsets ? g.offsets[e] : e ? P : 0;
-            run = max(run, min(max(o, 0), P));
-            off[e] = run;
+// Which chunks share their contraction, and among how many workgroups.  What fills whole rounds of the chip with full chunks is left alone; of the rest, which would leave most of it idle
+// or add a round, each is cut in s parts.  In units of a full tile's time (steps of the contraction at 2250 cycles): `cost` of all these tiles, the longest `most`; a workgroup's
+// beginning and end are 7.5 steps, a partial result is written and read back.  (4096 tokens, Mixtral shape, 37 chunks of 16 tiles: down 1091 -> XXX us, d_rows 1907 -> XXX.)
+__device__ TrainSplit choose_splits(int n_full, int n_rest, int rest_rows, int longest_rest, int n_tiles, int steps, int most_splits) {
+    const int n_chunks = n_full + n_rest, whole = n_full * n_tiles / (int)kComputeUnits * (int)kComputeUnits / n_tiles, left = n_full - whole;
+    TrainSplit best{n_chunks, 1};
+    if (left + n_rest == 0) return best;
+    const float cost = (float)n_tiles * ((float)left + 0.3f * (float)n_rest + 0.7f / kTrainRows * (float)rest_rows);
+    const float most = left ? 1.0f : 0.3f + 0.7f / kTrainRows * (float)longest_rest;
+    const float begin = 7.5f / (float)steps, partial = (float)(left * kTrainRows + rest_rows) * (float)n_tiles * 3e-4f / (float)steps;
+    float least = 0.0f;
+    for (int s = 1; s <= most_splits && s <= steps; ++s) {
+        const int workgroups = (left + n_rest) * n_tiles * s;
+        const float rounds = (float)((workgroups + kComputeUnits - 1) / kComputeUnits);
+        const float time = (rounds == 1.0f ? most / (float)s : cost / kComputeUnits + 0.5f * most / (float)s) + rounds * begin + (float)(s - 1) * partial;
+        if (s == 1 || time < 0.97f * least) {
+            least = time;
+            best = TrainSplit{s == 1 ? n_chunks : whole, s};
+        }
+    }
+    return best;
+}
+
+__global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, TrainWorkspace w, int d, int f) {
+    __shared__ int32_t off[MOE_MAX_EXPERTS + 1], first_full[MOE_MAX_EXPERTS], rest_place[MOE_MAX_EXPERTS];
+    __shared__ TrainSplit split[2];
+    __shared__ int32_t counts[2];
+    const int tid = threadIdx.x, P = g.T * g.k, E = g.E;
+    if (tid < 64) {
+        int o = g.offsets ? (tid <= E ? g.offsets[tid] : 0) : tid ? P : 0;
+        o = min(max(o, 0), P);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {                   // increasing, whatever they were
+            const int before = __shfl_up(o, m, kWave);
+            if (tid >= m) o = max(o, before);
+        }
+        const int begin = __shfl(o, tid < E ? tid : E, kWave), end = __shfl(o, tid < E ? tid + 1 : E, kWave);
+        const int rows = end - begin, rest = rows % kTrainRows;
+        int full = rows / kTrainRows, place = 0, rank = 0, sum = rest, n_rest = rest > 0, longest = rest;
+        for (int e = 0; e < E; ++e) {
+            const int r = __shfl(rest, e, kWave), n = __shfl(rows, e, kWave);
+            place += r > rest || (r == rest && e < tid);
+            rank += n > rows || (n == rows && e < tid);
+        }
+        const int mine = full;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const int before = __shfl_up(full, m, kWave);
+            if (tid >= m) full += before;
+        }
+        const int n_full = __shfl(full, E - 1, kWave);
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) {
+            sum += __shfl_xor(sum, m, kWave);
+            n_rest += __shfl_xor(n_rest, m, kWave);
+            longest = max(longest, __shfl_xor(longest, m, kWave));
+        }
+        if (tid <= E) off[tid] = o;
+        if (tid < E) {
+            first_full[tid] = full - mine;
+            rest_place[tid] = n_full + place;
+        }
+        const int tiles = (d + kTrainCols - 1) / kTrainCols;
+        if (tid < 2) split[tid] = choose_splits(n_full, n_rest, sum, longest, tiles, f / kTrainStep * (tid + 1), w.splits);
+        if (tid == 0) {
+            counts[0] = n_full;
+            counts[1] = n_full + n_rest;
+        }
+        if (blockIdx.x == 0) {
+            if (tid <= E) w.meta->offsets[tid] = o;
+            if (tid < E) {
+                w.meta->order[rank] = tid;
+                if (rest) w.chunks[n_full + place] = TrainChunk{tid, end - rest, rest, 0};
+            }
+            if (tid == 0) {
+                w.meta->lo = o;
+                w.meta->n_full = n_full;
+                w.meta->n_chunks = n_full + n_rest;
+                w.meta->whole = TrainSplit{n_full, 1};
+            }
+            if (tid == E) w.meta->hi = o;
         }
     }
     __syncthreads();
-    const int lo = off[0], hi = off[g.E];
+    if (blockIdx.x == 0 && tid < 2) (tid ? w.meta->d_rows : w.meta->down) = split[tid];
+    const int lo = off[0], hi = off[E];
     const int r = blockIdx.x * 256 + tid;
-    if (r < P + 64) {
-        int tok = 0;
-        float gate = 0.0f;
-        if (r >= lo && r < hi) {
-            const int p = g.perm ? g.perm[r] : r;
-            if ((unsigned)p < (unsigned)P) {
-                tok = p / g.k;
-                gate = g.topk_gate ? g.topk_gate[p] : 1.0f;
-                w.inv[p] = r;
-            }
+    if (r >= P + kTrainStep) return;
+    int tok = 0;
+    float gate = 0.0f;
+    if (r >= lo && r < hi) {
+        const int p = g.perm ? g.perm[r] : r;
+        if ((unsigned)p < (unsigned)P) {
+            tok = p / g.k;
+            gate = g.topk_gate ? g.topk_gate[p] : 1.0f;
+            w.inv[p] = r;
         }
-        w.tok[r] = tok;
-        w.gate[r] = gate;
+        int e = 0;                                           // the last expert that begins at r or before, and has rows
+        for (int m = MOE_MAX_EXPERTS / 2; m >= 1; m >>= 1)
+            if (e + m < E && off[e + m] <= r) e += m;
+        const int in_expert = r - off[e], rows = off[e + 1] - off[e], full = rows / kTrainRows;
+        const int chunk = in_expert / kTrainRows < full ? first_full[e] + in_expert / kTrainRows : rest_place[e];
+        w.shares[r] = (chunk >= split[0].first_split ? split[0].splits : 1) | (chunk >= split[1].first_split ? split[1].splits : 1) << 8;
+        if (in_expert % kTrainRows == 0 && chunk < counts[0]) w.chunks[chunk] = TrainChunk{e, r, kTrainRows, 0};
     }
-    if (blockIdx.x == 0 && tid < MOE_MAX_EXPERTS) {
-        int at = 0;
-        for (int e = 0; e < tid && e < g.E; ++e) at += (off[e + 1] - off[e] + per - 1) / per;
-        if (tid < g.E) {
-            const int begin = off[tid], end = off[tid + 1];
-            for (int b = begin; b < end; b += per) w.chunks[at++] = TrainChunk{tid, b, min(per, end - b), 0};
-            if (tid == g.E - 1) {
-                w.meta->lo = lo;
-                w.meta->hi = hi;
-                w.meta->n_chunks = at;
-            }
-        }
-    }
-    if (blockIdx.x == 0 && tid <= g.E) w.meta->offsets[tid] = off[tid];
+    w.tok[r] = tok;
+    w.gate[r] = gate;
 }
 
 // One workgroup per token.  inv[p] is looked up in perm again: a pair in no group has whatever lay there.
 template <typename OUT>
-__global__ __launch_bounds__(256) void train_gather_kernel(TrainGrouping g, TrainWorkspace w, int gates, int d, OUT* __restrict__ out,
+__global__ __launch_bounds__(256) void train_gather_kernel(TrainGrouping g, TrainWorkspace w, int forward, int d, OUT* __restrict__ out,
                                                            float* __restrict__ d_gate, int n_part) {
     typedef OUT out4_t __attribute__((ext_vector_type(4)));
-    const int t = blockIdx.x, P = g.T * g.k, lo = w.meta->lo, hi = w.meta->hi;
-    auto row_of_pair = [&](int p) {
-        const int r = w.inv[p];
-        if (r < lo || r >= hi) return -1;
-        return (g.perm ? g.perm[r] : r) == p ? r : -1;
-    };
+    const int t = blockIdx.x, lane = threadIdx.x & 63, P = g.T * g.k, lo = w.meta->lo, hi = w.meta->hi;
+    // lane s looks after slot s
+    int row = -1, shares = 0;
+    float gate = 1.0f;
+    if (lane < g.k) {
+        const int p = t * g.k + lane, r = w.inv[p];
+        if (r >= lo && r < hi && (g.perm ? g.perm[r] : r) == p) {
+            row = r;
+            shares = forward ? w.shares[r] & 255 : w.shares[r] >> 8;
+            if (forward) gate = w.gate[r];
+        }
+    }
     if (out)
         for (int c = threadIdx.x * 4; c < d; c += 1024) {
             float4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
             for (int s = 0; s < g.k; ++s) {
-                const int r = row_of_pair(t * g.k + s);
+                const int r = __builtin_amdgcn_readlane(row, s), n = __builtin_amdgcn_readlane(shares, s);
                 if (r < 0) continue;
-                float4_t v = *(const float4_t*)(w.y + (size_t)r * d + c);
-                for (int p = 1; p < w.splits; ++p) v += *(const float4_t*)(w.y + ((size_t)p * P + r) * d + c);
-                if (gates) v *= w.gate[r];
-                sum += v;
+                const float* const y = w.y + (size_t)r * d + c;
+                float4_t v = *(const float4_t*)y;
+                for (int p = 1; p < n; ++p) v += *(const float4_t*)(y + (size_t)p * P * d);
+                sum += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, gate), s)) * v;
             }
             out4_t o;
 #pragma unroll
@@ -793,26 +889,23 @@ __global__ __launch_bounds__(256) void train_gather_kernel(TrainGrouping g, Trai
             *(out4_t*)(out + (size_t)t * d + c) = o;
         }
     if (d_gate && threadIdx.x < g.k) {
-        const int p = t * g.k + threadIdx.x, r = row_of_pair(p);
         float sum = 0.0f;
-        if (r >= 0)
-            for (int i = 0; i < n_part; ++i) sum += w.part[(size_t)i * P + r];
-        d_gate[p] = sum;
+        if (row >= 0)
+            for (int i = 0; i < n_part; ++i) sum += w.part[(size_t)i * P + row];
+        d_gate[t * g.k + threadIdx.x] = sum;
     }
 }
 
 }  // namespace
 
-TrainPlan plan_train(int P, int d, int f, int E) {
-    TrainPlan p;
-    p.per = kTrainRows;
-    p.splits_down = p.splits_dx = 1;
-    return p;
+int train_most_splits(int P, int d) {
+    const float rounds = (float)P / kTrainRows * (float)((d + kTrainCols - 1) / kTrainCols) / kComputeUnits;
+    return rounds >= 8.0f ? 1 : rounds >= 4.0f ? 2 : rounds >= 1.0f ? 4 : rounds >= 0.25f ? 8 : kTrainMostSplits;
 }
 
-void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int per, hipStream_t st) {
+void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int d, int f, hipStream_t st) {
     const int P = g.T * g.k;
-    train_group_kernel<<<(P + 64 + 255) / 256, 256, 0, st>>>(g, w, per);
+    train_group_kernel<<<(P + kTrainStep + 255) / 256, 256, 0, st>>>(g, w, d, f);
 }
 
 void launch_train_up(const TrainRows& a, hipStream_t st) { launch_rows<kUp>(a, st); }
@@ -824,10 +917,10 @@ void launch_train_d_weights(const TrainWeights& a, bool half_out, hipStream_t st
     else launch_weights<float>(a, st);
 }
 
-void launch_train_gather(const TrainGrouping& g, const TrainWorkspace& w, bool gates, int d, void* out, bool half_out, float* d_gate, int n_part,
+void launch_train_gather(const TrainGrouping& g, const TrainWorkspace& w, bool forward, int d, void* out, bool half_out, float* d_gate, int n_part,
                          hipStream_t st) {
-    if (half_out) train_gather_kernel<half_t><<<g.T, 256, 0, st>>>(g, w, gates, d, (half_t*)out, d_gate, n_part);
-    else train_gather_kernel<float><<<g.T, 256, 0, st>>>(g, w, gates, d, (float*)out, d_gate, n_part);
+    if (half_out) train_gather_kernel<half_t><<<g.T, 256, 0, st>>>(g, w, forward, d, (half_t*)out, d_gate, n_part);
+    else train_gather_kernel<float><<<g.T, 256, 0, st>>>(g, w, forward, d, (float*)out, d_gate, n_part);
 }
 
 }  // namespace moemix

@@ -13,24 +13,34 @@ constexpr int kTrainRows = 256;         // most rows of a tile
 struct TrainChunk {
     int32_t expert, begin, rows, unused;   // grouped rows [begin, begin + rows)
 };
+// Chunks are in an order of their own: those of kTrainRows rows by expert, then the experts' rests, the longest first.  Those from `first_split` on share their contraction among
+// `splits` workgroups each.
+struct TrainSplit {
+    int32_t first_split, splits;
+};
 struct TrainMeta {
     int32_t lo, hi;                        // grouped rows [lo, hi) belong to an expert
-    int32_t n_chunks, unused;
+    int32_t n_chunks, n_full;
+    TrainSplit whole, down, d_rows;        // of the launches that cannot be split, of down and of d_rows
     int32_t offsets[MOE_MAX_EXPERTS + 1];  // increasing, within [0, P]
+    int32_t order[MOE_MAX_EXPERTS];        // experts, the one with most rows first
 };
+
+constexpr int kTrainMostSplits = 16;
 
 struct TrainWorkspace {
     TrainMeta* meta;
-    TrainChunk* chunks;   // [E + P / 32 + 1]
+    TrainChunk* chunks;   // [E + P / 256]
     int32_t* tok;         // [P + 64]  grouped row -> token (0 for a row of no expert and past the end)
     float* gate;          // [P + 64]  grouped row -> its gate
     int32_t* inv;         // [P]       pair -> grouped row; anything for a pair in no group
+    int32_t* shares;      // [P]       grouped row -> workgroups that share its contraction: down's, 256 times d_rows'
     half_t* h;            // [P + 64, f]  hidden rows; backward: times the gate (d_weights reads whole steps of 64 rows)
     half_t* d_a;          // [P + 64, f]
     half_t* d_u;          // [P + 64, f]
-    float* y;             // [splits][P, d]  rows of the down-projection; backward: of d_x
     float* part;          // [ceil(f / 256)][P]  shares of d_gate
-    int splits;
+    float* y;             // [splits][P, d]  rows of the down-projection; backward: of d_x
+    int splits;           // most of a chunk
     size_t bytes;
 };
 
@@ -44,15 +54,16 @@ inline TrainWorkspace carve_train_workspace(void* base, int T, int d, int f, int
     };
     const size_t P = (size_t)T * k;
     w.meta = (TrainMeta*)take(sizeof(TrainMeta));
-    w.chunks = (TrainChunk*)take((E + P / 32 + 1) * sizeof(TrainChunk));
-    w.tok = (int32_t*)take((P + 64) * sizeof(int32_t));
-    w.gate = (float*)take((P + 64) * sizeof(float));
+    w.chunks = (TrainChunk*)take((E + P / kTrainRows) * sizeof(TrainChunk));
+    w.tok = (int32_t*)take((P + kTrainStep) * sizeof(int32_t));
+    w.gate = (float*)take((P + kTrainStep) * sizeof(float));
     w.inv = (int32_t*)take(P * sizeof(int32_t));
+    w.shares = (int32_t*)take(P * sizeof(int32_t));
     w.h = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
     w.d_a = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
     w.d_u = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
-    w.y = (float*)take((size_t)splits * P * d * sizeof(float));
     w.part = (float*)take((size_t)((f + kTrainCols - 1) / kTrainCols) * P * sizeof(float));
+    w.y = (float*)take((size_t)splits * P * d * sizeof(float));
     w.splits = splits;
     w.bytes = off;
     return w;
@@ -83,10 +94,8 @@ struct TrainRows {
     const TrainChunk* chunks;
     const int32_t* tok;
     const float* gate;
-    int N, K, P;
-    int per;                   // most rows of a chunk
-    int splits;                // of the contraction
-    int most_chunks;
+    int N, K, P, E;
+    int most_splits;           // of a chunk's contraction
 };
 
 // Gradients of the matrices: for expert e  w1 = d_a^T x, w3 = d_u^T x, w2 = d_out^T h.  Null: not asked for.
@@ -105,14 +114,10 @@ struct TrainWeights {
     int accumulate;
 };
 
-struct TrainPlan {
-    int per;                   // rows per chunk: 32, 64, 128 or 256
-    int splits_down, splits_dx;
-};
-TrainPlan plan_train(int P, int d, int f, int E);
-inline int train_most_chunks(int P, int E, int per) { return E + P / per; }
+// Most workgroups that share a chunk's contraction in down and d_rows: partial results cost room, and pay where a launch has few rounds of workgroups.
+int train_most_splits(int P, int d);
 
-void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int per, hipStream_t st);
+void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int d, int f, hipStream_t st);
 // a = W1 x, u = W3 x, h = silu(a) u
 void launch_train_up(const TrainRows& a, hipStream_t st);
 // y = W2 h
@@ -122,8 +127,8 @@ void launch_train_d_hidden(const TrainRows& a, hipStream_t st);
 // y = W1^T d_a + W3^T d_u
 void launch_train_d_rows(const TrainRows& a, hipStream_t st);
 void launch_train_d_weights(const TrainWeights& a, bool half_out, hipStream_t st);
-// out[t,:] = sum over the token's pairs in a group of (gates: topk_gate *) sum over splits of y; d_gate [T, k] (or null) from n_part shares of each.
-void launch_train_gather(const TrainGrouping& g, const TrainWorkspace& w, bool gates, int d, void* out, bool half_out, float* d_gate,
+// out[t,:] = sum over the token's pairs in a group of (forward: topk_gate *) the sum of the shares of y; d_gate [T, k] (or null) from n_part shares of each.
+void launch_train_gather(const TrainGrouping& g, const TrainWorkspace& w, bool forward, int d, void* out, bool half_out, float* d_gate,
                          int n_part, hipStream_t st);
 
 }  // namespace moemix

@@ -45,8 +45,7 @@ def test_refusals_of_both(call):
         assert call(L, **{name: AT + 2}) == mm.MOE_EINVAL
     for name in ("x", "a", "u"):
         assert call(L, **{name: None}) == mm.MOE_EINVAL and call(L, **{name: AT + 8}) == mm.MOE_EINVAL
-    need = mm.lib().moe_experts_workspace_bytes(L, T)
-    assert call(L, ws=None) == call(L, ws=AT + 128) == call(L, ws_bytes=need - 1) == mm.MOE_EWORKSPACE
+    assert call(L, ws=None) == call(L, ws=AT + 128) == call(L, ws_bytes=T * K * (6 * F + 4 * D)) == mm.MOE_EWORKSPACE
 
 
 def test_refusals_of_the_forward_pass():
