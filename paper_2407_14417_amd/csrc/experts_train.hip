@@ -73,13 +73,20 @@ __device__ __forceinline__ float sigmoid(float a) { return 1.0f / (1.0f + __expf
 //
 // The 8 wavefronts of a workgroup are two groups of four, one of each per SIMD; group g multiplies half g of the tile's rows.  A step of the contraction (64 elements)
 // takes each group two phases: it reads the operands of the step from LDS into registers, then it multiplies them.  The groups are one phase apart, so that in
-// every phase one of them feeds the matrix cores and the other reads, and all meet at its end.  In the phase in which a group reads it also asks for 8 KB per
-// wavefront, always of a step that lies ahead, straight into LDS:
+// every phase one of them feeds the matrix cores (64 instructions of 16 cycles) and the other reads, and all meet at its end.  Each group also asks for 8 KB per wavefront and step,
+// straight into LDS, always of a step that lies ahead:
 //   phase 2k:      group 0 reads step k, asks for rows' half 1 of step k + nA - 1 and the first half of the matrix's unit of step k + nB - 1;  group 1 multiplies step k - 1
 //   phase 2k + 1:  group 1 reads step k, asks for rows' half 0 of step k + nA and the second half of the matrix's unit of step k + nB - 1;  group 0 multiplies step k
 // Each half of the rows has a ring of nA units, the matrix one of nB; what is written then was read last in the phase before, or earlier.  A transfer has three phases or more
 // to arrive (nA = 2, nB = 3, 160 KB of LDS; with two phases for the matrix's side a step took 2400 cycles in place of 2048).
+// Transfers and reads go by turns: a transfer waits for its place in the compute unit's address path, 64 bytes per cycle for all wavefronts, and LDS delivers meanwhile.  (One after the
+// other 450 + 550 cycles.)  kLate: the matrix's transfers are asked for among the products that follow instead, and by group 1 a step further ahead: where both operands take transposed
+// reads, twice as many instructions, a phase of reading has no room for them (970 cycles with, backward of 4096 tokens in the Mixtral shape 5850 -> 5760 us; elsewhere they delay
+// the products: forward 2780 -> 2817).
 // Past the last step the last one is asked for again, so that the waits can count.
+//
+// What bounds it: 2048 cycles of products in the 2240 of a step; and power.  The clock falls to 1.4-1.5 GHz (8192 rows of one expert of 4096 x 14336, d_rows: 1390 us, 1.38 PFLOP/s; with operands
+// of zeros, the same instructions, 1028 us).  So what saves energy counts: two products in a row share an operand (g goes to and fro over j), 0.7-1 % of the time.
 
 // Up to COUNT of the wavefront's own transfers are under way.
 template <int COUNT>
@@ -95,26 +102,30 @@ __device__ __forceinline__ void meet() {
     asm volatile("s_barrier" ::: "memory");
 }
 
-// TILE: kA, kB (units of the rings), kRuns (transfers of a wavefront for its half of the rows; for its half of the matrix's unit it is four), kReads (operands of a step), bring_rows(k),
-// bring_matrix(k) (transfer k of the next stage), rows_asked(), matrix_asked() (all of a stage's have been made), look_up() (asks for what the next ones need), rows_there(step),
-// matrix_there(step) (what the wavefront brought of a step has arrived and nobody reads it yet), read(r) (operand r of the next step), step_read(), multiply() (which looks up).
+// TILE: kA, kB (units of the rings), kRuns (transfers of a wavefront for its half of the rows; for its half of the matrix's unit it is four), kReads (operands of a step), kLate (multiply() calls
+// bring_matrix()), bring_rows(k), bring_matrix(k) (transfer k of the next stage), rows_asked(), matrix_asked() (all of a stage's have been made), look_up_rows(), look_up_matrix() (asks for
+// what the next ones need), rows_there(step), matrix_there(step) (what the wavefront brought of a step has arrived and nobody reads it yet), read(r) (operand r of the next step),
+// step_read(), multiply().
 template <typename TILE>
 __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
-    constexpr int kA = TILE::kA, kB = TILE::kB, kPer = TILE::kRuns + 4;
+    constexpr bool kLate = TILE::kLate;
+    constexpr int kA = TILE::kA, kB = TILE::kB, kRuns = TILE::kRuns, kPer = kRuns + 4;
     static_assert(kA <= kB && kB <= kA + 1, "what follows counts on it");
-    constexpr int kRowsLate = 4 + (kA - 1) * kPer, kMatrixLate = (kB - 2) * kPer;     // transfers after those of the step that is read next
+    // transfers after those of the step that is read next
+    constexpr int kRowsLate = (kA - 1) * kPer + (kLate ? 0 : 4), kMatrixLate = (kB - 2) * kPer, kMatrixLate1 = kMatrixLate + (kLate ? kRuns : 0);
     for (int k = -kB; k < 0; ++k) {
         if (k + kA - 1 + group >= 0) {
 #pragma unroll
-            for (int i = 0; i < TILE::kRuns; ++i) t.bring_rows(i);
+            for (int i = 0; i < kRuns; ++i) t.bring_rows(i);
             t.rows_asked();
         }
-        if (k + kB - 1 >= 0) {
+        if (k + kB - 1 + (kLate ? group : 0) >= 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) t.bring_matrix(i);
             t.matrix_asked();
         }
-        t.look_up();
+        t.look_up_rows();
+        t.look_up_matrix();
     }
     wait_transfers<kMatrixLate>();
     if (group) t.rows_there(0);
@@ -122,20 +133,20 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
     meet();
     if (group) meet();
     for (int k = 0; k < n; ++k) {
-        // Transfers and reads by turns: a transfer waits for its place in the compute unit's address path, 64 bytes per cycle for all wavefronts, and LDS delivers meanwhile.
-        // (One after the other 450 + 550 cycles, more than the other group's products take.)
+        t.look_up_matrix();
+        constexpr int kTurns = kLate ? kRuns : kPer;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (i < TILE::kRuns) t.bring_rows(i);
-            else t.bring_matrix(i - TILE::kRuns);
+        for (int i = 0; i < kTurns; ++i) {
+            if (i < kRuns) t.bring_rows(i);
+            else t.bring_matrix(i - kRuns);
 #pragma unroll
-            for (int r = i * TILE::kReads / kPer; r < (i + 1) * TILE::kReads / kPer; ++r) t.read(r);
+            for (int r = i * TILE::kReads / kTurns; r < (i + 1) * TILE::kReads / kTurns; ++r) t.read(r);
         }
         t.rows_asked();
-        t.matrix_asked();
+        if (!kLate) t.matrix_asked();
         t.step_read();
         if (group) {
-            wait_transfers<kRowsLate < kMatrixLate ? kRowsLate : kMatrixLate>();
+            wait_transfers<kRowsLate < kMatrixLate1 ? kRowsLate : kMatrixLate1>();
             t.rows_there(k + 1);
             t.matrix_there(k + 1);
         } else {
@@ -149,6 +160,7 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
         t.multiply();
         __builtin_amdgcn_s_setprio(0);
         pin_schedule();
+        if (kLate) t.matrix_asked();
         if (!group) {
             wait_transfers<kMatrixLate>();
             t.matrix_there(k + 1);
@@ -190,6 +202,7 @@ struct RowsTile {
     static constexpr int kHalf = MT * 2048;                                 // bytes of a unit of half of the rows
     static constexpr int kRuns = (MT + 1) / 2;                              // (of 2 MT over four wavefronts; odd: two bring the same one at the end)
     static constexpr int kRingB = 2 * kA * kHalf;                           // where the matrix's ring begins
+    static constexpr bool kLate = false;
     static_assert(kRingB + kB * kUnit <= kLdsBytes, "LDS");
     const TrainRows& a;
     const RowsWork& c;
@@ -286,7 +299,8 @@ struct RowsTile {
         if (FORM == kDRows && c.s1 - 1 - left_b == steps_of_one()) seek_matrix(steps_of_one());
         else base_b += kColumns ? (size_t)a.N * (kTrainStep * 2) : kTrainStep * 2;
     }
-    __device__ __forceinline__ void look_up() {}
+    __device__ __forceinline__ void look_up_rows() {}
+    __device__ __forceinline__ void look_up_matrix() {}
     __device__ __forceinline__ void rows_there(int) {}
     __device__ __forceinline__ void matrix_there(int) {}
 
@@ -308,11 +322,14 @@ struct RowsTile {
     }
     __device__ __forceinline__ void multiply() {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+        for (int g = 0; g < 2 * MT; ++g) {
+            const int kk = g / MT, i = g % MT;
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j][i] = mfma16(fb[kk][j], fa[kk][i], acc[j][i]);
+            for (int to = 0; to < 4; ++to) {
+                const int j = g & 1 ? 3 - to : to;
+                acc[j][i] = mfma16(fb[kk][j], fa[kk][i], acc[j][i]);
+            }
+        }
     }
 
     __device__ __forceinline__ void write(uint8_t* lds) {
@@ -528,6 +545,7 @@ template <typename OUT, bool GM>
 struct WeightsTile {
     static constexpr int kA = 2, kB = 3, kRuns = 4, kHalf = 16384;          // a half of m: 64 rows of 128 columns
     static constexpr int kRingB = 2 * kA * kHalf;
+    static constexpr bool kLate = true;
     const TrainWeights& a;
     const WeightsWork& c;
     uint8_t* lds;
@@ -584,6 +602,12 @@ struct WeightsTile {
     __device__ __forceinline__ void look_up() {
 #pragma unroll
         for (int k = 0; k < (GM ? 16 : 8); ++k) next[k] = tok[k];
+    }
+    __device__ __forceinline__ void look_up_rows() {
+        if (GM) look_up();
+    }
+    __device__ __forceinline__ void look_up_matrix() {
+        if (!GM) look_up();
     }
     // Where a token's row begins, worked out by the scalar unit.
     __device__ __forceinline__ uint32_t row_at(int i, uint32_t ld) const {
@@ -655,17 +679,20 @@ struct WeightsTile {
     }
     __device__ __forceinline__ void multiply() {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+        for (int g = 0; g < 16; ++g) {
+            const int kk = g / 8, i = g % 8;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j][i] = mfma16(fn[kk][j], fm[kk][i], acc[j][i]);
-                if (kk == 0 && i == 0) {     // (behind the first products: in front of them the wait for their operands would be one for the tokens too)
-                    pin_schedule();
-                    look_up();
-                    pin_schedule();
-                }
+            for (int to = 0; to < 4; ++to) {
+                const int j = g & 1 ? 3 - to : to;
+                acc[j][i] = mfma16(fn[kk][j], fm[kk][i], acc[j][i]);
             }
+            if (g % 4 == 0) {
+                pin_schedule();
+                if (g == 0) look_up_rows();
+                bring_matrix(g / 4);
+                pin_schedule();
+            }
+        }
     }
     __device__ __forceinline__ void write() {
         constexpr int W = 16 / sizeof(OUT), kLanes = 64 / W, kRows = 64 / kLanes;     // columns of a lane, lanes of a row, rows per instruction
