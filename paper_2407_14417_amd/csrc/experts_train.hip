@@ -474,8 +474,8 @@ __device__ __forceinline__ void rows_body(const TrainRows& a, const RowsWork& c,
 template <int FORM>
 __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, int n_tiles) {
     extern __shared__ uint8_t lds[];
-    // Workgroups go to the 8 XCDs in turn.  Each takes a run of neighbouring tiles of the chunks that are not split, eight chunks side by side, and then some columns of all the others, which
-    // are of many lengths.
+    // Workgroups go to the 8 XCDs in turn.  Each takes a run of neighbouring tiles of the chunks that are not split, up to eight chunks of one expert side by side (those that run at once share what
+    // they read in the XCD's L2), and then some columns of all the others, which are of many lengths.
     const TrainMeta* const meta = a.meta;
     const TrainSplit sp = FORM == kDown ? meta->down : FORM == kDRows ? meta->d_rows : meta->whole;
     const int first = sp.first_split, others = meta->n_chunks - first;
@@ -493,9 +493,15 @@ __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, in
         c.split = __builtin_amdgcn_readfirstlane(column / n_tiles);
         tile = column - c.split * n_tiles;
     } else {
-        const int group = t / (8 * n_tiles), rest = t - group * 8 * n_tiles, in_group = min(8, first - group * 8);
-        tile = rest / in_group;
-        chunk = group * 8 + rest - tile * in_group;
+        const int side = a.chunks[t / n_tiles].side, of = side >> 4, n = side & 15, rest = t - of * n_tiles;
+        tile = rest / n;
+        chunk = of + rest - tile * n;
+        // (a group that ends past the last chunk that is not split: its first ones, a column at a time)
+        if (of + n > first) {
+            const int here = first - of;
+            tile = rest / here;
+            chunk = of + rest - tile * here;
+        }
     }
     tile = __builtin_amdgcn_readfirstlane(tile);
     const TrainChunk ch = a.chunks[__builtin_amdgcn_readfirstlane(chunk)];
@@ -845,7 +851,7 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
             if (tid <= E) w.meta->offsets[tid] = o;
             if (tid < E) {
                 w.meta->order[rank] = tid;
-                if (rest) w.chunks[n_full + place] = TrainChunk{tid, end - rest, rest, 0};
+                if (rest) w.chunks[n_full + place] = TrainChunk{tid, end - rest, rest, (n_full + place) * 16 + 1};
             }
             if (tid == 0) {
                 w.meta->lo = o;
@@ -876,7 +882,10 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
         const int in_expert = r - off[e], rows = off[e + 1] - off[e], full = rows / kTrainRows;
         const int chunk = in_expert / kTrainRows < full ? first_full[e] + in_expert / kTrainRows : rest_place[e];
         w.shares[r] = (chunk >= split[0].first_split ? split[0].splits : 1) | (chunk >= split[1].first_split ? split[1].splits : 1) << 8;
-        if (in_expert % kTrainRows == 0 && chunk < counts[0]) w.chunks[chunk] = TrainChunk{e, r, kTrainRows, 0};
+        if (in_expert % kTrainRows == 0 && chunk < counts[0]) {
+            const int of = chunk - in_expert / kTrainRows % 8;
+            w.chunks[chunk] = TrainChunk{e, r, kTrainRows, of * 16 + min(8, first_full[e] + full - of)};
+        }
     }
     w.tok[r] = tok;
     w.gate[r] = gate;

@@ -11,7 +11,8 @@ constexpr int kTrainRows = 256;         // most rows of a tile
 
 // What the first launch of a call finds out about the grouping, whatever offsets and perm hold.
 struct TrainChunk {
-    int32_t expert, begin, rows, unused;   // grouped rows [begin, begin + rows)
+    int32_t expert, begin, rows;           // grouped rows [begin, begin + rows)
+    int32_t side;                          // full chunks: 16 times the first of the up to eight of its expert that go side by side, and how many these are
 };
 // Chunks are in an order of their own: those of kTrainRows rows by expert, then the experts' rests, the longest first.  Those from `first_split` on share their contraction among
 // `splits` workgroups each.
