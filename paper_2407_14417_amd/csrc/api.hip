@@ -1166,7 +1166,7 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
         r.K = f;
         launch_train_d_rows(r, st);
     }
-    if (d_x || d_gate) launch_train_gather(g, w, false, d, d_x, d_x_type == MOE_OUT_F16, d_gate, (f + kTrainCols - 1) / kTrainCols, st);
+    if (d_x || d_gate) launch_train_gather(g, w, false, d, d_x, d_x_type == MOE_OUT_F16, d_gate, f / 64, st);
     return check_hip(st);
 }
 

@@ -173,19 +173,34 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
 // ---- results
 
 // A wavefront's sums: lane l of tile (j, i) holds row l & 15 of 16 i .., columns 16 j + 4 (l >> 4) .. + 3.  Written as they lie, rows would go to memory in pieces of 32 bytes (fp16), which
-// took 30 000 cycles for 128 KB of a workgroup; so they are spread out as rows of 64 columns in 20 KB of LDS that the wavefront has for itself, 64 rows at a time.
-constexpr int kRegion = kLdsBytes / 8, kSpreadRow = 272;
+// took 30 000 cycles for 128 KB of a workgroup.  So the four j are exchanged among each four neighbouring lanes: afterwards v[k] of lane l is row (l & 12) + k, columns
+// 16 (l & 3) + 4 (l >> 4) .. + 3, and one instruction writes whole lines of four rows.
 
-template <int MT>
-__device__ __forceinline__ void spread(const float4_t (&acc)[4][MT], int i0, uint8_t* region, int lane) {
+// c odd (bit of the lane): `mine` stays in place of `theirs`
+template <int CTRL, typename V>
+__device__ __forceinline__ void exchange(bool odd, V& v0, V& v1) {
+    constexpr int N = sizeof(V) / 4;
+    typedef uint32_t words_t __attribute__((ext_vector_type(N)));
+    const words_t a = __builtin_bit_cast(words_t, v0), b = __builtin_bit_cast(words_t, v1);
+    words_t x, y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i0 + i < MT)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) *(float4_t*)(region + (i * 16 + (lane & 15)) * kSpreadRow + (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i0 + i];
-    wave_lds_handover();
+    for (int i = 0; i < N; ++i) {
+        const uint32_t ai = a[i], bi = b[i];
+        const uint32_t other_a = __builtin_amdgcn_update_dpp(0, ai, CTRL, 0xF, 0xF, true), other_b = __builtin_amdgcn_update_dpp(0, bi, CTRL, 0xF, 0xF, true);
+        x[i] = odd ? other_b : ai;
+        y[i] = odd ? bi : other_a;
+    }
+    v0 = __builtin_bit_cast(V, x);
+    v1 = __builtin_bit_cast(V, y);
 }
-__device__ __forceinline__ float4_t spread_at(const uint8_t* region, int row, int col) { return *(const float4_t*)(region + row * kSpreadRow + col * 4); }
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E;      // quad_perm: lanes 1 and 2 apart
+template <typename V>
+__device__ __forceinline__ void transpose4(int lane, V& v0, V& v1, V& v2, V& v3) {
+    exchange<kSwap1>(lane & 1, v0, v1);
+    exchange<kSwap1>(lane & 1, v2, v3);
+    exchange<kSwap2>(lane & 2, v0, v2);
+    exchange<kSwap2>(lane & 2, v1, v3);
+}
 
 // ---- products of rows
 
@@ -333,132 +348,113 @@ struct RowsTile {
     }
 
     __device__ __forceinline__ void write(uint8_t* lds) {
-        if (FORM == kUp) write_up(lds);
+        if (FORM == kUp) write_up();
         else if (FORM == kDHidden) write_d_hidden(lds);
-        else write_rows(lds);
+        else write_rows();
     }
 
-    // a, u and then h of the tile go through LDS, so that a row's 128 columns are written at once.
-    __device__ __forceinline__ void write_up(uint8_t* lds) {
-        constexpr int kRow = 272, kTile = 32 * MT * kRow;
-        const int r16 = lane & 15, q = lane >> 4;
-        uint8_t* const at = lds + (group * 16 * MT + r16) * kRow + (wn * 32 + 4 * q) * 2;
-        const int row0 = threadIdx.x >> 4, col = (threadIdx.x & 15) * 8;
-        const bool mine = c.n0 + col < a.N;
-        auto out = [&](half_t* to, int tile) {
+    // a and u together: their two tiles of 16 columns each make the four that are exchanged.  Then h: rows of 32 columns, two lanes exchange theirs.
+    __device__ __forceinline__ void write_up() {
+        const int n0 = c.n0 + wn * 32, N = a.N;
+        if (n0 >= N) return;
+        const int q = lane >> 4, r0 = group * 16 * MT;
+        half_t* const au = (lane & 2 ? a.u : a.a) + (size_t)c.begin * N + n0 + (lane & 1) * 16 + 4 * q;
+        half_t* const ph = a.h + (size_t)c.begin * N + n0 + (lane & 1) * 16 + 4 * q;
 #pragma unroll
-            for (int p = 0; p < MT; ++p) {
-                const int r = row0 + 32 * p;
-                if (r < c.rows && mine) *(half8_t*)(to + (size_t)(c.begin + r) * a.N + c.n0 + col) = *(const half8_t*)(lds + tile * kTile + r * kRow + col * 2);
+        for (int i = 0; i < MT; ++i) {
+            half4_t v[4], h[2];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j][k] = (half_t)acc[j][i][k];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) h[j][k] = (half_t)silu_mul(acc[j][i][k], acc[j + 2][i][k]);
             }
-        };
+            transpose4(lane, v[0], v[1], v[2], v[3]);
+            exchange<kSwap1>(lane & 1, h[0], h[1]);
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                half4_t va, vu;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    va[k] = (half_t)acc[j][i][k];
-                    vu[k] = (half_t)acc[j + 2][i][k];
-                }
-                *(half4_t*)(at + i * 16 * kRow + j * 32) = va;
-                *(half4_t*)(at + i * 16 * kRow + j * 32 + kTile) = vu;
+            for (int k = 0; k < 4; ++k) {
+                const int r = r0 + 16 * i + (lane & 12) + k;
+                if (r < c.rows) *(half4_t*)(au + (size_t)r * N) = v[k];
             }
-        __syncthreads();
-        out(a.a, 0);
-        out(a.u, 1);
-        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                half4_t vh;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) vh[k] = (half_t)silu_mul(acc[j][i][k], acc[j + 2][i][k]);
-                *(half4_t*)(at + i * 16 * kRow + j * 32) = vh;
+            for (int k = 0; k < 2; ++k) {
+                const int r = r0 + 16 * i + (lane & 14) + k;
+                if (r < c.rows) *(half4_t*)(ph + (size_t)r * N) = h[k];
             }
-        __syncthreads();
-        out(a.h, 0);
+        }
     }
 
-    // A wavefront turns its sums, up to 64 rows at a time, into whole lines of rows in LDS of its own: eight columns of eight rows per instruction.
+    // The operands' rings are free by now: a wavefront turns its sums, up to 64 rows at a time, into whole lines of rows in LDS of its own, eight columns of eight rows per instruction.
     __device__ __forceinline__ void write_d_hidden(uint8_t* lds) {
-        uint8_t* const region = lds + (4 * group + wn) * kRegion;
-        float* const shares = (float*)(region + 64 * kSpreadRow);            // of d_gate, for the wavefront's rows
-        const int N = a.N, col = c.n0 + wn * 64 + (lane & 7) * 8;
-        const bool any = c.n0 + wn * 64 < N;                                 // (64 divides N)
-        if (!any) {
-            for (int r = lane; r < 16 * MT; r += 64) shares[r] = 0.0f;
-        } else {
-#pragma unroll
-            for (int i0 = 0; i0 < MT; i0 += 4) {
-                constexpr int kMost = MT < 4 ? MT : 4;
-                half8_t va[2 * kMost], vu[2 * kMost];
-                float gate[2 * kMost];
-                const int r0 = (group * MT + i0) * 16 + (lane >> 3);
-#pragma unroll
-                for (int p = 0; p < 2 * kMost; ++p) {
-                    if (i0 * 2 + p >= 2 * MT) continue;
-                    const size_t row = (size_t)(c.begin + (r0 + 8 * p < c.rows ? r0 + 8 * p : 0));
-                    va[p] = *(const half8_t*)(a.a + row * N + col);
-                    vu[p] = *(const half8_t*)(a.u + row * N + col);
-                    gate[p] = a.gate[row];
-                }
-                spread<MT>(acc, i0, region, lane);
-#pragma unroll
-                for (int p = 0; p < 2 * kMost; ++p) {
-                    if (i0 * 2 + p >= 2 * MT) continue;
-                    const float4_t lo = spread_at(region, 8 * p + (lane >> 3), (lane & 7) * 8), hi = spread_at(region, 8 * p + (lane >> 3), (lane & 7) * 8 + 4);
-                    const float g = gate[p];
-                    half8_t da, du, gh;
-                    float share = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float x = (float)va[p][k], y = (float)vu[p][k], s = sigmoid(x), z = x * s, h = z * y, v = k < 4 ? lo[k & 3] : hi[k & 3];
-                        share = fmaf(v, h, share);
-                        du[k] = (half_t)(g * v * z);
-                        da[k] = (half_t)(g * v * y * (s * (1.0f + x * (1.0f - s))));
-                        gh[k] = (half_t)(g * h);
-                    }
-                    const int r = r0 + 8 * p;
-                    if (r < c.rows) {
-                        const size_t at = (size_t)(c.begin + r) * N + col;
-                        *(half8_t*)(a.d_a + at) = da;
-                        *(half8_t*)(a.d_u + at) = du;
-                        *(half8_t*)(a.h + at) = gh;
-                    }
-#pragma unroll
-                    for (int m = 1; m < 8; m <<= 1) share += __shfl_xor(share, m, kWave);
-                    if ((lane & 7) == 0) shares[i0 * 16 + 8 * p + (lane >> 3)] = share;
-                }
-                wave_lds_handover();
-            }
-        }
-        __syncthreads();
-        const int r = threadIdx.x;
-        if (r < c.rows) {
-            const int half = r / (16 * MT);
-            const float* const s = (const float*)(lds + 4 * half * kRegion + 64 * kSpreadRow) + r % (16 * MT);
-            constexpr int kNext = kRegion / 4;
-            a.part[(size_t)(c.n0 / kTrainCols) * a.P + c.begin + r] = (s[0] + s[kNext]) + (s[2 * kNext] + s[3 * kNext]);
-        }
-    }
-
-    __device__ __forceinline__ void write_rows(uint8_t* lds) {
-        if (c.n0 + wn * 64 >= a.N) return;
-        uint8_t* const region = lds + (4 * group + wn) * kRegion;
-        float* const y = a.y + (size_t)c.split * a.P * a.N + c.n0 + wn * 64 + (lane & 15) * 4;
+        constexpr int kRow = 272, kMost = MT < 4 ? MT : 4;
+        __syncthreads();                                     // (the rings are read no more)
+        uint8_t* const region = lds + (4 * group + wn) * (kLdsBytes / 8);
+        const int N = a.N, n0 = c.n0 + wn * 64, r8 = lane >> 3, c8 = (lane & 7) * 8;
+        if (n0 >= N) return;                                 // (64 divides N)
 #pragma unroll
         for (int i0 = 0; i0 < MT; i0 += 4) {
-            spread<MT>(acc, i0, region, lane);
+            half8_t va[2 * kMost], vu[2 * kMost];
+            float gate[2 * kMost];
+            const int r0 = (group * MT + i0) * 16 + r8;
 #pragma unroll
-            for (int p = 0; p < 16; ++p) {
-                if (i0 * 4 + p >= 4 * MT) continue;
-                const int r = (group * MT + i0) * 16 + 4 * p + (lane >> 4);
-                if (r < c.rows) *(float4_t*)(y + (size_t)(c.begin + r) * a.N) = spread_at(region, 4 * p + (lane >> 4), (lane & 15) * 4);
+            for (int p = 0; p < 2 * kMost; ++p) {
+                if (i0 * 2 + p >= 2 * MT) continue;
+                const size_t row = (size_t)(c.begin + (r0 + 8 * p < c.rows ? r0 + 8 * p : 0));
+                va[p] = *(const half8_t*)(a.a + row * N + n0 + c8);
+                vu[p] = *(const half8_t*)(a.u + row * N + n0 + c8);
+                gate[p] = a.gate[row];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i0 + i < MT)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *(float4_t*)(region + (i * 16 + (lane & 15)) * kRow + (j * 16 + 4 * (lane >> 4)) * 4) = acc[j][i0 + i];
+            wave_lds_handover();
+#pragma unroll
+            for (int p = 0; p < 2 * kMost; ++p) {
+                if (i0 * 2 + p >= 2 * MT) continue;
+                const float* const sums = (const float*)(region + (8 * p + r8) * kRow) + c8;
+                const float4_t lo = *(const float4_t*)sums, hi = *(const float4_t*)(sums + 4);
+                const float g = gate[p];
+                half8_t da, du, gh;
+                float share = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float x = (float)va[p][k], y = (float)vu[p][k], s = sigmoid(x), z = x * s, h = z * y, v = k < 4 ? lo[k & 3] : hi[k & 3];
+                    share = fmaf(v, h, share);
+                    du[k] = (half_t)(g * v * z);
+                    da[k] = (half_t)(g * v * y * (s * (1.0f + x * (1.0f - s))));
+                    gh[k] = (half_t)(g * h);
+                }
+                share += dpp_move<kSwap1>(share);
+                share += dpp_move<kSwap2>(share);
+                share += __shfl_xor(share, 4, kWave);
+                const int r = r0 + 8 * p;
+                if (r < c.rows) {
+                    const size_t at = (size_t)(c.begin + r) * N + n0 + c8;
+                    *(half8_t*)(a.d_a + at) = da;
+                    *(half8_t*)(a.d_u + at) = du;
+                    *(half8_t*)(a.h + at) = gh;
+                    if ((lane & 7) == 0) a.part[(size_t)(c.begin + r) * (N / 64) + n0 / 64] = share;
+                }
             }
             wave_lds_handover();
+        }
+    }
+
+    __device__ __forceinline__ void write_rows() {
+        if (c.n0 + wn * 64 >= a.N) return;
+        float* const y = a.y + ((size_t)c.split * a.P + c.begin) * a.N + c.n0 + wn * 64 + (lane & 3) * 16 + 4 * (lane >> 4);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            transpose4(lane, acc[0][i], acc[1][i], acc[2][i], acc[3][i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = group * 16 * MT + 16 * i + (lane & 12) + k;
+                if (r < c.rows) *(float4_t*)(y + (size_t)r * a.N) = acc[k][i];
+            }
         }
     }
 };
@@ -467,7 +463,6 @@ template <int FORM, int MT>
 __device__ __forceinline__ void rows_body(const TrainRows& a, const RowsWork& c, uint8_t* lds) {
     RowsTile<FORM, MT> t(a, c, lds);
     run_steps(t, c.s1 - c.s0, t.group);
-    __syncthreads();                     // (LDS is read no more)
     t.write(lds);
 }
 
@@ -519,7 +514,6 @@ __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, in
         case 4: rows_body<FORM, 4>(a, c, lds); break;
         case 5: rows_body<FORM, 5>(a, c, lds); break;
         case 6: rows_body<FORM, 6>(a, c, lds); break;
-        case 7: rows_body<FORM, 7>(a, c, lds); break;
         default: rows_body<FORM, 8>(a, c, lds);
     }
 }
@@ -701,35 +695,35 @@ struct WeightsTile {
         }
     }
     __device__ __forceinline__ void write() {
-        constexpr int W = 16 / sizeof(OUT), kLanes = 64 / W, kRows = 64 / kLanes;     // columns of a lane, lanes of a row, rows per instruction
-        typedef OUT wide_t __attribute__((ext_vector_type(W)));
+        typedef OUT out4_t __attribute__((ext_vector_type(4)));
         if (c.n0 + wn * 64 >= c.ln) return;
-        uint8_t* const region = lds + (4 * group + wn) * kRegion;
-        const int row0 = lane / kLanes, col = lane % kLanes * W;
-        OUT* const out = (OUT*)c.out + c.n0 + wn * 64 + col;
+        OUT* const out = (OUT*)c.out + c.n0 + wn * 64 + (lane & 3) * 16 + 4 * (lane >> 4);
 #pragma unroll
-        for (int i0 = 0; i0 < 8; i0 += 4) {
-            const int m0 = c.m0 + (group * 8 + i0) * 16 + row0;
-            wide_t before[64 / kRows];
-            if (a.accumulate)
+        for (int i = 0; i < 8; ++i) {
+            const int m = c.m0 + (group * 8 + i) * 16 + (lane & 12);
+            if (a.accumulate) {
+                transpose4(lane, acc[0][i], acc[1][i], acc[2][i], acc[3][i]);
+                out4_t before[4];
 #pragma unroll
-                for (int p = 0; p < 64 / kRows; ++p) before[p] = *(const wide_t*)(out + (size_t)min(m0 + p * kRows, c.lm - 1) * c.ln);
-            spread<8>(acc, i0, region, lane);
+                for (int k = 0; k < 4; ++k) before[k] = *(const out4_t*)(out + (size_t)min(m + k, c.lm - 1) * c.ln);
 #pragma unroll
-            for (int p = 0; p < 64 / kRows; ++p) {
-                wide_t w;
+                for (int k = 0; k < 4; ++k) {
+                    out4_t v;
 #pragma unroll
-                for (int k = 0; k < W; k += 4) {
-                    float4_t v = spread_at(region, p * kRows + row0, col + k);
-                    if (a.accumulate)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] += (float)before[p][k + i];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[k + i] = (OUT)v[i];
+                    for (int w = 0; w < 4; ++w) v[w] = (OUT)(acc[k][i][w] + (float)before[k][w]);
+                    if (m + k < c.lm) *(out4_t*)(out + (size_t)(m + k) * c.ln) = v;
                 }
-                if (m0 + p * kRows < c.lm) *(wide_t*)(out + (size_t)(m0 + p * kRows) * c.ln) = w;
+            } else {
+                out4_t v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v[j][w] = (OUT)acc[j][i][w];
+                transpose4(lane, v[0], v[1], v[2], v[3]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (m + k < c.lm) *(out4_t*)(out + (size_t)(m + k) * c.ln) = v[k];
             }
-            wave_lds_handover();
         }
     }
 };
@@ -761,7 +755,6 @@ __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights
     auto body = [&](auto gather_m) {
         WeightsTile<OUT, decltype(gather_m)::value> w(a, c, lds);
         if (c.rows) run_steps(w, (c.rows + kTrainStep - 1) / kTrainStep, w.group);
-        __syncthreads();                 // (LDS is read no more)
         w.write();
     };
     if (which == 2) body(std::true_type{});
@@ -924,12 +917,15 @@ __global__ __launch_bounds__(256) void train_gather_kernel(TrainGrouping g, Trai
             for (int k = 0; k < 4; ++k) o[k] = (OUT)sum[k];
             *(out4_t*)(out + (size_t)t * d + c) = o;
         }
-    if (d_gate && threadIdx.x < g.k) {
-        float sum = 0.0f;
-        if (row >= 0)
-            for (int i = 0; i < n_part; ++i) sum += w.part[(size_t)i * P + row];
-        d_gate[t * g.k + threadIdx.x] = sum;
-    }
+    if (d_gate)                                              // a wavefront per slot: its n_part shares lie side by side
+        for (int s = threadIdx.x >> 6; s < g.k; s += 4) {
+            const int r = __builtin_amdgcn_readlane(row, s);
+            float sum = 0.0f;
+            if (r >= 0)
+                for (int i = lane; i < n_part; i += 64) sum += w.part[(size_t)r * n_part + i];
+            sum = wave_sum(sum);
+            if (lane == 0) d_gate[t * g.k + s] = sum;
+        }
 }
 
 }  // namespace

@@ -39,7 +39,7 @@ struct TrainWorkspace {
     half_t* h;            // [P + 64, f]  hidden rows; backward: times the gate (d_weights reads whole steps of 64 rows)
     half_t* d_a;          // [P + 64, f]
     half_t* d_u;          // [P + 64, f]
-    float* part;          // [ceil(f / 256)][P]  shares of d_gate
+    float* part;          // [P][f / 64]  shares of d_gate
     float* y;             // [splits][P, d]  rows of the down-projection; backward: of d_x
     int splits;           // most of a chunk
     size_t bytes;
@@ -63,7 +63,7 @@ inline TrainWorkspace carve_train_workspace(void* base, int T, int d, int f, int
     w.h = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
     w.d_a = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
     w.d_u = (half_t*)take((P + kTrainStep) * f * sizeof(half_t));
-    w.part = (float*)take((size_t)((f + kTrainCols - 1) / kTrainCols) * P * sizeof(float));
+    w.part = (float*)take(P * (f / 64) * sizeof(float));
     w.y = (float*)take((size_t)splits * P * d * sizeof(float));
     w.splits = splits;
     w.bytes = off;
