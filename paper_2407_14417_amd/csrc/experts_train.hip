@@ -466,38 +466,40 @@ __device__ __forceinline__ void rows_body(const TrainRows& a, const RowsWork& c,
     t.write(lds);
 }
 
+// Workgroups go to the 8 XCDs in turn, each XCD with an L2 of its own and 32 compute units: n tiles are dealt out to the XCDs in blocks of 32 neighbours (fewer than 256 tiles: eight
+// blocks), so that those that run at once in an XCD share what they read, and that tiles of every length come to every XCD.
+__device__ __host__ __forceinline__ int block_of(int n) { return n >= 256 ? 32 : (n + 7) / 8; }
+__device__ __host__ __forceinline__ int slots_of(int n) {
+    const int block = block_of(n);
+    return block ? (n + 8 * block - 1) / (8 * block) * block : 0;
+}
+// (-1: none)
+__device__ __forceinline__ int place_in_blocks(int n, int slot, int xcd) {
+    const int block = block_of(n);
+    if (slot >= slots_of(n)) return -1;
+    const int round = slot / block, t = (round * 8 + xcd) * block + slot - round * block;
+    return t < n ? t : -1;
+}
+
 template <int FORM>
 __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, int n_tiles) {
     extern __shared__ uint8_t lds[];
-    // Workgroups go to the 8 XCDs in turn.  Each takes a run of neighbouring tiles of the chunks that are not split, up to eight chunks of one expert side by side (those that run at once share what
-    // they read in the XCD's L2), and then some columns of all the others, which are of many lengths.
     const TrainMeta* const meta = a.meta;
     const TrainSplit sp = FORM == kDown ? meta->down : FORM == kDRows ? meta->d_rows : meta->whole;
-    const int first = sp.first_split, others = meta->n_chunks - first;
-    const int n_a = first * n_tiles, n_b = others * n_tiles * sp.splits, per_a = (n_a + 7) >> 3, per_b = (n_b + 7) >> 3;
-    const int slot = blockIdx.x >> 3, xcd = blockIdx.x & 7;
-    const bool split = slot >= per_a;
-    const int t = split ? xcd * per_b + slot - per_a : xcd * per_a + slot;
-    if (split ? slot - per_a >= per_b || t >= n_b : t >= n_a) return;
+    const int first = sp.first_split, others = meta->n_chunks - first, n_a = first * n_tiles, units = others * n_tiles, n_b = units * sp.splits;
+    const int slot = blockIdx.x >> 3, xcd = blockIdx.x & 7, slots_a = slots_of(n_a);
+    const bool split = slot >= slots_a;
+    int t = split ? place_in_blocks(n_b, slot - slots_a, xcd) : place_in_blocks(n_a, slot, xcd);
+    if (t < 0) return;
     RowsWork c;
-    int tile, chunk;
-    c.split = 0;
-    if (split) {
-        const int column = t / others;
-        chunk = first + t - column * others;
-        c.split = __builtin_amdgcn_readfirstlane(column / n_tiles);
-        tile = column - c.split * n_tiles;
-    } else {
-        const int side = a.chunks[t / n_tiles].side, of = side >> 4, n = side & 15, rest = t - of * n_tiles;
-        tile = rest / n;
-        chunk = of + rest - tile * n;
-        // (a group that ends past the last chunk that is not split: its first ones, a column at a time)
-        if (of + n > first) {
-            const int here = first - of;
-            tile = rest / here;
-            chunk = of + rest - tile * here;
-        }
-    }
+    c.split = split ? __builtin_amdgcn_readfirstlane(t / units) : 0;
+    t -= c.split * units;
+    // up to eight chunks of one expert side by side, column after column (where a group reaches over the line between the split chunks and the others: its part)
+    const int chunk0 = (split ? first : 0) + t / n_tiles, side = a.chunks[chunk0].side;
+    const int of = max(side >> 4, split ? first : 0), n = min((side >> 4) + (side & 15), split ? first + others : first) - of;
+    const int rest = t - (of - (split ? first : 0)) * n_tiles;
+    int tile = rest / n;
+    const int chunk = of + rest - tile * n;
     tile = __builtin_amdgcn_readfirstlane(tile);
     const TrainChunk ch = a.chunks[__builtin_amdgcn_readfirstlane(chunk)];
     c.expert = __builtin_amdgcn_readfirstlane(ch.expert);
@@ -524,11 +526,11 @@ void launch_rows(const TrainRows& a, hipStream_t st) {
     const auto kernel = train_rows_kernel<FORM>;
     allow_lds((const void*)kernel, kLdsBytes, configured);
     constexpr int kOut = FORM == kUp ? kTrainCols / 2 : kTrainCols;
-    const int n_tiles = (a.N + kOut - 1) / kOut, full = a.P / kTrainRows, rests = a.E < a.P ? a.E : a.P;
-    // (as many full chunks as leave less than a round of workgroups may be split, and all rests: choose_splits)
-    const int splits = FORM == kDown || FORM == kDRows ? a.most_splits : 1, some = kComputeUnits / n_tiles + 1;
-    const long long most_a = (long long)full * n_tiles, most_b = (long long)((full < some ? full : some) + rests) * n_tiles * splits;
-    kernel<<<(unsigned)((most_a + 7) / 8 + (most_b + 7) / 8) * 8, kThreads, kLdsBytes, st>>>(a, n_tiles);
+    const int n_tiles = (a.N + kOut - 1) / kOut, most_chunks = a.P / kTrainRows + (a.E < a.P ? a.E : a.P);
+    // (fewer chunks than a round of workgroups, and one, are split: choose_splits)
+    const int most_a = most_chunks * n_tiles, most_b = FORM == kDown || FORM == kDRows ? ((int)kComputeUnits + n_tiles) * a.most_splits : 0;
+    const int slots = (most_a + 255) / 256 * 32 + (most_b + 255) / 256 * 32;
+    kernel<<<(unsigned)slots * 8, kThreads, kLdsBytes, st>>>(a, n_tiles);
 }
 
 // ---- gradients of the matrices
@@ -772,20 +774,16 @@ void launch_weights(const TrainWeights& a, hipStream_t st) {
 
 // ---- the grouping, and the rows of a token
 
-// Which chunks share their contraction, and among how many workgroups.  What fills whole rounds of the chip with full chunks is left alone; of the rest, which would leave most of it idle
-// or add a round, each is cut in s parts.  In units of a full tile's time (steps of the contraction at 2250 cycles): `cost` of all these tiles, the longest `most`; a workgroup's
-// beginning and end are 7.5 steps, a partial result is written and read back.  (4096 tokens, Mixtral shape, 37 chunks of 16 tiles: down 1091 -> XXX us, d_rows 1907 -> XXX.)
-__device__ TrainSplit choose_splits(int n_full, int n_rest, int rest_rows, int longest_rest, int n_tiles, int steps, int most_splits) {
-    const int n_chunks = n_full + n_rest, whole = n_full * n_tiles / (int)kComputeUnits * (int)kComputeUnits / n_tiles, left = n_full - whole;
+// Which chunks share their contraction, and among how many workgroups.  What fills whole rounds of the chip is left alone; of the rest, which would leave most of it idle
+// or add a round, each is cut in s parts.  In units of a full tile's time (steps of the contraction at 2250 cycles): `cost` of all tiles of the rest, the longest `most`; a workgroup's
+// beginning and end are 7.5 steps, a partial result is written and read back.
+__device__ TrainSplit choose_splits(int n_chunks, int whole, float chunk_cost, float most, int rows, int n_tiles, int steps, int most_splits) {
+    const int left = n_chunks - whole;
     TrainSplit best{n_chunks, 1};
-    if (left + n_rest == 0) return best;
-    const float cost = (float)n_tiles * ((float)left + 0.3f * (float)n_rest + 0.7f / kTrainRows * (float)rest_rows);
-    const float most = left ? 1.0f : 0.3f + 0.7f / kTrainRows * (float)longest_rest;
-    const float begin = 7.5f / (float)steps, partial = (float)(left * kTrainRows + rest_rows) * (float)n_tiles * 3e-4f / (float)steps;
+    const float cost = (float)n_tiles * chunk_cost, begin = 7.5f / (float)steps, partial = (float)rows * (float)n_tiles * 3e-4f / (float)steps;
     float least = 0.0f;
-    for (int s = 1; s <= most_splits && s <= steps; ++s) {
-        const int workgroups = (left + n_rest) * n_tiles * s;
-        const float rounds = (float)((workgroups + kComputeUnits - 1) / kComputeUnits);
+    for (int s = 1; s <= most_splits && s <= steps && left; ++s) {
+        const float rounds = (float)((left * n_tiles * s + kComputeUnits - 1) / kComputeUnits);
         const float time = (rounds == 1.0f ? most / (float)s : cost / kComputeUnits + 0.5f * most / (float)s) + rounds * begin + (float)(s - 1) * partial;
         if (s == 1 || time < 0.97f * least) {
             least = time;
@@ -796,11 +794,10 @@ __device__ TrainSplit choose_splits(int n_full, int n_rest, int rest_rows, int l
 }
 
 __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, TrainWorkspace w, int d, int f) {
-    __shared__ int32_t off[MOE_MAX_EXPERTS + 1], first_full[MOE_MAX_EXPERTS], rest_place[MOE_MAX_EXPERTS];
+    __shared__ int32_t off[MOE_MAX_EXPERTS + 1], first_chunk[MOE_MAX_EXPERTS], chunk_rows[MOE_MAX_EXPERTS];
     __shared__ TrainSplit split[2];
-    __shared__ int32_t counts[2];
     const int tid = threadIdx.x, P = g.T * g.k, E = g.E;
-    if (tid < 64) {
+    if (tid < 64) {                                          // lane e looks after expert e
         int o = g.offsets ? (tid <= E ? g.offsets[tid] : 0) : tid ? P : 0;
         o = min(max(o, 0), P);
 #pragma unroll
@@ -809,48 +806,39 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
             if (tid >= m) o = max(o, before);
         }
         const int begin = __shfl(o, tid < E ? tid : E, kWave), end = __shfl(o, tid < E ? tid + 1 : E, kWave);
-        const int rows = end - begin, rest = rows % kTrainRows;
-        int full = rows / kTrainRows, place = 0, rank = 0, sum = rest, n_rest = rest > 0, longest = rest;
+        const int rows = end - begin, fewest = (rows + kTrainRows - 1) / kTrainRows;
+        const int size = fewest ? (rows + 32 * fewest - 1) / (32 * fewest) * 32 : 0, chunks = size ? (rows + size - 1) / size : 0;
+        int first = 0, n_chunks = 0, rank = 0;
         for (int e = 0; e < E; ++e) {
-            const int r = __shfl(rest, e, kWave), n = __shfl(rows, e, kWave);
-            place += r > rest || (r == rest && e < tid);
-            rank += n > rows || (n == rows && e < tid);
+            const int s = __shfl(size, e, kWave), n = __shfl(chunks, e, kWave), r = __shfl(rows, e, kWave);
+            n_chunks += n;
+            if (s > size || (s == size && e < tid)) first += n;
+            rank += r > rows || (r == rows && e < tid);
         }
-        const int mine = full;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const int before = __shfl_up(full, m, kWave);
-            if (tid >= m) full += before;
-        }
-        const int n_full = __shfl(full, E - 1, kWave);
+        const int tiles = (d + kTrainCols - 1) / kTrainCols, whole = n_chunks * tiles / (int)kComputeUnits * (int)kComputeUnits / tiles;
+        // what is left of whole rounds: the lane's part
+        const int mine = chunks ? max(0, min(first + chunks, n_chunks) - max(first, whole)) : 0;
+        float cost = (float)mine * (0.25f + 0.75f / kTrainRows * (float)size), most = mine ? 0.25f + 0.75f / kTrainRows * (float)size : 0.0f;
+        int left_rows = mine * size;
 #pragma unroll
         for (int m = 32; m >= 1; m >>= 1) {
-            sum += __shfl_xor(sum, m, kWave);
-            n_rest += __shfl_xor(n_rest, m, kWave);
-            longest = max(longest, __shfl_xor(longest, m, kWave));
+            cost += __shfl_xor(cost, m, kWave);
+            most = fmaxf(most, __shfl_xor(most, m, kWave));
+            left_rows += __shfl_xor(left_rows, m, kWave);
         }
         if (tid <= E) off[tid] = o;
         if (tid < E) {
-            first_full[tid] = full - mine;
-            rest_place[tid] = n_full + place;
+            first_chunk[tid] = first;
+            chunk_rows[tid] = size;
         }
-        const int tiles = (d + kTrainCols - 1) / kTrainCols;
-        if (tid < 2) split[tid] = choose_splits(n_full, n_rest, sum, longest, tiles, f / kTrainStep * (tid + 1), w.splits);
-        if (tid == 0) {
-            counts[0] = n_full;
-            counts[1] = n_full + n_rest;
-        }
+        if (tid < 2) split[tid] = choose_splits(n_chunks, whole, cost, most, left_rows, tiles, f / kTrainStep * (tid + 1), w.splits);
         if (blockIdx.x == 0) {
             if (tid <= E) w.meta->offsets[tid] = o;
-            if (tid < E) {
-                w.meta->order[rank] = tid;
-                if (rest) w.chunks[n_full + place] = TrainChunk{tid, end - rest, rest, (n_full + place) * 16 + 1};
-            }
+            if (tid < E) w.meta->order[rank] = tid;
             if (tid == 0) {
                 w.meta->lo = o;
-                w.meta->n_full = n_full;
-                w.meta->n_chunks = n_full + n_rest;
-                w.meta->whole = TrainSplit{n_full, 1};
+                w.meta->n_chunks = n_chunks;
+                w.meta->whole = TrainSplit{n_chunks, 1};
             }
             if (tid == E) w.meta->hi = o;
         }
@@ -872,12 +860,11 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
         int e = 0;                                           // the last expert that begins at r or before, and has rows
         for (int m = MOE_MAX_EXPERTS / 2; m >= 1; m >>= 1)
             if (e + m < E && off[e + m] <= r) e += m;
-        const int in_expert = r - off[e], rows = off[e + 1] - off[e], full = rows / kTrainRows;
-        const int chunk = in_expert / kTrainRows < full ? first_full[e] + in_expert / kTrainRows : rest_place[e];
+        const int in_expert = r - off[e], rows = off[e + 1] - off[e], size = chunk_rows[e], c = in_expert / size, chunk = first_chunk[e] + c;
         w.shares[r] = (chunk >= split[0].first_split ? split[0].splits : 1) | (chunk >= split[1].first_split ? split[1].splits : 1) << 8;
-        if (in_expert % kTrainRows == 0 && chunk < counts[0]) {
-            const int of = chunk - in_expert / kTrainRows % 8;
-            w.chunks[chunk] = TrainChunk{e, r, kTrainRows, of * 16 + min(8, first_full[e] + full - of)};
+        if (in_expert == c * size) {                         // the chunk's first row
+            const int chunks = (rows + size - 1) / size, groups = (chunks + 7) / 8, abreast = (chunks + groups - 1) / groups, of = c / abreast * abreast;
+            w.chunks[chunk] = TrainChunk{e, r, min(size, rows - in_expert), (first_chunk[e] + of) * 16 + min(abreast, chunks - of)};
         }
     }
     w.tok[r] = tok;

@@ -12,16 +12,15 @@ constexpr int kTrainRows = 256;         // most rows of a tile
 // What the first launch of a call finds out about the grouping, whatever offsets and perm hold.
 struct TrainChunk {
     int32_t expert, begin, rows;           // grouped rows [begin, begin + rows)
-    int32_t side;                          // full chunks: 16 times the first of the up to eight of its expert that go side by side, and how many these are
+    int32_t side;                          // 16 times the first of the up to eight chunks of its expert that go side by side, and how many these are
 };
-// Chunks are in an order of their own: those of kTrainRows rows by expert, then the experts' rests, the longest first.  Those from `first_split` on share their contraction among
-// `splits` workgroups each.
+// An expert's chunks are as even as 32s of rows allow; the experts with the longest come first.  Those from `first_split` on share their contraction among `splits` workgroups each.
 struct TrainSplit {
     int32_t first_split, splits;
 };
 struct TrainMeta {
     int32_t lo, hi;                        // grouped rows [lo, hi) belong to an expert
-    int32_t n_chunks, n_full;
+    int32_t n_chunks, unused;
     TrainSplit whole, down, d_rows;        // of the launches that cannot be split, of down and of d_rows
     int32_t offsets[MOE_MAX_EXPERTS + 1];  // increasing, within [0, P]
     int32_t order[MOE_MAX_EXPERTS];        // experts, the one with most rows first
