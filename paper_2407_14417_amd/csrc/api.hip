@@ -1060,7 +1060,6 @@ TrainRows train_rows(const moe_layer* L, const TrainWorkspace& w, int T) {
     a.gate = w.gate;
     a.P = T * L->top_k;
     a.E = L->n_experts;
-    a.most_splits = w.splits;
     return a;
 }
 

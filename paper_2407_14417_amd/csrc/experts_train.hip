@@ -77,13 +77,13 @@ __device__ __forceinline__ float sigmoid(float a) { return 1.0f / (1.0f + __expf
 // straight into LDS, always of a step that lies ahead:
 //   phase 2k:      group 0 reads step k, asks for rows' half 1 of step k + nA - 1 and the first half of the matrix's unit of step k + nB - 1;  group 1 multiplies step k - 1
 //   phase 2k + 1:  group 1 reads step k, asks for rows' half 0 of step k + nA and the second half of the matrix's unit of step k + nB - 1;  group 0 multiplies step k
+// (past the last step the last one again, so that the waits can count).
 // Each half of the rows has a ring of nA units, the matrix one of nB; what is written then was read last in the phase before, or earlier.  A transfer has three phases or more
 // to arrive (nA = 2, nB = 3, 160 KB of LDS; with two phases for the matrix's side a step took 2400 cycles in place of 2048).
 // Transfers and reads go by turns: a transfer waits for its place in the compute unit's address path, 64 bytes per cycle for all wavefronts, and LDS delivers meanwhile.  (One after the
 // other 450 + 550 cycles.)  kLate: the matrix's transfers are asked for among the products that follow instead, and by group 1 a step further ahead: where both operands take transposed
 // reads, twice as many instructions, a phase of reading has no room for them (970 cycles with, backward of 4096 tokens in the Mixtral shape 5850 -> 5760 us; elsewhere they delay
 // the products: forward 2780 -> 2817).
-// Past the last step the last one is asked for again, so that the waits can count.
 //
 // What bounds it: 2048 cycles of products in the 2240 of a step; and power.  The clock falls to 1.4-1.5 GHz (8192 rows of one expert of 4096 x 14336, d_rows: 1390 us, 1.38 PFLOP/s; with operands
 // of zeros, the same instructions, 1028 us).  So what saves energy counts: two products in a row share an operand (g goes to and fro over j), 0.7-1 % of the time.
@@ -103,26 +103,27 @@ __device__ __forceinline__ void meet() {
 }
 
 // TILE: kA, kB (units of the rings), kRuns (transfers of a wavefront for its half of the rows; for its half of the matrix's unit it is four), kReads (operands of a step), kLate (multiply() calls
-// bring_matrix()), bring_rows(k), bring_matrix(k) (transfer k of the next stage), rows_asked(), matrix_asked() (all of a stage's have been made), look_up_rows(), look_up_matrix() (asks for
+// bring_matrix()), bring_rows(k), bring_matrix(k) (transfer k of the next stage), rows_asked(more), matrix_asked(more) (all of a stage's have been made; is there another one?), look_up_rows(), look_up_matrix() (asks for
 // what the next ones need), rows_there(step), matrix_there(step) (what the wavefront brought of a step has arrived and nobody reads it yet), read(r) (operand r of the next step),
 // step_read(), multiply().
 template <typename TILE>
 __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
     constexpr bool kLate = TILE::kLate;
-    constexpr int kA = TILE::kA, kB = TILE::kB, kRuns = TILE::kRuns, kPer = kRuns + 4;
+    constexpr int kA = TILE::kA, kB = TILE::kB, kRuns = TILE::kRuns, kPer = kRuns + 4, kTurns = kLate ? kRuns : kPer;
     static_assert(kA <= kB && kB <= kA + 1, "what follows counts on it");
     // transfers after those of the step that is read next
     constexpr int kRowsLate = (kA - 1) * kPer + (kLate ? 0 : 4), kMatrixLate = (kB - 2) * kPer, kMatrixLate1 = kMatrixLate + (kLate ? kRuns : 0);
+    const int rows_ahead = kA - 1 + group, matrix_ahead = kB - 1 + (kLate ? group : 0);
     for (int k = -kB; k < 0; ++k) {
-        if (k + kA - 1 + group >= 0) {
+        if (k + rows_ahead >= 0) {
 #pragma unroll
             for (int i = 0; i < kRuns; ++i) t.bring_rows(i);
-            t.rows_asked();
+            t.rows_asked(k + rows_ahead + 1 < n);
         }
-        if (k + kB - 1 + (kLate ? group : 0) >= 0) {
+        if (k + matrix_ahead >= 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) t.bring_matrix(i);
-            t.matrix_asked();
+            t.matrix_asked(k + matrix_ahead + 1 < n);
         }
         t.look_up_rows();
         t.look_up_matrix();
@@ -134,7 +135,6 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
     if (group) meet();
     for (int k = 0; k < n; ++k) {
         t.look_up_matrix();
-        constexpr int kTurns = kLate ? kRuns : kPer;
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
             if (i < kRuns) t.bring_rows(i);
@@ -142,17 +142,13 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
 #pragma unroll
             for (int r = i * TILE::kReads / kTurns; r < (i + 1) * TILE::kReads / kTurns; ++r) t.read(r);
         }
-        t.rows_asked();
-        if (!kLate) t.matrix_asked();
+        t.rows_asked(k + rows_ahead + 1 < n);
+        if (!kLate) t.matrix_asked(k + matrix_ahead + 1 < n);
         t.step_read();
-        if (group) {
-            wait_transfers<kRowsLate < kMatrixLate1 ? kRowsLate : kMatrixLate1>();
-            t.rows_there(k + 1);
-            t.matrix_there(k + 1);
-        } else {
-            wait_transfers<kRowsLate>();
-            t.rows_there(k);
-        }
+        if (group) wait_transfers<kRowsLate < kMatrixLate1 ? kRowsLate : kMatrixLate1>();
+        else wait_transfers<kRowsLate>();
+        t.rows_there(k + group);
+        if (group) t.matrix_there(k + 1);
         pin_schedule();
         meet();
         pin_schedule();
@@ -160,7 +156,7 @@ __device__ __forceinline__ void run_steps(TILE& t, int n, int group) {
         t.multiply();
         __builtin_amdgcn_s_setprio(0);
         pin_schedule();
-        if (kLate) t.matrix_asked();
+        if (kLate) t.matrix_asked(k + matrix_ahead + 1 < n);
         if (!group) {
             wait_transfers<kMatrixLate>();
             t.matrix_there(k + 1);
@@ -225,7 +221,7 @@ struct RowsTile {
     int lane, group, wn;
     gptr_t base_a, base_b;
     uint32_t va[kRuns], vb[4];
-    int left_a, left_b;                             // steps to bring after the next one
+    int step_a, step_b;                             // d_rows: the next one to bring
     uint32_t ra[2], rb[kColumns ? 4 : 2];
     float4_t acc[4][MT];
     half8_t fa[2][MT], fb[2][4];
@@ -273,7 +269,7 @@ struct RowsTile {
         put_a = lds0 + (1 - group) * kA * kHalf;
         get_a = lds0 + group * kA * kHalf;
         put_b = get_b = lds0 + kRingB;
-        left_a = left_b = c.s1 - c.s0 - 1;
+        step_a = step_b = c.s0;
         seek_rows(c.s0);
         seek_matrix(c.s0);
     }
@@ -296,22 +292,20 @@ struct RowsTile {
     }
 
     __device__ __forceinline__ void bring_rows(int k) { moemix::bring<0>(put_a + run_of(k) * 1024, base_a, va[k]); }
-    __device__ __forceinline__ void rows_asked() {
+    __device__ __forceinline__ void rows_asked(bool more) {
         const uint32_t ring = lds0 + (1 - group) * kA * kHalf;
         put_a = put_a == ring + (kA - 1) * kHalf ? ring : put_a + kHalf;
-        if (left_a <= 0) return;
-        --left_a;
-        if (FORM == kDRows && c.s1 - 1 - left_a == steps_of_one()) seek_rows(steps_of_one());
+        if (!more) return;
+        if (FORM == kDRows && ++step_a == steps_of_one()) seek_rows(step_a);
         else base_a += kTrainStep * 2;
     }
     __device__ __forceinline__ void bring_matrix(int k) {
         moemix::bring<0>(put_b + group * (kUnit / 2) + wn * (kColumns ? 4096 : 1024) + k * (kColumns ? 1024 : 4096), base_b, vb[k]);
     }
-    __device__ __forceinline__ void matrix_asked() {
+    __device__ __forceinline__ void matrix_asked(bool more) {
         put_b = put_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : put_b + kUnit;
-        if (left_b <= 0) return;
-        --left_b;
-        if (FORM == kDRows && c.s1 - 1 - left_b == steps_of_one()) seek_matrix(steps_of_one());
+        if (!more) return;
+        if (FORM == kDRows && ++step_b == steps_of_one()) seek_matrix(step_b);
         else base_b += kColumns ? (size_t)a.N * (kTrainStep * 2) : kTrainStep * 2;
     }
     __device__ __forceinline__ void look_up_rows() {}
@@ -481,6 +475,8 @@ __device__ __forceinline__ int place_in_blocks(int n, int slot, int xcd) {
     return t < n ? t : -1;
 }
 
+constexpr int kMostSplit = 512;          // workgroups of split chunks
+
 template <int FORM>
 __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, int n_tiles) {
     extern __shared__ uint8_t lds[];
@@ -494,17 +490,16 @@ __global__ __launch_bounds__(kThreads, 2) void train_rows_kernel(TrainRows a, in
     RowsWork c;
     c.split = split ? __builtin_amdgcn_readfirstlane(t / units) : 0;
     t -= c.split * units;
-    // up to eight chunks of one expert side by side, column after column (where a group reaches over the line between the split chunks and the others: its part)
-    const int chunk0 = (split ? first : 0) + t / n_tiles, side = a.chunks[chunk0].side;
-    const int of = max(side >> 4, split ? first : 0), n = min((side >> 4) + (side & 15), split ? first + others : first) - of;
-    const int rest = t - (of - (split ? first : 0)) * n_tiles;
-    int tile = rest / n;
-    const int chunk = of + rest - tile * n;
-    tile = __builtin_amdgcn_readfirstlane(tile);
-    const TrainChunk ch = a.chunks[__builtin_amdgcn_readfirstlane(chunk)];
+    // up to eight chunks of one expert side by side, column after column (where a group reaches over the line between the split chunks and the others: its part); what any of
+    // them says tells of all
+    const int zero = split ? first : 0, chunk0 = __builtin_amdgcn_readfirstlane(zero + t / n_tiles);
+    const TrainChunk ch = a.chunks[chunk0];
+    const int start = chunk0 - (ch.form >> 4 & 15), size = (ch.form & 15) * 32;
+    const int of = max(start, zero), n = min(start + (ch.form >> 8), split ? first + others : first) - of, rest = t - (of - zero) * n_tiles;
+    const int tile = __builtin_amdgcn_readfirstlane(rest / n);
     c.expert = __builtin_amdgcn_readfirstlane(ch.expert);
-    c.begin = __builtin_amdgcn_readfirstlane(ch.begin);
-    c.rows = __builtin_amdgcn_readfirstlane(ch.rows);
+    c.begin = __builtin_amdgcn_readfirstlane(ch.begin + (of + rest - tile * n - chunk0) * size);
+    c.rows = __builtin_amdgcn_readfirstlane(min(size, ch.end - c.begin));
     c.n0 = tile * (FORM == kUp ? kTrainCols / 2 : kTrainCols);
     const int steps = a.K / kTrainStep * (FORM == kDRows ? 2 : 1), shares = split ? sp.splits : 1;
     c.s0 = __builtin_amdgcn_readfirstlane(steps * c.split / shares);
@@ -527,8 +522,7 @@ void launch_rows(const TrainRows& a, hipStream_t st) {
     allow_lds((const void*)kernel, kLdsBytes, configured);
     constexpr int kOut = FORM == kUp ? kTrainCols / 2 : kTrainCols;
     const int n_tiles = (a.N + kOut - 1) / kOut, most_chunks = a.P / kTrainRows + (a.E < a.P ? a.E : a.P);
-    // (fewer chunks than a round of workgroups, and one, are split: choose_splits)
-    const int most_a = most_chunks * n_tiles, most_b = FORM == kDown || FORM == kDRows ? ((int)kComputeUnits + n_tiles) * a.most_splits : 0;
+    const int most_a = most_chunks * n_tiles, most_b = FORM == kDown || FORM == kDRows ? kMostSplit : 0;
     const int slots = (most_a + 255) / 256 * 32 + (most_b + 255) / 256 * 32;
     kernel<<<(unsigned)slots * 8, kThreads, kLdsBytes, st>>>(a, n_tiles);
 }
@@ -558,7 +552,6 @@ struct WeightsTile {
     const_ints_t tok;                    // tokens of the rows that are brought next of the gathered operand: 16 of m, 8 of n
     int next[GM ? 16 : 8];               // the same, asked for a phase before they are used
     uint32_t va[4], vb[4];               // gathered: what the lane brings of a row
-    int left_a, left_b;
     uint32_t at_m, at_n;
     float4_t acc[4][8];
     half8_t fm[2][8], fn[2][4];
@@ -591,7 +584,6 @@ struct WeightsTile {
         put_a = lds0 + (1 - group) * kA * kHalf;
         get_a = lds0 + group * kA * kHalf;
         put_b = get_b = lds0 + kRingB;
-        left_a = left_b = (c.rows + kTrainStep - 1) / kTrainStep - 1;
         const int row = 8 * (lane >> 4) + ((lane & 15) >> 2);
         at_m = row * 256 + (lane & 3) * 8 + (half_swizzle(row) << 5);
         at_n = columns_at(lane, 4 * wn);
@@ -627,11 +619,10 @@ struct WeightsTile {
         }
         moemix::bring<0>(put_a + wn * 4096 + k * 1024, base_a, v);
     }
-    __device__ __forceinline__ void rows_asked() {
+    __device__ __forceinline__ void rows_asked(bool more) {
         const uint32_t ring = lds0 + (1 - group) * kA * kHalf;
         put_a = put_a == ring + (kA - 1) * kHalf ? ring : put_a + kHalf;
-        if (left_a <= 0) return;
-        --left_a;
+        if (!more) return;
         if (GM) tok += kTrainStep;
         else base_a += (size_t)ld_a * kTrainStep;
     }
@@ -643,10 +634,9 @@ struct WeightsTile {
         }
         moemix::bring<0>(put_b + group * (kUnit / 2) + wn * 4096 + k * 1024, base_b, v);
     }
-    __device__ __forceinline__ void matrix_asked() {
+    __device__ __forceinline__ void matrix_asked(bool more) {
         put_b = put_b == lds0 + kRingB + (kB - 1) * kUnit ? lds0 + kRingB : put_b + kUnit;
-        if (left_b <= 0) return;
-        --left_b;
+        if (!more) return;
         if (!GM) tok += kTrainStep;
         else base_b += (size_t)ld_b * kTrainStep;
     }
@@ -777,20 +767,25 @@ void launch_weights(const TrainWeights& a, hipStream_t st) {
 // Which chunks share their contraction, and among how many workgroups.  What fills whole rounds of the chip is left alone; of the rest, which would leave most of it idle
 // or add a round, each is cut in s parts.  In units of a full tile's time (steps of the contraction at 2250 cycles): `cost` of all tiles of the rest, the longest `most`; a workgroup's
 // beginning and end are 7.5 steps, a partial result is written and read back.
-__device__ TrainSplit choose_splits(int n_chunks, int whole, float chunk_cost, float most, int rows, int n_tiles, int steps, int most_splits) {
-    const int left = n_chunks - whole;
-    TrainSplit best{n_chunks, 1};
-    const float cost = (float)n_tiles * chunk_cost, begin = 7.5f / (float)steps, partial = (float)rows * (float)n_tiles * 3e-4f / (float)steps;
-    float least = 0.0f;
-    for (int s = 1; s <= most_splits && s <= steps && left; ++s) {
-        const float rounds = (float)((left * n_tiles * s + kComputeUnits - 1) / kComputeUnits);
-        const float time = (rounds == 1.0f ? most / (float)s : cost / kComputeUnits + 0.5f * most / (float)s) + rounds * begin + (float)(s - 1) * partial;
-        if (s == 1 || time < 0.97f * least) {
-            least = time;
-            best = TrainSplit{s == 1 ? n_chunks : whole, s};
+// Lane l < 32 of a wavefront reckons with l % 16 + 1 parts, for down (l < 16) or d_rows.
+__device__ TrainSplit choose_splits(int lane, int n_chunks, int whole, float chunk_cost, float most, int rows, int n_tiles, int steps, int most_splits) {
+    const int s = (lane & 15) + 1, left = n_chunks - whole, workgroups = left * n_tiles * s;
+    const float parts = __builtin_amdgcn_rcpf((float)s), step = __builtin_amdgcn_rcpf((float)steps);
+    const float rounds = (float)((workgroups + kComputeUnits - 1) / kComputeUnits), partial = ((float)rows * (float)n_tiles * 3e-4f + 0.15f) * step;
+    float time = (rounds == 1.0f ? most * parts : (float)n_tiles * chunk_cost / kComputeUnits + 0.5f * most * parts) + rounds * 7.5f * step + (float)(s - 1) * partial;
+    if (s > 1) time *= 1.03f;                                // (worth it only if it is more than nothing)
+    if (s > most_splits || s > steps || (s > 1 && workgroups > kMostSplit)) time = 1e30f;
+    int best = s;
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) {
+        const float other = __shfl_xor(time, m, kWave);
+        const int other_s = __shfl_xor(best, m, kWave);
+        if (other < time || (other == time && other_s < best)) {
+            time = other;
+            best = other_s;
         }
     }
-    return best;
+    return best == 1 || !left ? TrainSplit{n_chunks, 1} : TrainSplit{whole, best};
 }
 
 __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, TrainWorkspace w, int d, int f) {
@@ -810,7 +805,7 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
         const int size = fewest ? (rows + 32 * fewest - 1) / (32 * fewest) * 32 : 0, chunks = size ? (rows + size - 1) / size : 0;
         int first = 0, n_chunks = 0, rank = 0;
         for (int e = 0; e < E; ++e) {
-            const int s = __shfl(size, e, kWave), n = __shfl(chunks, e, kWave), r = __shfl(rows, e, kWave);
+            const int s = __builtin_amdgcn_readlane(size, e), n = __builtin_amdgcn_readlane(chunks, e), r = __builtin_amdgcn_readlane(rows, e);
             n_chunks += n;
             if (s > size || (s == size && e < tid)) first += n;
             rank += r > rows || (r == rows && e < tid);
@@ -831,8 +826,11 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
             first_chunk[tid] = first;
             chunk_rows[tid] = size;
         }
-        if (tid < 2) split[tid] = choose_splits(n_chunks, whole, cost, most, left_rows, tiles, f / kTrainStep * (tid + 1), w.splits);
+        const TrainSplit chosen = choose_splits(tid, n_chunks, whole, cost, most, left_rows, tiles, f / kTrainStep * (tid < 16 ? 1 : 2), w.splits);
+        if (tid == 0 || tid == 16) split[tid >> 4] = chosen;
         if (blockIdx.x == 0) {
+            if (tid == 0) w.meta->down = chosen;
+            if (tid == 16) w.meta->d_rows = chosen;
             if (tid <= E) w.meta->offsets[tid] = o;
             if (tid < E) w.meta->order[rank] = tid;
             if (tid == 0) {
@@ -844,7 +842,6 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
         }
     }
     __syncthreads();
-    if (blockIdx.x == 0 && tid < 2) (tid ? w.meta->d_rows : w.meta->down) = split[tid];
     const int lo = off[0], hi = off[E];
     const int r = blockIdx.x * 256 + tid;
     if (r >= P + kTrainStep) return;
@@ -863,8 +860,8 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
         const int in_expert = r - off[e], rows = off[e + 1] - off[e], size = chunk_rows[e], c = in_expert / size, chunk = first_chunk[e] + c;
         w.shares[r] = (chunk >= split[0].first_split ? split[0].splits : 1) | (chunk >= split[1].first_split ? split[1].splits : 1) << 8;
         if (in_expert == c * size) {                         // the chunk's first row
-            const int chunks = (rows + size - 1) / size, groups = (chunks + 7) / 8, abreast = (chunks + groups - 1) / groups, of = c / abreast * abreast;
-            w.chunks[chunk] = TrainChunk{e, r, min(size, rows - in_expert), (first_chunk[e] + of) * 16 + min(abreast, chunks - of)};
+            const int chunks = (rows + size - 1) / size, groups = (chunks + 7) / 8, most = (chunks + groups - 1) / groups, of = c / most * most;
+            w.chunks[chunk] = TrainChunk{e, r, off[e + 1], size / 32 + (c - of) * 16 + min(most, chunks - of) * 256};
         }
     }
     w.tok[r] = tok;
@@ -896,7 +893,14 @@ __global__ __launch_bounds__(256) void train_gather_kernel(TrainGrouping g, Trai
                 if (r < 0) continue;
                 const float* const y = w.y + (size_t)r * d + c;
                 float4_t v = *(const float4_t*)y;
-                for (int p = 1; p < n; ++p) v += *(const float4_t*)(y + (size_t)p * P * d);
+                for (int p0 = 1; p0 < n; p0 += 4) {          // (four asked for at once)
+                    float4_t part[4];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) part[p] = *(const float4_t*)(y + (size_t)min(p0 + p, n - 1) * P * d);
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        if (p0 + p < n) v += part[p];
+                }
                 sum += __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, gate), s)) * v;
             }
             out4_t o;

@@ -10,9 +10,10 @@ constexpr int kTrainCols = 256;         // columns of a tile
 constexpr int kTrainRows = 256;         // most rows of a tile
 
 // What the first launch of a call finds out about the grouping, whatever offsets and perm hold.
+// Chunk i is rows [begin, min(begin + size, end)) of the grouped rows; up to eight chunks of an expert go side by side: i is number `at` of `abreast`.
 struct TrainChunk {
-    int32_t expert, begin, rows;           // grouped rows [begin, begin + rows)
-    int32_t side;                          // 16 times the first of the up to eight chunks of its expert that go side by side, and how many these are
+    int32_t expert, begin, end;
+    int32_t form;                          // size / 32 + 16 at + 256 abreast
 };
 // An expert's chunks are as even as 32s of rows allow; the experts with the longest come first.  Those from `first_split` on share their contraction among `splits` workgroups each.
 struct TrainSplit {
@@ -95,7 +96,6 @@ struct TrainRows {
     const int32_t* tok;
     const float* gate;
     int N, K, P, E;
-    int most_splits;           // of a chunk's contraction
 };
 
 // Gradients of the matrices: for expert e  w1 = d_a^T x, w3 = d_u^T x, w2 = d_out^T h.  Null: not asked for.
