@@ -357,7 +357,7 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
  * offsets: device int32 [n_experts + 1], NULL (one expert only): all P rows are its; perm: device int32 [P], NULL: row r is pair r.  (Whatever offsets and perm
  * hold, nothing outside the arrays is read or written.)
  * d_x: device, fp32 or fp16 (d_x_type, a moe_out) [T, d_model]; d_gate: device fp32 [T, top_k]; d_w: HOST array [n_experts] of the matrices' gradients,
- * device, all fp32 or all fp16 (d_w_type), of the matrices' shapes, a NULL entry is not asked for.  Each of d_x, d_gate and d_w may be NULL, not all.  accumulate != 0:
+ * device, all fp32 or all fp16 (d_w_type), of the matrices' shapes, none over another (MOE_EINVAL), a NULL entry is not asked for.  Each of d_x, d_gate and d_w may be NULL, not all.  accumulate != 0:
  * the gradients of the matrices are added to what is there (and an expert without rows leaves its as they are).  The same inputs give the same bits.
  * Tensors start on 16-byte boundaries (d_gate, topk_gate, offsets and perm: 4).  layer->w_gate and gate_bias are not looked at.
  * T >= 1, T * d_model <= 2^31 - 2048, T * top_k <= 2^22 (MOE_ESHAPE otherwise).  ws: moe_experts_workspace_bytes(layer, T) bytes, or what these were for more tokens (a
@@ -378,7 +378,7 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
  *   norm = unscale * sqrt( sum v^2 ),   out = v * c  with  c = unscale * min(1, max_norm / (norm + 1e-6))
  * Sums are held in 64 bits.  unscale: finite, > 0, 1 / loss scale; max_norm: >= 0, INFINITY: no limit.  If norm is not finite in 32 bits (a gradient was
  * not) only norm is written: the caller leaves out the step.
- * grads: HOST array of at most MOE_MAX_GRADS entries.  grad, out: device, fp32 or fp16 (a moe_out), on the boundary of their type, n elements (n < 2^40, 0: none);
+ * grads: HOST array of at most MOE_MAX_GRADS entries.  grad, out: device, fp32 or fp16 (a moe_out), on the boundary of their type, n elements (n < 2^38, 0: none);
  * out may be grad (with the same type); apart from that no out may overlap another out or a grad (MOE_EINVAL).
  * norm: device fp32 [1].  ws: at least moe_clip_workspace_bytes(n_tensors).  The same inputs give the same bits.
  */

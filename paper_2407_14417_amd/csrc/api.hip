@@ -1129,6 +1129,15 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
         g_w.w2[e] = d_w[e].w2;
         any |= d_w[e].w1 || d_w[e].w3 || d_w[e].w2;
     }
+    // workgroups of different matrices run side by side
+    uintptr_t at[3 * MOE_MAX_EXPERTS];
+    int n = 0;
+    for (int e = 0; e < E; ++e)
+        for (void* const m : {g_w.w1[e], g_w.w3[e], g_w.w2[e]})
+            if (m) at[n++] = (uintptr_t)m;
+    std::sort(at, at + n);
+    for (int i = 1; i < n; ++i)
+        if (at[i] - at[i - 1] < (size_t)d * f * (d_w_type == MOE_OUT_F16 ? 2 : 4)) return fail(MOE_EINVAL, "%s: gradients of matrices overlap", who);
     hipStream_t st = (hipStream_t)stream;
     const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
     launch_train_group(g, w, d, f, st);
@@ -1232,7 +1241,7 @@ int moe_clip_gradients(const moe_grad* grads, int n_tensors, float max_norm, flo
         const moe_grad& g = grads[i];
         if ((g.grad_type != MOE_OUT_F32 && g.grad_type != MOE_OUT_F16) || (g.out_type != MOE_OUT_F32 && g.out_type != MOE_OUT_F16))
             return fail(MOE_EINVAL, "%s: tensor %d: grad_type=%d, out_type=%d", who, i, g.grad_type, g.out_type);
-        if (g.n >= 1ull << 40) return fail(MOE_ESHAPE, "%s: tensor %d: %zu elements", who, i, g.n);
+        if (g.n >= 1ull << 38) return fail(MOE_ESHAPE, "%s: tensor %d: %zu elements", who, i, g.n);
         if (!g.n) continue;
         if (!g.grad || !g.out) return fail(MOE_EINVAL, "%s: tensor %d is NULL", who, i);
         if (misaligned(g.grad, g.grad_type == MOE_OUT_F16 ? 2 : 4) || misaligned(g.out, g.out_type == MOE_OUT_F16 ? 2 : 4))
@@ -1244,7 +1253,7 @@ int moe_clip_gradients(const moe_grad* grads, int n_tensors, float max_norm, flo
     if (ws_bytes < moe_clip_workspace_bytes(n_tensors))
         return fail(MOE_EWORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, moe_clip_workspace_bytes(n_tensors));
     hipStream_t st = (hipStream_t)stream;
-    // tables of up to kClipMost tensors, each with at most 2^31 chunks
+    // tables of up to kClipMost tensors, with less than 2^31 chunks together
     auto table = [&](int first, ClipTable& t) {
         memset(&t, 0, sizeof(t));
         for (int i = first; i < n_tensors && i < first + kClipMost; ++i) {
@@ -1257,15 +1266,22 @@ int moe_clip_gradients(const moe_grad* grads, int n_tensors, float max_norm, flo
         }
     };
     ClipTable t;
+    table(0, t);
+    unsigned long long elements = 0;
+    for (int i = 0; i < n_tensors; ++i) elements += grads[i].n;
+    if (n_tensors <= kClipMost && t.first[t.n] <= kClipAloneChunks && elements <= kClipAloneSize) {
+        launch_clip_alone(t, max_norm, unscale, norm, st);
+        return check_hip(st);
+    }
     double* const part = (double*)ws;
     int n_part = 0;
     for (int i = 0; i < n_tensors; i += kClipMost) {
-        table(i, t);
+        if (i) table(i, t);
         launch_clip_sums(t, part + n_part, st);
         n_part += clip_blocks(t);
     }
-    for (int i = 0; i < n_tensors || i == 0; i += kClipMost) {
-        if (n_tensors > kClipMost || n_tensors == 0) table(i, t);
+    for (int i = 0; i < n_tensors; i += kClipMost) {
+        if (n_tensors > kClipMost) table(i, t);
         launch_clip_scale(t, part, n_part, max_norm, unscale, i == 0 ? norm : nullptr, st);
     }
     return check_hip(st);

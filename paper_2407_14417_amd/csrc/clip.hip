@@ -2,10 +2,11 @@
 //
 //   norm = unscale sqrt(sum over all elements of v^2),  c = unscale min(1, max_norm / (norm + 1e-6)),  out = c v
 //
-// Two launches for up to 96 tensors: sums of squares, one per workgroup, then the product, before which every workgroup adds all the sums in the same order (16 KB
+// A list of a few thousand elements is done by one workgroup.  Else two launches for up to 96 tensors: sums of squares, one per workgroup, then the product, before which every workgroup adds all the sums in the same order (16 KB
 // from L2 at most).  Sums are held in 64 bits: squares of fp32 gradients leave the range of 32, and billions of them their precision; two
 // 64-bit instructions per element are a twentieth of what the vector units do in the time that its load takes.
-// Bound: every gradient is read twice, since the norm has to be known before the first is scaled.
+// Bound: every gradient is read twice, since the norm has to be known before the first is scaled (24 tensors of 4096 x 14336 in fp32: 16.9 GB in 3260 us, 5.2 TB/s; 48 of
+// 2048 x 1408 from fp16 to fp32, the second read mostly from the last-level cache: 257 us).
 #include "clip.hpp"
 #include "kernels.hpp"
 
@@ -24,39 +25,46 @@ __device__ __forceinline__ int tensor_of(const ClipTable& t, uint32_t c) {
     return lo;
 }
 
-// Sum of one value of each of 256 threads, the same in all of them.
-__device__ __forceinline__ double block_total(double v, double* lds) {
+// Sum of one value of each thread, the same in all of them.
+template <int THREADS>
+__device__ __forceinline__ double block_total(double v) {
+    __shared__ double lds[THREADS / 64];
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, kWave);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    double sum = lds[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 64; ++i) sum += lds[i];
+    return sum;
 }
 
-// f(i, v) for 16 bytes of values from element i on, f1(i) for single ones at the end; everything with f1 where the tensor is not on a 16-byte boundary.
+// What a group of 256 threads does with a chunk: f(i) for 16 bytes of values from element i on, f1(i) for single ones at the end; everything with f1 where the tensor is not
+// on a 16-byte boundary.
 template <typename IN, typename F, typename F1>
-__device__ __forceinline__ void each(bool wide, unsigned long long n, unsigned long long begin, unsigned long long end, F f, F1 f1) {
+__device__ __forceinline__ void each(bool wide, unsigned long long begin, unsigned long long end, F f, F1 f1) {
     constexpr int W = 16 / sizeof(IN);
+    const int tid = threadIdx.x & 255;
     unsigned long long at = begin;
     if (wide) {
         const unsigned long long whole = begin + (end - begin) / W * W;
         if (end - begin == kClipChunk) {
 #pragma unroll 4
-            for (int i = 0; i < kClipChunk / (256 * W); ++i) f(begin + (unsigned long long)(i * 256 + threadIdx.x) * W);
+            for (int i = 0; i < kClipChunk / (256 * W); ++i) f(begin + (unsigned long long)(i * 256 + tid) * W);
         } else {
-            for (unsigned long long i = begin + threadIdx.x * W; i < whole; i += 256 * W) f(i);
+            for (unsigned long long i = begin + tid * W; i < whole; i += 256 * W) f(i);
         }
         at = whole;
     }
-    for (unsigned long long i = at + threadIdx.x; i < end; i += 256) f1(i);
+    for (unsigned long long i = at + tid; i < end; i += 256) f1(i);
 }
 
 template <typename IN>
-__device__ __forceinline__ double chunk_sum(const IN* g, unsigned long long n, unsigned long long begin, unsigned long long end) {
+__device__ __forceinline__ double chunk_sum(const IN* g, unsigned long long begin, unsigned long long end) {
     constexpr int W = 16 / sizeof(IN);
     typedef IN wide_t __attribute__((ext_vector_type(W)));
     double sum[2] = {0.0, 0.0};
-    each<IN>((uintptr_t)g % 16 == 0, n, begin, end,
+    each<IN>((uintptr_t)g % 16 == 0, begin, end,
              [&](unsigned long long i) {
                  const wide_t v = *(const wide_t*)(g + i);
 #pragma unroll
@@ -67,11 +75,11 @@ __device__ __forceinline__ double chunk_sum(const IN* g, unsigned long long n, u
 }
 
 template <typename IN, typename OUT>
-__device__ __forceinline__ void chunk_scale(const IN* g, OUT* o, float c, unsigned long long n, unsigned long long begin, unsigned long long end) {
+__device__ __forceinline__ void chunk_scale(const IN* g, OUT* o, float c, unsigned long long begin, unsigned long long end) {
     constexpr int W = 16 / sizeof(IN);
     typedef IN wide_t __attribute__((ext_vector_type(W)));
     typedef OUT wide_out_t __attribute__((ext_vector_type(W)));
-    each<IN>(((uintptr_t)g % 16 | (uintptr_t)o % (W * sizeof(OUT) < 16 ? W * sizeof(OUT) : 16)) == 0, n, begin, end,
+    each<IN>(((uintptr_t)g % 16 | (uintptr_t)o % (W * sizeof(OUT) < 16 ? W * sizeof(OUT) : 16)) == 0, begin, end,
              [&](unsigned long long i) {
                  const wide_t v = *(const wide_t*)(g + i);
                  wide_out_t w;
@@ -83,42 +91,63 @@ __device__ __forceinline__ void chunk_scale(const IN* g, OUT* o, float c, unsign
              [&](unsigned long long i) { o[i] = (OUT)((float)g[i] * c); });
 }
 
-__global__ __launch_bounds__(256) void clip_sums_kernel(ClipTable t, double* __restrict__ part) {
-    __shared__ double lds[4];
+// Workgroups have GROUPS groups of 256 threads; group i of all takes chunks i, i + n ..
+template <int GROUPS>
+__device__ __forceinline__ uint32_t first_chunk() {
+    return GROUPS == 1 ? blockIdx.x : blockIdx.x * GROUPS + __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+}
+
+// Sum of squares of the workgroup's chunks.
+template <int GROUPS>
+__device__ __forceinline__ double sum_of_chunks(const ClipTable& t) {
     double sum = 0.0;
-    for (uint32_t c = blockIdx.x; c < t.first[t.n]; c += gridDim.x) {
+    for (uint32_t c = first_chunk<GROUPS>(); c < t.first[t.n]; c += gridDim.x * GROUPS) {
         const int i = tensor_of(t, c);
         const unsigned long long n = t.size[i] & kClipSize, begin = (unsigned long long)(c - t.first[i]) * kClipChunk;
         const unsigned long long end = n - begin < kClipChunk ? n : begin + kClipChunk;
-        if (t.size[i] & kClipGradHalf) sum += chunk_sum((const half_t*)t.grad[i], n, begin, end);
-        else sum += chunk_sum((const float*)t.grad[i], n, begin, end);
+        if (t.size[i] & kClipGradHalf) sum += chunk_sum((const half_t*)t.grad[i], begin, end);
+        else sum += chunk_sum((const float*)t.grad[i], begin, end);
     }
-    sum = block_total(sum, lds);
-    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+    return block_total<256 * GROUPS>(sum);
 }
 
-__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const double* __restrict__ part, int n_part, float max_norm, float unscale,
-                                                         float* __restrict__ norm_out) {
-    __shared__ double lds[4];
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < n_part; i += 256) sum += part[i];
-    const double norm = sqrt(block_total(sum, lds)) * (double)unscale;
+// total: the sum of all squares.
+template <int GROUPS>
+__device__ __forceinline__ void scale_chunks(const ClipTable& t, double total, float max_norm, float unscale, float* __restrict__ norm_out) {
+    const double norm = sqrt(total) * (double)unscale;
     const float rounded = (float)norm;
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = rounded;
     if (!isfinite(rounded)) return;
     const double ratio = (double)max_norm / (norm + 1e-6);
     const float c = (float)((double)unscale * (ratio < 1.0 ? ratio : 1.0));
-    for (uint32_t b = blockIdx.x; b < t.first[t.n]; b += gridDim.x) {
+    for (uint32_t b = first_chunk<GROUPS>(); b < t.first[t.n]; b += gridDim.x * GROUPS) {
         const int i = tensor_of(t, b);
         if (c == 1.0f && t.grad[i] == t.out[i]) continue;
         const unsigned long long n = t.size[i] & kClipSize, begin = (unsigned long long)(b - t.first[i]) * kClipChunk;
         const unsigned long long end = n - begin < kClipChunk ? n : begin + kClipChunk;
         const bool from16 = t.size[i] & kClipGradHalf, to16 = t.size[i] & kClipOutHalf;
-        if (from16 && to16) chunk_scale((const half_t*)t.grad[i], (half_t*)t.out[i], c, n, begin, end);
-        else if (from16) chunk_scale((const half_t*)t.grad[i], (float*)t.out[i], c, n, begin, end);
-        else if (to16) chunk_scale((const float*)t.grad[i], (half_t*)t.out[i], c, n, begin, end);
-        else chunk_scale((const float*)t.grad[i], (float*)t.out[i], c, n, begin, end);
+        if (from16 && to16) chunk_scale((const half_t*)t.grad[i], (half_t*)t.out[i], c, begin, end);
+        else if (from16) chunk_scale((const half_t*)t.grad[i], (float*)t.out[i], c, begin, end);
+        else if (to16) chunk_scale((const float*)t.grad[i], (half_t*)t.out[i], c, begin, end);
+        else chunk_scale((const float*)t.grad[i], (float*)t.out[i], c, begin, end);
     }
+}
+
+__global__ __launch_bounds__(256) void clip_sums_kernel(ClipTable t, double* __restrict__ part) {
+    const double sum = sum_of_chunks<1>(t);
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(256) void clip_scale_kernel(ClipTable t, const double* __restrict__ part, int n_part, float max_norm, float unscale,
+                                                         float* __restrict__ norm_out) {
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < n_part; i += 256) sum += part[i];
+    scale_chunks<1>(t, block_total<256>(sum), max_norm, unscale, norm_out);
+}
+
+// One workgroup does it all.
+__global__ __launch_bounds__(1024) void clip_alone_kernel(ClipTable t, float max_norm, float unscale, float* __restrict__ norm_out) {
+    scale_chunks<4>(t, sum_of_chunks<4>(t), max_norm, unscale, norm_out);
 }
 
 }  // namespace
@@ -128,8 +157,11 @@ void launch_clip_sums(const ClipTable& t, double* part, hipStream_t st) {
 }
 
 void launch_clip_scale(const ClipTable& t, const double* part, int n_part, float max_norm, float unscale, float* norm, hipStream_t st) {
-    const int blocks = clip_blocks(t);
-    if (blocks || norm) clip_scale_kernel<<<blocks ? blocks : 1, 256, 0, st>>>(t, part, n_part, max_norm, unscale, norm);
+    if (clip_blocks(t) || norm) clip_scale_kernel<<<clip_blocks(t) ? clip_blocks(t) : 1, 256, 0, st>>>(t, part, n_part, max_norm, unscale, norm);
+}
+
+void launch_clip_alone(const ClipTable& t, float max_norm, float unscale, float* norm, hipStream_t st) {
+    clip_alone_kernel<<<1, 1024, 0, st>>>(t, max_norm, unscale, norm);
 }
 
 }  // namespace moemix

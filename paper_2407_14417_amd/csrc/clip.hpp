@@ -7,6 +7,10 @@ namespace moemix {
 
 constexpr int kClipMost = 96;                  // tensors of one launch: their table travels as a kernel argument (2.8 KB)
 constexpr int kClipChunk = 16384;              // elements that a workgroup takes at a time
+// Lists of up to so many chunks and elements are one workgroup's (two launches, one: 32776 elements 10.2, 7.4 us; 65428, 11.1, 9.4; 98196, 11.3, 14.4; 9 tensors of 300, 10.2,
+// 7.1; 17 of them, 10.3, 11.6).
+constexpr uint32_t kClipAloneChunks = 12;
+constexpr unsigned long long kClipAloneSize = 65536;
 constexpr int kClipBlocks = 2048;              // most workgroups of a launch, eight per compute unit
 
 struct ClipTable {
@@ -24,5 +28,7 @@ inline int clip_blocks(const ClipTable& t) { return t.first[t.n] < kClipBlocks ?
 void launch_clip_sums(const ClipTable& t, double* part, hipStream_t st);
 // From n_part sums: norm (written if norm != null), and out = c * grad unless the norm is not finite.
 void launch_clip_scale(const ClipTable& t, const double* part, int n_part, float max_norm, float unscale, float* norm, hipStream_t st);
+// Both for a table of all tensors.
+void launch_clip_alone(const ClipTable& t, float max_norm, float unscale, float* norm, hipStream_t st);
 
 }  // namespace moemix

@@ -21,7 +21,7 @@ struct TrainSplit {
 };
 struct TrainMeta {
     int32_t lo, hi;                        // grouped rows [lo, hi) belong to an expert
-    int32_t n_chunks, unused;
+    int32_t n_chunks;
     TrainSplit whole, down, d_rows;        // of the launches that cannot be split, of down and of d_rows
     int32_t offsets[MOE_MAX_EXPERTS + 1];  // increasing, within [0, P]
     int32_t order[MOE_MAX_EXPERTS];        // experts, the one with most rows first

@@ -69,6 +69,18 @@ def test_refusals_of_the_backward_pass():
         assert backward(L, d_w=grads) == mm.MOE_EINVAL
 
 
+def test_gradients_over_one_another():
+    L, size = layer(), D * F * 4
+
+    def says(*at, kind=0):
+        entries = list(at) + [None] * (3 * E - len(at))
+        return backward(L, d_w=(mm.CExpertGrads * E)(*[mm.CExpertGrads(*entries[3 * e: 3 * e + 3]) for e in range(E)]), d_w_type=kind)
+    A = 16 * AT
+    assert says(A, A) == says(A, None, A) == says(A, None, None, None, A) == mm.MOE_EINVAL                  # the same twice
+    assert says(A, A + size - 16) == says(A + size - 16, None, None, A) == says(A, A + size // 2 - 16, kind=1) == mm.MOE_EINVAL
+    assert says(4 * A, A, 2 * A, 3 * A, None, 4 * A + 16) == mm.MOE_EINVAL and b"overlap" in mm.lib().moe_last_error()
+
+
 def test_workspace_bytes():
     ask = mm.lib().moe_experts_workspace_bytes
     assert ask(None, T) == ask(layer(), 0) == ask(layer(d=100), T) == 0
@@ -99,6 +111,7 @@ def test_refusals_of_clipping():
                 (2 * AT, 3 * AT + 1, 100, 1, 1)):
         assert clip([ok, bad]) == mm.MOE_EINVAL, bad
     assert clip([(2 * AT, 3 * AT, 1 << 40, 0, 0)]) == mm.MOE_ESHAPE
+    assert clip([(2 * AT, 3 * AT, 1 << 38, 0, 0)]) == mm.MOE_ESHAPE
     assert clip([ok], ws=None) == clip([ok], ws=AT + 16) == clip([ok], ws_bytes=100) == mm.MOE_EWORKSPACE
 
 

@@ -170,3 +170,23 @@ def test_more_than_2_32_elements():
     assert abs(float(norm) - want) <= 2.0 ** -23 * want
     c = torch.tensor(0.5 / (want + 1e-6), dtype=torch.float32).half()
     assert (g == c.cuda()).all()
+
+
+@pytest.mark.parametrize("sizes", [[65536], [65537], [65535, 2], [300] * 12, [300] * 13, [16384] * 4, [16385, 16385, 16385, 16381], [1] * 12, [0] * 20, [40000, 25000, 500] + [1] * 5])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_lists_that_one_workgroup_takes_and_longer_ones(sizes, dtype):
+    grads = tensors(len(sizes), sizes, dtype)
+    before = [g.clone() for g in grads]
+    other = torch.float16 if dtype == torch.float32 else torch.float32
+    outs = [torch.full_like(g, 7.0, dtype=other) for g in grads]
+    norm = clip(grads, outs, 0.5, 0.25)
+    check(before, outs, norm, 0.5, 0.25)
+    again = clip(grads, None, 0.5, 0.25)
+    check(before, grads, again, 0.5, 0.25)
+    assert torch.equal(norm, again)
+
+
+@pytest.mark.parametrize("sizes", [[], [0], [0, 0, 0]])
+def test_no_elements(sizes):
+    grads = tensors(1, sizes)
+    assert float(clip(grads, None, 0.5, 0.25)) == 0.0

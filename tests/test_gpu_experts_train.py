@@ -415,3 +415,58 @@ def test_in_place():
     d = b.d_out.clone()
     mm.moe_experts_backward(b.layer, b.x, b.gate, b.offsets, b.perm, b.a, b.u, d, b.ws, d_x=d)
     assert torch.equal(d, d_x)
+
+
+def test_workspaces_of_other_sizes():
+    """Room for fewer partial results, for none, and what more tokens ask for."""
+    T, d, f, E, k = 16, 256, 512, 4, 2
+    b = Block(81, T, d, f, E, k)
+    one, full = T * k * d * 4, b.ws.numel()                   # a set of rows; as many as 16 lie at the end of a workspace
+    for n in (full, full - 256, full - 6 * one, full - 15 * one, mm.experts_workspace_bytes(b.layer, 900)):
+        b.ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        for t in (b.a, b.u, b.out):
+            t.fill_(7.0)
+        b.forward()
+        b.check_forward()
+        b.grads()
+        b.backward()
+        b.check_backward()
+    b.ws = torch.empty(full - 15 * one - 256, dtype=torch.uint8, device="cuda")
+    for call in (b.forward, b.backward):
+        with pytest.raises(mm.MoeError) as e:
+            call()
+        assert e.value.code == mm.MOE_EWORKSPACE
+
+
+@pytest.mark.parametrize("counts", [(2600, 300, 9, 0, 91), (1, 2304, 1, 257, 513), (40, 40, 40, 40, 2048 + 33), (0, 0, 3000, 0, 0)])
+@pytest.mark.parametrize("d,f", [(192, 704), (1344, 128)])
+def test_loads_of_all_kinds(counts, d, f):
+    """Experts of more chunks than go side by side, beside small ones and none."""
+    idx = torch.cat([torch.full((n,), e) for e, n in enumerate(counts)])
+    idx = idx[torch.randperm(len(idx), generator=torch.Generator().manual_seed(d))].reshape(-1, 1).cuda()
+    b = Block(d + counts[0], len(idx), d, f, 5, 1, idx=idx)
+    b.forward()
+    b.check_forward()
+    b.grads(torch.float16)
+    b.backward()
+    b.check_backward()
+
+
+@pytest.mark.parametrize("T,d,f", [(262143, 8192, 64), (140000, 64, 16384)])
+def test_offsets_past_32_bits(T, d, f):
+    """The last hundred tokens are an expert's of their own: their rows, their gradients and the expert's."""
+    n = 100
+    idx = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    idx[-n:] = 1
+    b = Block(83, T, d, f, 2, 1, idx=idx)
+    b.forward()
+    b.grads()
+    b.backward()
+    ref = Ref(b.x[-n:], b.w1[1:], b.w3[1:], b.w2[1:], [torch.arange(n, device="cuda")], b.gate[-n:].double().reshape(-1), 1)
+    for got, (v, bound), what in zip((b.a, b.u, b.out), ref.forward(), ("a", "u", "out")):
+        assert_within(got[-n:], v, bound, what)
+    r = ref.backward(b.a[-n:], b.u[-n:], b.d_out[-n:])
+    assert_within(b.d_gate[-n:], *r["d_gate"], "d_gate")
+    assert_within(b.d_x[-n:], *r["d_x"], "d_x")
+    for name, got in (("w1", b.g1), ("w3", b.g3), ("w2", b.g2)):
+        assert_within(got[1], *r[name][0], name)
