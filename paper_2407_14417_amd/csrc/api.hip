@@ -1267,22 +1267,26 @@ int moe_clip_gradients(const moe_grad* grads, int n_tensors, float max_norm, flo
     };
     ClipTable t;
     table(0, t);
-    unsigned long long elements = 0;
-    for (int i = 0; i < n_tensors; ++i) elements += grads[i].n;
+    unsigned long long elements = 0, bytes = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        elements += grads[i].n;
+        bytes += grads[i].n * (grads[i].grad_type == MOE_OUT_F16 ? 2 : 4);
+    }
     if (n_tensors <= kClipMost && t.first[t.n] <= kClipAloneChunks && elements <= kClipAloneSize) {
         launch_clip_alone(t, max_norm, unscale, norm, st);
         return check_hip(st);
     }
+    const bool past_caches = bytes > kClipCached;
     double* const part = (double*)ws;
     int n_part = 0;
     for (int i = 0; i < n_tensors; i += kClipMost) {
         if (i) table(i, t);
-        launch_clip_sums(t, part + n_part, st);
+        launch_clip_sums(t, past_caches, part + n_part, st);
         n_part += clip_blocks(t);
     }
     for (int i = 0; i < n_tensors; i += kClipMost) {
         if (n_tensors > kClipMost) table(i, t);
-        launch_clip_scale(t, part, n_part, max_norm, unscale, i == 0 ? norm : nullptr, st);
+        launch_clip_scale(t, past_caches, part, n_part, max_norm, unscale, i == 0 ? norm : nullptr, st);
     }
     return check_hip(st);
 }

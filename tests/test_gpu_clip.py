@@ -190,3 +190,14 @@ def test_lists_that_one_workgroup_takes_and_longer_ones(sizes, dtype):
 def test_no_elements(sizes):
     grads = tensors(1, sizes)
     assert float(clip(grads, None, 0.5, 0.25)) == 0.0
+
+
+@pytest.mark.parametrize("kinds", [(torch.float32, None), (torch.float16, None), (torch.float32, torch.float16), (torch.float16, torch.float32)])
+def test_gradients_larger_than_the_last_level_cache(kinds):
+    step = 2 if kinds[0] == torch.float16 else 1
+    grads = tensors(9, [(1 << 25) * step, 12345, (1 << 25) * step + 3, 5, 70000], kinds[0])
+    grads[1] = grads[1][1:]                                     # on no 16-byte boundary
+    before = [g.clone() for g in grads]
+    outs = None if kinds[1] is None else [torch.full_like(g, 7.0, dtype=kinds[1]) for g in grads]
+    norm = clip(grads, outs, 0.5, 0.25)
+    check(before, grads if outs is None else outs, norm, 0.5, 0.25)
