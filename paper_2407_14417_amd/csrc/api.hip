@@ -1161,7 +1161,7 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
         g_w.f = f;
         g_w.E = E;
         g_w.accumulate = accumulate != 0;
-        launch_train_d_weights(g_w, d_w_type == MOE_OUT_F16, st);
+        launch_train_d_weights(g_w, T * k, d_w_type == MOE_OUT_F16, st);
     }
     if (d_x) {
         for (int e = 0; e < E; ++e) {

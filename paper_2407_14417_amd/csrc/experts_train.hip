@@ -8,6 +8,7 @@
 //
 // An operand whose contraction runs along memory ("rows") lies in LDS as rows of 64 elements, one whose contraction runs across it
 // ("columns") as 64 rows of 256 columns, and ds_read_b64_tr_b16 hands its columns to the lanes: no transposed copy of a matrix is made.
+#include <algorithm>
 #include <type_traits>
 
 #include "experts_train.hpp"
@@ -347,7 +348,8 @@ struct RowsTile {
         else write_rows();
     }
 
-    // a and u together: their two tiles of 16 columns each make the four that are exchanged.  Then h: rows of 32 columns, two lanes exchange theirs.
+    // a and u together: their two tiles of 16 columns each make the four that are exchanged.  Then h: rows of 32 columns, two lanes exchange theirs.  a and u go past the caches, h is
+    // read next (forward of 333 tokens, 1024 x 2816, 55.6 -> 53.5 us; 512 in the Mixtral shape 607 -> 596; 4096 of them 2575 -> 2595).
     __device__ __forceinline__ void write_up() {
         const int n0 = c.n0 + wn * 32, N = a.N;
         if (n0 >= N) return;
@@ -369,7 +371,7 @@ struct RowsTile {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int r = r0 + 16 * i + (lane & 12) + k;
-                if (r < c.rows) *(half4_t*)(au + (size_t)r * N) = v[k];
+                if (r < c.rows) __builtin_nontemporal_store(v[k], (half4_t*)(au + (size_t)r * N));
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -536,6 +538,43 @@ struct WeightsWork {
     void* out;                   // [lm, ln]
 };
 
+// 16 rows from row m on of 64 columns of a gradient, lm x ln.  Stored past the caches, which hold what the next workgroups read (backward of 2048 tokens, 32 experts of 2048 x 1408, four per token:
+// 558 -> 530 us; 256 tokens: 328 -> 278).
+template <typename OUT>
+__device__ __forceinline__ void write_sums(int lane, float4_t s0, float4_t s1, float4_t s2, float4_t s3, OUT* out, int m, int lm, int ln, bool accumulate) {
+    typedef OUT out4_t __attribute__((ext_vector_type(4)));
+    out += (lane & 3) * 16 + 4 * (lane >> 4);
+    m += lane & 12;
+    if (accumulate) {
+        transpose4(lane, s0, s1, s2, s3);
+        const float4_t sums[4] = {s0, s1, s2, s3};
+        out4_t before[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) before[k] = *(const out4_t*)(out + (size_t)min(m + k, lm - 1) * ln);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            out4_t v;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v[w] = (OUT)(sums[k][w] + (float)before[k][w]);
+            if (m + k < lm) __builtin_nontemporal_store(v, (out4_t*)(out + (size_t)(m + k) * ln));
+        }
+    } else {
+        const float4_t sums[4] = {s0, s1, s2, s3};
+        out4_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v[j][w] = (OUT)sums[j][w];
+        transpose4(lane, v[0], v[1], v[2], v[3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (m + k < lm) __builtin_nontemporal_store(v[k], (out4_t*)(out + (size_t)(m + k) * ln));
+    }
+}
+
+// Half a unit of "columns": rows of 8 slabs.  One transposed read takes its 16 rows in two goes of 8.
+__device__ __forceinline__ int half_swizzle(int r) { return (r & 3) | (((r >> 3) & 1) << 2); }
+
 // GM: the tokens' side is m (W2: d_out), else it is n (x).
 template <typename OUT, bool GM>
 struct WeightsTile {
@@ -556,8 +595,6 @@ struct WeightsTile {
     float4_t acc[4][8];
     half8_t fm[2][8], fn[2][4];
 
-    // Half a unit of m: rows of 8 slabs.  One transposed read takes its 16 rows in two goes of 8.
-    __device__ __forceinline__ static int half_swizzle(int r) { return (r & 3) | (((r >> 3) & 1) << 2); }
     __device__ __forceinline__ int row_a(int k) const { return 16 * wn + 4 * k + (lane >> 4); }
     __device__ __forceinline__ int row_b(int k) const { return 32 * group + 8 * wn + 2 * k + (lane >> 5); }
 
@@ -687,36 +724,10 @@ struct WeightsTile {
         }
     }
     __device__ __forceinline__ void write() {
-        typedef OUT out4_t __attribute__((ext_vector_type(4)));
         if (c.n0 + wn * 64 >= c.ln) return;
-        OUT* const out = (OUT*)c.out + c.n0 + wn * 64 + (lane & 3) * 16 + 4 * (lane >> 4);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int m = c.m0 + (group * 8 + i) * 16 + (lane & 12);
-            if (a.accumulate) {
-                transpose4(lane, acc[0][i], acc[1][i], acc[2][i], acc[3][i]);
-                out4_t before[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) before[k] = *(const out4_t*)(out + (size_t)min(m + k, c.lm - 1) * c.ln);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    out4_t v;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) v[w] = (OUT)(acc[k][i][w] + (float)before[k][w]);
-                    if (m + k < c.lm) *(out4_t*)(out + (size_t)(m + k) * c.ln) = v;
-                }
-            } else {
-                out4_t v[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) v[j][w] = (OUT)acc[j][i][w];
-                transpose4(lane, v[0], v[1], v[2], v[3]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (m + k < c.lm) *(out4_t*)(out + (size_t)(m + k) * c.ln) = v[k];
-            }
-        }
+        for (int i = 0; i < 8; ++i)
+            write_sums<OUT>(lane, acc[0][i], acc[1][i], acc[2][i], acc[3][i], (OUT*)c.out + c.n0 + wn * 64, c.m0 + (group * 8 + i) * 16, c.lm, c.ln, a.accumulate);
     }
 };
 
@@ -753,12 +764,137 @@ __global__ __launch_bounds__(kThreads, 2) void train_weights_kernel(TrainWeights
     else body(std::false_type{});
 }
 
+// Few rows for each expert, or little work in all: what counts is that the gradients are written, so a workgroup is small (four wavefronts, 32 KB of LDS, three of them per compute unit: two,
+// with 180 registers, took 238 us in place of 230 for 256 tokens, 32 experts of 2048 x 1408) and goes over `turns` tiles of 128 x 128 side by side; what the next one multiplies is on
+// the way, through registers, while a tile is written (16 tokens in the Mixtral shape with 1, 2, 4, 8 tiles: 1217, 1114, 1075, 1047 us; of 2048 x 1408: 278, 272, 266, 279).
+// Bound by the writes: 2.8 GB of fp16 gradients, 16 tokens in the Mixtral shape, in 550 us, 5.1 TB/s.
+constexpr int kFewTile = 128, kFewThreads = 256, kFewTurns = 4;
+
 template <typename OUT>
-void launch_weights(const TrainWeights& a, hipStream_t st) {
+__global__ __launch_bounds__(kFewThreads, 3) void train_weights_few_kernel(TrainWeights a, int per_matrix, int turns) {
+    __shared__ uint4_t lds[2][kTrainStep * kFewTile * 2 / 16];
+    const int matrix = __builtin_amdgcn_readfirstlane(blockIdx.x / per_matrix), t = blockIdx.x - matrix * per_matrix, e = matrix / 3, which = matrix - 3 * e;
+    const bool gather_m = which == 2;
+    const int lm = gather_m ? a.d : a.f, ln = gather_m ? a.f : a.d, tiles_m = (lm + kFewTile - 1) / kFewTile, tiles_n = (ln + kFewTile - 1) / kFewTile;
+    const int tn0 = __builtin_amdgcn_readfirstlane(t / tiles_m), m0 = (t - tn0 * tiles_m) * kFewTile, first = tn0 * turns, n_turns = min(turns, tiles_n - first);
+    OUT* const out = (OUT*)(which == 0 ? a.w1[e] : which == 1 ? a.w3[e] : a.w2[e]);
+    if (n_turns <= 0 || !out) return;
+    const int begin = __builtin_amdgcn_readfirstlane(a.meta->offsets[e]), rows = __builtin_amdgcn_readfirstlane(a.meta->offsets[e + 1]) - begin;
+    if (rows == 0 && a.accumulate) return;
+    const gptr_t m = uniform_ptr(which == 0 ? a.d_a + (size_t)begin * lm : which == 1 ? a.d_u + (size_t)begin * lm : a.d_out);
+    const gptr_t n = uniform_ptr(which == 2 ? a.h + (size_t)begin * ln : a.x);
+    const int steps = (rows + kTrainStep - 1) / kTrainStep, all = steps * n_turns;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1, row0 = tid >> 4, col = (tid & 15) * 8;
+    const int col_m = m0 + min(col, lm - 8 - m0);
+    const int put = row0 * 16 + (((((tid & 15) >> 1) ^ half_swizzle(row0)) << 1) | (tid & 1));     // in 16 bytes; 16 rows on the swizzle is the same
+    const int row = 8 * (lane >> 4) + ((lane & 15) >> 2);
+    const uint32_t at = row * 256 + (lane & 3) * 8 + (half_swizzle(row) << 5);
+    const uint32_t get_m = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4_t*)lds[0] + at, get_n = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4_t*)lds[1] + at;
+    int tok[4];
+    uint4_t vm[4], vn[4];
+    float4_t acc[4][4];
+    auto look_up = [&](int step) {
+        const int at = begin + step * kTrainStep + (int)fresh_offset(row0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tok[k] = a.tok[at + 16 * k];
+    };
+    auto ask = [&](int step, int turn) {
+        const int n0 = (first + turn) * kFewTile, col_n = n0 + min(col, ln - 8 - n0), at = (int)fresh_offset(row0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t r = step * kTrainStep + at + 16 * k, of_m = gather_m ? tok[k] : r, of_n = gather_m ? r : tok[k];
+            vm[k] = *(const uint4_t __attribute__((address_space(1)))*)(m + (of_m * (uint32_t)lm * 2 + col_m * 2));
+            vn[k] = *(const uint4_t __attribute__((address_space(1)))*)(n + (of_n * (uint32_t)ln * 2 + col_n * 2));
+        }
+    };
+    auto clear = [&]() {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[j][i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    auto write = [&](int turn) {
+        const int n0 = (first + turn) * kFewTile + wn * 64;
+        if (n0 >= ln) return;
+        const int l = (int)fresh_offset(lane);               // (worked out here: hoisted, the addresses would cost a workgroup its place beside two others)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            write_sums<OUT>(l, acc[0][i], acc[1][i], acc[2][i], acc[3][i], out + n0, m0 + wm * 64 + 16 * i, lm, ln, a.accumulate);
+            pin_schedule();
+        }
+    };
+    clear();
+    if (rows == 0) {
+        for (int turn = 0; turn < n_turns; ++turn) write(turn);
+        return;
+    }
+    look_up(0);
+    ask(0, 0);
+    if (steps > 1) look_up(1);
+    int step = 0, turn = 0;
+    for (int k = 0; k < all; ++k) {
+        const int there = rows - step * kTrainStep;          // rows past the expert's last one, whatever they hold, are zeros on both sides
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool is = row0 + 16 * i < there;
+            lds[0][put + 256 * i] = is ? vm[i] : uint4_t{0u, 0u, 0u, 0u};
+            lds[1][put + 256 * i] = is ? vn[i] : uint4_t{0u, 0u, 0u, 0u};
+        }
+        __syncthreads();
+        const int step1 = step + 1 == steps ? 0 : step + 1, turn1 = step1 ? turn : turn + 1;
+        if (k + 1 < all) {
+            ask(step1, turn1);
+            if (steps > 1) look_up(step1 + 1 == steps ? 0 : step1 + 1);
+        }
+        pin_schedule();
+        const uint32_t at_m = fresh_offset(get_m), at_n = fresh_offset(get_n);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            if (kk * 32 >= there) break;
+            half8_t fm[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fm[i] = read_columns<256>(at_m ^ ((4 * wm + i) << 5), kk);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const half8_t fn = read_columns<256>(at_n ^ ((4 * wn + j) << 5), kk);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j][i] = mfma16(fn, fm[i], acc[j][i]);
+            }
+        }
+        if (!step1) {
+            write(turn);
+            clear();
+        }
+        step = step1;
+        turn = turn1;
+    }
+}
+
+// Which of the two kernels, estimated (us) from the mean number of rows: a round of large tiles takes 9 and 1 per step, one of three small workgroups per compute unit 4 and 1.8 per step, 1
+// where each is alone.  Backward pass, large and small tiles: 64 rows for each of 32 experts of 2048 x 1408, 297, 261 us; 128 for each, 368, 346; 256, 542, 564; 300 for each of 6 of
+// 320 x 1408, 77, 64; 4096 for each of 2 of 2048 x 1408, 369, 408; 8 for each of 4 of 256 x 512, 33, 27.
+bool small_tiles(const TrainWeights& a, int P, int workgroups) {
+    const int tiles = ((a.f + kTrainCols - 1) / kTrainCols) * ((a.d + kTrainCols - 1) / kTrainCols), per_xcd = a.E * 3 * ((tiles + 7) / 8);
+    const float steps = (float)((P / a.E + kTrainStep - 1) / kTrainStep), full = 3.0f * kComputeUnits;
+    const float large = (float)((per_xcd + 31) / 32) * (9.0f + steps);
+    const float small = std::max((float)workgroups / full, 1.0f) * (4.0f + steps * (workgroups <= (int)kComputeUnits ? 1.0f : workgroups <= 2 * (int)kComputeUnits ? 1.4f : 1.8f));
+    return small <= large;
+}
+
+template <typename OUT>
+void launch_weights(const TrainWeights& a, int P, hipStream_t st) {
+    const int few_f = (a.f + kFewTile - 1) / kFewTile, few_d = (a.d + kFewTile - 1) / kFewTile, few = a.E * 3 * few_f * few_d;
+    if (small_tiles(a, P, few)) {
+        const int turns = few >= kFewTurns * 4 * 3 * (int)kComputeUnits ? kFewTurns : 1;
+        const int per_matrix = std::max(few_f * ((few_d + turns - 1) / turns), few_d * ((few_f + turns - 1) / turns));
+        train_weights_few_kernel<OUT><<<(unsigned)(a.E * 3 * per_matrix), kFewThreads, 0, st>>>(a, per_matrix, turns);
+        return;
+    }
+    const int tiles_f = (a.f + kTrainCols - 1) / kTrainCols, tiles_d = (a.d + kTrainCols - 1) / kTrainCols;
     static std::atomic<unsigned long long> configured{0};
     const auto kernel = train_weights_kernel<OUT>;
     allow_lds((const void*)kernel, kLdsBytes, configured);
-    const int tiles_f = (a.f + kTrainCols - 1) / kTrainCols, tiles_d = (a.d + kTrainCols - 1) / kTrainCols;
     kernel<<<(unsigned)(a.E * 3 * ((tiles_f * tiles_d + 7) / 8) * 8), kThreads, kLdsBytes, st>>>(a, tiles_f, tiles_d);
 }
 
@@ -935,9 +1071,9 @@ void launch_train_up(const TrainRows& a, hipStream_t st) { launch_rows<kUp>(a, s
 void launch_train_down(const TrainRows& a, hipStream_t st) { launch_rows<kDown>(a, st); }
 void launch_train_d_hidden(const TrainRows& a, hipStream_t st) { launch_rows<kDHidden>(a, st); }
 void launch_train_d_rows(const TrainRows& a, hipStream_t st) { launch_rows<kDRows>(a, st); }
-void launch_train_d_weights(const TrainWeights& a, bool half_out, hipStream_t st) {
-    if (half_out) launch_weights<half_t>(a, st);
-    else launch_weights<float>(a, st);
+void launch_train_d_weights(const TrainWeights& a, int P, bool half_out, hipStream_t st) {
+    if (half_out) launch_weights<half_t>(a, P, st);
+    else launch_weights<float>(a, P, st);
 }
 
 void launch_train_gather(const TrainGrouping& g, const TrainWorkspace& w, bool forward, int d, void* out, bool half_out, float* d_gate, int n_part,

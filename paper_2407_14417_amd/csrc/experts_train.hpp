@@ -126,7 +126,7 @@ void launch_train_down(const TrainRows& a, hipStream_t st);
 void launch_train_d_hidden(const TrainRows& a, hipStream_t st);
 // y = W1^T d_a + W3^T d_u
 void launch_train_d_rows(const TrainRows& a, hipStream_t st);
-void launch_train_d_weights(const TrainWeights& a, bool half_out, hipStream_t st);
+void launch_train_d_weights(const TrainWeights& a, int P, bool half_out, hipStream_t st);
 // out[t,:] = sum over the token's pairs in a group of (forward: topk_gate *) the sum of the shares of y; d_gate [T, k] (or null) from n_part shares of each.
 void launch_train_gather(const TrainGrouping& g, const TrainWorkspace& w, bool forward, int d, void* out, bool half_out, float* d_gate,
                          int n_part, hipStream_t st);

@@ -470,3 +470,34 @@ def test_offsets_past_32_bits(T, d, f):
     assert_within(b.d_x[-n:], *r["d_x"], "d_x")
     for name, got in (("w1", b.g1), ("w3", b.g3), ("w2", b.g2)):
         assert_within(got[1], *r[name][0], name)
+
+
+@pytest.mark.parametrize("counts", [(2600, 300, 9, 0, 91), (1, 2304, 1, 257, 513), (640, 576, 513, 600, 703), (3000, 1, 0, 0, 0)])
+@pytest.mark.parametrize("dtype,accumulate", [(torch.float32, False), (torch.float16, True)])
+def test_large_tiles(counts, dtype, accumulate):
+    """Matrices so large and experts with so many rows that the gradients of matrices are made of tiles of 256 x 256, whose last ones are cut off."""
+    idx = torch.cat([torch.full((n,), e) for e, n in enumerate(counts)])
+    idx = idx[torch.randperm(len(idx), generator=torch.Generator().manual_seed(counts[1]))].reshape(-1, 1).cuda()
+    b = Block(counts[0], len(idx), 1472, 2368, 5, 1, idx=idx)
+    b.forward()
+    b.check_forward()
+    b.grads(dtype, fill=0.25)
+    b.backward(accumulate=accumulate)
+    b.check_backward(before=0.25 if accumulate else None)
+
+
+@pytest.mark.parametrize("rows", [1, 31, 32, 33, 63, 64, 65, 128, 129, 200])
+@pytest.mark.parametrize("d,f", [(1088, 1984), (64, 64)])
+def test_small_tiles(rows, d, f):
+    """Rows of one expert beside one with three and one with none, in one tile after the other of 128 x 128."""
+    idx = torch.cat([torch.full((rows,), 7), torch.full((3,), 2)]).reshape(-1, 1).cuda()
+    b = Block(rows, rows + 3, d, f, 16, 1, idx=idx)
+    b.forward()
+    b.grads(torch.float16)
+    b.backward()
+    b.check_backward()
+    before = b.results()
+    b.backward(accumulate=True)
+    b.g1, b.g3, b.g2 = b.g1 / 2, b.g3 / 2, b.g2 / 2           # twice the same, rounded once more
+    for got, want in zip((b.g1, b.g3, b.g2), before[2:]):
+        assert float((got.double() - want.double()).abs().max()) <= 2.0 ** -10 * float(want.abs().max())
