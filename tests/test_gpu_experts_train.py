@@ -501,3 +501,15 @@ def test_small_tiles(rows, d, f):
     b.g1, b.g3, b.g2 = b.g1 / 2, b.g3 / 2, b.g2 / 2           # twice the same, rounded once more
     for got, want in zip((b.g1, b.g3, b.g2), before[2:]):
         assert float((got.double() - want.double()).abs().max()) <= 2.0 ** -10 * float(want.abs().max())
+
+
+@pytest.mark.parametrize("T,k", [(1, 2), (40, 2), (700, 4)])
+def test_matrices_larger_than_the_last_level_cache(T, k):
+    """277 MB of them; experts of up to 128 rows and of more, some split."""
+    idx = torch.rand(T, 16, generator=gen(T), device="cuda").mul(torch.linspace(0.2, 1, 16, device="cuda")).topk(k, 1).indices
+    b = Block(91 + T, T, 1024, 2816, 16, k, idx=idx)
+    b.forward()
+    b.check_forward()
+    b.grads()
+    b.backward()
+    b.check_backward()
