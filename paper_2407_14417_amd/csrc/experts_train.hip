@@ -533,7 +533,7 @@ void launch_rows_kernel(const TrainRows& a, hipStream_t st) {
     const auto kernel = train_rows_kernel<FORM, PAST>;
     allow_lds((const void*)kernel, kLdsBytes, configured);
     constexpr int kOut = FORM == kUp ? kTrainCols / 2 : kTrainCols;
-    const int n_tiles = (a.N + kOut - 1) / kOut, most_chunks = a.P / kTrainRows + (a.E < a.P ? a.E : a.P);
+    const int n_tiles = (a.N + kOut - 1) / kOut, most_chunks = a.P / a.most_rows + (a.E < a.P ? a.E : a.P);
     const int most_a = most_chunks * n_tiles, most_b = FORM == kDown || FORM == kDRows ? kMostSplit : 0;
     const int slots = (most_a + 255) / 256 * 32 + (most_b + 255) / 256 * 32;
     kernel<<<(unsigned)slots * 8, kThreads, kLdsBytes, st>>>(a, n_tiles);
@@ -953,7 +953,7 @@ __global__ __launch_bounds__(256) void train_group_kernel(TrainGrouping g, Train
             if (tid >= m) o = max(o, before);
         }
         const int begin = __shfl(o, tid < E ? tid : E, kWave), end = __shfl(o, tid < E ? tid + 1 : E, kWave);
-        const int rows = end - begin, fewest = (rows + kTrainRows - 1) / kTrainRows;
+        const int rows = end - begin, fewest = (rows + w.most_rows - 1) / w.most_rows;
         const int size = fewest ? (rows + 32 * fewest - 1) / (32 * fewest) * 32 : 0, chunks = size ? (rows + size - 1) / size : 0;
         int first = 0, n_chunks = 0, rank = 0;
         for (int e = 0; e < E; ++e) {
@@ -1076,6 +1076,13 @@ __global__ __launch_bounds__(256) void train_gather_kernel(TrainGrouping g, Trai
 int train_most_splits(int P, int d) {
     const float rounds = (float)P / kTrainRows * (float)((d + kTrainCols - 1) / kTrainCols) / kComputeUnits;
     return rounds >= 8.0f ? 1 : rounds >= 4.0f ? 2 : rounds >= 1.0f ? 4 : rounds >= 0.25f ? 8 : kTrainMostSplits;
+}
+
+// As long as all chunks, were they half as long, still made one round of workgroups, they are: a short one's steps are quicker (FIGURES).
+int train_most_rows(int P, int E, int tiles_f, int tiles_d) {
+    int rows = kTrainRows;
+    while (rows > 32 && (long long)(P / (rows / 2) + std::min(E, P)) * std::max(tiles_f, tiles_d) <= kComputeUnits) rows /= 2;
+    return rows;
 }
 
 void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int d, int f, hipStream_t st) {

@@ -7,7 +7,7 @@ namespace moemix {
 
 constexpr int kTrainStep = 64;          // contraction elements per stage
 constexpr int kTrainCols = 256;         // columns of a tile
-constexpr int kTrainRows = 256;         // most rows of a tile
+constexpr int kTrainRows = 256;         // most rows of a tile, of a chunk
 
 // What the first launch of a call finds out about the grouping, whatever offsets and perm hold.
 // Chunk i is rows [begin, min(begin + size, end)) of the grouped rows; up to eight chunks of an expert go side by side: i is number `at` of `abreast`.
@@ -31,7 +31,7 @@ constexpr int kTrainMostSplits = 16;
 
 struct TrainWorkspace {
     TrainMeta* meta;
-    TrainChunk* chunks;   // [E + P / 256]
+    TrainChunk* chunks;   // [E + P / 32]
     int32_t* tok;         // [P + 64]  grouped row -> token (0 for a row of no expert and past the end)
     float* gate;          // [P + 64]  grouped row -> its gate
     int32_t* inv;         // [P]       pair -> grouped row; anything for a pair in no group
@@ -42,6 +42,7 @@ struct TrainWorkspace {
     float* part;          // [P][f / 64]  shares of d_gate
     float* y;             // [splits][P, d]  rows of the down-projection; backward: of d_x
     int splits;           // most of a chunk
+    int most_rows;        // of a chunk: 32 .. 256
     size_t bytes;
 };
 
@@ -55,7 +56,7 @@ inline TrainWorkspace carve_train_workspace(void* base, int T, int d, int f, int
     };
     const size_t P = (size_t)T * k;
     w.meta = (TrainMeta*)take(sizeof(TrainMeta));
-    w.chunks = (TrainChunk*)take((E + P / kTrainRows) * sizeof(TrainChunk));
+    w.chunks = (TrainChunk*)take((E + P / 32) * sizeof(TrainChunk));
     w.tok = (int32_t*)take((P + kTrainStep) * sizeof(int32_t));
     w.gate = (float*)take((P + kTrainStep) * sizeof(float));
     w.inv = (int32_t*)take(P * sizeof(int32_t));
@@ -96,6 +97,7 @@ struct TrainRows {
     const int32_t* tok;
     const float* gate;
     int N, K, P, E;
+    int most_rows;             // of a chunk
 };
 
 // Gradients of the matrices: for expert e  w1 = d_a^T x, w3 = d_u^T x, w2 = d_out^T h.  Null: not asked for.
@@ -116,6 +118,9 @@ struct TrainWeights {
 
 // Most workgroups that share a chunk's contraction in down and d_rows: partial results cost room, and pay where a launch has few rounds of workgroups.
 int train_most_splits(int P, int d);
+
+// Most rows of a chunk, where the widest launch has tiles_f or tiles_d tiles of columns.
+int train_most_rows(int P, int E, int tiles_f, int tiles_d);
 
 void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int d, int f, hipStream_t st);
 // a = W1 x, u = W3 x, h = silu(a) u
