@@ -513,3 +513,18 @@ def test_matrices_larger_than_the_last_level_cache(T, k):
     b.grads()
     b.backward()
     b.check_backward()
+
+
+@pytest.mark.parametrize("counts", [(1, 15, 16, 17, 31, 32, 33, 47, 63, 64, 65, 96, 97, 128, 129, 160, 161, 192, 193, 225),
+                                    (257, 300, 0, 385, 511, 2, 640, 225, 513, 64, 255, 1, 100, 0, 31, 448, 7, 700, 321, 150)])
+@pytest.mark.parametrize("d,f", [(4032, 192), (192, 4032)])
+def test_chunks_of_every_length(counts, d, f):
+    """So many columns that chunks are not made shorter to fill the chip."""
+    idx = torch.cat([torch.full((n,), e) for e, n in enumerate(counts)])
+    idx = idx[torch.randperm(len(idx), generator=torch.Generator().manual_seed(f))].reshape(-1, 1).cuda()
+    b = Block(d + counts[0], len(idx), d, f, 20, 1, idx=idx)
+    b.forward()
+    b.check_forward()
+    b.grads(torch.float16)
+    b.backward()
+    b.check_backward()
