@@ -1085,7 +1085,7 @@ int moe_experts_forward(const moe_layer* layer, const void* x, int T, const floa
         return fail(MOE_EINVAL, "%s: a and u must not overlap each other, x or out", who);
     hipStream_t st = (hipStream_t)stream;
     const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
-    w.most_rows = train_most_rows(T * k, E, (f + kTrainCols / 2 - 1) / (kTrainCols / 2), (d + kTrainCols - 1) / kTrainCols);
+    w.most_rows = train_most_rows(T * k, E, d, f, (f + kTrainCols / 2 - 1) / (kTrainCols / 2), (d + kTrainCols - 1) / kTrainCols);
     launch_train_group(g, w, d, f, st);
     TrainRows r = train_rows(layer, w, T);
     for (int e = 0; e < E; ++e) {
@@ -1142,7 +1142,7 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
         if (at[i] - at[i - 1] < (size_t)d * f * (d_w_type == MOE_OUT_F16 ? 2 : 4)) return fail(MOE_EINVAL, "%s: gradients of matrices overlap", who);
     hipStream_t st = (hipStream_t)stream;
     const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
-    w.most_rows = train_most_rows(T * k, E, (f + kTrainCols - 1) / kTrainCols, (d + kTrainCols - 1) / kTrainCols);
+    w.most_rows = train_most_rows(T * k, E, d, f, (f + kTrainCols - 1) / kTrainCols, (d + kTrainCols - 1) / kTrainCols);
     launch_train_group(g, w, d, f, st);
     TrainRows r = train_rows(layer, w, T);
     for (int e = 0; e < E; ++e) r.w[e] = (const half_t*)layer->experts[e].w2.data;

@@ -22,7 +22,9 @@ namespace {
 constexpr int kLdsBytes = 163840;        // of a compute unit
 constexpr int kUnit = 32768;             // 256 rows of 64 elements, or 64 rows of 256
 constexpr int kThreads = 512;
-constexpr size_t kLastLevelCache = 256ull << 20;
+
+// Are a call's matrices more than the last-level cache holds?
+bool matrices_past_caches(int E, int d, int f) { return (size_t)E * 3 * d * f * 2 > 256ull << 20; }
 
 enum Form { kUp, kDown, kDHidden, kDRows };
 
@@ -541,7 +543,7 @@ void launch_rows_kernel(const TrainRows& a, hipStream_t st) {
 
 template <int FORM>
 void launch_rows(const TrainRows& a, hipStream_t st) {
-    if ((size_t)a.E * 3 * a.N * a.K * 2 > kLastLevelCache) launch_rows_kernel<FORM, true>(a, st);
+    if (matrices_past_caches(a.E, a.N, a.K)) launch_rows_kernel<FORM, true>(a, st);
     else launch_rows_kernel<FORM, false>(a, st);
 }
 
@@ -1079,10 +1081,12 @@ int train_most_splits(int P, int d) {
 }
 
 // As long as all chunks, were they half as long, still made one round of workgroups, they are: steps of few rows are quicker (forward of 400 tokens, 2 experts of 1024 x 1024, 47 -> 27 us, of 200
-// tokens, 4096 x 4096, 104 -> 58; up to two rounds in place of one: of 333 tokens, 8 experts of 1024 x 2816, 53 -> 60).
-int train_most_rows(int P, int E, int tiles_f, int tiles_d) {
+// tokens, 4096 x 4096, 104 -> 58; up to two rounds in place of one: of 333 tokens, 8 experts of 1024 x 2816, 53 -> 60).  Each chunk reads its matrix, so where that comes from memory they stay
+// longer (backward of 150 tokens, 2 experts of 4096 x 8192, chunks of up to 256, 128, 64, 32 rows: 222, 222, 214, 239 us; 120 tokens, one of 4096 x 14336: 241, 241, 221, 235).
+int train_most_rows(int P, int E, int d, int f, int tiles_f, int tiles_d) {
+    const int least = matrices_past_caches(E, d, f) ? 64 : 32;
     int rows = kTrainRows;
-    while (rows > 32 && (long long)(P / (rows / 2) + std::min(E, P)) * std::max(tiles_f, tiles_d) <= kComputeUnits) rows /= 2;
+    while (rows > least && (long long)(P / (rows / 2) + std::min(E, P)) * std::max(tiles_f, tiles_d) <= kComputeUnits) rows /= 2;
     return rows;
 }
 

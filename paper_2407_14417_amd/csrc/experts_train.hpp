@@ -120,7 +120,7 @@ struct TrainWeights {
 int train_most_splits(int P, int d);
 
 // Most rows of a chunk, where the widest launch has tiles_f or tiles_d tiles of columns.
-int train_most_rows(int P, int E, int tiles_f, int tiles_d);
+int train_most_rows(int P, int E, int d, int f, int tiles_f, int tiles_d);
 
 void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int d, int f, hipStream_t st);
 // a = W1 x, u = W3 x, h = silu(a) u
