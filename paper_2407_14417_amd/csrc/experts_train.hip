@@ -818,11 +818,13 @@ __global__ __launch_bounds__(kFewThreads, 3) void train_weights_few_kernel(Train
     };
     auto ask = [&](int step, int turn) {
         const int n0 = (first + turn) * kFewTile, col_n = n0 + min(col, ln - 8 - n0), at = (int)fresh_offset(row0);
+        // (32-bit offsets of tokens, and of rows within a step)
+        const gptr_t step_m = gather_m ? m : m + (size_t)step * kTrainStep * lm * 2, step_n = gather_m ? n + (size_t)step * kTrainStep * ln * 2 : n;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t r = step * kTrainStep + at + 16 * k, of_m = gather_m ? tok[k] : r, of_n = gather_m ? r : tok[k];
-            vm[k] = *(const uint4_t __attribute__((address_space(1)))*)(m + (of_m * (uint32_t)lm * 2 + col_m * 2));
-            vn[k] = *(const uint4_t __attribute__((address_space(1)))*)(n + (of_n * (uint32_t)ln * 2 + col_n * 2));
+            const uint32_t r = at + 16 * k, of_m = gather_m ? tok[k] : r, of_n = gather_m ? r : tok[k];
+            vm[k] = *(const uint4_t __attribute__((address_space(1)))*)(step_m + (of_m * (uint32_t)lm * 2 + col_m * 2));
+            vn[k] = *(const uint4_t __attribute__((address_space(1)))*)(step_n + (of_n * (uint32_t)ln * 2 + col_n * 2));
         }
     };
     auto clear = [&]() {

@@ -528,3 +528,21 @@ def test_chunks_of_every_length(counts, d, f):
     b.grads(torch.float16)
     b.backward()
     b.check_backward()
+
+
+def test_rows_of_one_expert_past_32_bits():
+    """Hidden rows of one expert that lie further apart than 2^32 bytes: gradients of the matrices, the last 64 hidden columns."""
+    T, d, f, n = 140000, 64, 16384, 64
+    idx = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    idx[-100:] = 1
+    b = Block(85, T, d, f, 2, 1, idx=idx)
+    b.forward()
+    b.grads()
+    b.backward()
+    cols = slice(f - n, f)
+    ref = Ref(b.x, b.w1[:, cols], b.w3[:, cols], b.w2[:, :, cols], list(b.perm.long().split(b.counts)), b.gate.double().reshape(-1), 1)
+    r = ref.backward(b.a[:, cols], b.u[:, cols], b.d_out)
+    for e in range(2):
+        assert_within(b.g1[e, cols], *r["w1"][e], "w1")
+        assert_within(b.g3[e, cols], *r["w3"][e], "w3")
+        assert_within(b.g2[e, :, cols], *r["w2"][e], "w2")
