@@ -1011,6 +1011,37 @@ bool misaligned(const void* p, int to) { return (uintptr_t)p % to != 0; }
 
 bool overlap(const void* a, size_t n, const void* b, size_t m) { return (uintptr_t)a < (uintptr_t)b + m && (uintptr_t)b < (uintptr_t)a + n; }
 
+// What a call reads until its end, and what it writes.
+struct TrainRanges {
+    struct Range {
+        uintptr_t begin, end;
+        bool written;
+    } v[6 * MOE_MAX_EXPERTS + 8];
+    int n = 0;
+
+    TrainRanges(const moe_layer* L, int T, const int32_t* offsets, const int32_t* perm, const void* ws, size_t ws_bytes) {
+        for (int e = 0; e < L->n_experts; ++e)
+            for (const void* const m : {L->experts[e].w1.data, L->experts[e].w3.data, L->experts[e].w2.data}) add(m, (size_t)L->d_model * L->d_ff * 2, false);
+        add(offsets, (L->n_experts + 1) * sizeof(int32_t), false);
+        add(perm, (size_t)T * L->top_k * sizeof(int32_t), false);
+        add(ws, ws_bytes, false);
+    }
+    void add(const void* p, size_t bytes, bool written) {
+        if (p) v[n++] = Range{(uintptr_t)p, (uintptr_t)p + bytes, written};
+    }
+    // Does something that is written overlap anything else here?
+    bool clash() {
+        std::sort(v, v + n, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+        uintptr_t any = 0, written = 0;      // where those before end
+        for (int i = 0; i < n; ++i) {
+            if (v[i].begin < (v[i].written ? any : written)) return true;
+            any = std::max(any, v[i].end);
+            if (v[i].written) written = std::max(written, v[i].end);
+        }
+        return false;
+    }
+};
+
 int check_train_shape(const char* who, const moe_layer* L, int T) {
     if (!L) return fail(MOE_EINVAL, "%s: layer is NULL", who);
     if (L->d_model < 64 || L->d_ff < 64 || L->d_model % MOE_GROUP || L->d_ff % MOE_GROUP || L->d_model > 8192 || L->d_ff > 16384)
@@ -1131,15 +1162,18 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
         g_w.w2[e] = d_w[e].w2;
         any |= d_w[e].w1 || d_w[e].w3 || d_w[e].w2;
     }
-    // workgroups of different matrices run side by side
-    uintptr_t at[3 * MOE_MAX_EXPERTS];
-    int n = 0;
+    // (gradients of matrices are written while x and d_out are read, before the matrices are read for d_x)
+    const size_t rows = (size_t)T * d, matrix = (size_t)d * f * (d_w_type == MOE_OUT_F16 ? 2 : 4);
+    TrainRanges ranges(layer, T, offsets, perm, ws, w.bytes);
     for (int e = 0; e < E; ++e)
         for (void* const m : {g_w.w1[e], g_w.w3[e], g_w.w2[e]})
-            if (m) at[n++] = (uintptr_t)m;
-    std::sort(at, at + n);
-    for (int i = 1; i < n; ++i)
-        if (at[i] - at[i - 1] < (size_t)d * f * (d_w_type == MOE_OUT_F16 ? 2 : 4)) return fail(MOE_EINVAL, "%s: gradients of matrices overlap", who);
+            if (m) {
+                if (overlap(m, matrix, x, rows * 2) || overlap(m, matrix, d_out, rows * 2)) return fail(MOE_EINVAL, "%s: a gradient of expert %d overlaps x or d_out", who, e);
+                ranges.add(m, matrix, true);
+            }
+    ranges.add(d_x, rows * (d_x_type == MOE_OUT_F16 ? 2 : 4), true);
+    ranges.add(d_gate, (size_t)T * k * sizeof(float), true);
+    if (ranges.clash()) return fail(MOE_EINVAL, "%s: gradients overlap one another, a matrix, offsets, perm or the workspace", who);
     hipStream_t st = (hipStream_t)stream;
     const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
     w.most_rows = train_most_rows(T * k, E, d, f, (f + kTrainCols - 1) / kTrainCols, (d + kTrainCols - 1) / kTrainCols);
