@@ -359,8 +359,8 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
  * d_x: device, fp32 or fp16 (d_x_type, a moe_out) [T, d_model]; d_gate: device fp32 [T, top_k]; d_w: HOST array [n_experts] of the matrices' gradients,
  * device, all fp32 or all fp16 (d_w_type), of the matrices' shapes, a NULL entry is not asked for.  Each of d_x, d_gate and d_w may be NULL, not all.  accumulate != 0:
  * the gradients of the matrices are added to what is there (and an expert without rows leaves its as they are).  The same inputs give the same bits.
- * No gradient overlaps another, a matrix of the layer, offsets, perm or ws, and none of d_w x or d_out (MOE_EINVAL).  Apart from that results may take the place of inputs that the
- * program needs no more: d_x that of x, d_out, a or u, d_w that of a or u, d_gate that of topk_gate.
+ * No result overlaps another, a matrix of the layer, offsets, perm or ws; a and u do not overlap x, and none of d_w x or d_out (MOE_EINVAL).  Apart from that results may take the place of
+ * inputs that the program needs no more: out that of x; d_x that of x, d_out, a or u; d_w that of a or u; d_gate that of topk_gate.
  * Tensors start on 16-byte boundaries (d_gate, topk_gate, offsets and perm: 4).  layer->w_gate and gate_bias are not looked at.
  * T >= 1, T * d_model <= 2^31 - 2048, T * top_k <= 2^22 (MOE_ESHAPE otherwise).  ws: moe_experts_workspace_bytes(layer, T) bytes, or what these were for more tokens (a
  * workspace that holds the call without partial results is enough; sums are then added in another order); it carries nothing from one call to the next.  Neither call sets a status that moe_read_status reads.

@@ -1112,8 +1112,13 @@ int moe_experts_forward(const moe_layer* layer, const void* x, int T, const floa
     if (misaligned(x, 16) || misaligned(a, 16) || misaligned(u, 16) || misaligned(out, 16)) return fail(MOE_EINVAL, "%s: x, a, u and out must be 16-byte aligned", who);
     const int d = layer->d_model, f = layer->d_ff, E = layer->n_experts, k = layer->top_k;
     const size_t kept = (size_t)T * k * f * 2, rows = (size_t)T * d * 2;
-    if (overlap(a, kept, u, kept) || overlap(a, kept, x, rows) || overlap(u, kept, x, rows) || overlap(a, kept, out, rows) || overlap(u, kept, out, rows))
-        return fail(MOE_EINVAL, "%s: a and u must not overlap each other, x or out", who);
+    // (a and u are written while x is read)
+    if (overlap(a, kept, x, rows) || overlap(u, kept, x, rows)) return fail(MOE_EINVAL, "%s: a or u overlaps x", who);
+    TrainRanges ranges(layer, T, offsets, perm, ws, w.bytes);
+    ranges.add(a, kept, true);
+    ranges.add(u, kept, true);
+    ranges.add(out, rows, true);
+    if (ranges.clash()) return fail(MOE_EINVAL, "%s: a, u and out overlap one another, a matrix, offsets, perm or the workspace", who);
     hipStream_t st = (hipStream_t)stream;
     const TrainGrouping g{offsets, perm, topk_gate, T, k, E};
     w.most_rows = train_most_rows(T * k, E, d, f, (f + kTrainCols / 2 - 1) / (kTrainCols / 2), (d + kTrainCols - 1) / kTrainCols);

@@ -42,6 +42,12 @@ def backward(grads=(), kind=0, **at):
                                          d_w if grads else None, kind, 0, p["ws"], 1 << 40, None)
 
 
+def forward(**at):
+    p = AT | at
+    L = layer()
+    return mm.lib().moe_experts_forward(ctypes.byref(L), p["x"], T, p["gate"], p["offsets"], p["perm"], p["a"], p["u"], p["out"], p["ws"], 1 << 40, None)
+
+
 def refused(rc):
     return rc == mm.MOE_EINVAL and b"overlap" in mm.lib().moe_last_error()
 
@@ -63,3 +69,12 @@ def test_gradients_of_tokens_and_gates_over_what_is_still_read(over, name):
         assert refused(backward(**{name: p}))
     for p in places("d_x", SIZE["d_gate"], 4):
         assert refused(backward(d_gate=p))
+
+
+@pytest.mark.parametrize("name", ["a", "u", "out"])
+@pytest.mark.parametrize("over", ["x", "offsets", "perm", "ws", "w10", "w32", "w21", "a", "u", "out"])
+def test_results_of_the_forward_pass_over_what_is_still_read(over, name):
+    """(out may lie over x)"""
+    if name != over and (name, over) != ("out", "x"):
+        for p in places(over, SIZE[name]):
+            assert refused(forward(**{name: p}))
