@@ -381,7 +381,7 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
  * Sums are held in 64 bits.  unscale: finite, > 0, 1 / loss scale; max_norm: >= 0, INFINITY: no limit.  If norm is not finite in 32 bits (a gradient was
  * not) only norm is written: the caller leaves out the step.
  * grads: HOST array of at most MOE_MAX_GRADS entries.  grad, out: device, fp32 or fp16 (a moe_out), on the boundary of their type, n elements (n < 2^38, 0: none);
- * out may be grad (with the same type); apart from that no out may overlap another out or a grad (MOE_EINVAL).
+ * out may be grad (with the same type); apart from that no out may overlap another out or a grad, nor norm or ws any of them or each other (MOE_EINVAL).
  * norm: device fp32 [1].  ws: at least moe_clip_workspace_bytes(n_tensors).  The same inputs give the same bits.
  */
 #define MOE_MAX_GRADS 1024

@@ -1232,10 +1232,12 @@ struct Interval {
     bool written;
 };
 
-// Does an out overlap another out, or a gradient that is not its own at the same place and of the same type?
-bool outs_overlap(const moe_grad* g, int n) {
-    Interval v[2 * MOE_MAX_GRADS];
+// Does an out overlap another out, or a gradient that is not its own at the same place and of the same type?  The norm and the workspace are as outs that have no gradient.
+bool outs_overlap(const moe_grad* g, int n, const float* norm, const void* ws, size_t ws_bytes) {
+    Interval v[2 * MOE_MAX_GRADS + 2];
     int count = 0;
+    v[count++] = Interval{(uintptr_t)norm, (uintptr_t)norm + sizeof(float), n, true};
+    v[count++] = Interval{(uintptr_t)ws, (uintptr_t)ws + ws_bytes, n + 1, true};
     for (int i = 0; i < n; ++i) {
         if (!g[i].n) continue;
         const uintptr_t r = (uintptr_t)g[i].grad, w = (uintptr_t)g[i].out;
@@ -1289,7 +1291,7 @@ int moe_clip_gradients(const moe_grad* grads, int n_tensors, float max_norm, flo
         if (misaligned(g.grad, g.grad_type == MOE_OUT_F16 ? 2 : 4) || misaligned(g.out, g.out_type == MOE_OUT_F16 ? 2 : 4))
             return fail(MOE_EINVAL, "%s: tensor %d is not aligned to its type", who, i);
     }
-    if (outs_overlap(grads, n_tensors)) return fail(MOE_EINVAL, "%s: an out overlaps another tensor", who);
+    if (outs_overlap(grads, n_tensors, norm, ws, ws ? moe_clip_workspace_bytes(n_tensors) : 0)) return fail(MOE_EINVAL, "%s: an out, norm or the workspace overlaps another tensor", who);
     if (!ws) return fail(MOE_EWORKSPACE, "workspace is NULL");
     if (misaligned(ws, 256)) return fail(MOE_EWORKSPACE, "workspace must be 256-byte aligned");
     if (ws_bytes < moe_clip_workspace_bytes(n_tensors))

@@ -78,3 +78,24 @@ def test_results_of_the_forward_pass_over_what_is_still_read(over, name):
     if name != over and (name, over) != ("out", "x"):
         for p in places(over, SIZE[name]):
             assert refused(forward(**{name: p}))
+
+
+def clip(entries, norm=AT["d_gate"], ws=AT["ws"]):
+    return mm.lib().moe_clip_gradients((mm.CGrad * len(entries))(*[mm.CGrad(*e) for e in entries]), len(entries), 1.0, 1.0, norm, ws, 1 << 40, None)
+
+
+@pytest.mark.parametrize("n", [1, 100, 200000])                # one workgroup, two launches
+@pytest.mark.parametrize("kind", [0, 1])
+def test_norm_and_workspace_of_clipping_over_a_tensor(n, kind):
+    """The norm is written while gradients are read and outs written; the workspace holds sums in between."""
+    g, o, size = AT["x"], AT["out"], n * (2 if kind else 4)
+    room = mm.lib().moe_clip_workspace_bytes(2)
+    other = (AT["a"], AT["u"], 10, 0, 0)
+    for entries in ([(g, o, n, kind, kind), other], [other, (g, g, n, kind, kind)]):
+        for tensor in {entries[0][0], entries[0][1], entries[1][0], entries[1][1]} & {g, o}:
+            last = tensor + size - 1
+            for norm in (tensor, last // 4 * 4):
+                assert refused(clip(entries, norm=norm))
+            for ws in (tensor, last // 256 * 256, (tensor - room) // 256 * 256 + 256):
+                assert refused(clip(entries, ws=ws))
+    assert refused(clip([other], norm=AT["ws"] + 8))
