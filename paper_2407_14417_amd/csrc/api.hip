@@ -1220,6 +1220,12 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
     return check_hip(st);
 }
 
+// For the tests, host-only: do the gradients of the matrices come from the kernel with small tiles?  (A negative status if the call would be refused.)
+int moemix_train_small_tiles(const moe_layer* layer, int T) {
+    if (int rc = check_train_shape("moemix_train_small_tiles", layer, T)) return rc;
+    return train_small_tiles(T * layer->top_k, layer->n_experts, layer->d_model, layer->d_ff);
+}
+
 // ---------------------------------------------------------------- global norm and clipping
 
 namespace {

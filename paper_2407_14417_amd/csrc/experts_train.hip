@@ -891,21 +891,12 @@ __global__ __launch_bounds__(kFewThreads, 3) void train_weights_few_kernel(Train
     }
 }
 
-// Which of the two kernels, estimated (us) from the mean number of rows: a round of large tiles takes 9 and 1 per step, one of three small workgroups per compute unit 4 and 1.8 per step, 1
-// where each is alone.  Backward pass, large and small tiles: 64 rows for each of 32 experts of 2048 x 1408, 297, 261 us; 128 for each, 368, 346; 256, 542, 564; 300 for each of 6 of
-// 320 x 1408, 77, 64; 4096 for each of 2 of 2048 x 1408, 369, 408; 8 for each of 4 of 256 x 512, 33, 27.
-bool small_tiles(const TrainWeights& a, int P, int workgroups) {
-    const int tiles = ((a.f + kTrainCols - 1) / kTrainCols) * ((a.d + kTrainCols - 1) / kTrainCols), per_xcd = a.E * 3 * ((tiles + 7) / 8);
-    const float steps = (float)((P / a.E + kTrainStep - 1) / kTrainStep), full = 3.0f * kComputeUnits;
-    const float large = (float)((per_xcd + 31) / 32) * (9.0f + steps);
-    const float small = std::max((float)workgroups / full, 1.0f) * (4.0f + steps * (workgroups <= (int)kComputeUnits ? 1.0f : workgroups <= 2 * (int)kComputeUnits ? 1.4f : 1.8f));
-    return small <= large;
-}
+int few_workgroups(int E, int d, int f) { return E * 3 * ((f + kFewTile - 1) / kFewTile) * ((d + kFewTile - 1) / kFewTile); }
 
 template <typename OUT>
 void launch_weights(const TrainWeights& a, int P, hipStream_t st) {
-    const int few_f = (a.f + kFewTile - 1) / kFewTile, few_d = (a.d + kFewTile - 1) / kFewTile, few = a.E * 3 * few_f * few_d;
-    if (small_tiles(a, P, few)) {
+    const int few_f = (a.f + kFewTile - 1) / kFewTile, few_d = (a.d + kFewTile - 1) / kFewTile, few = few_workgroups(a.E, a.d, a.f);
+    if (train_small_tiles(P, a.E, a.d, a.f)) {
         const int turns = few >= kFewTurns * 4 * 3 * (int)kComputeUnits ? kFewTurns : 1;
         const int per_matrix = std::max(few_f * ((few_d + turns - 1) / turns), few_d * ((few_f + turns - 1) / turns));
         train_weights_few_kernel<OUT><<<(unsigned)(a.E * 3 * per_matrix), kFewThreads, 0, st>>>(a, per_matrix, turns);
@@ -1076,6 +1067,18 @@ __global__ __launch_bounds__(256) void train_gather_kernel(TrainGrouping g, Trai
 }
 
 }  // namespace
+
+// Which of the two kernels, estimated (us) from the mean number of rows (how they are spread is known on the GPU only) for fp16 gradients that overwrite: a round of large tiles takes 9 and 1
+// per step, one of three small workgroups per compute unit 4 and 1.8 per step, 1 where each is alone.  Backward pass, large and small tiles: 64 rows for each of 32 experts of 2048 x 1408, 297, 261 us; 128 for each, 368, 346; 256, 542, 564; 300 for each of 6 of
+// 320 x 1408, 77, 64; 4096 for each of 2 of 2048 x 1408, 369, 408; 8 for each of 4 of 256 x 512, 33, 27.
+bool train_small_tiles(int P, int E, int d, int f) {
+    const int workgroups = few_workgroups(E, d, f);
+    const int tiles = ((f + kTrainCols - 1) / kTrainCols) * ((d + kTrainCols - 1) / kTrainCols), per_xcd = E * 3 * ((tiles + 7) / 8);
+    const float steps = (float)((P / E + kTrainStep - 1) / kTrainStep), full = 3.0f * kComputeUnits;
+    const float large = (float)((per_xcd + 31) / 32) * (9.0f + steps);
+    const float small = std::max((float)workgroups / full, 1.0f) * (4.0f + steps * (workgroups <= (int)kComputeUnits ? 1.0f : workgroups <= 2 * (int)kComputeUnits ? 1.4f : 1.8f));
+    return small <= large;
+}
 
 int train_most_splits(int P, int d) {
     const float rounds = (float)P / kTrainRows * (float)((d + kTrainCols - 1) / kTrainCols) / kComputeUnits;

@@ -122,6 +122,9 @@ int train_most_splits(int P, int d);
 // Most rows of a chunk, where the widest launch has tiles_f or tiles_d tiles of columns.
 int train_most_rows(int P, int E, int d, int f, int tiles_f, int tiles_d);
 
+// Are the gradients of the matrices made of small tiles (train_weights_few_kernel)?
+bool train_small_tiles(int P, int E, int d, int f);
+
 void launch_train_group(const TrainGrouping& g, const TrainWorkspace& w, int d, int f, hipStream_t st);
 // a = W1 x, u = W3 x, h = silu(a) u
 void launch_train_up(const TrainRows& a, hipStream_t st);
