@@ -637,6 +637,9 @@ class GradList:
         if len(self.grads) > MAX_GRADS or len(self.outs) != len(self.grads):
             raise MoeError(MOE_ESHAPE, f"{len(self.grads)} gradients, {len(self.outs)} outs: as many are needed, at most {MAX_GRADS}")
         self.device = dev
+        for i, g in enumerate(self.grads):
+            if not hasattr(g, "shape"):
+                raise MoeError(MOE_EINVAL, f"gradient {i}: a tensor is needed")
         self.c = (CGrad * max(1, len(self.grads)))(*[
             CGrad(_need(g, f"gradient {i}", _F32 + _F16, g.shape, dev), _need(o, f"out {i}", _F32 + _F16, g.shape, dev), g.numel(),
                   _out_type(g, f"gradient {i}"), _out_type(o, f"out {i}")) for i, (g, o) in enumerate(zip(self.grads, self.outs))])

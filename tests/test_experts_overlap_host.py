@@ -99,3 +99,12 @@ def test_norm_and_workspace_of_clipping_over_a_tensor(n, kind):
             for ws in (tensor, last // 256 * 256, (tensor - room) // 256 * 256 + 256):
                 assert refused(clip(entries, ws=ws))
     assert refused(clip([other], norm=AT["ws"] + 8))
+
+
+def test_a_gradient_that_is_none():
+    """A parameter without one is the caller's to leave out; the error is the binding's."""
+    torch = pytest.importorskip("torch")
+    for grads, outs in (([None], None), ([None], [torch.zeros(3)])):
+        with pytest.raises(mm.MoeError) as e:
+            mm.GradList(grads, outs)
+        assert e.value.code == mm.MOE_EINVAL and "gradient 0" in str(e.value)
