@@ -344,7 +344,8 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
  * Forward and backward pass of the experts of a grouping (moe_permute's), all of them held in 16 bits and resident (else MOE_EINVAL,
  * MOE_ENOTRESIDENT).  Grouped row r of expert e stands for pair p = perm[r], token t = p / top_k, with gate g = topk_gate[p]; P = T top_k.
  *   moe_experts_forward:   a[r,:] = W1 x[t,:],  u[r,:] = W3 x[t,:],  h = silu(a) * u,  out[t,:] = sum over the token's rows of g W2 h[r,:]
- *     a and u are kept for the backward pass, rounded to fp16; h, of the unrounded values, is rounded to fp16 as everywhere.
+ *     a and u are kept for the backward pass, rounded to fp16 (past 65504 to infinities, with which the gradients that such a row reaches are not finite); h, of the unrounded values, is
+ *     rounded to fp16 as everywhere.
  *   moe_experts_backward:  with q[r,:] = W2^T d_out[t,:] and s = 1 / (1 + exp(-a)), from the kept a and u:
  *     d_gate[p] = sum_f q h,   d_a = g q u s (1 + a (1 - s)),   d_u = g q a s        (d_a, d_u and g h are rounded to fp16)
  *     d_x[t,:] = sum over the token's rows of W1^T d_a[r,:] + W3^T d_u[r,:]          (without what flows through the gates: moe_route_backward)
@@ -353,6 +354,7 @@ int moe_route_backward(const moe_layer* layer, const void* x, const float* logit
  * A pair in no group (moe_permute drops indices outside [0, n_experts), so that is how tokens of padding are left out, whatever they hold) adds nothing
  * to its token and gets a d_gate of 0; grouped rows outside [offsets[0], offsets[n_experts]) of a and u are left as they were.  An expert without rows gets
  * gradients of zeros.
+ * A block that also has experts of other precisions is trained in a layer in which these stand as fp16 copies (moe_dequant_int4 or its like) whose gradients are not asked for.
  * x, d_out: device fp16 [T, d_model]; a, u: device fp16 [P, d_ff]; out: device fp16 [T, d_model]; topk_gate: device fp32 [T, top_k], NULL: all gates are 1;
  * offsets: device int32 [n_experts + 1], NULL (one expert only): all P rows are its; perm: device int32 [P], NULL: row r is pair r.  (Whatever offsets and perm
  * hold, nothing outside the arrays is read or written.)
@@ -380,7 +382,7 @@ int moe_experts_backward(const moe_layer* layer, const void* x, int T, const flo
  *   norm = unscale * sqrt( sum v^2 ),   out = v * c  with  c = unscale * min(1, max_norm / (norm + 1e-6))
  * Sums are held in 64 bits.  unscale: finite, > 0, 1 / loss scale; max_norm: >= 0, INFINITY: no limit.  If norm is not finite in 32 bits (a gradient was
  * not) only norm is written: the caller leaves out the step.
- * grads: HOST array of at most MOE_MAX_GRADS entries.  grad, out: device, fp32 or fp16 (a moe_out), on the boundary of their type, n elements (n < 2^38, 0: none);
+ * grads: HOST array of at most MOE_MAX_GRADS entries (gradients one behind the other in memory may be one entry: that is how more of them are clipped together).  grad, out: device, fp32 or fp16 (a moe_out), on the boundary of their type, n elements (n < 2^38, 0: none);
  * out may be grad (with the same type); apart from that no out may overlap another out or a grad, nor norm or ws any of them or each other (MOE_EINVAL).
  * norm: device fp32 [1].  ws: at least moe_clip_workspace_bytes(n_tensors).  The same inputs give the same bits.
  */

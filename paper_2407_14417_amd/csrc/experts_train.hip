@@ -215,8 +215,9 @@ struct RowsWork {
     int expert, begin, rows, n0, s0, s1, split;
 };
 
-// PAST: the matrices are more than the caches hold.  Then those of experts with up to 128 rows, of one chunk, are read past them, each once (4 and 64 tokens in the Mixtral shape, forward 540 -> 504
-// and 526 -> 493 us, 5.7 TB/s; with matrices that fit, 16 tokens of 256 x 512, 19.4 -> 21.3).
+// PAST: the matrices are more than the caches hold.  Then chunks of up to 128 rows read theirs past them: most are their expert's only one, and each matrix is read once (4 and 64 tokens in the
+// Mixtral shape, forward 540 -> 504 and 526 -> 493 us, 5.7 TB/s; with matrices that fit, 16 tokens of 256 x 512, 19.4 -> 21.3).  How many chunks an expert has is not looked at: several
+// short ones of one expert all read past the caches, and so does a short one beside a long one.
 template <int FORM, int MT, bool PAST>
 struct RowsTile {
     static constexpr bool kColumns = FORM == kDHidden || FORM == kDRows;     // how the matrix lies
