@@ -9,6 +9,15 @@ from tests.train_ref import Ref
 T, D, F, E, K = 50, 64, 128, 3, 2
 
 
+@pytest.fixture(scope="module", autouse=True)
+def one_thread():
+    """(many small products: threads of several test processes would wait for one another)"""
+    before = torch.get_num_threads()
+    torch.set_num_threads(1)
+    yield
+    torch.set_num_threads(before)
+
+
 @pytest.fixture(scope="module")
 def block():
     g = torch.Generator().manual_seed(41)
